@@ -376,6 +376,100 @@ ff_status ff_adamw_step_batched(int64_t count, int64_t n, float* const* c, const
 double ff_lr_linear_warmup(int64_t step, int64_t warmup, int64_t total, double base_lr);
 
 /*
+ * Operators around the adapter in a training step: layer norm, dropout and the loss of the head.  They need no
+ * frame and no plan.  Activations are T rows of n elements of type `act` as above, row t at X + t ldx.  The calls are
+ * asynchronous on `stream`, allocate nothing, synchronise nothing, may be captured into a graph, and write nothing
+ * when they return an error (FF_EINVAL, or FF_EDEVICE on a failed launch).  Equal inputs give equal bits.  A
+ * workspace belongs to the call until it has run: calls that overlap in time need one each.  Outputs must not
+ * overlap inputs or the workspace except where it is said.
+ */
+
+/*
+ * ff_layernorm_fwd -- y = weight (x - mean) rstd + bias for each row x, rstd = 1 / sqrt(var + eps) with the row's
+ * variance over n (not n - 1).  Sums are in fp32, the variance from the centred row.
+ *   X, Y         : device, element alignment, any leading dimension >= n (rows on 16 bytes with n a multiple of 8 in
+ *                  bf16, 4 in fp32, run fastest).  Y may be X.
+ *   weight, bias : device, n elements of type w_dtype; NULL for ones / zeros.
+ *   mean, rstd   : device, T fp32 each, for the backward; NULL where not wanted.
+ * T = 0 is a no-op.
+ */
+ff_status ff_layernorm_fwd(int64_t T, int64_t n, int act, const void* X, int64_t ldx, int w_dtype, const void* weight,
+                           const void* bias, float eps, void* Y, int64_t ldy, float* mean, float* rstd, void* stream);
+/*
+ * ff_layernorm_bwd -- with h = (x - mean) rstd, g a row of G and a = weight g:
+ *   dX      = beta_dx dX + rstd (a - mean(a) - h mean(a h))     (skipped if dX == NULL; beta_dx = 0 does not read it)
+ *   dweight = [dweight +] sum_t g h,   dbias = [dbias +] sum_t g  (fp32, n each; either may be NULL; added to what is
+ *             there when accumulate_dw != 0)
+ *   mean, rstd : as ff_layernorm_fwd wrote them.
+ *   workspace  : device, 16-byte aligned, at least ff_layernorm_workspace bytes; may be NULL without dweight and dbias.
+ * With T = 0 dweight and dbias become zero (or stay, accumulating).
+ */
+ff_status ff_layernorm_workspace(int64_t T, int64_t n, int64_t* bytes);
+ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t ldx, const void* G, int64_t ldg,
+                           int w_dtype, const void* weight, const float* mean, const float* rstd, float beta_dx, void* dX,
+                           int64_t lddx, int accumulate_dw, float* dweight, float* dbias, void* workspace,
+                           int64_t workspace_bytes, void* stream);
+
+/*
+ * ff_dropout -- y = [r +] m x / (1 - p') for each element, m in {0, 1} from a counter-based generator: a function of
+ * (seed, offset, row, column, n) alone, so that the mask is never stored and the backward pass is this call on the
+ * gradient with the same seed and offset (R then the gradient of another path, or NULL).
+ *   p          : share of elements to drop, 0 <= p <= 1.  p' = D / 65536 with D = p 65536 rounded to nearest (at most
+ *                65535 for p < 1); kept elements are scaled by 65536 / (65536 - D).  p = 1 drops all.
+ *   seed       : key of the generator, any 64 bits.   offset : number of the draw (another for every layer and step).
+ *   offset_dev : device, one uint64 added to offset when the call runs, or NULL: a captured step whose graph is
+ *                replayed draws another mask when the program changes that value.
+ *   R          : device, T x n of type act, added after scaling, or NULL.
+ *   X, Y, R    : element alignment, any leading dimension >= n; Y may be X or R.
+ * The mask: block b = t ceil(n / 8) + i / 8 of eight elements of row t takes the four 32-bit words of Philox 4x32-10 with
+ * counter (b, offset), low words first, and key seed; element i takes the 16 bits number i mod 8 of them, the low half
+ * of a word first, and is dropped where they are below D.
+ */
+ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, double p, uint64_t seed, uint64_t offset,
+                     const uint64_t* offset_dev, const void* R, int64_t ldr, void* Y, int64_t ldy, void* stream);
+
+/*
+ * ff_xent_* -- cross entropy of a head's logits z = H W^T over a vocabulary of V entries, without keeping the logits:
+ *   lse_t  = log sum_v exp z_tv,   loss_t = lse_t - z_t,target[t]
+ *   P_tv   = (exp(z_tv - lse_t) - [v = target[t]]) scale dloss[t]
+ *   dH     = beta_dh dH + P W,     dW = beta_dw dW + P^T H
+ * A token whose target lies outside [0, V) has none: its loss is 0, its row of P is 0 whatever H holds, its lse is
+ * still that of its logits.
+ *   H, dH  : device, T x n of type act, W, dW : device, V x n of type act; n a multiple of 8 (bf16) or 4 (fp32), 16-byte
+ *            aligned, leading dimensions multiples of 8 (4), at most 1048576.  beta = 0 does not read the output.
+ *   target : device, T int64.   loss, lse : device, T fp32.
+ *   dloss  : device, T fp32, gradient of the result with respect to each token's loss; NULL for ones.
+ *            `scale` multiplies it (1 / counted tokens for a mean).
+ *   workspace : device, 256-byte aligned, at least ff_xent_workspace bytes for the same T, n, V, act and the outputs wanted
+ *            (FF_XENT_DH, FF_XENT_DW or both; 0: loss alone).  It holds P, in type act, for a piece of the tokens or of
+ *            the vocabulary (at most 256 MiB, or 256 tokens of it where V is larger), fp32 partial sums of dH, and with dW
+ *            a copy of H.
+ * ff_xent_fwd  : loss and lse.
+ * ff_xent_step : loss, lse and the gradients in one call, which computes the logits once (twice with dW where P does not
+ *                fit one piece).
+ * ff_xent_bwd  : the gradients from the lse of an earlier ff_xent_fwd on the same H, W: for programs that know dloss only
+ *                after it.  It computes the logits again.  loss may be NULL; with the loss of that call the target's
+ *                P keeps its digits where its probability is near one, as in ff_xent_step (from lse alone it carries
+ *                lse's rounding).
+ * dH == NULL or dW == NULL skips that output.  Arithmetic: products accumulate in fp32, softmax statistics are fp32, P is
+ * rounded to type act before the products that read it (in ff_xent_step after one more rounding of exp(z - max)).
+ * With T = 0, dW = beta_dw dW.
+ */
+enum { FF_XENT_DH = 1, FF_XENT_DW = 2 };
+ff_status ff_xent_workspace(int64_t T, int64_t n, int64_t V, int act, int want, int64_t* bytes);
+ff_status ff_xent_fwd(int64_t T, int64_t n, int64_t V, int act, const void* H, int64_t ldh, const void* W, int64_t ldw,
+                      const int64_t* target, float* loss, float* lse, void* workspace, int64_t workspace_bytes,
+                      void* stream);
+ff_status ff_xent_bwd(int64_t T, int64_t n, int64_t V, int act, const void* H, int64_t ldh, const void* W, int64_t ldw,
+                      const int64_t* target, const float* lse, const float* loss, const float* dloss, float scale,
+                      float beta_dh, void* dH, int64_t lddh, float beta_dw, void* dW, int64_t lddw, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+ff_status ff_xent_step(int64_t T, int64_t n, int64_t V, int act, const void* H, int64_t ldh, const void* W, int64_t ldw,
+                       const int64_t* target, const float* dloss, float scale, float* loss, float* lse, float beta_dh,
+                       void* dH, int64_t lddh, float beta_dw, void* dW, int64_t lddw, void* workspace,
+                       int64_t workspace_bytes, void* stream);
+
+/*
  * ff_time_next_kernel -- instrumentation for benchmarks.  Arms this thread so
  * that the next hot-path call records the hipEvent_t `ev_start` just before and
  * `ev_stop` just after its main kernel (the fused forward, the fused backward,

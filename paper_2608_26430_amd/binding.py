@@ -43,6 +43,7 @@ def _load():
         raise FrameFTError(5, f"{_LIB_PATH} is not built (python -m paper_2608_26430_amd.build)")
     lib = ctypes.CDLL(_LIB_PATH)
     i64, i32, f32, vp = ctypes.c_int64, ctypes.c_int, ctypes.c_float, ctypes.c_void_p
+    u64, f64, pi64 = ctypes.c_uint64, ctypes.c_double, ctypes.POINTER(ctypes.c_int64)
     dp = ctypes.POINTER(ctypes.c_double)
     sig = {
         "ff_status_string": (ctypes.c_char_p, [i32]),
@@ -76,6 +77,17 @@ def _load():
         "ff_lr_linear_warmup": (ctypes.c_double, [i64, i64, i64, ctypes.c_double]),
         "ff_coef_to_plan": (i32, [vp, vp, vp, vp]),
         "ff_coef_to_user": (i32, [vp, vp, vp, i32, vp]),
+        "ff_layernorm_fwd": (i32, [i64, i64, i32, vp, i64, i32, vp, vp, f32, vp, i64, vp, vp, vp]),
+        "ff_layernorm_workspace": (i32, [i64, i64, pi64]),
+        "ff_layernorm_bwd": (i32, [i64, i64, i32, vp, i64, vp, i64, i32, vp, vp, vp, f32, vp, i64, i32, vp, vp, vp, i64,
+                                   vp]),
+        "ff_dropout": (i32, [i64, i64, i32, vp, i64, f64, u64, u64, vp, vp, i64, vp, i64, vp]),
+        "ff_xent_workspace": (i32, [i64, i64, i64, i32, i32, pi64]),
+        "ff_xent_fwd": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp]),
+        "ff_xent_bwd": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, f32, f32, vp, i64, f32, vp, i64, vp,
+                              i64, vp]),
+        "ff_xent_step": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, vp, f32, vp, vp, f32, vp, i64, f32, vp, i64, vp,
+                               i64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -588,6 +600,255 @@ def _tokens_ptr(tokens, count):
     if tokens.dtype != torch.int32 or not tokens.is_cuda or not tokens.is_contiguous() or tokens.numel() != count:
         raise ValueError("tokens must be a contiguous int32 device tensor with one count per adapter")
     return tokens.data_ptr()
+
+
+# ------------------------------------------------------------------ layer norm, dropout, loss
+
+def _new(shape, dtype, device, stream):
+    """An empty tensor for a call on `stream`: taken on that stream, so that its memory is not still in use there."""
+    torch = _T or _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rows(t, name, shape, dtype, device):
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and shape[1] != 1) or t.shape != shape or t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{name} must be a {shape[0]} x {shape[1]} {dtype} tensor with unit column stride on {device}")
+    # the stride of a single row says nothing
+    return t.data_ptr(), max(st[0], shape[1]) if shape[0] < 2 else st[0]
+
+
+def _input(t, name):
+    """Pointer, leading dimension, sizes of an activation that the call takes its type and device from."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-D device tensor")
+    return _rows(t, name, t.shape, t.dtype, t.device)
+
+
+def _array(t, name, n, dtype, device):
+    if t.dtype is not dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on {device}")
+    return t.data_ptr()
+
+
+def _workspace(ws, nbytes, device, stream):
+    if ws is None:
+        return _new((nbytes,), (_T or _torch()).uint8, device, stream)
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    return ws
+
+
+class _on_device:
+    """The call's device as the current one: launches and the default stream are the current device's."""
+
+    def __init__(self, device):
+        cuda = (_T or _torch())._C
+        self.prev = None if cuda._cuda_getDevice() == device.index else device
+
+    def __enter__(self):
+        if self.prev is not None:
+            self.prev = _torch().cuda.device(self.prev)
+            self.prev.__enter__()
+
+    def __exit__(self, *exc):
+        if self.prev is not None:
+            self.prev.__exit__(*exc)
+
+
+def _norm_vector(t, name, n, device):
+    """Pointer of a layer norm's weight or bias, None for none."""
+    if t is None:
+        return None
+    return _array(t, name, n, t.dtype, device)
+
+
+def layernorm_fwd(X, weight=None, bias=None, eps: float = 1e-5, Y=None, mean=None, rstd=None, stream=None):
+    """Layer norm of each row of X (bf16 or fp32): returns (Y, mean, rstd), the last two fp32 per row for
+    layernorm_bwd (ff_layernorm_fwd).  weight and bias: fp32 or bf16, both of one type; None for ones / zeros.  Y
+    may be X."""
+    torch = _T or _torch()
+    xp, ldx = _input(X, "X")
+    T, n = X.shape
+    dev = X.device
+    act = _act_code(X)
+    w_dtype = weight.dtype if weight is not None else (bias.dtype if bias is not None else torch.float32)
+    if w_dtype not in (torch.float32, torch.bfloat16) or (bias is not None and bias.dtype is not w_dtype):
+        raise ValueError("weight and bias must both be fp32 or both bf16")
+    with _on_device(dev):
+        Y = _new((T, n), X.dtype, dev, stream) if Y is None else Y
+        mean = _new((T,), torch.float32, dev, stream) if mean is None else mean
+        rstd = _new((T,), torch.float32, dev, stream) if rstd is None else rstd
+        yp, ldy = _rows(Y, "Y", X.shape, X.dtype, dev)
+        _check((_lib or _load()).ff_layernorm_fwd(
+            T, n, act, xp, ldx, FF_BF16 if w_dtype is torch.bfloat16 else FF_F32, _norm_vector(weight, "weight", n, dev),
+            _norm_vector(bias, "bias", n, dev), eps, yp, ldy, _array(mean, "mean", T, torch.float32, dev),
+            _array(rstd, "rstd", T, torch.float32, dev), _stream(stream)))
+    return Y, mean, rstd
+
+
+def _layernorm_bytes(T, n):
+    v = ctypes.c_int64()
+    _check((_lib or _load()).ff_layernorm_workspace(T, n, ctypes.byref(v)))
+    return v.value
+
+
+def layernorm_workspace(T: int, n: int, device="cuda"):
+    """A workspace for layernorm_bwd calls of up to T rows of n, one such call at a time."""
+    return _torch().empty((_layernorm_bytes(T, n),), dtype=_torch().uint8, device=device)
+
+
+def layernorm_bwd(X, G, weight, mean, rstd, dX=None, dweight=None, dbias=None, beta_dx: float = 0.0,
+                  accumulate: bool = False, want_dx: bool = True, want_dw: bool = True, workspace=None, stream=None):
+    """Backward of layernorm_fwd for upstream gradient G: returns (dX, dweight, dbias) (None where not wanted), dX =
+    beta_dx * dX + ..., dweight and dbias fp32, added to the given ones with `accumulate` (ff_layernorm_bwd)."""
+    torch = _T or _torch()
+    xp, ldx = _input(X, "X")
+    T, n = X.shape
+    dev, f32 = X.device, torch.float32
+    gp, ldg = _rows(G, "G", X.shape, X.dtype, dev)
+    w_dtype = weight.dtype if weight is not None else f32
+    if w_dtype not in (f32, torch.bfloat16):
+        raise ValueError("weight must be fp32 or bf16")
+    if want_dx and dX is None and beta_dx != 0.0:
+        raise ValueError("beta_dx != 0 needs an existing dX")
+    if want_dw and accumulate and (dweight is None or dbias is None):
+        raise ValueError("accumulate needs existing dweight and dbias")
+    with _on_device(dev):
+        dxp, lddx, dwp, dbp, wsp, wsn = None, n, None, None, None, 0
+        if want_dx:
+            dX = _new((T, n), X.dtype, dev, stream) if dX is None else dX
+            dxp, lddx = _rows(dX, "dX", X.shape, X.dtype, dev)
+        if want_dw:
+            dweight = _new((n,), f32, dev, stream) if dweight is None else dweight
+            dbias = _new((n,), f32, dev, stream) if dbias is None else dbias
+            dwp, dbp = _array(dweight, "dweight", n, f32, dev), _array(dbias, "dbias", n, f32, dev)
+            workspace = _workspace(workspace, _layernorm_bytes(T, n) if workspace is None else 0, dev, stream)
+            wsp, wsn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check((_lib or _load()).ff_layernorm_bwd(
+            T, n, _act_code(X), xp, ldx, gp, ldg, FF_BF16 if w_dtype is torch.bfloat16 else FF_F32,
+            _norm_vector(weight, "weight", n, dev), _array(mean, "mean", T, f32, dev), _array(rstd, "rstd", T, f32, dev),
+            beta_dx, dxp, lddx, int(accumulate), dwp, dbp, wsp, wsn, _stream(stream)))
+    return (dX if want_dx else None), (dweight if want_dw else None), (dbias if want_dw else None)
+
+
+def dropout(X, p: float, seed: int, offset: int = 0, residual=None, Y=None, offset_dev=None, stream=None):
+    """Y = [residual +] mask * X / (1 - p) with a mask that is a function of (seed, offset, row, column, width)
+    and is never stored (ff_dropout); the backward pass is the same call on the gradient.  offset_dev: a device int64
+    tensor of one element added to offset when the call runs (for captured graphs).  Y may be X or residual."""
+    torch = _T or _torch()
+    xp, ldx = _input(X, "X")
+    T, n = X.shape
+    dev = X.device
+    act = _act_code(X)
+    with _on_device(dev):
+        Y = _new((T, n), X.dtype, dev, stream) if Y is None else Y
+        yp, ldy = _rows(Y, "Y", X.shape, X.dtype, dev)
+        rp, ldr = _rows(residual, "residual", X.shape, X.dtype, dev) if residual is not None else (None, n)
+        op = _array(offset_dev.view(1), "offset_dev", 1, torch.int64, dev) if offset_dev is not None else None
+        _check((_lib or _load()).ff_dropout(T, n, act, xp, ldx, p, seed & (1 << 64) - 1, offset & (1 << 64) - 1, op, rp, ldr,
+                                            yp, ldy, _stream(stream)))
+    return Y
+
+
+def _xent_bytes(T, n, V, act, want):
+    v = ctypes.c_int64()
+    _check((_lib or _load()).ff_xent_workspace(T, n, V, act, want, ctypes.byref(v)))
+    return v.value
+
+
+def xent_workspace(T: int, n: int, V: int, dtype, want_dh: bool = False, want_dw: bool = False, device="cuda"):
+    """A workspace for xent_fwd, xent_bwd and xent_step calls of these sizes and outputs, one such call at a time."""
+    torch = _torch()
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported activation dtype {dtype}")
+    nbytes = _xent_bytes(T, n, V, FF_BF16 if dtype is torch.bfloat16 else FF_F32, int(want_dh) + 2 * int(want_dw))
+    return torch.empty((nbytes,), dtype=torch.uint8, device=device)
+
+
+def _head(H, W, target):
+    torch = _T or _torch()
+    hp, ldh = _input(H, "H")
+    T, n = H.shape
+    if W.dim() != 2 or W.shape[0] < 1 or W.shape[1] != n:
+        raise ValueError("W must be a V x n tensor, n the width of H")
+    wp, ldw = _rows(W, "W", W.shape, H.dtype, H.device)
+    return T, n, W.shape[0], _act_code(H), hp, ldh, wp, ldw, _array(target, "target", T, torch.int64, H.device)
+
+
+def xent_fwd(H, W, target, loss=None, lse=None, workspace=None, stream=None):
+    """Cross entropy of the logits H W^T of each token, without keeping the logits: returns (loss, lse), fp32 per token.
+    Targets outside [0, V) mark tokens without loss (ff_xent_fwd)."""
+    f32 = (_T or _torch()).float32
+    T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
+    dev = H.device
+    with _on_device(dev):
+        loss = _new((T,), f32, dev, stream) if loss is None else loss
+        lse = _new((T,), f32, dev, stream) if lse is None else lse
+        ws = _workspace(workspace, _xent_bytes(T, n, V, act, 0) if workspace is None else 0, dev, stream)
+        _check((_lib or _load()).ff_xent_fwd(T, n, V, act, hp, ldh, wp, ldw, tp, _array(loss, "loss", T, f32, dev),
+                                             _array(lse, "lse", T, f32, dev), ws.data_ptr(),
+                                             ws.numel() * ws.element_size(), _stream(stream)))
+    return loss, lse
+
+
+def _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream):
+    """(dH, its pointer and stride, dW, ...), made where they are wanted and not given."""
+    if (want_dh and dH is None and beta_dh != 0.0) or (want_dw and dW is None and beta_dw != 0.0):
+        raise ValueError("beta != 0 needs an existing output")
+    n, dev = H.shape[1], H.device
+    dhp = dwp = None
+    ldh = ldw = n
+    if want_dh:
+        dH = _new(H.shape, H.dtype, dev, stream) if dH is None else dH
+        dhp, ldh = _rows(dH, "dH", H.shape, H.dtype, dev)
+    if want_dw:
+        dW = _new(W.shape, H.dtype, dev, stream) if dW is None else dW
+        dwp, ldw = _rows(dW, "dW", W.shape, H.dtype, dev)
+    return (dH if want_dh else None), dhp, ldh, (dW if want_dw else None), dwp, ldw
+
+
+def xent_bwd(H, W, target, lse, dloss=None, scale: float = 1.0, dH=None, dW=None, beta_dh: float = 0.0,
+             beta_dw: float = 0.0, want_dh: bool = True, want_dw: bool = False, workspace=None, stream=None, loss=None):
+    """Gradients of sum_t scale dloss[t] loss[t] from the lse of xent_fwd: returns (dH, dW) (None where not wanted);
+    dloss: fp32 per token, None for ones; loss: that of xent_fwd, for the target's gradient of tokens whose loss is near
+    zero (ff_xent_bwd)."""
+    f32 = (_T or _torch()).float32
+    T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
+    dev = H.device
+    with _on_device(dev):
+        dH, dhp, lddh, dW, dwp, lddw = _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream)
+        want = int(want_dh) + 2 * int(want_dw)
+        ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, dev, stream)
+        _check((_lib or _load()).ff_xent_bwd(
+            T, n, V, act, hp, ldh, wp, ldw, tp, _array(lse, "lse", T, f32, dev),
+            _array(loss, "loss", T, f32, dev) if loss is not None else None,
+            _array(dloss, "dloss", T, f32, dev) if dloss is not None else None, scale, beta_dh, dhp, lddh, beta_dw, dwp,
+            lddw, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+    return dH, dW
+
+
+def xent_step(H, W, target, dloss=None, scale: float = 1.0, loss=None, lse=None, dH=None, dW=None, beta_dh: float = 0.0,
+              beta_dw: float = 0.0, want_dh: bool = True, want_dw: bool = False, workspace=None, stream=None):
+    """xent_fwd and xent_bwd in one call, which computes the logits once: returns (loss, lse, dH, dW), dH and dW the
+    gradients of sum_t scale dloss[t] loss[t] (None where not wanted; ff_xent_step)."""
+    f32 = (_T or _torch()).float32
+    T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
+    dev = H.device
+    with _on_device(dev):
+        loss = _new((T,), f32, dev, stream) if loss is None else loss
+        lse = _new((T,), f32, dev, stream) if lse is None else lse
+        dH, dhp, lddh, dW, dwp, lddw = _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream)
+        want = int(want_dh) + 2 * int(want_dw)
+        ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, dev, stream)
+        _check((_lib or _load()).ff_xent_step(
+            T, n, V, act, hp, ldh, wp, ldw, tp, _array(dloss, "dloss", T, f32, dev) if dloss is not None else None, scale,
+            _array(loss, "loss", T, f32, dev), _array(lse, "lse", T, f32, dev), beta_dh, dhp, lddh, beta_dw, dwp, lddw,
+            ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+    return loss, lse, dH, dW
 
 
 def time_next_kernel(ev_start, ev_stop):

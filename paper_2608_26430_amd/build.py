@@ -15,13 +15,16 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libframeft.so")
-# (source, object name, extra flags): the generic and slab kernels are instantiated by one source
+# (source, object name, extra flags): the generic, slab and loss kernels are instantiated by one source
 # each, compiled once per variant, so that their long compiles run in parallel
 SOURCES = [("capi.cpp", "capi.cpp.o", []), ("framegen.cpp", "framegen.cpp.o", []), ("plan.cpp", "plan.cpp.o", []),
            ("kernels.hip", "kernels.hip.o", []), ("kernels_w128.hip", "kernels_w128.hip.o", []),
            ("optim.hip", "optim.hip.o", []), ("group.cpp", "group.cpp.o", []),
            ("lift.hip", "lift.hip.o", []), ("slab.hip", "slab.hip.o", []),
-           ("slab_ms.hip", "slab_ms.hip.o", [])] + [
+           ("slab_ms.hip", "slab_ms.hip.o", []), ("norm.hip", "norm.hip.o", []), ("dropout.hip", "dropout.hip.o", []),
+           ("xent.hip", "xent.hip.o", [])] + [
+    ("xent_inst.hip", f"xent_{l}_{t}.o", [f"-DXENT_LAYOUT={l}", f"-DXENT_BF16={int(t == 'bf16')}"])
+    for l in (0, 1, 2) for t in ("bf16", "f32")] + [
     ("slab_inst.hip", f"slab_{r}.o", [f"-DSLAB_RADIX={int(r == 'radix')}"])
     for r in ("direct", "radix")] + [
     ("gen_inst.hip", f"gen_{d}_{t}{'_ms' if ms else ''}.o",

@@ -1,0 +1,562 @@
+// Layer norm, forward and backward, with the reduction of the weight's and bias's gradients.
+//
+//   mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps), h = (x - mu) r, y = w h + b          (a row x of n)
+//   a = w g;  dx = beta dx + r (a - mean a - h mean(a h));  dw = sum_t g h;  db = sum_t g
+// Every sum is in fp32; the variance is that of the centred row, which stays in registers, so that a large mean costs
+// no digits.  A row belongs to WV waves (1, 4 or 16) whose threads hold NV pieces of VEC consecutive elements each;
+// rows wider than that are read three times.  The backward's workgroups walk the rows with a stride, keep dw and db of
+// their columns in registers and leave one partial row each, added up in a fixed order by a second kernel: the same
+// inputs give the same bits.  Bound by memory: forward 2 T n, backward 3 T n elements.
+#include <cmath>
+
+#include "ff_internal.h"
+
+namespace ff {
+namespace norm {
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct Args {
+  const void* X;
+  const void* G;
+  void* Y;             // forward: y, backward: dx
+  int64_t ldx, ldg, ldy;
+  int64_t T;
+  int n;
+  const void* weight;  // NULL: ones
+  const void* bias;    // NULL: zeros
+  int w_bf16;
+  float eps;
+  float* mean;
+  float* rstd;
+  float beta;
+  float* part;         // [workgroups][2][n]: dw, db of a workgroup's rows (NULL: not wanted)
+  int vec_w;           // weight and bias may be read in whole pieces
+};
+
+template <class E, int VEC>
+struct Pack {
+  static __device__ __forceinline__ void get(const E* p, float* v) {
+    if constexpr (VEC == 1) {
+      v[0] = (float)p[0];
+    } else if constexpr (sizeof(E) == 2) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+        v[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+      }
+    } else {
+      const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = w[i];
+    }
+  }
+  static __device__ __forceinline__ void put(E* p, const float* v) {
+    if constexpr (VEC == 1) {
+      p[0] = (E)v[0];
+    } else if constexpr (sizeof(E) == 2) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = (unsigned)__builtin_bit_cast(unsigned short, (__bf16)v[2 * i]) |
+               (unsigned)__builtin_bit_cast(unsigned short, (__bf16)v[2 * i + 1]) << 16;
+      *reinterpret_cast<u32x4*>(p) = w;
+    } else {
+      const f32x4 w = {v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4*>(p) = w;
+    }
+  }
+};
+
+// VEC values of weight or bias at column c (absent: `none`)
+template <int VEC>
+__device__ __forceinline__ void vector_at(const void* p, int bf16, int vec, float none, int c, float* v) {
+  if (!p) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = none;
+  } else if (bf16) {
+    const __bf16* q = static_cast<const __bf16*>(p) + c;
+    if (VEC == 8 && vec) {
+      Pack<__bf16, 8>::get(q, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = (float)q[i];
+    }
+  } else {
+    const float* q = static_cast<const float*>(p) + c;
+    if (VEC >= 4 && vec) {
+#pragma unroll
+      for (int i = 0; i < VEC; i += 4) {
+        const f32x4 w = *reinterpret_cast<const f32x4*>(q + i);
+        v[i] = w[0], v[i + 1] = w[1], v[i + 2] = w[2], v[i + 3] = w[3];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = q[i];
+    }
+  }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// Sums over the WV waves of a row (the whole workgroup when WV > 1); `sh` has two floats per wave.
+template <int WV>
+__device__ __forceinline__ float2 row_sum(float2 v, float2* sh) {
+  v.x = wave_sum(v.x);
+  v.y = wave_sum(v.y);
+  if constexpr (WV > 1) {
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = sh[0];
+#pragma unroll
+    for (int i = 1; i < WV; ++i) v.x += sh[i].x, v.y += sh[i].y;
+  }
+  return v;
+}
+
+constexpr int threads_of(int wv) { return wv == 1 ? 256 : wv * 64; }
+
+template <class E, int VEC, int NV, int WV>
+__global__ void __launch_bounds__(threads_of(WV)) fwd_kernel(Args a) {
+  constexpr int kT = WV * 64, kRows = threads_of(WV) / kT;
+  __shared__ float2 sh[2][WV];
+  const int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / kT;
+  if (t >= a.T) return;      // whole waves; with WV > 1 a workgroup has one row
+  const int l = threadIdx.x % kT;
+  const E* x = static_cast<const E*>(a.X) + t * a.ldx;
+  E* y = static_cast<E*>(a.Y) + t * a.ldy;
+  const int nv = a.n / VEC;
+  float v[NV][VEC];
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = i * kT + l;
+    if (c < nv) {
+      Pack<E, VEC>::get(x + (int64_t)c * VEC, v[i]);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) s += v[i][k];
+    }
+  }
+  const float mu = row_sum<WV>(make_float2(s, 0.f), sh[0]).x / (float)a.n;
+  float q = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (i * kT + l < nv) {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        v[i][k] -= mu;
+        q = fmaf(v[i][k], v[i][k], q);
+      }
+    }
+  const float var = row_sum<WV>(make_float2(q, 0.f), sh[1]).x / (float)a.n;
+  const float r = 1.f / sqrtf(var + a.eps);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = i * kT + l;
+    if (c < nv) {
+      float w[VEC], b[VEC];
+      vector_at<VEC>(a.weight, a.w_bf16, a.vec_w, 1.f, c * VEC, w);
+      vector_at<VEC>(a.bias, a.w_bf16, a.vec_w, 0.f, c * VEC, b);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) w[k] = fmaf(v[i][k] * r, w[k], b[k]);
+      Pack<E, VEC>::put(y + (int64_t)c * VEC, w);
+    }
+  }
+  if (l == 0) {
+    if (a.mean) a.mean[t] = mu;
+    if (a.rstd) a.rstd[t] = r;
+  }
+}
+
+// Rows too wide for the registers: read three times.
+template <class E>
+__global__ void __launch_bounds__(1024) fwd_wide_kernel(Args a) {
+  __shared__ float2 sh[2][16];
+  const int64_t t = blockIdx.x;
+  const E* x = static_cast<const E*>(a.X) + t * a.ldx;
+  E* y = static_cast<E*>(a.Y) + t * a.ldy;
+  float s = 0.f;
+  for (int c = threadIdx.x; c < a.n; c += 1024) s += (float)x[c];
+  const float mu = row_sum<16>(make_float2(s, 0.f), sh[0]).x / (float)a.n;
+  float q = 0.f;
+  for (int c = threadIdx.x; c < a.n; c += 1024) {
+    const float d = (float)x[c] - mu;
+    q = fmaf(d, d, q);
+  }
+  const float r = 1.f / sqrtf(row_sum<16>(make_float2(q, 0.f), sh[1]).x / (float)a.n + a.eps);
+  for (int c = threadIdx.x; c < a.n; c += 1024) {
+    float w, b;
+    vector_at<1>(a.weight, a.w_bf16, 0, 1.f, c, &w);
+    vector_at<1>(a.bias, a.w_bf16, 0, 0.f, c, &b);
+    y[c] = (E)fmaf(((float)x[c] - mu) * r, w, b);
+  }
+  if (threadIdx.x == 0) {
+    if (a.mean) a.mean[t] = mu;
+    if (a.rstd) a.rstd[t] = r;
+  }
+}
+
+template <class E, int VEC, int NV, int WV>
+__global__ void __launch_bounds__(threads_of(WV)) bwd_kernel(Args a) {
+  constexpr int kT = WV * 64, kRows = threads_of(WV) / kT;
+  __shared__ float2 sh[2][WV];
+  __shared__ float comb[kRows > 1 ? 2 * NV * VEC * kT : 1];
+  const int l = threadIdx.x % kT, sub = threadIdx.x / kT;
+  const int nv = a.n / VEC;
+  float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = i * kT + l;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) w[i][k] = dw[i][k] = db[i][k] = 0.f;
+    if (c < nv) vector_at<VEC>(a.weight, a.w_bf16, a.vec_w, 1.f, c * VEC, w[i]);
+  }
+  const float inv_n = 1.f / (float)a.n;
+  int turn = 0;
+  for (int64_t t = (int64_t)blockIdx.x * kRows + sub; t < a.T; t += (int64_t)gridDim.x * kRows, turn ^= 1) {
+    const E* x = static_cast<const E*>(a.X) + t * a.ldx;
+    const E* g = static_cast<const E*>(a.G) + t * a.ldg;
+    const float mu = a.mean[t], r = a.rstd[t];
+    float h[NV][VEC], gg[NV][VEC];
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * kT + l;
+      if (c < nv) {
+        Pack<E, VEC>::get(x + (int64_t)c * VEC, h[i]);
+        Pack<E, VEC>::get(g + (int64_t)c * VEC, gg[i]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) h[i][k] = mu, gg[i][k] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        h[i][k] = (h[i][k] - mu) * r;
+        dw[i][k] = fmaf(gg[i][k], h[i][k], dw[i][k]);
+        db[i][k] += gg[i][k];
+        gg[i][k] *= w[i][k];
+        s.x += gg[i][k];
+        s.y = fmaf(gg[i][k], h[i][k], s.y);
+      }
+    if (!a.Y) continue;
+    s = row_sum<WV>(s, sh[turn]);
+    const float ma = s.x * inv_n, mh = s.y * inv_n;
+    E* dx = static_cast<E*>(a.Y) + t * a.ldy;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * kT + l;
+      if (c < nv) {
+        float o[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) o[k] = r * (gg[i][k] - ma - h[i][k] * mh);
+        if (a.beta != 0.f) {
+          float old[VEC];
+          Pack<E, VEC>::get(dx + (int64_t)c * VEC, old);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) o[k] = fmaf(a.beta, old[k], o[k]);
+        }
+        Pack<E, VEC>::put(dx + (int64_t)c * VEC, o);
+      }
+    }
+  }
+  if (!a.part) return;
+  if constexpr (kRows > 1) {
+    // the workgroup's rows in turn: a fixed order
+    float* mine = comb + l * VEC;
+    for (int q = 0; q < kRows; ++q) {
+      if (q == sub)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            float* p = mine + i * kT * VEC + k;
+            p[0] = q ? p[0] + dw[i][k] : dw[i][k];
+            p[NV * VEC * kT] = q ? p[NV * VEC * kT] + db[i][k] : db[i][k];
+          }
+      __syncthreads();
+    }
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+    for (int c = threadIdx.x; c < a.n; c += threads_of(WV)) {
+      part[c] = comb[c];
+      part[a.n + c] = comb[NV * VEC * kT + c];
+    }
+  } else {
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * kT + l;
+      if (c < nv)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          part[c * VEC + k] = dw[i][k];
+          part[a.n + c * VEC + k] = db[i][k];
+        }
+    }
+  }
+}
+
+// Rows too wide for the registers: dx row by row.
+template <class E>
+__global__ void __launch_bounds__(1024) bwd_wide_kernel(Args a) {
+  __shared__ float2 sh[16];
+  const int64_t t = blockIdx.x;
+  const E* x = static_cast<const E*>(a.X) + t * a.ldx;
+  const E* g = static_cast<const E*>(a.G) + t * a.ldg;
+  E* dx = static_cast<E*>(a.Y) + t * a.ldy;
+  const float mu = a.mean[t], r = a.rstd[t];
+  float2 s = make_float2(0.f, 0.f);
+  for (int c = threadIdx.x; c < a.n; c += 1024) {
+    float w;
+    vector_at<1>(a.weight, a.w_bf16, 0, 1.f, c, &w);
+    w *= (float)g[c];
+    s.x += w;
+    s.y = fmaf(w, ((float)x[c] - mu) * r, s.y);
+  }
+  s = row_sum<16>(s, sh);
+  const float ma = s.x / (float)a.n, mh = s.y / (float)a.n;
+  for (int c = threadIdx.x; c < a.n; c += 1024) {
+    float w;
+    vector_at<1>(a.weight, a.w_bf16, 0, 1.f, c, &w);
+    float o = r * (w * (float)g[c] - ma - ((float)x[c] - mu) * r * mh);
+    if (a.beta != 0.f) o = fmaf(a.beta, (float)dx[c], o);
+    dx[c] = (E)o;
+  }
+}
+// and dw, db: a workgroup takes 256 columns of a share of the rows
+template <class E>
+__global__ void __launch_bounds__(256) bwd_wide_vectors_kernel(Args a) {
+  const int c = blockIdx.y * 256 + threadIdx.x;
+  if (c >= a.n) return;
+  float dw = 0.f, db = 0.f;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const float g = (float)(static_cast<const E*>(a.G) + t * a.ldg)[c];
+    dw = fmaf(g, ((float)(static_cast<const E*>(a.X) + t * a.ldx)[c] - a.mean[t]) * a.rstd[t], dw);
+    db += g;
+  }
+  float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+  part[c] = dw;
+  part[a.n + c] = db;
+}
+
+// out (dw then db) = [out +] sum over the partial rows: 64 columns x 16 shares of the rows per workgroup.
+__global__ void __launch_bounds__(1024) vector_sum_kernel(const float* part, int rows, int n, int add, float* dw, float* db) {
+  __shared__ float sh[16][64];
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
+  float s = 0.f;
+  if (c < 2 * n)
+    for (int r = q; r < rows; r += 16) s += part[(int64_t)r * 2 * n + c];
+  sh[q][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (q || c >= 2 * n) return;
+  for (int i = 1; i < 16; ++i) s += sh[i][threadIdx.x];
+  float* out = c < n ? dw : db;
+  if (!out) return;
+  out += c < n ? c : c - n;
+  *out = add ? *out + s : s;
+}
+
+// ------------------------------------------------------------------------------------------- dispatch
+
+// The instance of a row of n: pieces of a thread and waves of a row.  A wave takes rows of up to four pieces a lane
+// (bf16: 2048 wide), four waves up to four, sixteen up to eight; wider rows (and unaligned ones past 32768) are read
+// three times.
+struct Shape {
+  int vec, nv, wv;   // wv 0: wide
+};
+Shape shape_of(int64_t n, int esz, bool aligned) {
+  const int vec = aligned && n % (16 / esz) == 0 ? 16 / esz : 1;
+  const int64_t p = n / vec;
+  const int most = vec == 1 ? 32 : 4;
+  auto fit = [&](int wv, int limit) -> int {
+    for (int nv : {1, 2, 4, 8, 16, 32})
+      if (nv <= limit && p <= (int64_t)nv * wv * 64) return nv;
+    return 0;
+  };
+  if (int nv = fit(1, vec == 1 ? 16 : most)) return {vec, nv, 1};
+  if (int nv = fit(4, vec == 1 ? 16 : most)) return {vec, nv, 4};
+  if (int nv = fit(16, vec == 1 ? 32 : (esz == 4 ? 8 : 4))) return {vec, nv, 16};
+  return {vec, 0, 0};
+}
+
+constexpr int kGroups = 512;    // workgroups (partial rows) of a backward at most
+int groups_of(int64_t T, const Shape& s) {
+  const int rows = s.wv == 1 ? 4 : 1;
+  const int64_t g = (T + rows - 1) / rows;
+  return (int)(g < kGroups ? g : kGroups);
+}
+
+template <class E, int VEC, int NV, int WV>
+void launch(const Args& a, bool bwd, int groups, hipStream_t s) {
+  constexpr int kRows = threads_of(WV) / (WV * 64);
+  const dim3 block(threads_of(WV));
+  if (bwd)
+    hipLaunchKernelGGL((bwd_kernel<E, VEC, NV, WV>), dim3((unsigned)groups), block, 0, s, a);
+  else
+    hipLaunchKernelGGL((fwd_kernel<E, VEC, NV, WV>), dim3((unsigned)((a.T + kRows - 1) / kRows)), block, 0, s, a);
+}
+
+template <class E, int VEC, int WV>
+bool launch_nv(const Args& a, int nv, bool bwd, int groups, hipStream_t s) {
+  if constexpr (VEC == 1) {
+    switch (nv) {
+      case 1: case 2: case 4: launch<E, VEC, 4, WV>(a, bwd, groups, s); return true;
+      case 8: case 16: launch<E, VEC, 16, WV>(a, bwd, groups, s); return true;
+      case 32:
+        if constexpr (WV == 16) {
+          launch<E, VEC, 32, WV>(a, bwd, groups, s);
+          return true;
+        }
+    }
+  } else {
+    switch (nv) {
+      case 1: launch<E, VEC, 1, WV>(a, bwd, groups, s); return true;
+      case 2: launch<E, VEC, 2, WV>(a, bwd, groups, s); return true;
+      case 4: launch<E, VEC, 4, WV>(a, bwd, groups, s); return true;
+      case 8:
+        if constexpr (sizeof(E) == 4 && WV == 16) {
+          launch<E, VEC, 8, WV>(a, bwd, groups, s);
+          return true;
+        }
+    }
+  }
+  return false;
+}
+
+template <class E>
+hipError_t run(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t s) {
+  constexpr int V = 16 / (int)sizeof(E);
+  if (sh.wv == 0) {
+    if (!bwd) {
+      hipLaunchKernelGGL(fwd_wide_kernel<E>, dim3((unsigned)a.T), dim3(1024), 0, s, a);
+    } else {
+      if (a.Y) hipLaunchKernelGGL(bwd_wide_kernel<E>, dim3((unsigned)a.T), dim3(1024), 0, s, a);
+      if (a.part)
+        hipLaunchKernelGGL(bwd_wide_vectors_kernel<E>, dim3((unsigned)groups, (unsigned)((a.n + 255) / 256)), dim3(256), 0,
+                           s, a);
+    }
+    return hipGetLastError();
+  }
+  bool ok;
+  if (sh.vec == 1)
+    ok = sh.wv == 1 ? launch_nv<E, 1, 1>(a, sh.nv, bwd, groups, s)
+         : sh.wv == 4 ? launch_nv<E, 1, 4>(a, sh.nv, bwd, groups, s)
+                      : launch_nv<E, 1, 16>(a, sh.nv, bwd, groups, s);
+  else
+    ok = sh.wv == 1 ? launch_nv<E, V, 1>(a, sh.nv, bwd, groups, s)
+         : sh.wv == 4 ? launch_nv<E, V, 4>(a, sh.nv, bwd, groups, s)
+                      : launch_nv<E, V, 16>(a, sh.nv, bwd, groups, s);
+  return ok ? hipGetLastError() : hipErrorInvalidConfiguration;
+}
+
+ff_status check_rows(const char* name, const void* p, int64_t ld, int64_t n, int esz) {
+  if (!p) return fail(FF_EINVAL, "%s is NULL", name);
+  if (ld < n) return fail(FF_EINVAL, "leading dimension of %s (%lld) < %lld", name, (long long)ld, (long long)n);
+  if ((uintptr_t)p % esz) return fail(FF_EINVAL, "%s is misaligned", name);
+  return FF_OK;
+}
+
+ff_status check_sizes(int64_t T, int64_t n, int act, int w_dtype) {
+  if (act != FF_F32 && act != FF_BF16) return fail(FF_EINVAL, "unknown activation dtype %d", act);
+  if (w_dtype != FF_F32 && w_dtype != FF_BF16) return fail(FF_EINVAL, "unknown weight dtype %d", w_dtype);
+  if (T < 0 || T > ((int64_t)1 << 30) || n < 1 || n > ((int64_t)1 << 24))
+    return fail(FF_EINVAL, "T=%lld or n=%lld out of range", (long long)T, (long long)n);
+  return FF_OK;
+}
+
+bool whole(const void* p, int64_t ld, int esz) { return (uintptr_t)p % 16 == 0 && ld * esz % 16 == 0; }
+
+}  // namespace norm
+}  // namespace ff
+
+extern "C" {
+
+ff_status ff_layernorm_fwd(int64_t T, int64_t n, int act, const void* X, int64_t ldx, int w_dtype, const void* weight,
+                           const void* bias, float eps, void* Y, int64_t ldy, float* mean, float* rstd, void* stream) {
+  using namespace ff::norm;
+  ff::clear_error();
+  ff_status st = check_sizes(T, n, act, w_dtype);
+  if (st != FF_OK) return st;
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return ff::fail(FF_EINVAL, "eps=%g must be finite and >= 0", (double)eps);
+  if (T == 0) return FF_OK;
+  const int esz = act == FF_BF16 ? 2 : 4, wsz = w_dtype == FF_BF16 ? 2 : 4;
+  if ((st = check_rows("X", X, ldx, n, esz)) != FF_OK) return st;
+  if ((st = check_rows("Y", Y, ldy, n, esz)) != FF_OK) return st;
+  if ((uintptr_t)weight % wsz || (uintptr_t)bias % wsz || (uintptr_t)mean % 4 || (uintptr_t)rstd % 4)
+    return ff::fail(FF_EINVAL, "weight, bias, mean or rstd is misaligned");
+  Args a{};
+  a.X = X, a.Y = Y, a.ldx = ldx, a.ldy = ldy, a.T = T, a.n = (int)n, a.weight = weight, a.bias = bias;
+  a.w_bf16 = w_dtype == FF_BF16, a.eps = eps, a.mean = mean, a.rstd = rstd;
+  a.vec_w = (uintptr_t)weight % 16 == 0 && (uintptr_t)bias % 16 == 0;
+  const Shape sh = shape_of(n, esz, whole(X, ldx, esz) && whole(Y, ldy, esz));
+  const hipError_t e = act == FF_BF16 ? run<__bf16>(a, sh, false, 0, (hipStream_t)stream)
+                                      : run<float>(a, sh, false, 0, (hipStream_t)stream);
+  return e == hipSuccess ? FF_OK : ff::fail(FF_EDEVICE, "layer norm forward: %s", hipGetErrorString(e));
+}
+
+ff_status ff_layernorm_workspace(int64_t T, int64_t n, int64_t* bytes) {
+  ff::clear_error();
+  ff_status st = ff::norm::check_sizes(T, n, FF_F32, FF_F32);
+  if (st != FF_OK) return st;
+  if (!bytes) return ff::fail(FF_EINVAL, "bytes is NULL");
+  const int64_t rows = T < ff::norm::kGroups ? (T ? T : 1) : ff::norm::kGroups;
+  *bytes = rows * 2 * n * 4;
+  return FF_OK;
+}
+
+ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t ldx, const void* G, int64_t ldg,
+                           int w_dtype, const void* weight, const float* mean, const float* rstd, float beta_dx, void* dX,
+                           int64_t lddx, int accumulate_dw, float* dweight, float* dbias, void* workspace,
+                           int64_t workspace_bytes, void* stream) {
+  using namespace ff::norm;
+  ff::clear_error();
+  ff_status st = check_sizes(T, n, act, w_dtype);
+  if (st != FF_OK) return st;
+  if ((uintptr_t)dweight % 4 || (uintptr_t)dbias % 4) return ff::fail(FF_EINVAL, "dweight or dbias is misaligned");
+  const bool vectors = dweight || dbias;
+  if (!dX && !vectors) return FF_OK;
+  const int esz = act == FF_BF16 ? 2 : 4, wsz = w_dtype == FF_BF16 ? 2 : 4;
+  int groups = 0;
+  Args a{};
+  if (T > 0) {
+    if ((st = check_rows("X", X, ldx, n, esz)) != FF_OK) return st;
+    if ((st = check_rows("G", G, ldg, n, esz)) != FF_OK) return st;
+    if (dX && (st = check_rows("dX", dX, lddx, n, esz)) != FF_OK) return st;
+    if (!mean || !rstd) return ff::fail(FF_EINVAL, "mean or rstd is NULL");
+    if ((uintptr_t)weight % wsz || (uintptr_t)mean % 4 || (uintptr_t)rstd % 4)
+      return ff::fail(FF_EINVAL, "weight, mean or rstd is misaligned");
+    const Shape sh = shape_of(n, esz, whole(X, ldx, esz) && whole(G, ldg, esz) && (!dX || whole(dX, lddx, esz)));
+    groups = groups_of(T, sh);
+    if (vectors) {
+      if (!workspace || (uintptr_t)workspace % 16) return ff::fail(FF_EINVAL, "the workspace is NULL or not 16-byte aligned");
+      const int64_t need = (int64_t)groups * 2 * n * 4;
+      if (workspace_bytes < need)
+        return ff::fail(FF_EINVAL, "the workspace holds %lld bytes, the call needs %lld", (long long)workspace_bytes,
+                        (long long)need);
+    }
+    a.X = X, a.G = G, a.Y = dX, a.ldx = ldx, a.ldg = ldg, a.ldy = lddx, a.T = T, a.n = (int)n, a.weight = weight;
+    a.w_bf16 = w_dtype == FF_BF16, a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd), a.beta = beta_dx;
+    a.part = vectors ? static_cast<float*>(workspace) : nullptr;
+    a.vec_w = (uintptr_t)weight % 16 == 0;
+    const hipError_t e = act == FF_BF16 ? run<__bf16>(a, sh, true, groups, (hipStream_t)stream)
+                                        : run<float>(a, sh, true, groups, (hipStream_t)stream);
+    if (e != hipSuccess) return ff::fail(FF_EDEVICE, "layer norm backward: %s", hipGetErrorString(e));
+  }
+  if (vectors) {
+    hipLaunchKernelGGL(vector_sum_kernel, dim3((unsigned)((2 * n + 63) / 64)), dim3(1024), 0, (hipStream_t)stream, a.part,
+                       groups, (int)n, accumulate_dw, dweight, dbias);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return ff::fail(FF_EDEVICE, "layer norm backward: %s", hipGetErrorString(e));
+  }
+  return FF_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,581 @@
+// Cross entropy of a head's logits, forward and gradient, without keeping the logits.
+//
+// With H (T x n) the activations, W (V x n) the head, z = H W^T:
+//   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,target
+//   P_tv  = (exp(z_tv - lse_t) - [v = target_t]) scale dloss_t,   dH = P W,   dW = P^T H
+// Tokens whose target is no vocabulary entry have loss 0 and P = 0.
+//
+// The products run on MFMA (xent_gemm.h).  Only P, in the activations' type, passes through memory, a bounded
+// piece of it at a time:
+//   loss alone      logits product whose epilogue leaves (maximum, sum of exponentials) per token and wave's columns
+//                   and the target's logit; nothing of the logits is written.
+//   loss + gradient the same product also writes e = exp(z - maximum of the wave's columns); when the statistics
+//                   of a token are joined, e becomes P in place: 2 products (3 with dW) instead of the 3 (4) of a
+//                   backward that computes the logits again.
+//   backward alone  logits product whose epilogue writes P from the saved lse.
+// P is kept in the activations' type: each of its values carries one rounding (two where e is stored first, each of
+// 2^-9 relative in bf16), as do the factors W and H.  The sums of exponentials leave the target out: its own value of P,
+// exp(z - lse) - 1, is then minus the others' share, and the loss of a token whose target has the largest logit is log(1 +
+// others), so that both keep their digits when the target's probability is near one.
+// Long calls are cut into pieces of tokens (P of a piece at most kPieceBytes), whose dH are complete.  With dW a cut
+// by tokens would have to add up V x n sums in fp32, so there the pieces are of the vocabulary (dW rows complete,
+// dH summed in fp32), and the forward runs by itself first.
+#include <cmath>
+
+#include "xent_gemm.h"
+
+namespace ff {
+namespace xent {
+
+hipError_t launch_gemm_0_0(int tile, const GemmArgs& a, hipStream_t s);
+hipError_t launch_gemm_0_1(int tile, const GemmArgs& a, hipStream_t s);
+hipError_t launch_gemm_1_0(int tile, const GemmArgs& a, hipStream_t s);
+hipError_t launch_gemm_1_1(int tile, const GemmArgs& a, hipStream_t s);
+hipError_t launch_gemm_2_0(int tile, const GemmArgs& a, hipStream_t s);
+hipError_t launch_gemm_2_1(int tile, const GemmArgs& a, hipStream_t s);
+
+hipError_t launch_gemm(int layout, int bf16, int tile, const GemmArgs& a, hipStream_t s) {
+  switch (layout * 2 + bf16) {
+    case 0: return launch_gemm_0_0(tile, a, s);
+    case 1: return launch_gemm_0_1(tile, a, s);
+    case 2: return launch_gemm_1_0(tile, a, s);
+    case 3: return launch_gemm_1_1(tile, a, s);
+    case 4: return launch_gemm_2_0(tile, a, s);
+    default: return launch_gemm_2_1(tile, a, s);
+  }
+}
+
+namespace {
+
+// Joins the statistics of a token's columns: 16 tokens x 16 shares of the entries per workgroup.
+__global__ void __launch_bounds__(256) combine_kernel(const float2* stats, int nstat, int N, const int64_t* target,
+                                                      int64_t vocab, float* zt, float* loss, float* lse) {
+  __shared__ float2 sh[16][17];
+  const int tk = threadIdx.x & 15, part = threadIdx.x >> 4;
+  const int t = blockIdx.x * 16 + tk;
+  float top = -INFINITY, sum = 0.f;
+  if (t < N)
+    for (int i = part; i < nstat; i += 16) {
+      const float2 s = stats[(int64_t)i * N + t];
+      const float m = fmaxf(top, s.x);
+      // columns of -inf have sum 0, a NaN logit makes the sum NaN
+      const float ref = m == -INFINITY ? 0.f : m;
+      sum = sum * expf(top - ref) + s.y * expf(s.x - ref);
+      top = m;
+    }
+  sh[part][tk] = make_float2(top, sum);
+  __syncthreads();
+  if (part || t >= N) return;
+  float m = -INFINITY;
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, sh[i][tk].x);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float others = 0.f;
+  for (int i = 0; i < 16; ++i) others += sh[i][tk].y * expf(sh[i][tk].x - ref);
+  const int64_t tg = target[t];
+  if (tg >= 0 && tg < vocab) {
+    const float z = zt[t], total = others + expf(z - m), ls = logf(total);
+    lse[t] = m + ls;
+    loss[t] = z == m ? log1pf(others) : (m - z) + ls;
+    zt[t] = -others / total;     // the target's value of P before its weight
+  } else {
+    lse[t] = m + logf(others);
+    loss[t] = 0.f;
+  }
+}
+
+template <class E>
+struct Piece16;   // a 16-byte piece as floats
+template <>
+struct Piece16<__bf16> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ void get(const __bf16* p, float* v) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+      v[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ void put(__bf16* p, const float* v) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (unsigned)bf16_bits(v[2 * i]) | (unsigned)bf16_bits(v[2 * i + 1]) << 16;
+    *reinterpret_cast<u32x4*>(p) = w;
+  }
+};
+template <>
+struct Piece16<float> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ void get(const float* p, float* v) {
+    const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = w[i];
+  }
+  static __device__ __forceinline__ void put(float* p, const float* v) {
+    const f32x4 w = {v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4*>(p) = w;
+  }
+};
+
+// e = exp(z - maximum of its columns) -> P, in place.  Bound by memory: P is read and written once.
+constexpr int kRescaleRow = 4;   // pieces per thread
+template <class E>
+__global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int N, int V, const float2* stats, int cols,
+                                                      const int64_t* target, const float* own, const float* lse,
+                                                      const float* dloss, float scale) {
+  constexpr int kN = Piece16<E>::kN;
+  const int t = blockIdx.y;
+  const int64_t tg = target[t];
+  const bool counted = tg >= 0 && tg < V;
+  const float w = counted ? scale * (dloss ? dloss[t] : 1.f) : 0.f;
+  const float ls = lse[t];
+  E* row = P + (int64_t)t * ldp;
+#pragma unroll
+  for (int q = 0; q < kRescaleRow; ++q) {
+    const int c = ((blockIdx.x * kRescaleRow + q) * 256 + threadIdx.x) * kN;
+    if (c >= ldp) return;
+    float v[kN];
+    if (counted) {
+      Piece16<E>::get(row + c, v);
+      // columns past V hold zeros; their entry may be one past the statistics' last
+      const float f = c < V ? expf(stats[(int64_t)(c / cols) * N + t].x - ls) * w : 0.f;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) v[i] *= f;
+      if (tg >= c && tg < c + kN) {
+        const float p = own[t] * w;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] = tg == c + i ? p : v[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) v[i] = 0.f;
+    }
+    Piece16<E>::put(row + c, v);
+  }
+}
+
+// out = beta out + sum over the splits of part: N x M, M a multiple of four.
+template <class E>
+__global__ void __launch_bounds__(256) sum_kernel(const float* part, int splits, int64_t N, int M, float beta, E* out,
+                                                  int64_t ldo) {
+  const int64_t per = M / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= N * per) return;
+  const int64_t row = id / per;
+  const int c = (int)(id - row * per) * 4;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) v += load4(part + ((int64_t)s * N + row) * M + c);
+  E* p = out + row * ldo + c;
+  if (beta != 0.f) v += beta * load4(p);
+  store4(p, v);
+}
+
+// Rows of H with a target; zeros elsewhere, so that nothing a skipped token holds (NaN, infinities) reaches dW, where
+// its zero of P would be multiplied by it.
+template <class E>
+__global__ void __launch_bounds__(256) live_rows_kernel(const E* H, int64_t ldh, int64_t T, int n, const int64_t* target,
+                                                        int64_t vocab, E* out) {
+  constexpr int kN = Piece16<E>::kN;
+  const int64_t per = n / kN, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= T * per) return;
+  const int64_t t = id / per;
+  const int c = (int)(id - t * per) * kN;
+  const int64_t tg = target[t];
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (tg >= 0 && tg < vocab) v = *reinterpret_cast<const u32x4*>(H + t * ldh + c);
+  *reinterpret_cast<u32x4*>(out + t * n + c) = v;
+}
+
+// ------------------------------------------------------------------------------------------- plan of a call
+
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // P of one piece
+constexpr int64_t kStatBytes = (int64_t)64 << 20;     // statistics of one piece
+constexpr int kCUs = 256;
+
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+int64_t tiles_of(int64_t M, int64_t N, int t) { return up(M, tile_m(t)) / tile_m(t) * (up(N, tile_n(t)) / tile_n(t)); }
+
+struct Product {
+  int tile;
+  int splits;
+  int kt_split;
+};
+
+// Tile and split of k of a product with M columns, N rows and kt k tiles.
+Product choose(int64_t M, int64_t N, int64_t kt, bool may_split) {
+  Product p{kSmall, 1, (int)kt};
+  if (N > 32) {
+    if (N >= 192 && M >= 192 && tiles_of(M, N, kLarge) * (may_split ? kt / 8 + 1 : 1) >= kCUs / 2) p.tile = kLarge;
+    else if (tiles_of(M, N, kMedium) * (may_split ? kt / 8 + 1 : 1) >= kCUs / 2) p.tile = kMedium;
+  }
+  if (may_split) {
+    const int64_t want = p.tile == kLarge ? kCUs : 2 * kCUs, have = tiles_of(M, N, p.tile);
+    int64_t s = want / have;
+    if (s > kt / 8) s = kt / 8;
+    if (s > 64) s = 64;
+    if (s < 1) s = 1;
+    p.kt_split = (int)((kt + s - 1) / s);
+    p.splits = (int)((kt + p.kt_split - 1) / p.kt_split);
+  }
+  return p;
+}
+
+struct Call {
+  int64_t T, n, V;
+  int bf16, esz, kk;        // kk: k of a tile
+  bool dh, dw;
+  int64_t Tp, Vp;           // tokens and vocabulary entries of a piece of P
+  int64_t Tf;               // tokens of a piece of the forward alone
+  bool by_vocab;            // pieces of the vocabulary (dW of a long call)
+  size_t off_p, off_stats, off_zt, off_part, off_live, bytes;
+};
+
+Product logits_product(const Call& c, int64_t N, int64_t M) { return choose(M, N, up(c.n, c.kk) / c.kk, false); }
+Product dh_product(const Call& c, int64_t N, int64_t K) { return choose(c.n, N, up(K, c.kk) / c.kk, true); }
+Product dw_product(const Call& c, int64_t M, int64_t K) {
+  // sums of a whole head are not worth a pass through memory
+  return choose(c.n, M, up(K, c.kk) / c.kk, M <= 4096);
+}
+
+Call plan(int64_t T, int64_t n, int64_t V, int act, bool dh, bool dw) {
+  Call c{};
+  c.T = T, c.n = n, c.V = V, c.bf16 = act == FF_BF16, c.esz = c.bf16 ? 2 : 4, c.kk = 128 / c.esz;
+  c.dh = dh, c.dw = dw;
+  c.bytes = 256;
+  if (T == 0) return c;
+  const int64_t ldp = up(V, 64);
+  int64_t most = kPieceBytes / (ldp * c.esz) / 256 * 256;
+  if (most < 256) most = 256;
+  c.by_vocab = dw && T > most;
+  c.Tp = c.by_vocab || T < most ? T : most;
+  c.Vp = V;
+  if (c.by_vocab) {
+    c.Vp = kPieceBytes / (T * c.esz) / 256 * 256;
+    if (c.Vp < 256) c.Vp = 256;
+    if (c.Vp > V) c.Vp = V;
+  }
+  const int64_t entries = up(V, 32) / 32;   // at most, with the small tile's columns
+  c.Tf = kStatBytes / (8 * entries) / 256 * 256;
+  if (c.Tf < 256) c.Tf = 256;
+  if (c.Tf > T) c.Tf = T;
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t o = at;
+    at += (size_t)up(bytes, 256);
+    return o;
+  };
+  const bool grad = dh || dw;
+  c.off_p = take(grad ? c.Tp * up(c.Vp, 64) * c.esz : 0);
+  // small tiles have 32 columns per entry; they serve few tokens or few columns
+  const int64_t rows = c.by_vocab || !grad ? c.Tf : (c.Tp > c.Tf ? c.Tp : c.Tf);
+  c.off_stats = take(rows * entries * 8);
+  c.off_zt = take(rows * 4);
+  int64_t part = 0;
+  auto more = [&](int64_t b) { part = b > part ? b : part; };
+  if (dh)
+    for (int64_t N : {c.Tp, T % c.Tp ? T % c.Tp : c.Tp}) {
+      const Product p = dh_product(c, N, c.Vp);
+      if (p.splits > 1 || c.by_vocab) more((int64_t)p.splits * N * n * 4);
+    }
+  if (dw && !c.by_vocab) {
+    const Product p = dw_product(c, V, T);
+    if (p.splits > 1) more((int64_t)p.splits * V * n * 4);
+  }
+  c.off_part = take(part);
+  c.off_live = take(dw ? T * n * c.esz : 0);
+  c.bytes = at < 256 ? 256 : at;
+  return c;
+}
+
+struct Tensors {
+  const char* H;
+  int64_t ldh;
+  const char* W;
+  int64_t ldw;
+  const int64_t* target;
+  const float* dloss;
+  float scale;
+  float* loss;
+  float* lse;
+  float beta_dh, beta_dw;
+  char* dH;
+  int64_t lddh;
+  char* dW;
+  int64_t lddw;
+  char* ws;
+  hipStream_t s;
+};
+
+#define XENT_TRY(call)                   \
+  do {                                   \
+    const hipError_t e_ = (call);        \
+    if (e_ != hipSuccess) return e_;     \
+  } while (0)
+
+// tokens t0 .. t0 + N - 1, vocabulary entries v0 .. v0 + M - 1
+hipError_t run_logits(const Call& c, const Tensors& x, int64_t t0, int64_t N, int64_t v0, int64_t M, int mode,
+                      int* stat) {
+  const Product p = logits_product(c, N, M);
+  GemmArgs a{};
+  a.A = x.W + v0 * x.ldw * c.esz, a.lda = x.ldw;
+  a.B = x.H + t0 * x.ldh * c.esz, a.ldb = x.ldh;
+  a.M = (int)M, a.N = (int)N, a.K = (int)c.n;
+  a.tm = (int)(up(M, tile_m(p.tile)) / tile_m(p.tile)), a.tn = (int)(up(N, tile_n(p.tile)) / tile_n(p.tile));
+  a.kt = a.kt_split = p.kt_split, a.splits = 1, a.mode = mode;
+  a.out = x.ws + c.off_p, a.ldo = up(M, 64), a.ocols = (int)up(M, 64);
+  a.stats = reinterpret_cast<float2*>(x.ws + c.off_stats);
+  a.target = x.target + t0, a.v0 = v0, a.vocab = c.V;
+  a.zt = reinterpret_cast<float*>(x.ws + c.off_zt);
+  a.lse = x.lse + t0, a.loss = x.loss ? x.loss + t0 : nullptr, a.dloss = x.dloss ? x.dloss + t0 : nullptr, a.scale = x.scale;
+  *stat = stat_cols(p.tile);
+  return launch_gemm(0, c.bf16, p.tile, a, x.s);
+}
+
+hipError_t run_combine(const Call& c, const Tensors& x, int64_t t0, int64_t N, int stat) {
+  hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((N + 15) / 16)), dim3(256), 0, x.s,
+                     reinterpret_cast<const float2*>(x.ws + c.off_stats), (int)(up(c.V, stat) / stat), (int)N,
+                     x.target + t0, c.V, reinterpret_cast<float*>(x.ws + c.off_zt), x.loss + t0, x.lse + t0);
+  return hipGetLastError();
+}
+
+template <class E>
+void rescale(const Call& c, const Tensors& x, int64_t t0, int64_t N, int stat) {
+  const int64_t ldp = up(c.V, 64), seg = 256 * kRescaleRow * Piece16<E>::kN;
+  // rows in groups that fit the grid's second dimension
+  for (int64_t r = 0; r < N; r += 32768) {
+    const int64_t rows = N - r < 32768 ? N - r : 32768;
+    hipLaunchKernelGGL(rescale_kernel<E>, dim3((unsigned)((ldp + seg - 1) / seg), (unsigned)rows), dim3(256), 0, x.s,
+                       reinterpret_cast<E*>(x.ws + c.off_p) + r * ldp, ldp, (int)N, (int)c.V,
+                       reinterpret_cast<const float2*>(x.ws + c.off_stats) + r, stat, x.target + t0 + r,
+                       reinterpret_cast<const float*>(x.ws + c.off_zt) + r, x.lse + t0 + r, x.dloss ? x.dloss + t0 + r : nullptr, x.scale);
+  }
+}
+
+hipError_t run_sum(const Call& c, const Tensors& x, int splits, int64_t N, int64_t M, float beta, void* out, int64_t ldo) {
+  const int64_t threads = N * (M / 4);
+  if (threads == 0) return hipSuccess;
+  const dim3 grid((unsigned)((threads + 255) / 256));
+  const float* part = reinterpret_cast<const float*>(x.ws + c.off_part);
+  if (c.bf16)
+    hipLaunchKernelGGL(sum_kernel<__bf16>, grid, dim3(256), 0, x.s, part, splits, N, (int)M, beta,
+                       static_cast<__bf16*>(out), ldo);
+  else
+    hipLaunchKernelGGL(sum_kernel<float>, grid, dim3(256), 0, x.s, part, splits, N, (int)M, beta, static_cast<float*>(out),
+                       ldo);
+  return hipGetLastError();
+}
+
+// dH of tokens t0 .. from P of vocabulary entries v0 ..; first / last piece of the vocabulary
+hipError_t run_dh(const Call& c, const Tensors& x, int64_t t0, int64_t N, int64_t v0, int64_t M, bool first, bool last) {
+  const Product p = dh_product(c, N, c.Vp);     // the same split for every piece of the vocabulary
+  GemmArgs a{};
+  a.A = x.W + v0 * x.ldw * c.esz, a.lda = x.ldw;
+  a.B = x.ws + c.off_p, a.ldb = up(M, 64);
+  a.M = (int)c.n, a.N = (int)N, a.K = (int)M;
+  a.tm = (int)(up(c.n, tile_m(p.tile)) / tile_m(p.tile)), a.tn = (int)(up(N, tile_n(p.tile)) / tile_n(p.tile));
+  a.kt = (int)(up(M, c.kk) / c.kk), a.kt_split = p.kt_split, a.splits = p.splits;
+  const bool direct = p.splits == 1 && first && last;
+  void* out = x.dH + t0 * x.lddh * c.esz;
+  a.mode = direct ? kOut : kPart;
+  a.out = out, a.ldo = x.lddh, a.beta = x.beta_dh;
+  a.part = reinterpret_cast<float*>(x.ws + c.off_part), a.part_add = !first;
+  XENT_TRY(launch_gemm(1, c.bf16, p.tile, a, x.s));
+  return direct || !last ? hipSuccess : run_sum(c, x, p.splits, N, c.n, x.beta_dh, out, x.lddh);
+}
+
+// rows v0 .. v0 + M - 1 of dW from P of all tokens
+hipError_t run_dw(const Call& c, const Tensors& x, int64_t v0, int64_t M) {
+  Product p = dw_product(c, M, c.T);
+  if (c.by_vocab) p.splits = 1, p.kt_split = (int)(up(c.T, c.kk) / c.kk);   // the partial sums' place holds dH's
+  GemmArgs a{};
+  a.A = x.ws + c.off_live, a.lda = c.n;
+  a.B = x.ws + c.off_p, a.ldb = up(M, 64);
+  a.M = (int)c.n, a.N = (int)M, a.K = (int)c.T;
+  a.tm = (int)(up(c.n, tile_m(p.tile)) / tile_m(p.tile)), a.tn = (int)(up(M, tile_n(p.tile)) / tile_n(p.tile));
+  a.kt = (int)(up(c.T, c.kk) / c.kk), a.kt_split = p.kt_split, a.splits = p.splits;
+  void* out = x.dW + v0 * x.lddw * c.esz;
+  a.mode = p.splits == 1 ? kOut : kPart;
+  a.out = out, a.ldo = x.lddw, a.beta = x.beta_dw;
+  a.part = reinterpret_cast<float*>(x.ws + c.off_part);
+  XENT_TRY(launch_gemm(2, c.bf16, p.tile, a, x.s));
+  return p.splits == 1 ? hipSuccess : run_sum(c, x, p.splits, M, c.n, x.beta_dw, out, x.lddw);
+}
+
+hipError_t run_live_rows(const Call& c, const Tensors& x) {
+  const int64_t threads = c.T * (c.n * c.esz / 16);
+  const dim3 grid((unsigned)((threads + 255) / 256));
+  if (c.bf16)
+    hipLaunchKernelGGL(live_rows_kernel<__bf16>, grid, dim3(256), 0, x.s, reinterpret_cast<const __bf16*>(x.H), x.ldh,
+                       c.T, (int)c.n, x.target, c.V, reinterpret_cast<__bf16*>(x.ws + c.off_live));
+  else
+    hipLaunchKernelGGL(live_rows_kernel<float>, grid, dim3(256), 0, x.s, reinterpret_cast<const float*>(x.H), x.ldh, c.T,
+                       (int)c.n, x.target, c.V, reinterpret_cast<float*>(x.ws + c.off_live));
+  return hipGetLastError();
+}
+
+hipError_t run_fwd(const Call& c, const Tensors& x) {
+  for (int64_t t0 = 0; t0 < c.T; t0 += c.Tf) {
+    const int64_t N = c.T - t0 < c.Tf ? c.T - t0 : c.Tf;
+    int stat = 0;
+    XENT_TRY(run_logits(c, x, t0, N, 0, c.V, kStats, &stat));
+    XENT_TRY(run_combine(c, x, t0, N, stat));
+  }
+  return hipSuccess;
+}
+
+// step: with the forward (loss and lse written); otherwise from the saved lse
+hipError_t run_bwd(const Call& c, const Tensors& x, bool step) {
+  if (c.T == 0) return c.dw ? run_sum(c, x, 0, c.V, c.n, x.beta_dw, x.dW, x.lddw) : hipSuccess;
+  if (c.dw) XENT_TRY(run_live_rows(c, x));
+  int stat = 0;
+  if (c.by_vocab) {
+    if (step) XENT_TRY(run_fwd(c, x));
+    for (int64_t v0 = 0; v0 < c.V; v0 += c.Vp) {
+      const int64_t M = c.V - v0 < c.Vp ? c.V - v0 : c.Vp;
+      XENT_TRY(run_logits(c, x, 0, c.T, v0, M, kGrad, &stat));
+      if (c.dh) XENT_TRY(run_dh(c, x, 0, c.T, v0, M, v0 == 0, v0 + M == c.V));
+      XENT_TRY(run_dw(c, x, v0, M));
+    }
+    return hipSuccess;
+  }
+  for (int64_t t0 = 0; t0 < c.T; t0 += c.Tp) {
+    const int64_t N = c.T - t0 < c.Tp ? c.T - t0 : c.Tp;
+    XENT_TRY(run_logits(c, x, t0, N, 0, c.V, step ? kExp : kGrad, &stat));
+    if (step) {
+      XENT_TRY(run_combine(c, x, t0, N, stat));
+      if (c.bf16) rescale<__bf16>(c, x, t0, N, stat);
+      else rescale<float>(c, x, t0, N, stat);
+      XENT_TRY(hipGetLastError());
+    }
+    if (c.dh) XENT_TRY(run_dh(c, x, t0, N, 0, c.V, true, true));
+    if (c.dw) XENT_TRY(run_dw(c, x, 0, c.V));
+  }
+  return hipSuccess;
+}
+
+// ------------------------------------------------------------------------------------------- argument checks
+
+ff_status check_sizes(int64_t T, int64_t n, int64_t V, int act) {
+  if (act != FF_F32 && act != FF_BF16) return fail(FF_EINVAL, "unknown activation dtype %d", act);
+  const int64_t mult = act == FF_BF16 ? 8 : 4;
+  if (T < 0 || T > ((int64_t)1 << 28)) return fail(FF_EINVAL, "T=%lld out of range", (long long)T);
+  if (V < 1 || V > ((int64_t)1 << 24)) return fail(FF_EINVAL, "V=%lld out of range", (long long)V);
+  if (n < mult || n > ((int64_t)1 << 18) || n % mult)
+    return fail(FF_EINVAL, "n=%lld must be a multiple of %lld, at most 262144", (long long)n, (long long)mult);
+  return FF_OK;
+}
+
+ff_status check_rows(const char* name, const void* p, int64_t ld, int64_t n, int act) {
+  const int64_t mult = act == FF_BF16 ? 8 : 4;
+  if (!p) return fail(FF_EINVAL, "%s is NULL", name);
+  if (ld < n || ld > ((int64_t)1 << 20) || ld % mult)
+    return fail(FF_EINVAL, "leading dimension of %s (%lld) must be a multiple of %lld, from %lld to 1048576", name,
+                (long long)ld, (long long)mult, (long long)n);
+  if ((uintptr_t)p % 16) return fail(FF_EINVAL, "%s is not 16-byte aligned", name);
+  return FF_OK;
+}
+
+ff_status check_vector(const char* name, const void* p, int align) {
+  if (!p) return fail(FF_EINVAL, "%s is NULL", name);
+  if ((uintptr_t)p % align) return fail(FF_EINVAL, "%s is not %d-byte aligned", name, align);
+  return FF_OK;
+}
+
+ff_status check_workspace(const Call& c, const void* ws, int64_t bytes) {
+  if (!ws || (uintptr_t)ws % 256) return fail(FF_EINVAL, "the workspace is NULL or not 256-byte aligned");
+  if (bytes < (int64_t)c.bytes)
+    return fail(FF_EINVAL, "the workspace holds %lld bytes, the call needs %lld", (long long)bytes, (long long)c.bytes);
+  return FF_OK;
+}
+
+ff_status done(hipError_t e, const char* what) {
+  return e == hipSuccess ? FF_OK : fail(FF_EDEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+#define XENT_CHECK(call)                 \
+  do {                                   \
+    const ff_status st_ = (call);        \
+    if (st_ != FF_OK) return st_;        \
+  } while (0)
+
+ff_status check_grad(const Call& c, const Tensors& x, int act, int64_t ws_bytes) {
+  if (c.T > 0) {
+    XENT_CHECK(check_rows("H", x.H, x.ldh, c.n, act));
+    XENT_CHECK(check_rows("W", x.W, x.ldw, c.n, act));
+    XENT_CHECK(check_vector("target", x.target, 8));
+    XENT_CHECK(check_vector("lse", x.lse, 4));
+    if (x.loss) XENT_CHECK(check_vector("loss", x.loss, 4));
+    if (x.dloss) XENT_CHECK(check_vector("dloss", x.dloss, 4));
+    if (c.dh) XENT_CHECK(check_rows("dH", x.dH, x.lddh, c.n, act));
+    XENT_CHECK(check_workspace(c, x.ws, ws_bytes));
+  }
+  if (c.dw) XENT_CHECK(check_rows("dW", x.dW, x.lddw, c.n, act));
+  return FF_OK;
+}
+
+}  // namespace
+}  // namespace xent
+}  // namespace ff
+
+using ff::xent::Call;
+using ff::xent::Tensors;
+
+extern "C" {
+
+ff_status ff_xent_workspace(int64_t T, int64_t n, int64_t V, int act, int want, int64_t* bytes) {
+  ff::clear_error();
+  XENT_CHECK(ff::xent::check_sizes(T, n, V, act));
+  if (want < 0 || want > (FF_XENT_DH | FF_XENT_DW)) return ff::fail(FF_EINVAL, "unknown outputs %d", want);
+  if (!bytes) return ff::fail(FF_EINVAL, "bytes is NULL");
+  *bytes = (int64_t)ff::xent::plan(T, n, V, act, want & FF_XENT_DH, want & FF_XENT_DW).bytes;
+  return FF_OK;
+}
+
+ff_status ff_xent_fwd(int64_t T, int64_t n, int64_t V, int act, const void* H, int64_t ldh, const void* W, int64_t ldw,
+                      const int64_t* target, float* loss, float* lse, void* workspace, int64_t workspace_bytes,
+                      void* stream) {
+  ff::clear_error();
+  XENT_CHECK(ff::xent::check_sizes(T, n, V, act));
+  if (T == 0) return FF_OK;
+  const Call c = ff::xent::plan(T, n, V, act, false, false);
+  XENT_CHECK(ff::xent::check_rows("H", H, ldh, n, act));
+  XENT_CHECK(ff::xent::check_rows("W", W, ldw, n, act));
+  XENT_CHECK(ff::xent::check_vector("target", target, 8));
+  XENT_CHECK(ff::xent::check_vector("loss", loss, 4));
+  XENT_CHECK(ff::xent::check_vector("lse", lse, 4));
+  XENT_CHECK(ff::xent::check_workspace(c, workspace, workspace_bytes));
+  Tensors x{};
+  x.H = (const char*)H, x.ldh = ldh, x.W = (const char*)W, x.ldw = ldw, x.target = target, x.loss = loss, x.lse = lse;
+  x.ws = (char*)workspace, x.s = (hipStream_t)stream;
+  return ff::xent::done(ff::xent::run_fwd(c, x), "loss forward");
+}
+
+ff_status ff_xent_bwd(int64_t T, int64_t n, int64_t V, int act, const void* H, int64_t ldh, const void* W, int64_t ldw,
+                      const int64_t* target, const float* lse, const float* loss, const float* dloss, float scale,
+                      float beta_dh, void* dH, int64_t lddh, float beta_dw, void* dW, int64_t lddw, void* workspace,
+                      int64_t workspace_bytes, void* stream) {
+  ff::clear_error();
+  XENT_CHECK(ff::xent::check_sizes(T, n, V, act));
+  if (!dH && !dW) return FF_OK;
+  const Call c = ff::xent::plan(T, n, V, act, dH != nullptr, dW != nullptr);
+  Tensors x{(const char*)H, ldh, (const char*)W, ldw, target, dloss, scale, const_cast<float*>(loss), const_cast<float*>(lse), beta_dh,
+            beta_dw, (char*)dH, lddh, (char*)dW, lddw, (char*)workspace, (hipStream_t)stream};
+  XENT_CHECK(ff::xent::check_grad(c, x, act, workspace_bytes));
+  return ff::xent::done(ff::xent::run_bwd(c, x, false), "loss backward");
+}
+
+ff_status ff_xent_step(int64_t T, int64_t n, int64_t V, int act, const void* H, int64_t ldh, const void* W, int64_t ldw,
+                       const int64_t* target, const float* dloss, float scale, float* loss, float* lse, float beta_dh,
+                       void* dH, int64_t lddh, float beta_dw, void* dW, int64_t lddw, void* workspace,
+                       int64_t workspace_bytes, void* stream) {
+  ff::clear_error();
+  XENT_CHECK(ff::xent::check_sizes(T, n, V, act));
+  const Call c = ff::xent::plan(T, n, V, act, dH != nullptr, dW != nullptr);
+  Tensors x{(const char*)H, ldh, (const char*)W, ldw, target, dloss, scale, loss, lse, beta_dh, beta_dw, (char*)dH, lddh,
+            (char*)dW, lddw, (char*)workspace, (hipStream_t)stream};
+  if (T > 0) XENT_CHECK(ff::xent::check_vector("loss", loss, 4));
+  XENT_CHECK(ff::xent::check_grad(c, x, act, workspace_bytes));
+  if (!dH && !dW) return T == 0 ? FF_OK : ff::xent::done(ff::xent::run_fwd(c, x), "loss forward");
+  return ff::xent::done(ff::xent::run_bwd(c, x, true), "loss step");
+}
+
+}  // extern "C"

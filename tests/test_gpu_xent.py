@@ -1,0 +1,306 @@
+"""The head's loss (ff_xent_fwd, ff_xent_step, ff_xent_bwd) against the fp64 reference.
+
+Bounds per element.  v = 2^-24, u the activations' unit roundoff (2^-8 bf16, 2^-24 fp32).
+  * A logit is a sum of n products accumulated in fp32, at most 32 of them per step of the running sum and 16 roundings
+    within a step: |dz| <= (n / 16 + 48) 2 v sum_c |h_c w_c| (products of bf16 are exact in fp32; of fp32, one rounding
+    more, within the constant).  Ez = that with the token's largest sum.
+  * lse and the loss: 2 Ez + 16 v (1 + |lse| + max|z|) + (V / 64 + 64) v (the sum of V terms: 128 columns per wave, joined).
+  * P: relative 2 Ez (z and lse) + 3 u (stored twice) + 32 v, and exp's argument's rounding 64 v |z - lse| (at most 64 v 90).
+  * dH: sum of the P errors' products + (V / 16 + 48) 2 v |P| |W| + u |dH| (beta: + the old value's rounding); dW alike with
+    T terms."""
+import numpy as np
+import pytest
+
+from oracle import train_oracle as TO
+from paper_2608_26430_amd import inputs
+from tests.parity_util import TOL, rel, to_np, torch_act
+
+torch = pytest.importorskip("torch")
+import paper_2608_26430_amd as ff  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+V32 = 2.0 ** -24
+U = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+    return torch.device("cuda:0")
+
+
+def _case(T, n, V, dtype, seed, skip=0.2):
+    g = inputs.rng(seed)
+    H = inputs.gaussian(g, (T, n), dtype=dtype)
+    W = inputs.gaussian(g, (V, n), std=2.0 / np.sqrt(n), dtype=dtype)
+    target = g.integers(0, V, T)
+    target[g.random(T) < skip] = -100
+    dloss = g.random(T).astype(np.float32) + 0.25
+    return H, W, target.astype(np.int64), dloss
+
+
+def _dev(dev, dtype, H, W, target, dloss):
+    return (torch_act(H, dtype, dev), torch_act(W, dtype, dev), torch.from_numpy(target).to(dev),
+            torch.from_numpy(dloss).to(dev))
+
+
+def _garbage(T, n, V, dtype, dw, dev, dh=True):
+    """A workspace holding NaN patterns: results must not depend on what is there."""
+    ws = ff.xent_workspace(T, n, V, torch.bfloat16 if dtype == "bf16" else torch.float32, want_dh=dh, want_dw=dw, device=dev)
+    return ws.fill_(255)
+
+
+def _verify(ref, got, n, V, dtype, old=None, beta=0.0):
+    """got: dict of loss, lse, dH, dW (any may be missing)."""
+    loss, lse, dH, dW, (zabs, dHa, dWa) = ref
+    u, T = U[dtype], len(loss)
+    Ez = (n / 16 + 48) * 2 * V32 * zabs
+    El = 2 * Ez + 16 * V32 * (1 + np.abs(lse) + zabs) + (V / 64 + 64) * V32
+    rp = 2 * Ez.max(initial=0) + 3 * u + 32 * V32 + 64 * V32 * 90
+    fl = {k: to_np(v) for k, v in got.items()}
+
+    def close(name, want, bound):
+        d = np.abs(fl[name] - want)
+        assert np.isfinite(fl[name]).all(), name
+        assert np.all(d <= bound * 1.05 + 1e-37), (name, float((d / (bound + 1e-37)).max()))
+
+    if "loss" in fl:
+        close("loss", loss, El)
+        close("lse", lse, El)
+        assert np.all(fl["loss"][loss == 0] == 0) or V == 1
+    for name, want, sums, terms in (("dH", dH, dHa, V), ("dW", dW, dWa, T)):
+        if name not in fl:
+            continue
+        bound = (rp + (terms / 16 + 48) * 2 * V32) * sums
+        total = want if old is None else want + beta * old[name]
+        bound = bound + u * np.abs(total) + (0 if old is None else 4 * V32 * np.abs(old[name]))
+        close(name, total, bound)
+        if np.linalg.norm(total) > 0 and V > 1 and dtype in TOL:
+            assert rel(fl[name], total) <= TOL[dtype], (name, rel(fl[name], total))
+
+
+SIZES = [(1, 8, 1), (1, 64, 2), (2, 16, 3), (31, 72, 63), (33, 64, 65), (32, 136, 129), (64, 200, 257), (100, 768, 1000),
+         (129, 64, 1001), (257, 320, 500), (193, 128, 34000), (40, 64, 20011), (1, 4096, 5000), (1000, 16, 2), (300, 1032, 33025)]
+
+
+@pytest.mark.parametrize("T,n,V", SIZES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_loss_and_gradients_match_oracle(dev, T, n, V, dtype):
+    """One token to many, odd sizes, every tile: the step, the forward alone and the backward from its lse."""
+    H, W, target, dloss = _case(T, n, V, dtype, T + n + V)
+    ref = TO.xent(H, W, target, dloss, 0.3)
+    Ht, Wt, tt, dt = _dev(dev, dtype, H, W, target, dloss)
+    ws = _garbage(T, n, V, dtype, True, dev)
+    loss, lse, dH, dW = ff.xent_step(Ht, Wt, tt, dloss=dt, scale=0.3, want_dw=True, workspace=ws)
+    torch.cuda.synchronize()
+    _verify(ref, dict(loss=loss, lse=lse, dH=dH, dW=dW), n, V, dtype)
+    ws.fill_(255)
+    loss2, lse2 = ff.xent_fwd(Ht, Wt, tt, workspace=ws)
+    ws.fill_(255)
+    dH2, dW2 = ff.xent_bwd(Ht, Wt, tt, lse2, loss=loss2, dloss=dt, scale=0.3, want_dw=True, workspace=ws)
+    torch.cuda.synchronize()
+    _verify(ref, dict(loss=loss2, lse=lse2, dH=dH2, dW=dW2), n, V, dtype)
+    # one output alone, and the same bits again
+    ws.fill_(255)
+    dH3 = ff.xent_bwd(Ht, Wt, tt, lse2, loss=loss2, dloss=dt, scale=0.3, workspace=ws)[0]
+    again = ff.xent_step(Ht, Wt, tt, dloss=dt, scale=0.3, want_dw=True)
+    torch.cuda.synchronize()
+    _verify(ref, dict(dH=dH3), n, V, dtype)
+    assert all(torch.equal(a, b) for a, b in zip(again, (loss, lse, dH, dW)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_and_accumulation(dev, dtype):
+    """Rows inside wider ones (NaN beside them), outputs added to, nothing written beside them."""
+    T, n, V, ld = 75, 96, 301, 112
+    H, W, target, dloss = _case(T, n, V, dtype, 5)
+    ref = TO.xent(H, W, target, dloss, 2.0)
+    g = inputs.rng(6)
+    old = dict(dH=inputs.gaussian(g, (T, n), dtype=dtype), dW=inputs.gaussian(g, (V, n), dtype=dtype))
+
+    def place(a):
+        buf = torch.full((a.shape[0], ld), float("nan"), device=dev, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+        buf[:, :n] = torch_act(a, dtype, dev)
+        return buf[:, :n], buf
+
+    (Ht, _), (Wt, _), (dH, bh), (dW, bw) = place(H), place(W), place(old["dH"]), place(old["dW"])
+    tt, dt = torch.from_numpy(target).to(dev), torch.from_numpy(dloss).to(dev)
+    loss, lse, _, _ = ff.xent_step(Ht, Wt, tt, dloss=dt, scale=2.0, dH=dH, dW=dW, beta_dh=0.5, beta_dw=0.5, want_dw=True,
+                                   workspace=_garbage(T, n, V, dtype, True, dev))
+    torch.cuda.synchronize()
+    _verify(ref, dict(loss=loss, lse=lse, dH=dH, dW=dW), n, V, dtype, old, 0.5)
+    assert bool(torch.isnan(bh[:, n:]).all()) and bool(torch.isnan(bw[:, n:]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tokens_without_target(dev, dtype):
+    """Skipped tokens may hold NaN and infinities: their loss and row of dH are zero, and nothing of them reaches dW.  Any
+    value outside [0, V) skips; a call whose tokens are all skipped gives zeros."""
+    T, n, V = 90, 64, 700
+    H, W, target, dloss = _case(T, n, V, dtype, 9, skip=0.0)
+    bad = {0: -1, 5: -100, 17: V, 40: V + 1, 41: 1 << 40, 89: -(1 << 62)}
+    for t, v in bad.items():
+        target[t] = v
+    ref = TO.xent(H, W, target, dloss, 1.0)
+    H2 = H.copy()
+    for i, t in enumerate(bad):
+        H2[t] = (np.nan, np.inf, -np.inf)[i % 3]
+    Ht, Wt, tt, dt = _dev(dev, dtype, H2, W, target, dloss)
+    ws = _garbage(T, n, V, dtype, True, dev)
+    loss, lse, dH, dW = ff.xent_step(Ht, Wt, tt, dloss=dt, want_dw=True, workspace=ws)
+    dH2, dW2 = ff.xent_bwd(Ht, Wt, tt, lse, loss=loss, dloss=dt, want_dw=True)
+    torch.cuda.synchronize()
+    rows = list(bad)
+    assert bool((loss[rows] == 0).all()) and bool((dH[rows] == 0).all()) and bool((dH2[rows] == 0).all())
+    live = np.setdiff1d(np.arange(T), rows)
+    np_ref = (ref[0][live], ref[1][live], ref[2][live], ref[3], (ref[4][0][live], ref[4][1][live], ref[4][2]))
+    _verify(np_ref, dict(loss=loss[live], lse=lse[live], dH=dH[live], dW=dW), n, V, dtype)
+    _verify(np_ref, dict(dH=dH2[live], dW=dW2), n, V, dtype)
+    none = torch.full_like(tt, -100)
+    loss, _, dH, dW = ff.xent_step(Ht, Wt, none, want_dw=True)
+    torch.cuda.synchronize()
+    assert bool((loss == 0).all()) and bool((dH == 0).all()) and bool((dW == 0).all())
+
+
+@pytest.mark.parametrize("dtype,T,n,V,dw", [("bf16", 600, 16, 230_000, True), ("bf16", 1500, 16, 100_000, False),
+                                            ("f32", 300, 8, 240_001, True), ("f32", 600, 8, 130_000, False)])
+def test_pieces(dev, dtype, T, n, V, dw):
+    """Calls whose P exceeds one piece: pieces of the vocabulary (with dW) and of the tokens; the last piece is short."""
+    H, W, target, dloss = _case(T, n, V, dtype, 31)
+    ref = TO.xent(H, W, target, dloss, 0.01)
+    Ht, Wt, tt, dt = _dev(dev, dtype, H, W, target, dloss)
+    ws = _garbage(T, n, V, dtype, dw, dev)
+    got = ff.xent_step(Ht, Wt, tt, dloss=dt, scale=0.01, want_dw=dw, workspace=ws)
+    torch.cuda.synchronize()
+    names = ("loss", "lse", "dH", "dW") if dw else ("loss", "lse", "dH")
+    _verify(ref, dict(zip(names, got)), n, V, dtype)
+    ws.fill_(255)
+    got2 = ff.xent_bwd(Ht, Wt, tt, got[1], loss=got[0], dloss=dt, scale=0.01, want_dw=dw, workspace=ws)
+    torch.cuda.synchronize()
+    _verify(ref, dict(zip(("dH", "dW") if dw else ("dH",), got2)), n, V, dtype)
+
+
+def test_confident_tokens_keep_their_digits(dev):
+    """Where the target's probability is near one, its gradient is minus the others' sum, not a difference of ones: with
+    logits 0 and z the gradient's size is exp(-z), here down to 1e-5, and the result keeps it to bf16's rounding."""
+    n, V = 64, 2
+    z = np.linspace(1, 11.5, 64)
+    H = np.zeros((64, n), dtype=np.float32)
+    H[:, 0] = z
+    H = inputs.bf16_round(H)
+    W = np.zeros((V, n), dtype=np.float32)
+    W[1, 0] = 1.0
+    target = np.ones(64, dtype=np.int64)
+    ref = TO.xent(H, W, target)
+    Ht, Wt, tt, _ = _dev(dev, "bf16", H, W, target, np.ones(64, dtype=np.float32))
+    loss, lse, dH, _ = ff.xent_step(Ht, Wt, tt)
+    dH2 = ff.xent_bwd(Ht, Wt, tt, lse)[0]
+    torch.cuda.synchronize()
+    want = ref[2][:, 0]
+    # the loss is log(1 + exp(-z)): its sum in fp32 leaves 2^-24 absolute, 6e-3 of 1e-5
+    bound = 3 * 2.0 ** -8 * np.abs(want) + 4 * 2.0 ** -24
+    assert np.all(np.abs(to_np(dH)[:, 0] - want) <= bound)
+    # from the saved lse: its own rounding, 2^-24 of up to 16
+    assert np.all(np.abs(to_np(dH2)[:, 0] - want) <= bound + 16 * 2.0 ** -24)
+    # and without any absolute term in the step, and from the saved loss
+    dH3 = ff.xent_bwd(Ht, Wt, tt, lse, loss=loss)[0]
+    torch.cuda.synchronize()
+    for d in (dH, dH3):
+        assert np.all(np.abs(to_np(d)[:, 0] - want) <= 4 * 2.0 ** -8 * np.abs(want))
+    assert np.all(np.abs(to_np(loss) - ref[0]) <= 64 * V32 * ref[0])
+
+
+def test_large_logits(dev):
+    """Logits of +-2000: no overflow, and -inf weights (a vocabulary entry that is switched off) take no probability."""
+    T, n, V = 20, 16, 400
+    g = inputs.rng(12)
+    H = inputs.gaussian(g, (T, n))
+    W = inputs.gaussian(g, (V, n), std=150.0)
+    target = g.integers(0, V, T).astype(np.int64)
+    ref = TO.xent(H, W, target)
+    Ht, Wt, tt, _ = _dev(dev, "f32", H, W, target, np.ones(T, dtype=np.float32))
+    loss, lse = ff.xent_fwd(Ht, Wt, tt)
+    torch.cuda.synchronize()
+    assert np.isfinite(to_np(loss)).all()
+    Ez = (n / 16 + 48) * 2 * V32 * ref[4][0]
+    assert np.all(np.abs(to_np(loss) - ref[0]) <= 2 * Ez + 16 * V32 * (1 + np.abs(ref[1]) + ref[4][0]) + 128 * V32)
+
+
+def test_a_nan_row_stays_in_its_row(dev):
+    T, n, V = 40, 64, 500
+    H, W, target, dloss = _case(T, n, V, "bf16", 14, skip=0.0)
+    H[7, 3] = np.nan
+    Ht, Wt, tt, _ = _dev(dev, "bf16", H, W, target, dloss)
+    loss, lse, dH, _ = ff.xent_step(Ht, Wt, tt)
+    torch.cuda.synchronize()
+    others = [t for t in range(T) if t != 7]
+    assert torch.isnan(loss[7]) and bool(torch.isnan(dH[7]).all())
+    assert bool(torch.isfinite(loss[others]).all()) and bool(torch.isfinite(dH[others]).all())
+
+
+def test_no_tokens(dev):
+    W = torch.ones((10, 16), device=dev)
+    H, t = torch.empty((0, 16), device=dev), torch.empty((0,), dtype=torch.int64, device=dev)
+    dW = torch.full((10, 16), 2.0, device=dev)
+    loss, lse, dH, _ = ff.xent_step(H, W, t, dW=dW, beta_dw=0.5, want_dw=True)
+    torch.cuda.synchronize()
+    assert loss.shape == (0,) and dH.shape == (0, 16) and bool((dW == 1).all())
+    assert ff.xent_fwd(H, W, t)[0].shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_graph_replays_and_streams(dev, dtype):
+    """A captured step on new inputs at every replay, with eager work in between, and a call on another stream: the eager
+    call's bits."""
+    T, n, V = 70, 64, 900
+    feeds = [_case(T, n, V, dtype, 50 + i) for i in range(4)]
+    Ht, Wt, tt, dt = _dev(dev, dtype, *feeds[0])
+    ws = ff.xent_workspace(T, n, V, Ht.dtype, want_dh=True, want_dw=True, device=dev)
+    out = [torch.empty(T, device=dev), torch.empty(T, device=dev), torch.empty_like(Ht), torch.empty_like(Wt)]
+
+    def step():
+        ff.xent_step(Ht, Wt, tt, dloss=dt, loss=out[0], lse=out[1], dH=out[2], dW=out[3], want_dw=True, workspace=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for feed in feeds[1:] + feeds[:1]:
+        for buf, new in zip((Ht, Wt, tt, dt), _dev(dev, dtype, *feed)):
+            buf.copy_(new)
+        eager = [t.clone() for t in ff.xent_step(Ht, Wt, tt, dloss=dt, want_dw=True)]
+        for o in out:
+            o.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager))
+    other = ff.xent_step(Ht, Wt, tt, dloss=dt, want_dw=True, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(other, eager))
+
+
+def test_refusals(dev):
+    H, W = torch.zeros((4, 16), device=dev), torch.zeros((9, 16), device=dev)
+    t = torch.zeros(4, dtype=torch.int64, device=dev)
+    for bad in (lambda: ff.xent_fwd(H, W[:, :8], t), lambda: ff.xent_fwd(H, W, t.int()), lambda: ff.xent_fwd(H, W, t[:2]),
+                lambda: ff.xent_fwd(H, W.bfloat16(), t), lambda: ff.xent_fwd(H, W.cpu(), t),
+                lambda: ff.xent_step(H, W, t, beta_dh=1.0), lambda: ff.xent_step(H, W, t, dH=torch.zeros((4, 8), device=dev)),
+                lambda: ff.xent_bwd(H, W, t, torch.zeros(3, device=dev))):
+        with pytest.raises(ValueError):
+            bad()
+    loss = torch.full((4,), 3.0, device=dev)
+    with pytest.raises(ff.FrameFTError) as ei:
+        ff.xent_fwd(H, W, t, loss=loss, workspace=torch.empty(8, dtype=torch.uint8, device=dev))
+    assert ei.value.name == "FF_EINVAL" and "workspace" in str(ei.value)
+    with pytest.raises(ff.FrameFTError):     # rows that do not start on 16 bytes
+        ff.xent_fwd(torch.zeros((4, 18), device=dev)[:, :16], W, t)
+    torch.cuda.synchronize()
+    assert bool((loss == 3).all())
