@@ -3,10 +3,12 @@
 //   mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps), h = (x - mu) r, y = w h + b          (a row x of n)
 //   a = w g;  dx = beta dx + r (a - mean a - h mean(a h));  dw = sum_t g h;  db = sum_t g
 // Every sum is in fp32; the variance is that of the centred row, which stays in registers, so that a large mean costs
-// no digits.  A row belongs to WV waves (1, 4 or 16) whose threads hold NV pieces of VEC consecutive elements each;
-// rows wider than that are read three times.  The backward's workgroups walk the rows with a stride, keep dw and db of
-// their columns in registers and leave one partial row each, added up in a fixed order by a second kernel: the same
-// inputs give the same bits.  Bound by memory: forward 2 T n, backward 3 T n elements.
+// no digits.  A row belongs to WV waves (1, 8 or 16) whose threads hold NV pieces of VEC consecutive elements each;
+// rows wider than that are read three times.  Workgroups walk the rows with a stride, the vectors of their columns in
+// registers (fp32 weight and bias read for every row were twice a bf16 row's own bytes: 8192 x 8192 forward 67 -> 46
+// us), reading the next row under the arithmetic of one.  The backward's also keep dw and db of their columns and leave one
+// partial row each, added up in a fixed order by a second kernel: the same inputs give the same bits.  Bound by
+// memory: forward 2 T n, backward 3 T n elements; 8192 x 8192 in bf16 5.8 and 4.9 TB/s, where a large copy has 5.2.
 #include <cmath>
 
 #include "ff_internal.h"
@@ -35,28 +37,29 @@ struct Args {
   int vec_w;           // weight and bias may be read in whole pieces
 };
 
+// A piece of VEC consecutive elements as it lies in memory: one element, or 16 bytes.
 template <class E, int VEC>
 struct Pack {
-  static __device__ __forceinline__ void get(const E* p, float* v) {
-    if constexpr (VEC == 1) {
-      v[0] = (float)p[0];
-    } else if constexpr (sizeof(E) == 2) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+  typedef u32x4 Raw;
+  static __device__ __forceinline__ Raw load(const E* p) { return *reinterpret_cast<const u32x4*>(p); }
+  static __device__ __forceinline__ void widen(Raw w, float* v) {
+    if constexpr (sizeof(E) == 2) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[2 * i] = __builtin_bit_cast(float, w[i] << 16);
         v[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
       }
     } else {
-      const f32x4 w = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = w[i];
+      for (int i = 0; i < 4; ++i) {
+        const unsigned u = w[i];
+        v[i] = __builtin_bit_cast(float, u);
+      }
     }
   }
+  static __device__ __forceinline__ void get(const E* p, float* v) { widen(load(p), v); }
   static __device__ __forceinline__ void put(E* p, const float* v) {
-    if constexpr (VEC == 1) {
-      p[0] = (E)v[0];
-    } else if constexpr (sizeof(E) == 2) {
+    if constexpr (sizeof(E) == 2) {
       u32x4 w;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -68,6 +71,14 @@ struct Pack {
       *reinterpret_cast<f32x4*>(p) = w;
     }
   }
+};
+template <class E>
+struct Pack<E, 1> {
+  typedef E Raw;
+  static __device__ __forceinline__ Raw load(const E* p) { return *p; }
+  static __device__ __forceinline__ void widen(Raw w, float* v) { v[0] = (float)w; }
+  static __device__ __forceinline__ void get(const E* p, float* v) { v[0] = (float)*p; }
+  static __device__ __forceinline__ void put(E* p, const float* v) { *p = (E)v[0]; }
 };
 
 // VEC values of weight or bias at column c (absent: `none`)
@@ -122,55 +133,85 @@ __device__ __forceinline__ float2 row_sum(float2 v, float2* sh) {
 
 constexpr int threads_of(int wv) { return wv == 1 ? 256 : wv * 64; }
 
+// The pieces of a thread in row t of an operand.
+template <class E, int VEC, int NV, int WV>
+struct Row {
+  typename Pack<E, VEC>::Raw raw[NV];
+  __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t t, int l, int nv) {
+    const E* p = static_cast<const E*>(base) + t * ld;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * WV * 64 + l;
+      if (c < nv) raw[i] = Pack<E, VEC>::load(p + (int64_t)c * VEC);
+    }
+  }
+};
+
+// A workgroup walks rows with a stride, weight and bias of its columns in registers; the next row is read while one is
+// normalised.
 template <class E, int VEC, int NV, int WV>
 __global__ void __launch_bounds__(threads_of(WV)) fwd_kernel(Args a) {
   constexpr int kT = WV * 64, kRows = threads_of(WV) / kT;
   __shared__ float2 sh[2][WV];
-  const int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / kT;
-  if (t >= a.T) return;      // whole waves; with WV > 1 a workgroup has one row
   const int l = threadIdx.x % kT;
-  const E* x = static_cast<const E*>(a.X) + t * a.ldx;
-  E* y = static_cast<E*>(a.Y) + t * a.ldy;
   const int nv = a.n / VEC;
-  float v[NV][VEC];
-  float s = 0.f;
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / kT;
+  if (t >= a.T) return;      // whole waves; with WV > 1 a workgroup has one row at a time
+  Row<E, VEC, NV, WV> x;
+  x.load(a.X, a.ldx, t, l, nv);
+  float w[NV][VEC], b[NV][VEC];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = i * kT + l;
     if (c < nv) {
-      Pack<E, VEC>::get(x + (int64_t)c * VEC, v[i]);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) s += v[i][k];
+      vector_at<VEC>(a.weight, a.w_bf16, a.vec_w, 1.f, c * VEC, w[i]);
+      vector_at<VEC>(a.bias, a.w_bf16, a.vec_w, 0.f, c * VEC, b[i]);
     }
   }
-  const float mu = row_sum<WV>(make_float2(s, 0.f), sh[0]).x / (float)a.n;
-  float q = 0.f;
+  for (;;) {
+    float v[NV][VEC];
+    float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (i * kT + l < nv) {
+    for (int i = 0; i < NV; ++i)
+      if (i * kT + l < nv) {
+        Pack<E, VEC>::widen(x.raw[i], v[i]);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        v[i][k] -= mu;
-        q = fmaf(v[i][k], v[i][k], q);
+        for (int k = 0; k < VEC; ++k) s += v[i][k];
+      }
+    const int64_t next = t + stride;
+    if (next < a.T) x.load(a.X, a.ldx, next, l, nv);
+    const float mu = row_sum<WV>(make_float2(s, 0.f), sh[0]).x / (float)a.n;
+    float q = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i * kT + l < nv) {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          v[i][k] -= mu;
+          q = fmaf(v[i][k], v[i][k], q);
+        }
+      }
+    // (the barrier within keeps sh[0] until every wave has read it)
+    const float var = row_sum<WV>(make_float2(q, 0.f), sh[1]).x / (float)a.n;
+    const float r = 1.f / sqrtf(var + a.eps);
+    E* y = static_cast<E*>(a.Y) + t * a.ldy;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * kT + l;
+      if (c < nv) {
+        float o[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) o[k] = fmaf(v[i][k] * r, w[i][k], b[i][k]);
+        Pack<E, VEC>::put(y + (int64_t)c * VEC, o);
       }
     }
-  const float var = row_sum<WV>(make_float2(q, 0.f), sh[1]).x / (float)a.n;
-  const float r = 1.f / sqrtf(var + a.eps);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = i * kT + l;
-    if (c < nv) {
-      float w[VEC], b[VEC];
-      vector_at<VEC>(a.weight, a.w_bf16, a.vec_w, 1.f, c * VEC, w);
-      vector_at<VEC>(a.bias, a.w_bf16, a.vec_w, 0.f, c * VEC, b);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) w[k] = fmaf(v[i][k] * r, w[k], b[k]);
-      Pack<E, VEC>::put(y + (int64_t)c * VEC, w);
+    if (l == 0) {
+      if (a.mean) a.mean[t] = mu;
+      if (a.rstd) a.rstd[t] = r;
     }
-  }
-  if (l == 0) {
-    if (a.mean) a.mean[t] = mu;
-    if (a.rstd) a.rstd[t] = r;
+    if (next >= a.T) break;
+    t = next;
   }
 }
 
@@ -209,6 +250,18 @@ __global__ void __launch_bounds__(threads_of(WV)) bwd_kernel(Args a) {
   __shared__ float comb[kRows > 1 ? 2 * NV * VEC * kT : 1];
   const int l = threadIdx.x % kT, sub = threadIdx.x / kT;
   const int nv = a.n / VEC;
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  int64_t t = (int64_t)blockIdx.x * kRows + sub;
+  Row<E, VEC, NV, WV> x, g;
+  float mu_next = 0.f, r_next = 0.f;
+  auto fetch = [&](int64_t row) {
+    if (row >= a.T) return;
+    x.load(a.X, a.ldx, row, l, nv);
+    g.load(a.G, a.ldg, row, l, nv);
+    mu_next = a.mean[row];
+    r_next = a.rstd[row];
+  };
+  fetch(t);
   float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -219,23 +272,20 @@ __global__ void __launch_bounds__(threads_of(WV)) bwd_kernel(Args a) {
   }
   const float inv_n = 1.f / (float)a.n;
   int turn = 0;
-  for (int64_t t = (int64_t)blockIdx.x * kRows + sub; t < a.T; t += (int64_t)gridDim.x * kRows, turn ^= 1) {
-    const E* x = static_cast<const E*>(a.X) + t * a.ldx;
-    const E* g = static_cast<const E*>(a.G) + t * a.ldg;
-    const float mu = a.mean[t], r = a.rstd[t];
+  for (; t < a.T; t += stride, turn ^= 1) {
+    const float mu = mu_next, r = r_next;
     float h[NV][VEC], gg[NV][VEC];
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = i * kT + l;
-      if (c < nv) {
-        Pack<E, VEC>::get(x + (int64_t)c * VEC, h[i]);
-        Pack<E, VEC>::get(g + (int64_t)c * VEC, gg[i]);
+    for (int i = 0; i < NV; ++i)
+      if (i * kT + l < nv) {
+        Pack<E, VEC>::widen(x.raw[i], h[i]);
+        Pack<E, VEC>::widen(g.raw[i], gg[i]);
       } else {
 #pragma unroll
         for (int k = 0; k < VEC; ++k) h[i][k] = mu, gg[i][k] = 0.f;
       }
-    }
+    fetch(t + stride);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -347,17 +397,20 @@ __global__ void __launch_bounds__(256) bwd_wide_vectors_kernel(Args a) {
   part[a.n + c] = db;
 }
 
-// out (dw then db) = [out +] sum over the partial rows: 64 columns x 16 shares of the rows per workgroup.
+// out (dw then db) = [out +] sum over the partial rows: 32 columns x 32 shares of the rows per workgroup.
 __global__ void __launch_bounds__(1024) vector_sum_kernel(const float* part, int rows, int n, int add, float* dw, float* db) {
-  __shared__ float sh[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
+  __shared__ float sh[32][33];
+  const int k = threadIdx.x & 31, c = blockIdx.x * 32 + k, q = threadIdx.x >> 5;
   float s = 0.f;
-  if (c < 2 * n)
-    for (int r = q; r < rows; r += 16) s += part[(int64_t)r * 2 * n + c];
-  sh[q][threadIdx.x & 63] = s;
+  if (c < 2 * n) {
+#pragma unroll 8
+    for (int r = q; r < rows; r += 32) s += part[(int64_t)r * 2 * n + c];
+  }
+  sh[q][k] = s;
   __syncthreads();
   if (q || c >= 2 * n) return;
-  for (int i = 1; i < 16; ++i) s += sh[i][threadIdx.x];
+#pragma unroll
+  for (int i = 1; i < 32; ++i) s += sh[i][k];
   float* out = c < n ? dw : db;
   if (!out) return;
   out += c < n ? c : c - n;
@@ -366,95 +419,85 @@ __global__ void __launch_bounds__(1024) vector_sum_kernel(const float* part, int
 
 // ------------------------------------------------------------------------------------------- dispatch
 
-// The instance of a row of n: pieces of a thread and waves of a row.  A wave takes rows of up to four pieces a lane
-// (bf16: 2048 wide), four waves up to four, sixteen up to eight; wider rows (and unaligned ones past 32768) are read
-// three times.
+// The instance of a row of n: NV pieces of a thread and WV waves of a row.  A wave takes rows of up to four pieces a
+// lane (bf16: 2048 wide; 2048 wide and 8192 rows, forward / backward: 15 / 21 us against 21 / 24 with four waves), eight
+// waves up to two (8192: 46 / 83 us against 49 / 85 with four waves of four and 51 / 84 with sixteen of one), sixteen
+// waves up to 16384; wider rows are read three times.  Rows that do not start on 16 bytes, or whose width is no
+// whole number of pieces, have pieces of one element.
 struct Shape {
   int vec, nv, wv;   // wv 0: wide
 };
 Shape shape_of(int64_t n, int esz, bool aligned) {
   const int vec = aligned && n % (16 / esz) == 0 ? 16 / esz : 1;
   const int64_t p = n / vec;
-  const int most = vec == 1 ? 32 : 4;
   auto fit = [&](int wv, int limit) -> int {
-    for (int nv : {1, 2, 4, 8, 16, 32})
+    for (int nv : {1, 2, 4, 8, 16})
       if (nv <= limit && p <= (int64_t)nv * wv * 64) return nv;
     return 0;
   };
-  if (int nv = fit(1, vec == 1 ? 16 : most)) return {vec, nv, 1};
-  if (int nv = fit(4, vec == 1 ? 16 : most)) return {vec, nv, 4};
-  if (int nv = fit(16, vec == 1 ? 32 : (esz == 4 ? 8 : 4))) return {vec, nv, 16};
+  if (int nv = fit(1, vec == 1 ? 16 : 4)) return {vec, nv, 1};
+  if (int nv = fit(8, vec == 1 ? 16 : 2)) return {vec, nv, 8};
+  if (int nv = fit(16, vec == 1 ? 16 : (esz == 4 ? 4 : 2))) return {vec, nv, 16};
   return {vec, 0, 0};
 }
 
-constexpr int kGroups = 512;    // workgroups (partial rows) of a backward at most
-int groups_of(int64_t T, const Shape& s) {
+// Workgroups of a forward: about two waves more than fill the card (12,608 rows of 768: 9.5 us with 1024 workgroups, 11.6
+// with 512, 10.3 with one per four rows; 8192 of 8192: 46, 48 and 48).
+int64_t fwd_groups(int64_t T, const Shape& s) {
   const int rows = s.wv == 1 ? 4 : 1;
-  const int64_t g = (T + rows - 1) / rows;
-  return (int)(g < kGroups ? g : kGroups);
+  const int64_t g = (T + rows - 1) / rows, most = s.wv == 16 ? 512 : 1024;
+  return g < most ? g : most;
+}
+// And of a backward, each with a partial row of dw and db to write and add up (12,608 rows of 768: 13.4 us with 512, 17.5
+// with 256, 15.6 with 1024; 8192 of 8192: 83 with 256, 91 with 512).
+constexpr int kGroups = 512;
+int groups_of(int64_t T, int64_t n, const Shape& s) {
+  const int rows = s.wv == 1 ? 4 : 1;
+  const int64_t g = (T + rows - 1) / rows, most = n <= 4096 ? kGroups : kGroups / 2;
+  return (int)(g < most ? g : most);
 }
 
 template <class E, int VEC, int NV, int WV>
 void launch(const Args& a, bool bwd, int groups, hipStream_t s) {
-  constexpr int kRows = threads_of(WV) / (WV * 64);
-  const dim3 block(threads_of(WV));
-  if (bwd)
-    hipLaunchKernelGGL((bwd_kernel<E, VEC, NV, WV>), dim3((unsigned)groups), block, 0, s, a);
-  else
-    hipLaunchKernelGGL((fwd_kernel<E, VEC, NV, WV>), dim3((unsigned)((a.T + kRows - 1) / kRows)), block, 0, s, a);
+  const dim3 grid((unsigned)groups), block(threads_of(WV));
+  if (bwd) hipLaunchKernelGGL((bwd_kernel<E, VEC, NV, WV>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((fwd_kernel<E, VEC, NV, WV>), grid, block, 0, s, a);
 }
 
+// One-element pieces have instances of four and sixteen a thread, whole ones of one, two and four.
 template <class E, int VEC, int WV>
-bool launch_nv(const Args& a, int nv, bool bwd, int groups, hipStream_t s) {
+void launch_nv(const Args& a, int nv, bool bwd, int groups, hipStream_t s) {
   if constexpr (VEC == 1) {
-    switch (nv) {
-      case 1: case 2: case 4: launch<E, VEC, 4, WV>(a, bwd, groups, s); return true;
-      case 8: case 16: launch<E, VEC, 16, WV>(a, bwd, groups, s); return true;
-      case 32:
-        if constexpr (WV == 16) {
-          launch<E, VEC, 32, WV>(a, bwd, groups, s);
-          return true;
-        }
-    }
+    if (nv <= 4) launch<E, VEC, 4, WV>(a, bwd, groups, s);
+    else launch<E, VEC, 16, WV>(a, bwd, groups, s);
   } else {
-    switch (nv) {
-      case 1: launch<E, VEC, 1, WV>(a, bwd, groups, s); return true;
-      case 2: launch<E, VEC, 2, WV>(a, bwd, groups, s); return true;
-      case 4: launch<E, VEC, 4, WV>(a, bwd, groups, s); return true;
-      case 8:
-        if constexpr (sizeof(E) == 4 && WV == 16) {
-          launch<E, VEC, 8, WV>(a, bwd, groups, s);
-          return true;
-        }
-    }
+    if (nv == 1) launch<E, VEC, 1, WV>(a, bwd, groups, s);
+    else if (nv == 2) launch<E, VEC, 2, WV>(a, bwd, groups, s);
+    else if constexpr (WV == 1 || (WV == 16 && sizeof(E) == 4)) launch<E, VEC, 4, WV>(a, bwd, groups, s);
   }
-  return false;
+}
+
+template <class E, int VEC>
+void launch_wv(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t s) {
+  if (sh.wv == 1) launch_nv<E, VEC, 1>(a, sh.nv, bwd, groups, s);
+  else if (sh.wv == 8) launch_nv<E, VEC, 8>(a, sh.nv, bwd, groups, s);
+  else launch_nv<E, VEC, 16>(a, sh.nv, bwd, groups, s);
 }
 
 template <class E>
 hipError_t run(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t s) {
-  constexpr int V = 16 / (int)sizeof(E);
   if (sh.wv == 0) {
-    if (!bwd) {
-      hipLaunchKernelGGL(fwd_wide_kernel<E>, dim3((unsigned)a.T), dim3(1024), 0, s, a);
-    } else {
-      if (a.Y) hipLaunchKernelGGL(bwd_wide_kernel<E>, dim3((unsigned)a.T), dim3(1024), 0, s, a);
-      if (a.part)
-        hipLaunchKernelGGL(bwd_wide_vectors_kernel<E>, dim3((unsigned)groups, (unsigned)((a.n + 255) / 256)), dim3(256), 0,
-                           s, a);
-    }
-    return hipGetLastError();
+    if (!bwd) hipLaunchKernelGGL(fwd_wide_kernel<E>, dim3((unsigned)a.T), dim3(1024), 0, s, a);
+    if (bwd && a.Y) hipLaunchKernelGGL(bwd_wide_kernel<E>, dim3((unsigned)a.T), dim3(1024), 0, s, a);
+    if (bwd && a.part)
+      hipLaunchKernelGGL(bwd_wide_vectors_kernel<E>, dim3((unsigned)groups, (unsigned)((a.n + 255) / 256)), dim3(256), 0, s,
+                         a);
+  } else if (sh.vec == 1) {
+    launch_wv<E, 1>(a, sh, bwd, groups, s);
+  } else {
+    launch_wv<E, 16 / (int)sizeof(E)>(a, sh, bwd, groups, s);
   }
-  bool ok;
-  if (sh.vec == 1)
-    ok = sh.wv == 1 ? launch_nv<E, 1, 1>(a, sh.nv, bwd, groups, s)
-         : sh.wv == 4 ? launch_nv<E, 1, 4>(a, sh.nv, bwd, groups, s)
-                      : launch_nv<E, 1, 16>(a, sh.nv, bwd, groups, s);
-  else
-    ok = sh.wv == 1 ? launch_nv<E, V, 1>(a, sh.nv, bwd, groups, s)
-         : sh.wv == 4 ? launch_nv<E, V, 4>(a, sh.nv, bwd, groups, s)
-                      : launch_nv<E, V, 16>(a, sh.nv, bwd, groups, s);
-  return ok ? hipGetLastError() : hipErrorInvalidConfiguration;
+  return hipGetLastError();
 }
 
 ff_status check_rows(const char* name, const void* p, int64_t ld, int64_t n, int esz) {
@@ -497,8 +540,9 @@ ff_status ff_layernorm_fwd(int64_t T, int64_t n, int act, const void* X, int64_t
   a.w_bf16 = w_dtype == FF_BF16, a.eps = eps, a.mean = mean, a.rstd = rstd;
   a.vec_w = (uintptr_t)weight % 16 == 0 && (uintptr_t)bias % 16 == 0;
   const Shape sh = shape_of(n, esz, whole(X, ldx, esz) && whole(Y, ldy, esz));
-  const hipError_t e = act == FF_BF16 ? run<__bf16>(a, sh, false, 0, (hipStream_t)stream)
-                                      : run<float>(a, sh, false, 0, (hipStream_t)stream);
+  const int groups = (int)fwd_groups(T, sh);
+  const hipError_t e = act == FF_BF16 ? run<__bf16>(a, sh, false, groups, (hipStream_t)stream)
+                                      : run<float>(a, sh, false, groups, (hipStream_t)stream);
   return e == hipSuccess ? FF_OK : ff::fail(FF_EDEVICE, "layer norm forward: %s", hipGetErrorString(e));
 }
 
@@ -534,7 +578,7 @@ ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t
     if ((uintptr_t)weight % wsz || (uintptr_t)mean % 4 || (uintptr_t)rstd % 4)
       return ff::fail(FF_EINVAL, "weight, mean or rstd is misaligned");
     const Shape sh = shape_of(n, esz, whole(X, ldx, esz) && whole(G, ldg, esz) && (!dX || whole(dX, lddx, esz)));
-    groups = groups_of(T, sh);
+    groups = groups_of(T, n, sh);
     if (vectors) {
       if (!workspace || (uintptr_t)workspace % 16) return ff::fail(FF_EINVAL, "the workspace is NULL or not 16-byte aligned");
       const int64_t need = (int64_t)groups * 2 * n * 4;
@@ -551,7 +595,7 @@ ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t
     if (e != hipSuccess) return ff::fail(FF_EDEVICE, "layer norm backward: %s", hipGetErrorString(e));
   }
   if (vectors) {
-    hipLaunchKernelGGL(vector_sum_kernel, dim3((unsigned)((2 * n + 63) / 64)), dim3(1024), 0, (hipStream_t)stream, a.part,
+    hipLaunchKernelGGL(vector_sum_kernel, dim3((unsigned)((2 * n + 31) / 32)), dim3(1024), 0, (hipStream_t)stream, a.part,
                        groups, (int)n, accumulate_dw, dweight, dbias);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return ff::fail(FF_EDEVICE, "layer norm backward: %s", hipGetErrorString(e));
