@@ -47,30 +47,44 @@ hipError_t launch_gemm(int layout, int bf16, int tile, const GemmArgs& a, hipStr
 
 namespace {
 
-// Joins the statistics of a token's columns: 16 tokens x 16 shares of the entries per workgroup.
+// Joins the statistics of a token's columns: a workgroup takes TK tokens, its 256 / TK shares of the entries are joined
+// through LDS.
+template <int TK>
 __global__ void __launch_bounds__(256) combine_kernel(const float2* stats, int nstat, int N, const int64_t* target,
                                                       int64_t vocab, float* zt, float* loss, float* lse) {
-  __shared__ float2 sh[16][17];
-  const int tk = threadIdx.x & 15, part = threadIdx.x >> 4;
-  const int t = blockIdx.x * 16 + tk;
+  constexpr int kShares = 256 / TK;
+  __shared__ float2 sh[kShares][TK];
+  const int tk = threadIdx.x % TK, part = threadIdx.x / TK;
+  const int t = blockIdx.x * TK + tk;
   float top = -INFINITY, sum = 0.f;
-  if (t < N)
-    for (int i = part; i < nstat; i += 16) {
-      const float2 s = stats[(int64_t)i * N + t];
-      const float m = fmaxf(top, s.x);
-      // columns of -inf have sum 0, a NaN logit makes the sum NaN
-      const float ref = m == -INFINITY ? 0.f : m;
-      sum = sum * expf(top - ref) + s.y * expf(s.x - ref);
-      top = m;
+  auto join = [&](float2 s) {
+    const float m = fmaxf(top, s.x);
+    // columns of -inf have sum 0, a NaN logit makes the sum NaN
+    const float ref = m == -INFINITY ? 0.f : m;
+    sum = sum * expf(top - ref) + s.y * expf(s.x - ref);
+    top = m;
+  };
+  if (t < N) {
+    int i = part;
+    for (; i + 7 * kShares < nstat; i += 8 * kShares) {      // eight loads in flight
+      float2 s[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[k] = stats[(int64_t)(i + k * kShares) * N + t];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) join(s[k]);
     }
+    for (; i < nstat; i += kShares) join(stats[(int64_t)i * N + t]);
+  }
   sh[part][tk] = make_float2(top, sum);
-  __syncthreads();
+  for (int h = kShares / 2; h; h >>= 1) {
+    __syncthreads();
+    if (part < h) {
+      join(sh[part + h][tk]);
+      sh[part][tk] = make_float2(top, sum);
+    }
+  }
   if (part || t >= N) return;
-  float m = -INFINITY;
-  for (int i = 0; i < 16; ++i) m = fmaxf(m, sh[i][tk].x);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float others = 0.f;
-  for (int i = 0; i < 16; ++i) others += sh[i][tk].y * expf(sh[i][tk].x - ref);
+  const float m = top, others = sum;
   const int64_t tg = target[t];
   if (tg >= 0 && tg < vocab) {
     const float z = zt[t], total = others + expf(z - m), ls = logf(total);
@@ -189,7 +203,6 @@ __global__ void __launch_bounds__(256) live_rows_kernel(const E* H, int64_t ldh,
 
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // P of one piece
 constexpr int64_t kStatBytes = (int64_t)64 << 20;     // statistics of one piece
-constexpr int kCUs = 256;
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 int64_t tiles_of(int64_t M, int64_t N, int t) { return up(M, tile_m(t)) / tile_m(t) * (up(N, tile_n(t)) / tile_n(t)); }
@@ -201,10 +214,10 @@ struct Product {
 };
 
 // Tile and split of k of a product with M columns, N rows and kt k tiles.
-Product choose(int64_t M, int64_t N, int64_t kt, bool may_split) {
+Product choose(int64_t M, int64_t N, int64_t kt, bool may_split, bool bf16) {
   Product p{kSmall, 1, (int)kt};
   if (N > 32) {
-    if (N >= 192 && M >= 192 && tiles_of(M, N, kLarge) * (may_split ? kt / 8 + 1 : 1) >= kCUs / 2) p.tile = kLarge;
+    if (bf16 && N >= 192 && M >= 192 && tiles_of(M, N, kLarge) * (may_split ? kt / 8 + 1 : 1) >= kCUs / 2) p.tile = kLarge;
     else if (tiles_of(M, N, kMedium) * (may_split ? kt / 8 + 1 : 1) >= kCUs / 2) p.tile = kMedium;
   }
   if (may_split) {
@@ -229,11 +242,11 @@ struct Call {
   size_t off_p, off_stats, off_zt, off_part, off_live, bytes;
 };
 
-Product logits_product(const Call& c, int64_t N, int64_t M) { return choose(M, N, up(c.n, c.kk) / c.kk, false); }
-Product dh_product(const Call& c, int64_t N, int64_t K) { return choose(c.n, N, up(K, c.kk) / c.kk, true); }
+Product logits_product(const Call& c, int64_t N, int64_t M) { return choose(M, N, up(c.n, c.kk) / c.kk, false, c.bf16); }
+Product dh_product(const Call& c, int64_t N, int64_t K) { return choose(c.n, N, up(K, c.kk) / c.kk, true, c.bf16); }
 Product dw_product(const Call& c, int64_t M, int64_t K) {
   // sums of a whole head are not worth a pass through memory
-  return choose(c.n, M, up(K, c.kk) / c.kk, M <= 4096);
+  return choose(c.n, M, up(K, c.kk) / c.kk, M <= 4096, c.bf16);
 }
 
 Call plan(int64_t T, int64_t n, int64_t V, int act, bool dh, bool dw) {
@@ -331,9 +344,16 @@ hipError_t run_logits(const Call& c, const Tensors& x, int64_t t0, int64_t N, in
 }
 
 hipError_t run_combine(const Call& c, const Tensors& x, int64_t t0, int64_t N, int stat) {
-  hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((N + 15) / 16)), dim3(256), 0, x.s,
-                     reinterpret_cast<const float2*>(x.ws + c.off_stats), (int)(up(c.V, stat) / stat), (int)N,
-                     x.target + t0, c.V, reinterpret_cast<float*>(x.ws + c.off_zt), x.loss + t0, x.lse + t0);
+  const float2* stats = reinterpret_cast<const float2*>(x.ws + c.off_stats);
+  float* zt = reinterpret_cast<float*>(x.ws + c.off_zt);
+  const int nstat = (int)(up(c.V, stat) / stat);
+  // few tokens: all threads on one (a token's entries lie N apart, so that many tokens are read side by side)
+  if (N <= 64)
+    hipLaunchKernelGGL(combine_kernel<1>, dim3((unsigned)N), dim3(256), 0, x.s, stats, nstat, (int)N, x.target + t0, c.V, zt,
+                       x.loss + t0, x.lse + t0);
+  else
+    hipLaunchKernelGGL(combine_kernel<8>, dim3((unsigned)((N + 7) / 8)), dim3(256), 0, x.s, stats, nstat, (int)N,
+                       x.target + t0, c.V, zt, x.loss + t0, x.lse + t0);
   return hipGetLastError();
 }
 

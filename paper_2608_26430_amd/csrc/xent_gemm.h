@@ -14,8 +14,8 @@
 // A workgroup computes a BM x BN tile (BM along i), its waves as WVM x WVN; NB tiles of 128 bytes
 // of k are in flight.  In a 16 x 16 MFMA the lane holds four consecutive i of one j, so that results are
 // stored along the rows of memory and the softmax statistics of one token stay in one lane's registers.
-// For logits the rows of A are dealt to the MFMA in an order that gives a lane 4 PF consecutive
-// vocabulary entries over PF tiles.
+// For bf16 logits the rows of A are dealt to the MFMA in an order that gives a lane eight consecutive
+// vocabulary entries over two tiles (PF = 2), one store of 16 bytes; the four lanes of a token store 64 bytes.
 #pragma once
 
 #include "ff_internal.h"
@@ -95,11 +95,10 @@ __device__ __forceinline__ void ring_wait() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(N) : "memory");
 }
 
-__device__ __forceinline__ u32x4 make_rsrc(uint64_t base, int64_t bytes) {
-  const uint32_t n = bytes <= 0 ? 0u : (bytes > 0x7fffffffll ? 0x7fffffffu : (uint32_t)bytes);
+__device__ __forceinline__ u32x4 make_rsrc(uint64_t base, unsigned bytes) {
   u32x4 r = {(unsigned)__builtin_amdgcn_readfirstlane((int)(uint32_t)base),
              (unsigned)__builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32)),
-             (unsigned)__builtin_amdgcn_readfirstlane((int)n), 0x00020000u};
+             (unsigned)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
   return r;
 }
 
@@ -114,58 +113,64 @@ struct Operand {
   static constexpr int kLoads = kBytes / 1024 / NW;
   static constexpr int kRow = TR ? BX * kE : 128; // bytes of an LDS row
   static constexpr int kPieces = kRow / 16;
+  static constexpr int kReads = !TR ? 1 : (kE == 2 ? 2 : 4);   // LDS reads of a fragment
   static_assert(kBytes % (1024 * NW) == 0, "a whole number of loads per wave");
 
-  uint64_t base;
-  int64_t total;      // bytes from base to the operand's end
-  int64_t step;       // bytes per k tile
+  uint64_t base;      // next k tile
+  uint64_t step;      // bytes per k tile
+  unsigned records;   // bytes of a whole k tile that may be read
   unsigned voff[kLoads];
-  int kq[kLoads];     // first k of the lane's piece within the tile (K-major)
 
   static __device__ __forceinline__ int swizzle(int row) {
     if (!TR) {
       if (PF == 0) return row & 7;
-      constexpr int lg = PF == 4 ? 4 : 3;
-      return (row & 3) | (((row >> lg) & 1) << 2);
+      return (row & 3) | (((row >> 3) & 1) << 2);
     }
     const int s = kE == 2 ? (((row & 3) << 1) ^ (((row >> 3) & 1) << 3)) : (((row >> 2) & 3) << 2);
     return s & (kPieces - 1);
   }
 
-  // x0: first i (j) of the tile, X its extent, kt0: first k tile.  The memory of a row reaches to the next whole
-  // piece (H and W by their widths, P by its zero padding).
-  __device__ __forceinline__ void init(const void* p, int64_t ld, int x0, int X, int K, int kt0, int wave, int lane) {
-    const char* b = static_cast<const char*>(p);
-    X = (X + kPer - 1) / kPer * kPer;
-    K = TR ? K : (K + kPer - 1) / kPer * kPer;
-    if (TR) {
-      step = (int64_t)kK * ld * kE;
-      base = (uint64_t)(b + (int64_t)x0 * kE + kt0 * step);
-      total = ((int64_t)(K - 1) * ld + X - x0) * kE - kt0 * step;
-    } else {
-      step = 128;
-      base = (uint64_t)(b + (int64_t)x0 * ld * kE + kt0 * step);
-      const int rows = X - x0 < BX ? X - x0 : BX;
-      total = ((int64_t)(rows - 1) * ld + K) * kE - kt0 * step;
-    }
+  __device__ __forceinline__ void init(int64_t ld, int wave, int lane) {
+    step = TR ? (uint64_t)kK * ld * kE : 128;
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
       const int byte = (wave * kLoads + q) * 1024 + lane * 16;
       const int row = byte / kRow, piece = (byte % kRow / 16) ^ swizzle(row);
       voff[q] = (unsigned)((int64_t)row * ld * kE) + piece * 16;
-      kq[q] = piece * kPer;
     }
   }
 
-  // k tile t (counted from init's) into the LDS buffer; left: k from that tile's start on
-  __device__ __forceinline__ void issue(int t, int left, unsigned lds, int wave) const {
-    const u32x4 r = make_rsrc(base + t * step, left > 0 ? total - t * step : 0);
+  // x0: first i (j) of the tile, X its extent, kt0: first k tile.  The memory of a row reaches to the next whole
+  // piece (H and W by their widths, P by its zero padding).
+  __device__ __forceinline__ void seek(const void* p, int64_t ld, int x0, int X, int kt0) {
+    X = (X + kPer - 1) / kPer * kPer;
+    base = (uint64_t)((const char*)p + (int64_t)x0 * (TR ? 1 : ld) * kE) + kt0 * step;
+    const int rows = X - x0 < BX ? X - x0 : BX;
+    records = TR ? (unsigned)(((int64_t)(kK - 1) * ld + X - x0) * kE) : (unsigned)((int64_t)(rows - 1) * ld * kE) + 128;
+  }
+
+  // The last k tile, `tile` steps on, of which `left` of k remain: zero beyond them.
+  __device__ __forceinline__ void issue_last(int tile, int left, int64_t ld, unsigned lds, int wave, int lane) const {
+    const int pieces = (left + kPer - 1) / kPer;
+    const unsigned n = TR ? records - (unsigned)((int64_t)(kK - left) * ld * kE) : records - 128 + pieces * 16;
+    const u32x4 r = make_rsrc(base + tile * step, n);
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
       unsigned v = voff[q];
-      if (!TR && left < kK) v = kq[q] < left ? v : kFar;
+      if (!TR) {
+        const int byte = (wave * kLoads + q) * 1024 + lane * 16;
+        v = ((byte % kRow / 16) ^ swizzle(byte / kRow)) < pieces ? v : kFar;
+      }
       load_lds(v, r, lds + (wave * kLoads + q) * 1024);
     }
+  }
+
+  // The next whole k tile (nothing, as zeros, unless `more`).
+  __device__ __forceinline__ void issue(bool more, unsigned lds, int wave) {
+    const u32x4 r = make_rsrc(base, more ? records : 0u);
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) load_lds(voff[q], r, lds + (wave * kLoads + q) * 1024);
+    base += step;
   }
 
   // Fragment of 16 i starting at x (a multiple of 16; PF > 0: tile f of the wave's part at x) of half kk of the tile.
@@ -210,16 +215,31 @@ __device__ __forceinline__ f32x4 mma<float>(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
-template <class E>
-__device__ __forceinline__ float exp_of(float x) {
-  return sizeof(E) == 2 ? __expf(x) : expf(x);
+// Asks the scheduler to spread READS LDS reads evenly over the MMAS multiplications beside them.
+template <int READS, int MMAS, int I = 0>
+__device__ __forceinline__ void interleave() {
+  if constexpr (I < READS) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                         // one LDS read
+    __builtin_amdgcn_sched_group_barrier(0x008, MMAS * (I + 1) / READS - MMAS * I / READS, 0);   // its share of MFMA
+    interleave<READS, MMAS, I + 1>();
+  }
 }
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ unsigned short bf16_bits(float x) {
   return __builtin_bit_cast(unsigned short, (__bf16)x);
 }
 __device__ __forceinline__ float bf16_value(unsigned short b) { return __builtin_bit_cast(float, (unsigned)b << 16); }
 
+// eight consecutive results
+__device__ __forceinline__ void store8(__bf16* p, f32x4 v, f32x4 w) {
+  const u32x4 x = {(unsigned)bf16_bits(v[0]) | (unsigned)bf16_bits(v[1]) << 16,
+                   (unsigned)bf16_bits(v[2]) | (unsigned)bf16_bits(v[3]) << 16,
+                   (unsigned)bf16_bits(w[0]) | (unsigned)bf16_bits(w[1]) << 16,
+                   (unsigned)bf16_bits(w[2]) | (unsigned)bf16_bits(w[3]) << 16};
+  *reinterpret_cast<u32x4*>(p) = x;
+}
 // four consecutive results (the address is a multiple of four elements)
 __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
   u32x2 w = {(unsigned)bf16_bits(v[0]) | (unsigned)bf16_bits(v[1]) << 16,
@@ -234,12 +254,15 @@ __device__ __forceinline__ f32x4 load4(const __bf16* p) {
 }
 __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
-// Tile of a workgroup.  Workgroups go round the eight XCDs; each XCD takes a contiguous run of tiles, in groups of
-// eight along j and then along i, so that the tiles that run at once on an XCD share their operands in its L2.
-__device__ __forceinline__ void tile_of(int wg, int total, int tm, int tn, int* im, int* in) {
-  const int xcd = wg & 7, idx = wg >> 3;
-  const int per = total >> 3, rem = total & 7;
-  const int id = xcd * per + (xcd < rem ? xcd : rem) + idx;
+// Workgroups go round the eight XCDs; each XCD takes a contiguous run of the `total` tiles.
+__device__ __forceinline__ int share_of(int wg, int total) {
+  const int xcd = wg & 7, per = total >> 3, rem = total & 7;
+  return xcd * per + (xcd < rem ? xcd : rem) + (wg >> 3);
+}
+
+// Tiles run in groups of eight along j and then along i, so that those that run at once on an XCD share their operands
+// in its L2.
+__device__ __forceinline__ void tile_of(int id, int tm, int tn, int* im, int* in) {
   const int group = 8 * tm;
   const int g = id / group, first = g * 8;
   const int w = tn - first < 8 ? tn - first : 8;
@@ -248,76 +271,11 @@ __device__ __forceinline__ void tile_of(int wg, int total, int tm, int tn, int* 
   *im = in_group / w;
 }
 
-template <class E, int BM, int BN, int WVM, int WVN, int NB, bool TRA, bool TRB, int WPE>
-__global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
-  constexpr int NW = WVM * WVN;
-  constexpr int TM = BM / WVM, TN = BN / WVN;
-  constexpr int FM = TM / 16, FN = TN / 16;
-  constexpr int PF = TRA ? 0 : (FM < 4 ? FM : 4);
-  typedef Operand<E, BM, NW, TRA, PF> OpA;
-  typedef Operand<E, BN, NW, TRB, 0> OpB;
-  constexpr int kBuf = OpA::kBytes + OpB::kBytes;
-  constexpr int kLoads = OpA::kLoads + OpB::kLoads;
-  constexpr int kK = OpA::kK;
-  __shared__ __align__(1024) char lds[NB * kBuf];
-
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave % WVM, wn = wave / WVM;
-  const int tiles = a.tm * a.tn;
-  const int split = blockIdx.x / tiles;
-  int im, in;
-  tile_of(blockIdx.x - split * tiles, tiles, a.tm, a.tn, &im, &in);
-  const int kt0 = split * a.kt_split;
-  const int nkt = a.kt - kt0 < a.kt_split ? a.kt - kt0 : a.kt_split;
-
-  OpA oa;
-  OpB ob;
-  oa.init(a.A, a.lda, im * BM, a.M, a.K, kt0, wave, lane);
-  ob.init(a.B, a.ldb, in * BN, a.N, a.K, kt0, wave, lane);
-  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  const int kleft = a.K - kt0 * kK;
-  auto issue = [&](int t, int buf) {
-    const int left = t < nkt ? kleft - t * kK : 0;
-    oa.issue(t, left, lds0 + buf * kBuf, wave);
-    ob.issue(t, left, lds0 + buf * kBuf + OpA::kBytes, wave);
-  };
-
-  f32x4 acc[FM][FN];
-#pragma unroll
-  for (int f = 0; f < FM; ++f)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[f][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-#pragma unroll
-  for (int t = 0; t < NB - 1; ++t) issue(t, t);
-  for (int t0 = 0; t0 < nkt; t0 += NB) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if (t0 + b >= nkt) break;
-      ring_wait<(NB - 2) * kLoads>();
-      issue(t0 + b + NB - 1, (b + NB - 1) % NB);
-      const char* la = lds + b * kBuf;
-      const char* lb = la + OpA::kBytes;
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        f32x4 fa[FM], fb[FN];
-#pragma unroll
-        for (int f = 0; f < FM; ++f) fa[f] = OpA::read(la, wm * TM, f, kk, lane);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) fb[j] = OpB::read(lb, wn * TN, j, kk, lane);
-#pragma unroll
-        for (int f = 0; f < FM; ++f)
-#pragma unroll
-          for (int j = 0; j < FN; ++j) acc[f][j] = mma<E>(fa[f], fb[j], acc[f][j]);
-      }
-    }
-  }
-  // no direct load may be in flight when the workgroup's LDS is given to another one
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-
+// The results of a wave's tile: FM x FN tiles of 16 x 16 from (i0, j0).
+template <class E, int FM, int FN, int TM, int PF, bool TRA>
+__device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], const int (&target)[FN], int i0, int j0,
+                                       int split, int lane) {
   const int g = lane >> 4, r = lane & 15;
-  const int i0 = im * BM + wm * TM, j0 = in * BN + wn * TN;
   // first of the four i of tile f that the lane holds
   auto col = [&](int f) {
     if (TRA) return i0 + f * 16 + g * 4;
@@ -325,95 +283,258 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
     return i0 + (f / P) * P * 16 + g * (P * 4) + (f % P) * 4;
   };
   if constexpr (TRA) {
-    if (a.mode == kPart) {
-      float* part = a.part + (int64_t)split * a.N * a.M;
+    const bool partial = a.mode == kPart;
+    float* part = partial ? a.part + (int64_t)split * a.N * a.M : nullptr;
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int row = j0 + j * 16 + r;
-        if (row >= a.N) continue;
+    for (int j = 0; j < FN; ++j) {
+      const int row = j0 + j * 16 + r;
+      if (row >= a.N) continue;
 #pragma unroll
-        for (int f = 0; f < FM; ++f) {
-          const int c = col(f);
-          if (c >= a.M) continue;
+      for (int f = 0; f < FM; ++f) {
+        const int c = col(f);
+        if (c >= a.M) continue;
+        f32x4 v = acc[f][j];
+        if (partial) {
           float* p = part + (int64_t)row * a.M + c;
-          f32x4 v = acc[f][j];
           if (a.part_add) v += load4(p);
           store4(p, v);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int row = j0 + j * 16 + r;
-        if (row >= a.N) continue;
-#pragma unroll
-        for (int f = 0; f < FM; ++f) {
-          const int c = col(f);
-          if (c >= a.M) continue;
+        } else {
           E* p = static_cast<E*>(a.out) + (int64_t)row * a.ldo + c;
-          f32x4 v = acc[f][j];
           if (a.beta != 0.f) v += a.beta * load4(p);
           store4(p, v);
         }
       }
     }
   } else {
+    constexpr float kLog2e = 1.4426950408889634f;
+    // tile f's results of a token: the two tiles of a pair go out together
+    f32x4 first;
+    auto put = [&](E* out, int f, f32x4 v, bool live) {
+      if constexpr (PF == 2) {
+        if (f % 2 == 0) first = v;
+        else if (live && col(f - 1) < a.ocols) store8(out + col(f - 1), first, v);
+      } else {
+        if (live && col(f) < a.ocols) store4(out + col(f), v);
+      }
+    };
+    const bool edge = i0 + TM > a.M;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int row = j0 + j * 16 + r;
       const bool live = row < a.N;
-      const int64_t tg = live ? a.target[row] : -1;
-      const bool counted = tg >= 0 && tg < a.vocab;
-      const int at = counted && tg >= a.v0 && tg - a.v0 < a.M ? (int)(tg - a.v0) : -1;
+      const bool counted = target[j] != -1;
+      const int at = target[j] >= i0 && target[j] < i0 + TM ? target[j] : -1;
+      const bool hit = __any(at >= 0);      // a token of the wave has its target in these columns
       E* out = static_cast<E*>(a.out) + (int64_t)row * a.ldo;
       if (a.mode == kGrad) {
         const float lse = live ? a.lse[row] : 0.f;
-        const float own = at >= 0 && a.loss ? expm1f(-a.loss[row]) : 0.f;
         const float w = counted ? a.scale * (a.dloss ? a.dloss[row] : 1.f) : 0.f;
+        const float own = at >= 0 && a.loss ? expm1f(-a.loss[row]) : 0.f;
 #pragma unroll
         for (int f = 0; f < FM; ++f) {
           const int c = col(f);
           f32x4 v;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float z = acc[f][j][i] - lse;
-            const float p = c + i == at ? (a.loss ? own : expm1f(z)) : exp_of<E>(z);
-            v[i] = counted && c + i < a.M ? p * w : 0.f;
+            const float p = sizeof(E) == 2 ? exp2_fast(fmaf(acc[f][j][i], kLog2e, -lse * kLog2e)) : expf(acc[f][j][i] - lse);
+            v[i] = counted ? p * w : 0.f;
           }
-          if (live && c < a.ocols) store4(out + c, v);
+          if (hit) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (c + i == at) v[i] = (a.loss ? own : expm1f(acc[f][j][i] - lse)) * w;
+          }
+          if (edge) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = c + i < a.M ? v[i] : 0.f;
+          }
+          put(out, f, v, live);
         }
         continue;
+      }
+      if (edge) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (col(f) + i >= a.M) acc[f][j][i] = -INFINITY;
       }
       float top = -INFINITY;
 #pragma unroll
       for (int f = 0; f < FM; ++f)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c = col(f) + i;
-          if (c >= a.M) acc[f][j][i] = -INFINITY;
-          if (c == at) a.zt[row] = acc[f][j][i];
-          top = fmaxf(top, acc[f][j][i]);
-        }
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, acc[f][j][i]);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float ref = top == -INFINITY ? 0.f : top;    // columns of nothing: exp(-inf) = 0, not NaN
+      const float ref2 = ref * kLog2e;
       float sum = 0.f;
 #pragma unroll
       for (int f = 0; f < FM; ++f) {
         const int c = col(f);
         f32x4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = exp_of<E>(acc[f][j][i] - ref);
-          sum += c + i == at ? 0.f : v[i];
+        for (int i = 0; i < 4; ++i)
+          v[i] = sizeof(E) == 2 ? exp2_fast(fmaf(acc[f][j][i], kLog2e, -ref2)) : expf(acc[f][j][i] - ref);
+        if (a.mode == kExp) put(out, f, v, live);
+        if (hit) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (c + i == at) {
+              a.zt[row] = acc[f][j][i];
+              v[i] = 0.f;
+            }
         }
-        if (a.mode == kExp && live && c < a.ocols) store4(out + c, v);
+        sum += (v[0] + v[1]) + (v[2] + v[3]);
       }
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
       if (g == 0 && live && i0 < a.M) a.stats[(int64_t)(i0 / TM) * a.N + row] = make_float2(top, sum);
     }
   }
+}
+
+template <class E, int BM, int BN, int WVM, int WVN, int NB, bool TRA, bool TRB, int WPE>
+__global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
+  constexpr int NW = WVM * WVN;
+  constexpr int TM = BM / WVM, TN = BN / WVN;
+  constexpr int FM = TM / 16, FN = TN / 16;
+  constexpr int PF = TRA || sizeof(E) == 4 ? 0 : 2;
+  typedef Operand<E, BM, NW, TRA, PF> OpA;
+  typedef Operand<E, BN, NW, TRB, 0> OpB;
+  constexpr int kBuf = OpA::kBytes + OpB::kBytes;
+  constexpr int kLoads = OpA::kLoads + OpB::kLoads;
+  constexpr int kK = OpA::kK;
+  constexpr int kReads = FM * OpA::kReads + FN * OpB::kReads;      // LDS reads and MFMA of half a tile
+  constexpr int kMmas = FM * FN * (sizeof(E) == 2 ? 1 : 4);
+  __shared__ __align__(1024) char lds[NB * kBuf];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WVM, wn = wave / WVM;
+  const int tiles = a.tm * a.tn, total = tiles * a.splits;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+
+  OpA oa;
+  OpB ob;
+  oa.init(a.lda, wave, lane);
+  ob.init(a.ldb, wave, lane);
+  int i0, j0, split, nkt;      // the tile whose operands are being read
+  auto seek = [&](int wg) {
+    const int id = share_of(wg, total);
+    split = id / tiles;
+    int im, in;
+    tile_of(id - split * tiles, a.tm, a.tn, &im, &in);
+    i0 = im * BM, j0 = in * BN;
+    const int kt0 = split * a.kt_split;
+    nkt = a.kt - kt0 < a.kt_split ? a.kt - kt0 : a.kt_split;
+    oa.seek(a.A, a.lda, i0, a.M, kt0);
+    ob.seek(a.B, a.ldb, j0, a.N, kt0);
+  };
+  // k is walked with its last tile first, so that only the first loads look at its end
+  auto issue_last = [&]() {
+    if (nkt <= 0) return;
+    const int last = a.K - (split * a.kt_split + nkt - 1) * kK;
+    oa.issue_last(nkt - 1, last < kK ? last : kK, a.lda, lds0, wave, lane);
+    ob.issue_last(nkt - 1, last < kK ? last : kK, a.ldb, lds0 + OpA::kBytes, wave, lane);
+  };
+  auto issue = [&](int t, int buf) {
+    oa.issue(t < nkt, lds0 + buf * kBuf, wave);
+    ob.issue(t < nkt, lds0 + buf * kBuf + OpA::kBytes, wave);
+  };
+  int64_t raw[FN];             // targets of that tile's tokens
+  auto start = [&](int wg) {
+    seek(wg);
+    if constexpr (!TRA) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const int row = j0 + wn * TN + j * 16 + (lane & 15);
+        raw[j] = row < a.N ? a.target[row] : -1;
+      }
+    }
+    issue_last();
+#pragma unroll
+    for (int t = 1; t < (NB == 2 ? 2 : NB - 1); ++t) issue(t, t);
+  };
+
+  start(blockIdx.x);
+  for (int wg = blockIdx.x;;) {
+  // the token's target as a column of A (-1: none, -2: in another piece of the vocabulary)
+  int target[FN] = {};
+  if constexpr (!TRA) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      target[j] = raw[j] < 0 || raw[j] >= a.vocab ? -1 : (raw[j] >= a.v0 && raw[j] - a.v0 < a.M ? (int)(raw[j] - a.v0) : -2);
+  }
+  f32x4 acc[FM][FN];
+#pragma unroll
+  for (int f = 0; f < FM; ++f)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[f][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto read = [&](int buf, int kk, f32x4 (&fa)[FM], f32x4 (&fb)[FN]) {
+    const char* la = lds + buf * kBuf;
+    const char* lb = la + OpA::kBytes;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[j] = OpB::read(lb, wn * TN, j, kk, lane);
+#pragma unroll
+    for (int f = 0; f < FM; ++f) fa[f] = OpA::read(la, wm * TM, f, kk, lane);
+  };
+  auto multiply = [&](const f32x4 (&fa)[FM], const f32x4 (&fb)[FN]) {
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[f][j] = mma<E>(fa[f], fb[j], acc[f][j]);
+  };
+
+  if constexpr (NB == 2) {
+    // Two buffers.  The fragments of a half tile are read while the other half is multiplied; in the middle of tile
+    // t every wave has read all of it, so that its buffer takes tile t + 2.
+    f32x4 fa[2][FM], fb[2][FN];
+    ring_wait<kLoads>();
+    read(0, 0, fa[0], fb[0]);
+    for (int t0 = 0; t0 < nkt; t0 += 2) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if (t0 + b >= nkt) break;
+        read(b, 1, fa[1], fb[1]);
+        multiply(fa[0], fb[0]);
+        interleave<kReads, kMmas>();
+        ring_wait<0>();
+        if (t0 + b + 2 < nkt) issue(t0 + b + 2, b);
+        read(1 - b, 0, fa[0], fb[0]);
+        multiply(fa[1], fb[1]);
+        interleave<kReads, kMmas>();
+      }
+    }
+  } else {
+    for (int t0 = 0; t0 < nkt; t0 += NB) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if (t0 + b >= nkt) break;
+        ring_wait<(NB - 2) * kLoads>();
+        issue(t0 + b + NB - 1, (b + NB - 1) % NB);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          f32x4 fa[FM], fb[FN];
+          read(b, kk, fa, fb);
+          multiply(fa, fb);
+        }
+      }
+    }
+  }
+  // this tile's place, and the next one's first loads under the results' arithmetic and stores
+  const int wi0 = i0 + wm * TM, wj0 = j0 + wn * TN, wsplit = split;
+  wg += gridDim.x;
+  const bool more = wg < total;
+  if (more) {
+    ring_wait<0>();      // every wave's reads of the buffers are done
+    start(wg);
+  }
+  finish<E, FM, FN, TM, PF, TRA>(a, acc, target, wi0, wj0, wsplit, lane);
+  if (!more) break;
+  }
+  // no direct load may be in flight when the workgroup's LDS is given to another one
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 // Tile sizes of the instances: large (256 x 256, wave 128 x 64), medium (128 x 128, wave 64 x 64), small (128 x 32,
@@ -423,6 +544,8 @@ constexpr int tile_m(int t) { return t == kLarge ? 256 : 128; }
 constexpr int tile_n(int t) { return t == kLarge ? 256 : (t == kMedium ? 128 : 32); }
 // columns of one entry of the logits' statistics
 constexpr int stat_cols(int t) { return t == kLarge ? 128 : (t == kMedium ? 64 : 32); }
+
+constexpr int kCUs = 256;
 
 // layout 0: logits, 1: dH, 2: dW
 hipError_t launch_gemm(int layout, int bf16, int tile, const GemmArgs& a, hipStream_t s);

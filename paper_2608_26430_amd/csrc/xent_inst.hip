@@ -19,10 +19,17 @@ hipError_t XENT_NAME(XENT_LAYOUT, XENT_BF16)(int tile, const GemmArgs& a, hipStr
   typedef float E;
 #endif
   constexpr bool TRA = XENT_LAYOUT != 0, TRB = XENT_LAYOUT == 2;
-  const dim3 grid((unsigned)(a.tm * a.tn * a.splits));
+  // large tiles: one workgroup per CU walks all of its tiles, each tile's first loads under the last one's results;
+  // medium tiles hide them under the other workgroup of the CU, and walking cost them 7 to 24%
+  const int total = a.tm * a.tn * a.splits;
+  const dim3 grid((unsigned)(total > kCUs && tile == kLarge ? kCUs : total));
+#if XENT_BF16
   if (tile == kLarge) {
     hipLaunchKernelGGL((gemm_kernel<E, 256, 256, 2, 4, 2, TRA, TRB, 2>), grid, dim3(512), 0, s, a);
-  } else if (tile == kMedium) {
+    return hipGetLastError();
+  }
+#endif
+  if (tile == kMedium) {
     hipLaunchKernelGGL((gemm_kernel<E, 128, 128, 2, 2, 2, TRA, TRB, 2>), grid, dim3(256), 0, s, a);
   } else {
     hipLaunchKernelGGL((gemm_kernel<E, 128, 32, 4, 1, 4, TRA, TRB, 2>), grid, dim3(256), 0, s, a);
