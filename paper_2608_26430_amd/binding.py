@@ -613,9 +613,28 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _out_rows(t, name, like, stream, beta=0.0):
+    """(tensor, pointer, leading dimension) of a result shaped as `like`, made when t is None."""
+    if t is None:
+        if beta != 0.0:
+            raise ValueError(f"beta != 0 needs an existing {name}")
+        t = _new(like.shape, like.dtype, like.device, stream)
+        return t, t.data_ptr(), t.shape[1]
+    return (t,) + _rows(t, name, like.shape, like.dtype, like.device)
+
+
+def _out_array(t, name, n, device, stream):
+    """(tensor, pointer) of n fp32 results, made when t is None."""
+    f32 = (_T or _torch()).float32
+    if t is None:
+        t = _new((n,), f32, device, stream)
+        return t, t.data_ptr()
+    return t, _array(t, name, n, f32, device)
+
+
 def _rows(t, name, shape, dtype, device):
     st = t.stride()
-    if len(st) != 2 or (st[1] != 1 and shape[1] != 1) or t.shape != shape or t.dtype is not dtype or t.device != device:
+    if t.shape != shape or len(st) != 2 or (st[1] != 1 and shape[1] != 1) or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name} must be a {shape[0]} x {shape[1]} {dtype} tensor with unit column stride on {device}")
     # the stride of a single row says nothing
     return t.data_ptr(), max(st[0], shape[1]) if shape[0] < 2 else st[0]
@@ -623,13 +642,14 @@ def _rows(t, name, shape, dtype, device):
 
 def _input(t, name):
     """Pointer, leading dimension, sizes of an activation that the call takes its type and device from."""
-    if t.dim() != 2 or not t.is_cuda:
-        raise ValueError(f"{name} must be a 2-D device tensor")
-    return _rows(t, name, t.shape, t.dtype, t.device)
+    st = t.stride()
+    if len(st) != 2 or not t.is_cuda or (st[1] != 1 and t.shape[1] != 1):
+        raise ValueError(f"{name} must be a 2-D device tensor with unit column stride")
+    return t.data_ptr(), max(st[0], t.shape[1]) if t.shape[0] < 2 else st[0]
 
 
 def _array(t, name, n, dtype, device):
-    if t.dtype is not dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.dtype is not dtype or t.device != device or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on {device}")
     return t.data_ptr()
 
@@ -642,21 +662,9 @@ def _workspace(ws, nbytes, device, stream):
     return ws
 
 
-class _on_device:
-    """The call's device as the current one: launches and the default stream are the current device's."""
-
-    def __init__(self, device):
-        cuda = (_T or _torch())._C
-        self.prev = None if cuda._cuda_getDevice() == device.index else device
-
-    def __enter__(self):
-        if self.prev is not None:
-            self.prev = _torch().cuda.device(self.prev)
-            self.prev.__enter__()
-
-    def __exit__(self, *exc):
-        if self.prev is not None:
-            self.prev.__exit__(*exc)
+def _elsewhere(device):
+    """True when the call's device is not the current one (launches and the default stream are the current one's)."""
+    return device.index != (_T or _torch())._C._cuda_getDevice()
 
 
 def _norm_vector(t, name, n, device):
@@ -674,19 +682,19 @@ def layernorm_fwd(X, weight=None, bias=None, eps: float = 1e-5, Y=None, mean=Non
     xp, ldx = _input(X, "X")
     T, n = X.shape
     dev = X.device
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return layernorm_fwd(X, weight, bias, eps, Y, mean, rstd, stream)
     act = _act_code(X)
     w_dtype = weight.dtype if weight is not None else (bias.dtype if bias is not None else torch.float32)
     if w_dtype not in (torch.float32, torch.bfloat16) or (bias is not None and bias.dtype is not w_dtype):
         raise ValueError("weight and bias must both be fp32 or both bf16")
-    with _on_device(dev):
-        Y = _new((T, n), X.dtype, dev, stream) if Y is None else Y
-        mean = _new((T,), torch.float32, dev, stream) if mean is None else mean
-        rstd = _new((T,), torch.float32, dev, stream) if rstd is None else rstd
-        yp, ldy = _rows(Y, "Y", X.shape, X.dtype, dev)
-        _check((_lib or _load()).ff_layernorm_fwd(
-            T, n, act, xp, ldx, FF_BF16 if w_dtype is torch.bfloat16 else FF_F32, _norm_vector(weight, "weight", n, dev),
-            _norm_vector(bias, "bias", n, dev), eps, yp, ldy, _array(mean, "mean", T, torch.float32, dev),
-            _array(rstd, "rstd", T, torch.float32, dev), _stream(stream)))
+    Y, yp, ldy = _out_rows(Y, "Y", X, stream)
+    mean, mp = _out_array(mean, "mean", T, dev, stream)
+    rstd, rp = _out_array(rstd, "rstd", T, dev, stream)
+    _check((_lib or _load()).ff_layernorm_fwd(
+        T, n, act, xp, ldx, FF_BF16 if w_dtype is torch.bfloat16 else FF_F32, _norm_vector(weight, "weight", n, dev),
+        _norm_vector(bias, "bias", n, dev), eps, yp, ldy, mp, rp, _stream(stream)))
     return Y, mean, rstd
 
 
@@ -709,29 +717,28 @@ def layernorm_bwd(X, G, weight, mean, rstd, dX=None, dweight=None, dbias=None, b
     xp, ldx = _input(X, "X")
     T, n = X.shape
     dev, f32 = X.device, torch.float32
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return layernorm_bwd(X, G, weight, mean, rstd, dX, dweight, dbias, beta_dx, accumulate, want_dx, want_dw,
+                                 workspace, stream)
     gp, ldg = _rows(G, "G", X.shape, X.dtype, dev)
     w_dtype = weight.dtype if weight is not None else f32
     if w_dtype not in (f32, torch.bfloat16):
         raise ValueError("weight must be fp32 or bf16")
-    if want_dx and dX is None and beta_dx != 0.0:
-        raise ValueError("beta_dx != 0 needs an existing dX")
     if want_dw and accumulate and (dweight is None or dbias is None):
         raise ValueError("accumulate needs existing dweight and dbias")
-    with _on_device(dev):
-        dxp, lddx, dwp, dbp, wsp, wsn = None, n, None, None, None, 0
-        if want_dx:
-            dX = _new((T, n), X.dtype, dev, stream) if dX is None else dX
-            dxp, lddx = _rows(dX, "dX", X.shape, X.dtype, dev)
-        if want_dw:
-            dweight = _new((n,), f32, dev, stream) if dweight is None else dweight
-            dbias = _new((n,), f32, dev, stream) if dbias is None else dbias
-            dwp, dbp = _array(dweight, "dweight", n, f32, dev), _array(dbias, "dbias", n, f32, dev)
-            workspace = _workspace(workspace, _layernorm_bytes(T, n) if workspace is None else 0, dev, stream)
-            wsp, wsn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        _check((_lib or _load()).ff_layernorm_bwd(
-            T, n, _act_code(X), xp, ldx, gp, ldg, FF_BF16 if w_dtype is torch.bfloat16 else FF_F32,
-            _norm_vector(weight, "weight", n, dev), _array(mean, "mean", T, f32, dev), _array(rstd, "rstd", T, f32, dev),
-            beta_dx, dxp, lddx, int(accumulate), dwp, dbp, wsp, wsn, _stream(stream)))
+    dxp, lddx, dwp, dbp, wsp, wsn = None, n, None, None, None, 0
+    if want_dx:
+        dX, dxp, lddx = _out_rows(dX, "dX", X, stream, beta_dx)
+    if want_dw:
+        dweight, dwp = _out_array(dweight, "dweight", n, dev, stream)
+        dbias, dbp = _out_array(dbias, "dbias", n, dev, stream)
+        workspace = _workspace(workspace, _layernorm_bytes(T, n) if workspace is None else 0, dev, stream)
+        wsp, wsn = workspace.data_ptr(), workspace.nbytes
+    _check((_lib or _load()).ff_layernorm_bwd(
+        T, n, _act_code(X), xp, ldx, gp, ldg, FF_BF16 if w_dtype is torch.bfloat16 else FF_F32,
+        _norm_vector(weight, "weight", n, dev), _array(mean, "mean", T, f32, dev), _array(rstd, "rstd", T, f32, dev),
+        beta_dx, dxp, lddx, int(accumulate), dwp, dbp, wsp, wsn, _stream(stream)))
     return (dX if want_dx else None), (dweight if want_dw else None), (dbias if want_dw else None)
 
 
@@ -743,14 +750,15 @@ def dropout(X, p: float, seed: int, offset: int = 0, residual=None, Y=None, offs
     xp, ldx = _input(X, "X")
     T, n = X.shape
     dev = X.device
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return dropout(X, p, seed, offset, residual, Y, offset_dev, stream)
     act = _act_code(X)
-    with _on_device(dev):
-        Y = _new((T, n), X.dtype, dev, stream) if Y is None else Y
-        yp, ldy = _rows(Y, "Y", X.shape, X.dtype, dev)
-        rp, ldr = _rows(residual, "residual", X.shape, X.dtype, dev) if residual is not None else (None, n)
-        op = _array(offset_dev.view(1), "offset_dev", 1, torch.int64, dev) if offset_dev is not None else None
-        _check((_lib or _load()).ff_dropout(T, n, act, xp, ldx, p, seed & (1 << 64) - 1, offset & (1 << 64) - 1, op, rp, ldr,
-                                            yp, ldy, _stream(stream)))
+    Y, yp, ldy = _out_rows(Y, "Y", X, stream)
+    rp, ldr = _rows(residual, "residual", X.shape, X.dtype, dev) if residual is not None else (None, n)
+    op = _array(offset_dev.view(1), "offset_dev", 1, torch.int64, dev) if offset_dev is not None else None
+    _check((_lib or _load()).ff_dropout(T, n, act, xp, ldx, p, seed & (1 << 64) - 1, offset & (1 << 64) - 1, op, rp, ldr,
+                                        yp, ldy, _stream(stream)))
     return Y
 
 
@@ -782,32 +790,27 @@ def _head(H, W, target):
 def xent_fwd(H, W, target, loss=None, lse=None, workspace=None, stream=None):
     """Cross entropy of the logits H W^T of each token, without keeping the logits: returns (loss, lse), fp32 per token.
     Targets outside [0, V) mark tokens without loss (ff_xent_fwd)."""
-    f32 = (_T or _torch()).float32
     T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
     dev = H.device
-    with _on_device(dev):
-        loss = _new((T,), f32, dev, stream) if loss is None else loss
-        lse = _new((T,), f32, dev, stream) if lse is None else lse
-        ws = _workspace(workspace, _xent_bytes(T, n, V, act, 0) if workspace is None else 0, dev, stream)
-        _check((_lib or _load()).ff_xent_fwd(T, n, V, act, hp, ldh, wp, ldw, tp, _array(loss, "loss", T, f32, dev),
-                                             _array(lse, "lse", T, f32, dev), ws.data_ptr(),
-                                             ws.numel() * ws.element_size(), _stream(stream)))
+    if _elsewhere(dev):
+        with _torch().cuda.device(dev):
+            return xent_fwd(H, W, target, loss, lse, workspace, stream)
+    loss, lop = _out_array(loss, "loss", T, dev, stream)
+    lse, lsp = _out_array(lse, "lse", T, dev, stream)
+    ws = _workspace(workspace, _xent_bytes(T, n, V, act, 0) if workspace is None else 0, dev, stream)
+    _check((_lib or _load()).ff_xent_fwd(T, n, V, act, hp, ldh, wp, ldw, tp, lop, lsp, ws.data_ptr(), ws.nbytes,
+                                         _stream(stream)))
     return loss, lse
 
 
 def _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream):
-    """(dH, its pointer and stride, dW, ...), made where they are wanted and not given."""
-    if (want_dh and dH is None and beta_dh != 0.0) or (want_dw and dW is None and beta_dw != 0.0):
-        raise ValueError("beta != 0 needs an existing output")
-    n, dev = H.shape[1], H.device
+    """(dH, its pointer and leading dimension, dW, ...), made where they are wanted and not given."""
     dhp = dwp = None
-    ldh = ldw = n
+    ldh = ldw = H.shape[1]
     if want_dh:
-        dH = _new(H.shape, H.dtype, dev, stream) if dH is None else dH
-        dhp, ldh = _rows(dH, "dH", H.shape, H.dtype, dev)
+        dH, dhp, ldh = _out_rows(dH, "dH", H, stream, beta_dh)
     if want_dw:
-        dW = _new(W.shape, H.dtype, dev, stream) if dW is None else dW
-        dwp, ldw = _rows(dW, "dW", W.shape, H.dtype, dev)
+        dW, dwp, ldw = _out_rows(dW, "dW", W, stream, beta_dw)
     return (dH if want_dh else None), dhp, ldh, (dW if want_dw else None), dwp, ldw
 
 
@@ -819,15 +822,18 @@ def xent_bwd(H, W, target, lse, dloss=None, scale: float = 1.0, dH=None, dW=None
     f32 = (_T or _torch()).float32
     T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
     dev = H.device
-    with _on_device(dev):
-        dH, dhp, lddh, dW, dwp, lddw = _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream)
-        want = int(want_dh) + 2 * int(want_dw)
-        ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, dev, stream)
-        _check((_lib or _load()).ff_xent_bwd(
-            T, n, V, act, hp, ldh, wp, ldw, tp, _array(lse, "lse", T, f32, dev),
-            _array(loss, "loss", T, f32, dev) if loss is not None else None,
-            _array(dloss, "dloss", T, f32, dev) if dloss is not None else None, scale, beta_dh, dhp, lddh, beta_dw, dwp,
-            lddw, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+    if _elsewhere(dev):
+        with _torch().cuda.device(dev):
+            return xent_bwd(H, W, target, lse, dloss, scale, dH, dW, beta_dh, beta_dw, want_dh, want_dw, workspace, stream,
+                            loss)
+    dH, dhp, lddh, dW, dwp, lddw = _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream)
+    want = int(want_dh) + 2 * int(want_dw)
+    ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, dev, stream)
+    _check((_lib or _load()).ff_xent_bwd(
+        T, n, V, act, hp, ldh, wp, ldw, tp, _array(lse, "lse", T, f32, dev),
+        _array(loss, "loss", T, f32, dev) if loss is not None else None,
+        _array(dloss, "dloss", T, f32, dev) if dloss is not None else None, scale, beta_dh, dhp, lddh, beta_dw, dwp,
+        lddw, ws.data_ptr(), ws.nbytes, _stream(stream)))
     return dH, dW
 
 
@@ -838,16 +844,18 @@ def xent_step(H, W, target, dloss=None, scale: float = 1.0, loss=None, lse=None,
     f32 = (_T or _torch()).float32
     T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
     dev = H.device
-    with _on_device(dev):
-        loss = _new((T,), f32, dev, stream) if loss is None else loss
-        lse = _new((T,), f32, dev, stream) if lse is None else lse
-        dH, dhp, lddh, dW, dwp, lddw = _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream)
-        want = int(want_dh) + 2 * int(want_dw)
-        ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, dev, stream)
-        _check((_lib or _load()).ff_xent_step(
-            T, n, V, act, hp, ldh, wp, ldw, tp, _array(dloss, "dloss", T, f32, dev) if dloss is not None else None, scale,
-            _array(loss, "loss", T, f32, dev), _array(lse, "lse", T, f32, dev), beta_dh, dhp, lddh, beta_dw, dwp, lddw,
-            ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+    if _elsewhere(dev):
+        with _torch().cuda.device(dev):
+            return xent_step(H, W, target, dloss, scale, loss, lse, dH, dW, beta_dh, beta_dw, want_dh, want_dw, workspace,
+                             stream)
+    loss, lop = _out_array(loss, "loss", T, dev, stream)
+    lse, lsp = _out_array(lse, "lse", T, dev, stream)
+    dH, dhp, lddh, dW, dwp, lddw = _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream)
+    want = int(want_dh) + 2 * int(want_dw)
+    ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, dev, stream)
+    _check((_lib or _load()).ff_xent_step(
+        T, n, V, act, hp, ldh, wp, ldw, tp, _array(dloss, "dloss", T, f32, dev) if dloss is not None else None, scale,
+        lop, lsp, beta_dh, dhp, lddh, beta_dw, dwp, lddw, ws.data_ptr(), ws.nbytes, _stream(stream)))
     return loss, lse, dH, dW
 
 

@@ -213,23 +213,39 @@ struct Product {
   int kt_split;
 };
 
-// Tile and split of k of a product with M columns, N rows and kt k tiles.
+// Microseconds of a k tile on one CU, from measured calls: with workgroups enough to fill the CU, and with one workgroup
+// per CU at most; and the k tiles that a tile's start and end cost.
+//   bf16 large  1.53 / 1.53    4096 tokens x 32,000 entries, 4096 wide: logits 840 us (medium 1040), dH 770 (1030)
+//        medium 0.51 / 0.80    1003 x 30,001, 768 wide: dW 52 us (large 61); 128 x 32,000, 4096 wide: logits 60 (97, small 73)
+//        small  0.30 / 0.60    16 x 32,000, 4096 wide: logits 41 us (medium 58); 64 tokens 48 (60)
+//   fp32 medium 1.92 / 1.92    2048 x 33,000, 1024 wide: logits 1060 us (small 1120)
+//        small  0.50 / 0.75    200 x 3000, 512 wide: logits 14 us (medium 39); 500 x 8001, 768 wide: dW 59 (68)
+// The large tile has no fp32 instance: its registers spill.
+struct TileCost {
+  double full, single, ends;
+};
+constexpr TileCost kCosts[2][3] = {{{0, 0, 0}, {1.92, 1.92, 2}, {0.50, 0.75, 2}},
+                                   {{1.53, 1.53, 5}, {0.51, 0.80, 3}, {0.30, 0.60, 4}}};
+
+// Tile and split of k of a product with M columns, N rows and kt k tiles: the least estimated time, where partial sums are
+// written and read at about 4.5 TB/s by a launch more.
 Product choose(int64_t M, int64_t N, int64_t kt, bool may_split, bool bf16) {
-  Product p{kSmall, 1, (int)kt};
-  if (N > 32) {
-    if (bf16 && N >= 192 && M >= 192 && tiles_of(M, N, kLarge) * (may_split ? kt / 8 + 1 : 1) >= kCUs / 2) p.tile = kLarge;
-    else if (tiles_of(M, N, kMedium) * (may_split ? kt / 8 + 1 : 1) >= kCUs / 2) p.tile = kMedium;
+  Product best{kSmall, 1, (int)kt};
+  double least = 1e30;
+  for (int tile = bf16 ? kLarge : kMedium; tile <= kSmall; ++tile) {
+    const TileCost& u = kCosts[bf16][tile];
+    const int64_t tiles = tiles_of(M, N, tile);
+    for (int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64}) {
+      if (s > 1 && (!may_split || s > kt / 4)) break;
+      const int64_t per = (kt + s - 1) / s, splits = (kt + per - 1) / per, wgs = tiles * splits;
+      const int64_t rounds = (wgs + kCUs - 1) / kCUs;
+      double t = (double)rounds * ((double)per + u.ends) * (rounds == 1 ? u.single : u.full);
+      if (splits > 1) t += 3.0 + (double)splits * (double)N * (double)M * 8.0 / 4.5e6;
+      if (t < least) least = t, best = Product{tile, (int)splits, (int)per};
+      if (wgs >= 4 * kCUs) break;
+    }
   }
-  if (may_split) {
-    const int64_t want = p.tile == kLarge ? kCUs : 2 * kCUs, have = tiles_of(M, N, p.tile);
-    int64_t s = want / have;
-    if (s > kt / 8) s = kt / 8;
-    if (s > 64) s = 64;
-    if (s < 1) s = 1;
-    p.kt_split = (int)((kt + s - 1) / s);
-    p.splits = (int)((kt + p.kt_split - 1) / p.kt_split);
-  }
-  return p;
+  return best;
 }
 
 struct Call {
