@@ -618,39 +618,49 @@ def _out_rows(t, name, like, stream, beta=0.0):
     if t is None:
         if beta != 0.0:
             raise ValueError(f"beta != 0 needs an existing {name}")
-        t = _new(like.shape, like.dtype, like.device, stream)
+        if stream is None and like.is_contiguous():
+            t = (_T or _torch()).empty_like(like)
+        else:
+            t = _new(like.shape, like.dtype, like.device, stream)
         return t, t.data_ptr(), t.shape[1]
-    return (t,) + _rows(t, name, like.shape, like.dtype, like.device)
+    return (t,) + _rows(t, name, like)
 
 
 def _out_array(t, name, n, device, stream):
     """(tensor, pointer) of n fp32 results, made when t is None."""
     f32 = (_T or _torch()).float32
     if t is None:
-        t = _new((n,), f32, device, stream)
+        t = _new(n, f32, device, stream)
         return t, t.data_ptr()
-    return t, _array(t, name, n, f32, device)
+    return t, _array(t, name, n, f32, device.index)
 
 
-def _rows(t, name, shape, dtype, device):
+def _rows(t, name, like):
+    """Pointer and leading dimension of a tensor that must be shaped as `like`, with rows of its own."""
     st = t.stride()
-    if t.shape != shape or len(st) != 2 or (st[1] != 1 and shape[1] != 1) or t.dtype is not dtype or t.device != device:
-        raise ValueError(f"{name} must be a {shape[0]} x {shape[1]} {dtype} tensor with unit column stride on {device}")
+    if (t.dtype is not like.dtype or t.shape != like.shape or t.get_device() != like.get_device()
+            or (st[1] != 1 and t.shape[1] != 1)):
+        raise ValueError(f"{name} must be a {like.shape[0]} x {like.shape[1]} {like.dtype} tensor with unit column stride "
+                         f"on {like.device}")
     # the stride of a single row says nothing
-    return t.data_ptr(), max(st[0], shape[1]) if shape[0] < 2 else st[0]
-
-
-def _input(t, name):
-    """Pointer, leading dimension, sizes of an activation that the call takes its type and device from."""
-    st = t.stride()
-    if len(st) != 2 or not t.is_cuda or (st[1] != 1 and t.shape[1] != 1):
-        raise ValueError(f"{name} must be a 2-D device tensor with unit column stride")
     return t.data_ptr(), max(st[0], t.shape[1]) if t.shape[0] < 2 else st[0]
 
 
-def _array(t, name, n, dtype, device):
-    if t.dtype is not dtype or t.device != device or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on {device}")
+def _input(t, name):
+    """Pointer, leading dimension, sizes and device index of an activation that the call takes type and device from."""
+    st = t.stride()
+    dev = t.get_device()
+    if len(st) != 2 or dev < 0:
+        raise ValueError(f"{name} must be a 2-D device tensor with unit column stride")
+    T, n = t.shape
+    if st[1] != 1 and n != 1:
+        raise ValueError(f"{name} must be a 2-D device tensor with unit column stride")
+    return t.data_ptr(), (max(st[0], n) if T < 2 else st[0]), T, n, dev
+
+
+def _array(t, name, n, dtype, dev):
+    if t.dtype is not dtype or t.get_device() != dev or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on device {dev}")
     return t.data_ptr()
 
 
@@ -662,16 +672,16 @@ def _workspace(ws, nbytes, device, stream):
     return ws
 
 
-def _elsewhere(device):
+def _elsewhere(dev):
     """True when the call's device is not the current one (launches and the default stream are the current one's)."""
-    return device.index != (_T or _torch())._C._cuda_getDevice()
+    return dev != (_T or _torch())._C._cuda_getDevice()
 
 
-def _norm_vector(t, name, n, device):
+def _norm_vector(t, name, n, dev):
     """Pointer of a layer norm's weight or bias, None for none."""
     if t is None:
         return None
-    return _array(t, name, n, t.dtype, device)
+    return _array(t, name, n, t.dtype, dev)
 
 
 def layernorm_fwd(X, weight=None, bias=None, eps: float = 1e-5, Y=None, mean=None, rstd=None, stream=None):
@@ -679,9 +689,7 @@ def layernorm_fwd(X, weight=None, bias=None, eps: float = 1e-5, Y=None, mean=Non
     layernorm_bwd (ff_layernorm_fwd).  weight and bias: fp32 or bf16, both of one type; None for ones / zeros.  Y
     may be X."""
     torch = _T or _torch()
-    xp, ldx = _input(X, "X")
-    T, n = X.shape
-    dev = X.device
+    xp, ldx, T, n, dev = _input(X, "X")
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return layernorm_fwd(X, weight, bias, eps, Y, mean, rstd, stream)
@@ -690,8 +698,8 @@ def layernorm_fwd(X, weight=None, bias=None, eps: float = 1e-5, Y=None, mean=Non
     if w_dtype not in (torch.float32, torch.bfloat16) or (bias is not None and bias.dtype is not w_dtype):
         raise ValueError("weight and bias must both be fp32 or both bf16")
     Y, yp, ldy = _out_rows(Y, "Y", X, stream)
-    mean, mp = _out_array(mean, "mean", T, dev, stream)
-    rstd, rp = _out_array(rstd, "rstd", T, dev, stream)
+    mean, mp = _out_array(mean, "mean", T, X.device, stream)
+    rstd, rp = _out_array(rstd, "rstd", T, X.device, stream)
     _check((_lib or _load()).ff_layernorm_fwd(
         T, n, act, xp, ldx, FF_BF16 if w_dtype is torch.bfloat16 else FF_F32, _norm_vector(weight, "weight", n, dev),
         _norm_vector(bias, "bias", n, dev), eps, yp, ldy, mp, rp, _stream(stream)))
@@ -714,14 +722,13 @@ def layernorm_bwd(X, G, weight, mean, rstd, dX=None, dweight=None, dbias=None, b
     """Backward of layernorm_fwd for upstream gradient G: returns (dX, dweight, dbias) (None where not wanted), dX =
     beta_dx * dX + ..., dweight and dbias fp32, added to the given ones with `accumulate` (ff_layernorm_bwd)."""
     torch = _T or _torch()
-    xp, ldx = _input(X, "X")
-    T, n = X.shape
-    dev, f32 = X.device, torch.float32
+    xp, ldx, T, n, dev = _input(X, "X")
+    f32 = torch.float32
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return layernorm_bwd(X, G, weight, mean, rstd, dX, dweight, dbias, beta_dx, accumulate, want_dx, want_dw,
                                  workspace, stream)
-    gp, ldg = _rows(G, "G", X.shape, X.dtype, dev)
+    gp, ldg = _rows(G, "G", X)
     w_dtype = weight.dtype if weight is not None else f32
     if w_dtype not in (f32, torch.bfloat16):
         raise ValueError("weight must be fp32 or bf16")
@@ -731,9 +738,9 @@ def layernorm_bwd(X, G, weight, mean, rstd, dX=None, dweight=None, dbias=None, b
     if want_dx:
         dX, dxp, lddx = _out_rows(dX, "dX", X, stream, beta_dx)
     if want_dw:
-        dweight, dwp = _out_array(dweight, "dweight", n, dev, stream)
-        dbias, dbp = _out_array(dbias, "dbias", n, dev, stream)
-        workspace = _workspace(workspace, _layernorm_bytes(T, n) if workspace is None else 0, dev, stream)
+        dweight, dwp = _out_array(dweight, "dweight", n, X.device, stream)
+        dbias, dbp = _out_array(dbias, "dbias", n, X.device, stream)
+        workspace = _workspace(workspace, _layernorm_bytes(T, n) if workspace is None else 0, X.device, stream)
         wsp, wsn = workspace.data_ptr(), workspace.nbytes
     _check((_lib or _load()).ff_layernorm_bwd(
         T, n, _act_code(X), xp, ldx, gp, ldg, FF_BF16 if w_dtype is torch.bfloat16 else FF_F32,
@@ -747,15 +754,13 @@ def dropout(X, p: float, seed: int, offset: int = 0, residual=None, Y=None, offs
     and is never stored (ff_dropout); the backward pass is the same call on the gradient.  offset_dev: a device int64
     tensor of one element added to offset when the call runs (for captured graphs).  Y may be X or residual."""
     torch = _T or _torch()
-    xp, ldx = _input(X, "X")
-    T, n = X.shape
-    dev = X.device
+    xp, ldx, T, n, dev = _input(X, "X")
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return dropout(X, p, seed, offset, residual, Y, offset_dev, stream)
     act = _act_code(X)
     Y, yp, ldy = _out_rows(Y, "Y", X, stream)
-    rp, ldr = _rows(residual, "residual", X.shape, X.dtype, dev) if residual is not None else (None, n)
+    rp, ldr = _rows(residual, "residual", X) if residual is not None else (None, n)
     op = _array(offset_dev.view(1), "offset_dev", 1, torch.int64, dev) if offset_dev is not None else None
     _check((_lib or _load()).ff_dropout(T, n, act, xp, ldx, p, seed & (1 << 64) - 1, offset & (1 << 64) - 1, op, rp, ldr,
                                         yp, ldy, _stream(stream)))
@@ -778,26 +783,23 @@ def xent_workspace(T: int, n: int, V: int, dtype, want_dh: bool = False, want_dw
 
 
 def _head(H, W, target):
-    torch = _T or _torch()
-    hp, ldh = _input(H, "H")
-    T, n = H.shape
-    if W.dim() != 2 or W.shape[0] < 1 or W.shape[1] != n:
-        raise ValueError("W must be a V x n tensor, n the width of H")
-    wp, ldw = _rows(W, "W", W.shape, H.dtype, H.device)
-    return T, n, W.shape[0], _act_code(H), hp, ldh, wp, ldw, _array(target, "target", T, torch.int64, H.device)
+    hp, ldh, T, n, dev = _input(H, "H")
+    wp, ldw, V, nw, wdev = _input(W, "W")
+    if V < 1 or nw != n or W.dtype is not H.dtype or wdev != dev:
+        raise ValueError(f"W must be a V x {n} {H.dtype} tensor on {H.device}")
+    return T, n, V, _act_code(H), hp, ldh, wp, ldw, _array(target, "target", T, (_T or _torch()).int64, dev), dev
 
 
 def xent_fwd(H, W, target, loss=None, lse=None, workspace=None, stream=None):
     """Cross entropy of the logits H W^T of each token, without keeping the logits: returns (loss, lse), fp32 per token.
     Targets outside [0, V) mark tokens without loss (ff_xent_fwd)."""
-    T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
-    dev = H.device
+    T, n, V, act, hp, ldh, wp, ldw, tp, dev = _head(H, W, target)
     if _elsewhere(dev):
         with _torch().cuda.device(dev):
             return xent_fwd(H, W, target, loss, lse, workspace, stream)
-    loss, lop = _out_array(loss, "loss", T, dev, stream)
-    lse, lsp = _out_array(lse, "lse", T, dev, stream)
-    ws = _workspace(workspace, _xent_bytes(T, n, V, act, 0) if workspace is None else 0, dev, stream)
+    loss, lop = _out_array(loss, "loss", T, H.device, stream)
+    lse, lsp = _out_array(lse, "lse", T, H.device, stream)
+    ws = _workspace(workspace, _xent_bytes(T, n, V, act, 0) if workspace is None else 0, H.device, stream)
     _check((_lib or _load()).ff_xent_fwd(T, n, V, act, hp, ldh, wp, ldw, tp, lop, lsp, ws.data_ptr(), ws.nbytes,
                                          _stream(stream)))
     return loss, lse
@@ -820,15 +822,14 @@ def xent_bwd(H, W, target, lse, dloss=None, scale: float = 1.0, dH=None, dW=None
     dloss: fp32 per token, None for ones; loss: that of xent_fwd, for the target's gradient of tokens whose loss is near
     zero (ff_xent_bwd)."""
     f32 = (_T or _torch()).float32
-    T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
-    dev = H.device
+    T, n, V, act, hp, ldh, wp, ldw, tp, dev = _head(H, W, target)
     if _elsewhere(dev):
         with _torch().cuda.device(dev):
             return xent_bwd(H, W, target, lse, dloss, scale, dH, dW, beta_dh, beta_dw, want_dh, want_dw, workspace, stream,
                             loss)
     dH, dhp, lddh, dW, dwp, lddw = _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream)
     want = int(want_dh) + 2 * int(want_dw)
-    ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, dev, stream)
+    ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, H.device, stream)
     _check((_lib or _load()).ff_xent_bwd(
         T, n, V, act, hp, ldh, wp, ldw, tp, _array(lse, "lse", T, f32, dev),
         _array(loss, "loss", T, f32, dev) if loss is not None else None,
@@ -842,17 +843,16 @@ def xent_step(H, W, target, dloss=None, scale: float = 1.0, loss=None, lse=None,
     """xent_fwd and xent_bwd in one call, which computes the logits once: returns (loss, lse, dH, dW), dH and dW the
     gradients of sum_t scale dloss[t] loss[t] (None where not wanted; ff_xent_step)."""
     f32 = (_T or _torch()).float32
-    T, n, V, act, hp, ldh, wp, ldw, tp = _head(H, W, target)
-    dev = H.device
+    T, n, V, act, hp, ldh, wp, ldw, tp, dev = _head(H, W, target)
     if _elsewhere(dev):
         with _torch().cuda.device(dev):
             return xent_step(H, W, target, dloss, scale, loss, lse, dH, dW, beta_dh, beta_dw, want_dh, want_dw, workspace,
                              stream)
-    loss, lop = _out_array(loss, "loss", T, dev, stream)
-    lse, lsp = _out_array(lse, "lse", T, dev, stream)
+    loss, lop = _out_array(loss, "loss", T, H.device, stream)
+    lse, lsp = _out_array(lse, "lse", T, H.device, stream)
     dH, dhp, lddh, dW, dwp, lddw = _head_grads(H, W, dH, dW, beta_dh, beta_dw, want_dh, want_dw, stream)
     want = int(want_dh) + 2 * int(want_dw)
-    ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, dev, stream)
+    ws = _workspace(workspace, _xent_bytes(T, n, V, act, want) if workspace is None else 0, H.device, stream)
     _check((_lib or _load()).ff_xent_step(
         T, n, V, act, hp, ldh, wp, ldw, tp, _array(dloss, "dloss", T, f32, dev) if dloss is not None else None, scale,
         lop, lsp, beta_dh, dhp, lddh, beta_dw, dwp, lddw, ws.data_ptr(), ws.nbytes, _stream(stream)))

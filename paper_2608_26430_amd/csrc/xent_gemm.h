@@ -126,6 +126,7 @@ struct Operand {
       if (PF == 0) return row & 7;
       return (row & 3) | (((row >> 3) & 1) << 2);
     }
+    if (kE == 2 && kPieces == 4) return row & 2;
     const int s = kE == 2 ? (((row & 3) << 1) ^ (((row >> 3) & 1) << 3)) : (((row >> 2) & 3) << 2);
     return s & (kPieces - 1);
   }
@@ -420,12 +421,16 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
   oa.init(a.lda, wave, lane);
   ob.init(a.ldb, wave, lane);
   int i0, j0, split, nkt;      // the tile whose operands are being read
-  auto seek = [&](int wg) {
+  int i_next, j_next, split_next;
+  auto place = [&](int wg) {   // of a workgroup's next tile: divisions, done while its loads are awaited
     const int id = share_of(wg, total);
-    split = id / tiles;
+    split_next = id / tiles;
     int im, in;
-    tile_of(id - split * tiles, a.tm, a.tn, &im, &in);
-    i0 = im * BM, j0 = in * BN;
+    tile_of(id - split_next * tiles, a.tm, a.tn, &im, &in);
+    i_next = im * BM, j_next = in * BN;
+  };
+  auto seek = [&]() {
+    split = split_next, i0 = i_next, j0 = j_next;
     const int kt0 = split * a.kt_split;
     nkt = a.kt - kt0 < a.kt_split ? a.kt - kt0 : a.kt_split;
     oa.seek(a.A, a.lda, i0, a.M, kt0);
@@ -443,8 +448,8 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
     ob.issue(t < nkt, lds0 + buf * kBuf + OpA::kBytes, wave);
   };
   int64_t raw[FN];             // targets of that tile's tokens
-  auto start = [&](int wg) {
-    seek(wg);
+  auto start = [&]() {
+    seek();
     if constexpr (!TRA) {
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
@@ -457,8 +462,10 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
     for (int t = 1; t < (NB == 2 ? 2 : NB - 1); ++t) issue(t, t);
   };
 
-  start(blockIdx.x);
+  place(blockIdx.x);
+  start();
   for (int wg = blockIdx.x;;) {
+  place(wg + gridDim.x);
   // the token's target as a column of A (-1: none, -2: in another piece of the vocabulary)
   int target[FN] = {};
   if constexpr (!TRA) {
@@ -528,7 +535,7 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
   const bool more = wg < total;
   if (more) {
     ring_wait<0>();      // every wave's reads of the buffers are done
-    start(wg);
+    start();
   }
   finish<E, FM, FN, TM, PF, TRA>(a, acc, target, wi0, wj0, wsplit, lane);
   if (!more) break;
