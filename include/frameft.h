@@ -452,7 +452,7 @@ ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, 
  *                P keeps its digits where its probability is near one, as in ff_xent_step (from lse alone it carries
  *                lse's rounding).
  * dH == NULL or dW == NULL skips that output.  Arithmetic: products accumulate in fp32, softmax statistics are fp32, P is
- * rounded to type act before the products that read it (in ff_xent_step after one more rounding of exp(z - max)).
+ * rounded to type act before the products that read it (in ff_xent_step with bf16, after exp(z - max) was rounded to fp16).
  * With T = 0, dW = beta_dw dW.
  */
 enum { FF_XENT_DH = 1, FF_XENT_DW = 2 };

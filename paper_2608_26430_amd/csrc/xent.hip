@@ -13,8 +13,8 @@
 //                   of a token are joined, e becomes P in place: 2 products (3 with dW) instead of the 3 (4) of a
 //                   backward that computes the logits again.
 //   backward alone  logits product whose epilogue writes P from the saved lse.
-// P is kept in the activations' type: each of its values carries one rounding (two where e is stored first, each of
-// 2^-9 relative in bf16), as do the factors W and H.  The sums of exponentials leave the target out: its own value of P,
+// P is kept in the activations' type: each of its values carries one rounding (2^-9 relative in bf16), as do the
+// factors W and H; e, stored first, is in fp16 (2^-12, and what is under 2^-25 of the columns' maximum is lost).  The sums of exponentials leave the target out: its own value of P,
 // exp(z - lse) - 1, is then minus the others' share, and the loss of a token whose target has the largest logit is log(1 +
 // others), so that both keep their digits when the target's probability is near one.
 // Long calls are cut into pieces of tokens (P of a piece at most kPieceBytes), whose dH are complete.  With dW a cut
@@ -102,13 +102,12 @@ struct Piece16;   // a 16-byte piece as floats
 template <>
 struct Piece16<__bf16> {
   static constexpr int kN = 8;
-  static __device__ __forceinline__ void get(const __bf16* p, float* v) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+  // exponentials, stored in fp16
+  static __device__ __forceinline__ void get_exp(const __bf16* p, float* v) {
+    typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+    const f16x8 w = *reinterpret_cast<const f16x8*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __builtin_bit_cast(float, w[i] << 16);
-      v[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 8; ++i) v[i] = (float)w[i];
   }
   static __device__ __forceinline__ void put(__bf16* p, const float* v) {
     u32x4 w;
@@ -120,7 +119,7 @@ struct Piece16<__bf16> {
 template <>
 struct Piece16<float> {
   static constexpr int kN = 4;
-  static __device__ __forceinline__ void get(const float* p, float* v) {
+  static __device__ __forceinline__ void get_exp(const float* p, float* v) {
     const f32x4 w = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = w[i];
@@ -150,7 +149,7 @@ __global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int N, 
     if (c >= ldp) return;
     float v[kN];
     if (counted) {
-      Piece16<E>::get(row + c, v);
+      Piece16<E>::get_exp(row + c, v);
       // columns past V hold zeros; their entry may be one past the statistics' last
       const float f = c < V ? expf(stats[(int64_t)(c / cols) * N + t].x - ls) * w : 0.f;
 #pragma unroll
