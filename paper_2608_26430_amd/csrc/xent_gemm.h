@@ -19,6 +19,7 @@
 #pragma once
 
 #include "ff_internal.h"
+#include "xent_span.h"
 
 namespace ff {
 namespace xent {
@@ -108,8 +109,8 @@ template <class E, int BX, int NW, bool TR, int PF>
 struct Operand {
   static constexpr int kE = ElemTraits<E>::kSize;
   static constexpr int kPer = 16 / kE;            // elements of a 16-byte piece
-  static constexpr int kK = 128 / kE;             // k of a tile
-  static constexpr int kBytes = BX * 128;
+  static constexpr int kK = kTileBytes / kE;      // k of a tile
+  static constexpr int kBytes = BX * kTileBytes;
   static constexpr int kLoads = kBytes / 1024 / NW;
   static constexpr int kRow = TR ? BX * kE : 128; // bytes of an LDS row
   static constexpr int kPieces = kRow / 16;
@@ -132,7 +133,7 @@ struct Operand {
   }
 
   __device__ __forceinline__ void init(int64_t ld, int wave, int lane) {
-    step = TR ? (uint64_t)kK * ld * kE : 128;
+    step = (uint64_t)k_step(!TR, kE, ld);
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
       const int byte = (wave * kLoads + q) * 1024 + lane * 16;
@@ -141,19 +142,18 @@ struct Operand {
     }
   }
 
-  // x0: first i (j) of the tile, X its extent, kt0: first k tile.  The memory of a row reaches to the next whole
-  // piece (H and W by their widths, P by its zero padding).
+  // x0: first i (j) of the tile, X its extent, kt0: first k tile
   __device__ __forceinline__ void seek(const void* p, int64_t ld, int x0, int X, int kt0) {
-    X = (X + kPer - 1) / kPer * kPer;
-    base = (uint64_t)((const char*)p + (int64_t)x0 * (TR ? 1 : ld) * kE) + kt0 * step;
-    const int rows = X - x0 < BX ? X - x0 : BX;
-    records = TR ? (unsigned)(((int64_t)(kK - 1) * ld + X - x0) * kE) : (unsigned)((int64_t)(rows - 1) * ld * kE) + 128;
+    const Span s = span_of(!TR, kE, BX, ld, x0, X, kt0, kK);
+    base = (uint64_t)((const char*)p + s.first);
+    records = s.bytes;
   }
 
-  // The last k tile, `tile` steps on, of which `left` of k remain: zero beyond them.
-  __device__ __forceinline__ void issue_last(int tile, int left, int64_t ld, unsigned lds, int wave, int lane) const {
+  // The last k tile of the tile at x0, `tile` steps on, of which `left` of k remain: zero beyond them.
+  __device__ __forceinline__ void issue_last(int tile, int left, int64_t ld, int x0, int X, unsigned lds, int wave,
+                                             int lane) const {
     const int pieces = (left + kPer - 1) / kPer;
-    const unsigned n = TR ? records - (unsigned)((int64_t)(kK - left) * ld * kE) : records - 128 + pieces * 16;
+    const unsigned n = span_of(!TR, kE, BX, ld, x0, X, 0, left).bytes;
     const u32x4 r = make_rsrc(base + tile * step, n);
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
@@ -261,23 +261,6 @@ __device__ __forceinline__ f32x4 load4(const __bf16* p) {
   return v;
 }
 __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-
-// Workgroups go round the eight XCDs; each XCD takes a contiguous run of the `total` tiles.
-__device__ __forceinline__ int share_of(int wg, int total) {
-  const int xcd = wg & 7, per = total >> 3, rem = total & 7;
-  return xcd * per + (xcd < rem ? xcd : rem) + (wg >> 3);
-}
-
-// Tiles run in groups of eight along j and then along i, so that those that run at once on an XCD share their operands
-// in its L2.
-__device__ __forceinline__ void tile_of(int id, int tm, int tn, int* im, int* in) {
-  const int group = 8 * tm;
-  const int g = id / group, first = g * 8;
-  const int w = tn - first < 8 ? tn - first : 8;
-  const int in_group = id - g * group;
-  *in = first + in_group % w;
-  *im = in_group / w;
-}
 
 // The results of a wave's tile: FM x FN tiles of 16 x 16 from (i0, j0).
 template <class E, int FM, int FN, int TM, int PF, bool TRA>
@@ -451,8 +434,8 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
   auto issue_last = [&]() {
     if (nkt <= 0) return;
     const int last = a.K - (split * a.kt_split + nkt - 1) * kK;
-    oa.issue_last(nkt - 1, last < kK ? last : kK, a.lda, lds0, wave, lane);
-    ob.issue_last(nkt - 1, last < kK ? last : kK, a.ldb, lds0 + OpA::kBytes, wave, lane);
+    oa.issue_last(nkt - 1, last < kK ? last : kK, a.lda, i0, a.M, lds0, wave, lane);
+    ob.issue_last(nkt - 1, last < kK ? last : kK, a.ldb, j0, a.N, lds0 + OpA::kBytes, wave, lane);
   };
   auto issue = [&](int t, int buf) {
     oa.issue(t < nkt, lds0 + buf * kBuf, wave);

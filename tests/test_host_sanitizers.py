@@ -53,3 +53,17 @@ def test_slab_streams_hold_the_support(tmp_path):
                          env=dict(os.environ, ASAN_OPTIONS="verify_asan_link_order=0"))
     out = run.stdout + run.stderr
     assert run.returncode == 0 and "streams: 0 failed checks" in out, out[-6000:]
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
+def test_loss_products_read_inside_their_tensors(tmp_path):
+    """The ranges that the head's matrix products may read, over random sizes, strides, tiles and splits
+    (tests/sanitize/spans.cpp): none ends past its tensor, and every tile is one workgroup's."""
+    exe = str(tmp_path / "spans")
+    build = subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-fsanitize=address,undefined",
+                            "-fno-sanitize-recover=undefined", "-I" + CSRC, os.path.join(HERE, "spans.cpp"), "-o", exe],
+                           capture_output=True, text=True, timeout=600)
+    assert build.returncode == 0, build.stderr[-4000:]
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=600,
+                         env=dict(os.environ, ASAN_OPTIONS="verify_asan_link_order=0"))
+    assert run.returncode == 0 and " 0 failed checks" in run.stdout, (run.stdout + run.stderr)[-6000:]
