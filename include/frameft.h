@@ -443,7 +443,7 @@ ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, 
  *   workspace : device, 256-byte aligned, at least ff_xent_workspace bytes for the same T, n, V, act and the outputs wanted
  *            (FF_XENT_DH, FF_XENT_DW or both; 0: loss alone).  It holds P, in type act, for a piece of the tokens or of
  *            the vocabulary (at most 256 MiB, or 256 tokens of it where V is larger), fp32 partial sums of dH, and with dW
- *            a copy of H.
+ *            a copy of H (two up to 128 tokens in bf16).
  * ff_xent_fwd  : loss and lse.
  * ff_xent_step : loss, lse and the gradients in one call, which computes the logits once (twice with dW where P does not
  *                fit one piece).
@@ -452,7 +452,8 @@ ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, 
  *                P keeps its digits where its probability is near one, as in ff_xent_step (from lse alone it carries
  *                lse's rounding).
  * dH == NULL or dW == NULL skips that output.  Arithmetic: products accumulate in fp32, softmax statistics are fp32, P is
- * rounded to type act before the products that read it (in ff_xent_step with bf16, after exp(z - max) was rounded to fp16).
+ * rounded to type act before the products that read it (in ff_xent_step with bf16, after exp(z - max) was
+ * rounded to fp16; up to 128 tokens in bf16, P is kept as the sum of two roundings).
  * With T = 0, dW = beta_dw dW.
  */
 enum { FF_XENT_DH = 1, FF_XENT_DW = 2 };

@@ -14,9 +14,12 @@
 //                   backward that computes the logits again.
 //   backward alone  logits product whose epilogue writes P from the saved lse.
 // P is kept in the activations' type: each of its values carries one rounding (2^-9 relative in bf16), as do the
-// factors W and H; e, stored first, is in fp16 (2^-12, and what is under 2^-25 of the columns' maximum is lost).  The sums of exponentials leave the target out: its own value of P,
+// factors W and H; e, stored first, is in fp16 (2^-12 down to 2^-29 of the columns' maximum).  The sums of exponentials leave the target out: its own value of P,
 // exp(z - lse) - 1, is then minus the others' share, and the loss of a token whose target has the largest logit is log(1 +
 // others), so that both keep their digits when the target's probability is near one.
+// With few tokens (kPairTokens) a handful of those roundings would decide the result (one token's dH would be off by its
+// target's, up to 2^-8), so P is kept as a sum of two bf16 matrices there, the second one what rounding left of the
+// first, as further tokens of dH's product and further k of dW's; the products are bound by reading W and writing dW.
 // Long calls are cut into pieces of tokens (P of a piece at most kPieceBytes), whose dH are complete.  With dW a cut
 // by tokens would have to add up V x n sums in fp32, so there the pieces are of the vocabulary (dW rows complete,
 // dH summed in fp32), and the forward runs by itself first.
@@ -107,7 +110,7 @@ struct Piece16<__bf16> {
     typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
     const f16x8 w = *reinterpret_cast<const f16x8*>(p);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)w[i];
+    for (int i = 0; i < 8; ++i) v[i] = (float)w[i] * (1.f / (1 << kExpShift));
   }
   static __device__ __forceinline__ void put(__bf16* p, const float* v) {
     u32x4 w;
@@ -130,10 +133,11 @@ struct Piece16<float> {
   }
 };
 
-// e = exp(z - maximum of its columns) -> P, in place.  Bound by memory: P is read and written once.
+// e = exp(z - maximum of its columns) -> P, in place; rest: elements from a row to the one that takes what rounding left
+// (0: none).  Bound by memory: P is read and written once (4096 x 32,000 in bf16: 74 us, 7 TB/s out of the last-level cache).
 constexpr int kRescaleRow = 4;   // pieces per thread
 template <class E>
-__global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int N, int V, const float2* stats, int cols,
+__global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int64_t rest, int N, int V, const float2* stats, int cols,
                                                       const int64_t* target, const float* own, const float* lse,
                                                       const float* dloss, float scale) {
   constexpr int kN = Piece16<E>::kN;
@@ -164,6 +168,11 @@ __global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int N, 
       for (int i = 0; i < kN; ++i) v[i] = 0.f;
     }
     Piece16<E>::put(row + c, v);
+    if (sizeof(E) == 2 && rest) {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) v[i] -= (float)(E)v[i];
+      Piece16<E>::put(row + rest + c, v);
+    }
   }
 }
 
@@ -186,7 +195,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const float* part, int splits,
 // its zero of P would be multiplied by it.
 template <class E>
 __global__ void __launch_bounds__(256) live_rows_kernel(const E* H, int64_t ldh, int64_t T, int n, const int64_t* target,
-                                                        int64_t vocab, E* out) {
+                                                        int64_t vocab, int copies, E* out) {
   constexpr int kN = Piece16<E>::kN;
   const int64_t per = n / kN, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= T * per) return;
@@ -195,12 +204,13 @@ __global__ void __launch_bounds__(256) live_rows_kernel(const E* H, int64_t ldh,
   const int64_t tg = target[t];
   u32x4 v = {0u, 0u, 0u, 0u};
   if (tg >= 0 && tg < vocab) v = *reinterpret_cast<const u32x4*>(H + t * ldh + c);
-  *reinterpret_cast<u32x4*>(out + t * n + c) = v;
+  for (int k = 0; k < copies; ++k) *reinterpret_cast<u32x4*>(out + (k * T + t) * n + c) = v;
 }
 
 // ------------------------------------------------------------------------------------------- plan of a call
 
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // P of one piece
+constexpr int64_t kPairTokens = 128;                  // tokens up to which bf16 P is kept in two terms
 constexpr int64_t kStatBytes = (int64_t)64 << 20;     // statistics of one piece
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -253,6 +263,7 @@ struct Call {
   bool dh, dw;
   int64_t Tp, Vp;           // tokens and vocabulary entries of a piece of P
   int64_t Tf;               // tokens of a piece of the forward alone
+  int terms;                // of P: 2 for few tokens in bf16
   bool by_vocab;            // pieces of the vocabulary (dW of a long call)
   size_t off_p, off_stats, off_zt, off_part, off_live, bytes;
 };
@@ -270,6 +281,7 @@ Call plan(int64_t T, int64_t n, int64_t V, int act, bool dh, bool dw) {
   c.dh = dh, c.dw = dw;
   c.bytes = 256;
   if (T == 0) return c;
+  c.terms = c.bf16 && T <= kPairTokens ? 2 : 1;
   const int64_t ldp = up(V, 64);
   int64_t most = kPieceBytes / (ldp * c.esz) / 256 * 256;
   if (most < 256) most = 256;
@@ -292,7 +304,7 @@ Call plan(int64_t T, int64_t n, int64_t V, int act, bool dh, bool dw) {
     return o;
   };
   const bool grad = dh || dw;
-  c.off_p = take(grad ? c.Tp * up(c.Vp, 64) * c.esz : 0);
+  c.off_p = take(grad ? c.terms * c.Tp * up(c.Vp, 64) * c.esz : 0);
   // small tiles have 32 columns per entry; they serve few tokens or few columns
   const int64_t rows = c.by_vocab || !grad ? c.Tf : (c.Tp > c.Tf ? c.Tp : c.Tf);
   c.off_stats = take(rows * entries * 8);
@@ -301,15 +313,15 @@ Call plan(int64_t T, int64_t n, int64_t V, int act, bool dh, bool dw) {
   auto more = [&](int64_t b) { part = b > part ? b : part; };
   if (dh)
     for (int64_t N : {c.Tp, T % c.Tp ? T % c.Tp : c.Tp}) {
-      const Product p = dh_product(c, N, c.Vp);
-      if (p.splits > 1 || c.by_vocab) more((int64_t)p.splits * N * n * 4);
+      const Product p = dh_product(c, c.terms * N, c.Vp);
+      if (p.splits * c.terms > 1 || c.by_vocab) more((int64_t)p.splits * c.terms * N * n * 4);
     }
   if (dw && !c.by_vocab) {
-    const Product p = dw_product(c, V, T);
+    const Product p = dw_product(c, V, c.terms * T);
     if (p.splits > 1) more((int64_t)p.splits * V * n * 4);
   }
   c.off_part = take(part);
-  c.off_live = take(dw ? T * n * c.esz : 0);
+  c.off_live = take(dw ? c.terms * T * n * c.esz : 0);
   c.bytes = at < 256 ? 256 : at;
   return c;
 }
@@ -350,6 +362,7 @@ hipError_t run_logits(const Call& c, const Tensors& x, int64_t t0, int64_t N, in
   a.tm = (int)(up(M, tile_m(p.tile)) / tile_m(p.tile)), a.tn = (int)(up(N, tile_n(p.tile)) / tile_n(p.tile));
   a.kt = a.kt_split = p.kt_split, a.splits = 1, a.mode = mode;
   a.out = x.ws + c.off_p, a.ldo = up(M, 64), a.ocols = (int)up(M, 64);
+  a.rest = c.terms == 2 ? N * a.ldo : 0;
   a.stats = reinterpret_cast<float2*>(x.ws + c.off_stats);
   a.target = x.target + t0, a.v0 = v0, a.vocab = c.V;
   a.zt = reinterpret_cast<float*>(x.ws + c.off_zt);
@@ -379,7 +392,7 @@ void rescale(const Call& c, const Tensors& x, int64_t t0, int64_t N, int stat) {
   for (int64_t r = 0; r < N; r += 32768) {
     const int64_t rows = N - r < 32768 ? N - r : 32768;
     hipLaunchKernelGGL(rescale_kernel<E>, dim3((unsigned)((ldp + seg - 1) / seg), (unsigned)rows), dim3(256), 0, x.s,
-                       reinterpret_cast<E*>(x.ws + c.off_p) + r * ldp, ldp, (int)N, (int)c.V,
+                       reinterpret_cast<E*>(x.ws + c.off_p) + r * ldp, ldp, c.terms == 2 ? N * ldp : 0, (int)N, (int)c.V,
                        reinterpret_cast<const float2*>(x.ws + c.off_stats) + r, stat, x.target + t0 + r,
                        reinterpret_cast<const float*>(x.ws + c.off_zt) + r, x.lse + t0 + r, x.dloss ? x.dloss + t0 + r : nullptr, x.scale);
   }
@@ -401,32 +414,34 @@ hipError_t run_sum(const Call& c, const Tensors& x, int splits, int64_t N, int64
 
 // dH of tokens t0 .. from P of vocabulary entries v0 ..; first / last piece of the vocabulary
 hipError_t run_dh(const Call& c, const Tensors& x, int64_t t0, int64_t N, int64_t v0, int64_t M, bool first, bool last) {
-  const Product p = dh_product(c, N, c.Vp);     // the same split for every piece of the vocabulary
+  const int64_t rows = c.terms * N;
+  const Product p = dh_product(c, rows, c.Vp);     // the same split for every piece of the vocabulary
   GemmArgs a{};
   a.A = x.W + v0 * x.ldw * c.esz, a.lda = x.ldw;
   a.B = x.ws + c.off_p, a.ldb = up(M, 64);
-  a.M = (int)c.n, a.N = (int)N, a.K = (int)M;
-  a.tm = (int)(up(c.n, tile_m(p.tile)) / tile_m(p.tile)), a.tn = (int)(up(N, tile_n(p.tile)) / tile_n(p.tile));
+  a.M = (int)c.n, a.N = (int)rows, a.K = (int)M;
+  a.tm = (int)(up(c.n, tile_m(p.tile)) / tile_m(p.tile)), a.tn = (int)(up(rows, tile_n(p.tile)) / tile_n(p.tile));
   a.kt = (int)(up(M, c.kk) / c.kk), a.kt_split = p.kt_split, a.splits = p.splits;
-  const bool direct = p.splits == 1 && first && last;
+  const bool direct = p.splits * c.terms == 1 && first && last;
   void* out = x.dH + t0 * x.lddh * c.esz;
   a.mode = direct ? kOut : kPart;
   a.out = out, a.ldo = x.lddh, a.beta = x.beta_dh;
   a.part = reinterpret_cast<float*>(x.ws + c.off_part), a.part_add = !first;
   XENT_TRY(launch_gemm(1, c.bf16, p.tile, a, x.s));
-  return direct || !last ? hipSuccess : run_sum(c, x, p.splits, N, c.n, x.beta_dh, out, x.lddh);
+  return direct || !last ? hipSuccess : run_sum(c, x, p.splits * c.terms, N, c.n, x.beta_dh, out, x.lddh);
 }
 
 // rows v0 .. v0 + M - 1 of dW from P of all tokens
 hipError_t run_dw(const Call& c, const Tensors& x, int64_t v0, int64_t M) {
-  Product p = dw_product(c, M, c.T);
-  if (c.by_vocab) p.splits = 1, p.kt_split = (int)(up(c.T, c.kk) / c.kk);   // the partial sums' place holds dH's
+  const int64_t K = c.terms * c.T;
+  Product p = dw_product(c, M, K);
+  if (c.by_vocab) p.splits = 1, p.kt_split = (int)(up(K, c.kk) / c.kk);   // the partial sums' place holds dH's
   GemmArgs a{};
   a.A = x.ws + c.off_live, a.lda = c.n;
   a.B = x.ws + c.off_p, a.ldb = up(M, 64);
-  a.M = (int)c.n, a.N = (int)M, a.K = (int)c.T;
+  a.M = (int)c.n, a.N = (int)M, a.K = (int)K;
   a.tm = (int)(up(c.n, tile_m(p.tile)) / tile_m(p.tile)), a.tn = (int)(up(M, tile_n(p.tile)) / tile_n(p.tile));
-  a.kt = (int)(up(c.T, c.kk) / c.kk), a.kt_split = p.kt_split, a.splits = p.splits;
+  a.kt = (int)(up(K, c.kk) / c.kk), a.kt_split = p.kt_split, a.splits = p.splits;
   void* out = x.dW + v0 * x.lddw * c.esz;
   a.mode = p.splits == 1 ? kOut : kPart;
   a.out = out, a.ldo = x.lddw, a.beta = x.beta_dw;
@@ -440,10 +455,10 @@ hipError_t run_live_rows(const Call& c, const Tensors& x) {
   const dim3 grid((unsigned)((threads + 255) / 256));
   if (c.bf16)
     hipLaunchKernelGGL(live_rows_kernel<__bf16>, grid, dim3(256), 0, x.s, reinterpret_cast<const __bf16*>(x.H), x.ldh,
-                       c.T, (int)c.n, x.target, c.V, reinterpret_cast<__bf16*>(x.ws + c.off_live));
+                       c.T, (int)c.n, x.target, c.V, c.terms, reinterpret_cast<__bf16*>(x.ws + c.off_live));
   else
     hipLaunchKernelGGL(live_rows_kernel<float>, grid, dim3(256), 0, x.s, reinterpret_cast<const float*>(x.H), x.ldh, c.T,
-                       (int)c.n, x.target, c.V, reinterpret_cast<float*>(x.ws + c.off_live));
+                       (int)c.n, x.target, c.V, c.terms, reinterpret_cast<float*>(x.ws + c.off_live));
   return hipGetLastError();
 }
 

@@ -33,7 +33,7 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 enum Mode {
   kStats = 0,     // logits: maximum and sum of exponentials (the target's left out) of each wave's columns, the target's logit
-  kExp = 1,       // the same, and exp(z - maximum) to out (fp16 for bf16 activations)
+  kExp = 1,       // the same, and exp(z - maximum) to out (bf16 activations: store8_half)
   kGrad = 2,      // logits: out = (softmax - onehot) weight from the saved log-sum-exp
   kOut = 3,       // out = beta out + product
   kPart = 4,      // fp32 partial sums of one share of k
@@ -51,6 +51,7 @@ struct GemmArgs {
   int mode;
   void* out;              // [N][ldo], written up to column ocols (columns past M as zero: P's padding)
   int64_t ldo;
+  int64_t rest;           // kGrad: elements from a row of out to that of what its rounding left, 0: not kept
   int ocols;
   float beta;
   float* part;            // [splits][N][M] fp32
@@ -233,6 +234,12 @@ __device__ __forceinline__ unsigned short bf16_bits(float x) {
 }
 __device__ __forceinline__ float bf16_value(unsigned short b) { return __builtin_bit_cast(float, (unsigned)b << 16); }
 
+// What rounding to bf16 leaves of v.
+__device__ __forceinline__ f32x4 rounding_of(f32x4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] -= bf16_value(bf16_bits(v[i]));
+  return v;
+}
 // eight consecutive results
 __device__ __forceinline__ void store8(__bf16* p, f32x4 v, f32x4 w) {
   const u32x4 x = {(unsigned)bf16_bits(v[0]) | (unsigned)bf16_bits(v[1]) << 16,
@@ -241,7 +248,9 @@ __device__ __forceinline__ void store8(__bf16* p, f32x4 v, f32x4 w) {
                    (unsigned)bf16_bits(w[2]) | (unsigned)bf16_bits(w[3]) << 16};
   *reinterpret_cast<u32x4*>(p) = x;
 }
-// and eight exponentials of kExp: values up to one, in fp16, whose 11 bits leave the rounding of P to bf16 nearly the only one
+// and eight exponentials of kExp, times 2^kExpShift, in fp16: its 11 bits leave the rounding of P to bf16 nearly the only
+// one, and the shift keeps them down to 2^-29 of the columns' maximum
+constexpr int kExpShift = 15;
 __device__ __forceinline__ void store8_half(void* p, f32x4 v, f32x4 w) {
   typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
   const f16x8 x = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3],
@@ -305,8 +314,12 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
         if (f % 2 == 0) {
           first = v;
         } else if (live && col(f - 1) < a.ocols) {
-          if (a.mode == kExp) store8_half(out + col(f - 1), first, v);
-          else store8(out + col(f - 1), first, v);
+          if (a.mode == kExp) {
+            store8_half(out + col(f - 1), first, v);
+          } else {
+            store8(out + col(f - 1), first, v);
+            if (a.rest) store8(out + a.rest + col(f - 1), rounding_of(first), rounding_of(v));
+          }
         }
       } else {
         if (live && col(f) < a.ocols) store4(out + col(f), v);
@@ -362,7 +375,8 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float ref = top == -INFINITY ? 0.f : top;    // columns of nothing: exp(-inf) = 0, not NaN
-      const float ref2 = ref * kLog2e;
+      // bf16: all exponentials of this mode carry the shift of their storage
+      const float ref2 = ref * kLog2e - kExpShift;
       float sum = 0.f;
 #pragma unroll
       for (int f = 0; f < FM; ++f) {
@@ -384,6 +398,7 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
       }
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
+      if (sizeof(E) == 2) sum *= 1.f / (1 << kExpShift);
       if (g == 0 && live && i0 < a.M) a.stats[(int64_t)(i0 / TM) * a.N + row] = make_float2(top, sum);
     }
   }

@@ -304,3 +304,22 @@ def test_refusals(dev):
         ff.xent_fwd(torch.zeros((4, 18), device=dev)[:, :16], W, t)
     torch.cuda.synchronize()
     assert bool((loss == 3).all())
+
+
+@pytest.mark.parametrize("T,n,V,dw", [(1, 512, 4000, True), (1, 64, 2, True), (7, 256, 31, True), (60, 128, 900, True),
+                                      (128, 768, 5001, False)])
+def test_few_tokens_are_off_by_their_results_rounding_only(dev, T, n, V, dw):
+    """Up to 128 tokens in bf16, P keeps what rounding left of it: dH and dW are off by their own rounding, at most u / 2 of
+    each element (u = 2^-7 between neighbours), and by 2^-11 (exponentials in fp16) and 2^-14 of the absolute sums."""
+    H, W, target, dloss = _case(T, n, V, "bf16", 7 * T + V, skip=0.0)
+    ref = TO.xent(H, W, target, dloss, 0.5)
+    Ht, Wt, tt, dt = _dev(dev, "bf16", H, W, target, dloss)
+    ws = _garbage(T, n, V, "bf16", dw, dev)
+    step = ff.xent_step(Ht, Wt, tt, dloss=dt, scale=0.5, want_dw=dw, workspace=ws)
+    ws.fill_(255)
+    back = ff.xent_bwd(Ht, Wt, tt, step[1], loss=step[0], dloss=dt, scale=0.5, want_dw=dw, workspace=ws)
+    torch.cuda.synchronize()
+    for got, want, sums in [(step[2], ref[2], ref[4][1]), (back[0], ref[2], ref[4][1])] + \
+            ([(step[3], ref[3], ref[4][2]), (back[1], ref[3], ref[4][2])] if dw else []):
+        bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2.0 ** -14) * sums
+        assert np.all(np.abs(to_np(got) - want) <= 1.05 * bound + 1e-37)
