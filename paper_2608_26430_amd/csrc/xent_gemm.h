@@ -155,6 +155,7 @@ struct Operand {
                                              int lane) const {
     const int pieces = (left + kPer - 1) / kPer;
     const unsigned n = span_of(!TR, kE, BX, ld, x0, X, 0, left).bytes;
+    asm volatile("" : "+v"(lane));   // places made here, not kept (and spilled) from one tile to the next
     const u32x4 r = make_rsrc(base + tile * step, n);
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
