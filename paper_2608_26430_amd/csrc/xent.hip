@@ -229,19 +229,22 @@ struct Product {
 //        small  0.30 / 0.60    16 x 32,000, 4096 wide: logits 41 us (medium 58); 64 tokens 48 (60)
 //   fp32 medium 1.92 / 1.92    2048 x 33,000, 1024 wide: logits 1060 us (small 1120)
 //        small  0.50 / 0.75    200 x 3000, 512 wide: logits 14 us (medium 39); 500 x 8001, 768 wide: dW 59 (68)
+//   logits of few classes, tiny: bf16 0.14 / 0.16, fp32 0.20 / 0.28
+//                              4000 x 100, 768 wide, bf16: 6.1 us (small 7.4); 190 x 44, 1024 wide, fp32: 10 us (small 23)
 // The large tile has no fp32 instance: its registers spill.
 struct TileCost {
   double full, single, ends;
 };
-constexpr TileCost kCosts[2][3] = {{{0, 0, 0}, {1.92, 1.92, 2}, {0.50, 0.75, 2}},
-                                   {{1.53, 1.53, 5}, {0.51, 0.80, 3}, {0.30, 0.60, 4}}};
+constexpr TileCost kCosts[2][4] = {{{0, 0, 0}, {1.92, 1.92, 2}, {0.50, 0.75, 2}, {0.20, 0.28, 3}},
+                                   {{1.53, 1.53, 5}, {0.51, 0.80, 3}, {0.30, 0.60, 4}, {0.14, 0.16, 6}}};
+constexpr int64_t kTinyVocab = 4096;   // entries up to which the tiny tile is looked at
 
 // Tile and split of k of a product with M columns, N rows and kt k tiles: the least estimated time, where partial sums are
 // written and read at about 4.5 TB/s by a launch more.
-Product choose(int64_t M, int64_t N, int64_t kt, bool may_split, bool bf16) {
+Product choose(int64_t M, int64_t N, int64_t kt, bool may_split, bool bf16, bool tiny = false) {
   Product best{kSmall, 1, (int)kt};
   double least = 1e30;
-  for (int tile = bf16 ? kLarge : kMedium; tile <= kSmall; ++tile) {
+  for (int tile = bf16 ? kLarge : kMedium; tile <= (tiny ? kTiny : kSmall); ++tile) {
     const TileCost& u = kCosts[bf16][tile];
     const int64_t tiles = tiles_of(M, N, tile);
     for (int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64}) {
@@ -268,7 +271,7 @@ struct Call {
   size_t off_p, off_stats, off_zt, off_part, off_live, bytes;
 };
 
-Product logits_product(const Call& c, int64_t N, int64_t M) { return choose(M, N, up(c.n, c.kk) / c.kk, false, c.bf16); }
+Product logits_product(const Call& c, int64_t N, int64_t M) { return choose(M, N, up(c.n, c.kk) / c.kk, false, c.bf16, c.V <= kTinyVocab); }
 Product dh_product(const Call& c, int64_t N, int64_t K) { return choose(c.n, N, up(K, c.kk) / c.kk, true, c.bf16); }
 Product dw_product(const Call& c, int64_t M, int64_t K) {
   // sums of a whole head are not worth a pass through memory
@@ -293,7 +296,8 @@ Call plan(int64_t T, int64_t n, int64_t V, int act, bool dh, bool dw) {
     if (c.Vp < 256) c.Vp = 256;
     if (c.Vp > V) c.Vp = V;
   }
-  const int64_t entries = up(V, 32) / 32;   // at most, with the small tile's columns
+  // at most, with the smallest tile's columns
+  const int64_t cols = stat_cols(V <= kTinyVocab ? kTiny : kSmall), entries = up(V, cols) / cols;
   c.Tf = kStatBytes / (8 * entries) / 256 * 256;
   if (c.Tf < 256) c.Tf = 256;
   if (c.Tf > T) c.Tf = T;
@@ -305,7 +309,6 @@ Call plan(int64_t T, int64_t n, int64_t V, int act, bool dh, bool dw) {
   };
   const bool grad = dh || dw;
   c.off_p = take(grad ? c.terms * c.Tp * up(c.Vp, 64) * c.esz : 0);
-  // small tiles have 32 columns per entry; they serve few tokens or few columns
   const int64_t rows = c.by_vocab || !grad ? c.Tf : (c.Tp > c.Tf ? c.Tp : c.Tf);
   c.off_stats = take(rows * entries * 8);
   c.off_zt = take(rows * 4);

@@ -15,7 +15,8 @@
 // of k are in flight.  In a 16 x 16 MFMA the lane holds four consecutive i of one j, so that results are
 // stored along the rows of memory and the softmax statistics of one token stay in one lane's registers.
 // For bf16 logits the rows of A are dealt to the MFMA in an order that gives a lane eight consecutive
-// vocabulary entries over two tiles (PF = 2), one store of 16 bytes; the four lanes of a token store 64 bytes.
+// vocabulary entries over two tiles (PF = 2), one store of 16 bytes; the four lanes of a token store 64 bytes.  kExp's
+// results are stored as fp16 either way.
 #pragma once
 
 #include "ff_internal.h"
@@ -205,18 +206,23 @@ struct Operand {
 };
 
 template <class E>
-__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c);
+struct Mma;
 template <>
-__device__ __forceinline__ f32x4 mma<__bf16>(f32x4 a, f32x4 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
+struct Mma<__bf16> {
+  static constexpr int kSteps = 1;
+  static __device__ __forceinline__ f32x4 step(int, f32x4 a, f32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                   0);
+  }
+};
 // fp32: lane group g holds k = 4 g + s in element s, so that step s of the four covers k = s, s + 4, s + 8, s + 12
 template <>
-__device__ __forceinline__ f32x4 mma<float>(f32x4 a, f32x4 b, f32x4 c) {
-#pragma unroll
-  for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], c, 0, 0, 0);
-  return c;
-}
+struct Mma<float> {
+  static constexpr int kSteps = 4;
+  static __device__ __forceinline__ f32x4 step(int s, f32x4 a, f32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], c, 0, 0, 0);
+  }
+};
 
 // Asks the scheduler to spread READS LDS reads evenly over the MMAS multiplications beside them.
 template <int READS, int MMAS, int I = 0>
@@ -257,6 +263,11 @@ __device__ __forceinline__ void store8_half(void* p, f32x4 v, f32x4 w) {
   const f16x8 x = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3],
                    (_Float16)w[0], (_Float16)w[1], (_Float16)w[2], (_Float16)w[3]};
   *reinterpret_cast<f16x8*>(p) = x;
+}
+__device__ __forceinline__ void store4_half(void* p, f32x4 v) {
+  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+  const f16x4 x = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+  *reinterpret_cast<f16x4*>(p) = x;
 }
 // four consecutive results (the address is a multiple of four elements)
 __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
@@ -322,8 +333,13 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
             if (a.rest) store8(out + a.rest + col(f - 1), rounding_of(first), rounding_of(v));
           }
         }
-      } else {
-        if (live && col(f) < a.ocols) store4(out + col(f), v);
+      } else if (live && col(f) < a.ocols) {
+        if (sizeof(E) == 2 && a.mode == kExp) {
+          store4_half(out + col(f), v);
+        } else {
+          store4(out + col(f), v);
+          if (sizeof(E) == 2 && a.rest) store4(out + a.rest + col(f), rounding_of(v));
+        }
       }
     };
     const bool edge = i0 + TM > a.M;
@@ -410,7 +426,7 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
   constexpr int NW = WVM * WVN;
   constexpr int TM = BM / WVM, TN = BN / WVN;
   constexpr int FM = TM / 16, FN = TN / 16;
-  constexpr int PF = TRA || sizeof(E) == 4 ? 0 : 2;
+  constexpr int PF = TRA || sizeof(E) == 4 || FM < 2 ? 0 : 2;
   typedef Operand<E, BM, NW, TRA, PF> OpA;
   typedef Operand<E, BN, NW, TRB, 0> OpB;
   constexpr int kBuf = OpA::kBytes + OpB::kBytes;
@@ -513,10 +529,13 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
     for (int f = 0; f < FM; ++f) fa[f] = OpA::read(la, wm * TM, f, kk, lane);
   };
   auto multiply = [&](const f32x4 (&fa)[FM], const f32x4 (&fb)[FN]) {
+    // fp32: a step of k over all tiles, so that no product waits for the one before
 #pragma unroll
-    for (int f = 0; f < FM; ++f)
+    for (int k = 0; k < Mma<E>::kSteps; ++k)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[f][j] = mma<E>(fa[f], fb[j], acc[f][j]);
+      for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[f][j] = Mma<E>::step(k, fa[f], fb[j], acc[f][j]);
   };
 
   if constexpr (NB == 2) {
@@ -578,13 +597,13 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// Tile sizes of the instances: large (256 x 256, wave 128 x 64), medium (128 x 128, wave 64 x 64), small (128 x 32,
-// wave 32 x 32).
-enum Tile { kLarge = 0, kMedium = 1, kSmall = 2 };
-constexpr int tile_m(int t) { return t == kLarge ? 256 : 128; }
+// Tile sizes of the instances: large (256 x 256, wave 128 x 64; bf16 only), medium (128 x 128, wave 64 x 64), small (128 x
+// 32, wave 32 x 32), and tiny (32 x 32, wave 16 x 16) for the logits of a few classes.
+enum Tile { kLarge = 0, kMedium = 1, kSmall = 2, kTiny = 3 };
+constexpr int tile_m(int t) { return t == kLarge ? 256 : (t == kTiny ? 32 : 128); }
 constexpr int tile_n(int t) { return t == kLarge ? 256 : (t == kMedium ? 128 : 32); }
 // columns of one entry of the logits' statistics
-constexpr int stat_cols(int t) { return t == kLarge ? 128 : (t == kMedium ? 64 : 32); }
+constexpr int stat_cols(int t) { return t == kLarge ? 128 : (t == kMedium ? 64 : (t == kSmall ? 32 : 16)); }
 
 constexpr int kCUs = 256;
 

@@ -29,6 +29,12 @@ hipError_t XENT_NAME(XENT_LAYOUT, XENT_BF16)(int tile, const GemmArgs& a, hipStr
     return hipGetLastError();
   }
 #endif
+#if XENT_LAYOUT == 0
+  if (tile == kTiny) {
+    hipLaunchKernelGGL((gemm_kernel<E, 32, 32, 2, 2, 4, TRA, TRB, 2>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+#endif
   if (tile == kMedium) {
     hipLaunchKernelGGL((gemm_kernel<E, 128, 128, 2, 2, 2, TRA, TRB, 2>), grid, dim3(256), 0, s, a);
   } else {

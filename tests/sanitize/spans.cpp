@@ -49,7 +49,7 @@ static void walk(int esz, int bm, int bn, const Side& A, const Side& B, int64_t 
 
 int main() {
   std::srand(3);
-  const int tiles[3][2] = {{256, 256}, {128, 128}, {128, 32}};
+  const int tiles[4][2] = {{256, 256}, {128, 128}, {128, 32}, {32, 32}};
   for (int round = 0; round < 600; ++round) {
     const int esz = round % 2 ? 2 : 4, mult = 16 / esz;
     const int64_t T = round < 40 ? round / 2 + 1 : 1 + std::rand() % 700, n = mult * (1 + std::rand() % 90);

@@ -82,7 +82,8 @@ def _verify(ref, got, n, V, dtype, old=None, beta=0.0):
 
 
 SIZES = [(1, 8, 1), (1, 64, 2), (2, 16, 3), (31, 72, 63), (33, 64, 65), (32, 136, 129), (64, 200, 257), (100, 768, 1000),
-         (129, 64, 1001), (257, 320, 500), (193, 128, 34000), (40, 64, 20011), (1, 4096, 5000), (1000, 16, 2), (300, 1032, 33025)]
+         (129, 64, 1001), (257, 320, 500), (193, 128, 34000), (40, 64, 20011), (1, 4096, 5000), (1000, 16, 2), (300, 1032, 33025),
+         (50, 72, 4097), (513, 40, 4096), (1500, 24, 10), (3, 4104, 31)]
 
 
 @pytest.mark.parametrize("T,n,V", SIZES)
