@@ -387,8 +387,7 @@ double ff_lr_linear_warmup(int64_t step, int64_t warmup, int64_t total, double b
 /*
  * ff_layernorm_fwd -- y = weight (x - mean) rstd + bias for each row x, rstd = 1 / sqrt(var + eps) with the row's
  * variance over n (not n - 1).  Sums are in fp32, the variance from the centred row.
- *   X, Y         : device, element alignment, any leading dimension >= n (rows on 16 bytes with n a multiple of 8 in
- *                  bf16, 4 in fp32, run fastest).  Y may be X.
+ *   X, Y         : device, element alignment, any leading dimension >= n.  Y may be X.
  *   weight, bias : device, n elements of type w_dtype; NULL for ones / zeros.
  *   mean, rstd   : device, T fp32 each, for the backward; NULL where not wanted.
  * T = 0 is a no-op.

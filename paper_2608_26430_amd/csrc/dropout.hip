@@ -16,7 +16,9 @@ namespace ff {
 namespace {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes on any element: rows of odd widths start anywhere, and the memory unit takes such pieces whole
+typedef u32x4 Loose __attribute__((aligned(2)));
 
 struct DropArgs {
   const void* X;
@@ -53,7 +55,7 @@ template <class E>
 __device__ __forceinline__ void get8(const E* p, float* v);
 template <>
 __device__ __forceinline__ void get8<__bf16>(const __bf16* p, float* v) {
-  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+  const u32x4 w = *reinterpret_cast<const Loose*>(p);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     v[2 * i] = __builtin_bit_cast(float, w[i] << 16);
@@ -62,9 +64,12 @@ __device__ __forceinline__ void get8<__bf16>(const __bf16* p, float* v) {
 }
 template <>
 __device__ __forceinline__ void get8<float>(const float* p, float* v) {
-  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+  const u32x4 a = reinterpret_cast<const Loose*>(p)[0], b = reinterpret_cast<const Loose*>(p)[1];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  for (int i = 0; i < 4; ++i) {
+    const unsigned x = a[i], y = b[i];
+    v[i] = __builtin_bit_cast(float, x), v[4 + i] = __builtin_bit_cast(float, y);
+  }
 }
 template <class E>
 __device__ __forceinline__ void put8(E* p, const float* v);
@@ -75,17 +80,18 @@ __device__ __forceinline__ void put8<__bf16>(__bf16* p, const float* v) {
   for (int i = 0; i < 4; ++i)
     w[i] = (unsigned)__builtin_bit_cast(unsigned short, (__bf16)v[2 * i]) |
            (unsigned)__builtin_bit_cast(unsigned short, (__bf16)v[2 * i + 1]) << 16;
-  *reinterpret_cast<u32x4*>(p) = w;
+  *reinterpret_cast<Loose*>(p) = w;
 }
 template <>
 __device__ __forceinline__ void put8<float>(float* p, const float* v) {
-  const f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
-  reinterpret_cast<f32x4*>(p)[0] = a;
-  reinterpret_cast<f32x4*>(p)[1] = b;
+  u32x4 a, b;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = __builtin_bit_cast(unsigned, v[i]), b[i] = __builtin_bit_cast(unsigned, v[4 + i]);
+  reinterpret_cast<Loose*>(p)[0] = a;
+  reinterpret_cast<Loose*>(p)[1] = b;
 }
 
-// VEC: every row starts on 16 bytes; whole blocks then move in 16-byte pieces.
-template <class E, bool VEC, bool RES>
+template <class E, bool RES>
 __global__ void __launch_bounds__(256) dropout_kernel(DropArgs a) {
   const int64_t stride = (int64_t)gridDim.x * 256;
   int64_t b = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -101,7 +107,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropArgs a) {
     E* y = static_cast<E*>(a.Y) + t * a.ldy + c * 8;
     const int left = a.n - c * 8;
     float v[8], q[8];
-    if (VEC && left >= 8) {
+    if (left >= 8) {
       get8<E>(x, v);
       if (RES) get8<E>(r, q);
     } else {
@@ -118,7 +124,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropArgs a) {
       v[i] = u >= a.drop ? v[i] * a.scale : 0.f;     // a dropped NaN or infinity is zero
       if (RES) v[i] += q[i];
     }
-    if (VEC && left >= 8) {
+    if (left >= 8) {
       put8<E>(y, v);
     } else {
 #pragma unroll
@@ -132,14 +138,12 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropArgs a) {
 }
 
 template <class E>
-void launch(const DropArgs& a, bool vec, hipStream_t s) {
+void launch(const DropArgs& a, hipStream_t s) {
   int64_t grid = (a.blocks + 255) / 256;
   if (grid > 256 * 32) grid = 256 * 32;
   const dim3 g((unsigned)grid), t(256);
-  if (vec && a.R) hipLaunchKernelGGL((dropout_kernel<E, true, true>), g, t, 0, s, a);
-  else if (vec) hipLaunchKernelGGL((dropout_kernel<E, true, false>), g, t, 0, s, a);
-  else if (a.R) hipLaunchKernelGGL((dropout_kernel<E, false, true>), g, t, 0, s, a);
-  else hipLaunchKernelGGL((dropout_kernel<E, false, false>), g, t, 0, s, a);
+  if (a.R) hipLaunchKernelGGL((dropout_kernel<E, true>), g, t, 0, s, a);
+  else hipLaunchKernelGGL((dropout_kernel<E, false>), g, t, 0, s, a);
 }
 
 ff_status check_rows(const char* name, const void* p, int64_t ld, int64_t n, int esz) {
@@ -171,10 +175,8 @@ extern "C" ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, in
   ff::DropArgs a{X, R, Y, ldx, R ? ldr : 0, ldy, T, 0, (int)n, (int)((n + 7) / 8), (int64_t)seed, offset, offset_dev, drop,
                  drop < 65536u ? 65536.f / (float)(65536u - drop) : 0.f};
   a.blocks = T * a.nb;
-  const auto whole = [&](const void* q, int64_t ld) { return (uintptr_t)q % 16 == 0 && ld * esz % 16 == 0; };
-  const bool vec = whole(X, ldx) && whole(Y, ldy) && (!R || whole(R, ldr));
-  if (act == FF_BF16) ff::launch<__bf16>(a, vec, (hipStream_t)stream);
-  else ff::launch<float>(a, vec, (hipStream_t)stream);
+  if (act == FF_BF16) ff::launch<__bf16>(a, (hipStream_t)stream);
+  else ff::launch<float>(a, (hipStream_t)stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? FF_OK : ff::fail(FF_EDEVICE, "dropout launch: %s", hipGetErrorString(e));
 }

@@ -3,7 +3,7 @@
 //   mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps), h = (x - mu) r, y = w h + b          (a row x of n)
 //   a = w g;  dx = beta dx + r (a - mean a - h mean(a h));  dw = sum_t g h;  db = sum_t g
 // Every sum is in fp32; the variance is that of the centred row, which stays in registers, so that a large mean costs
-// no digits.  A row belongs to WV waves (1, 8 or 16) whose threads hold NV pieces of VEC consecutive elements each;
+// no digits.  A row belongs to WV waves (1 or 8) whose threads hold NV pieces of 16 bytes each;
 // rows wider than that are read three times.  Workgroups walk the rows with a stride, the vectors of their columns in
 // registers (fp32 weight and bias read for every row were twice a bf16 row's own bytes: 8192 x 8192 forward 67 -> 46
 // us), reading the next row under the arithmetic of one.  The backward's also keep dw and db of their columns and leave one
@@ -18,6 +18,7 @@ namespace norm {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 Loose __attribute__((aligned(2)));   // on any element
 
 struct Args {
   const void* X;
@@ -34,14 +35,15 @@ struct Args {
   float* rstd;
   float beta;
   float* part;         // [workgroups][2][n]: dw, db of a workgroup's rows (NULL: not wanted)
-  int vec_w;           // weight and bias may be read in whole pieces
 };
 
-// A piece of VEC consecutive elements as it lies in memory: one element, or 16 bytes.
-template <class E, int VEC>
+// A piece of 16 bytes as it lies in memory, on any element: rows of odd widths start anywhere, and the memory unit
+// takes such pieces whole.
+template <class E>
 struct Pack {
+  static constexpr int kN = 16 / (int)sizeof(E);
   typedef u32x4 Raw;
-  static __device__ __forceinline__ Raw load(const E* p) { return *reinterpret_cast<const u32x4*>(p); }
+  static __device__ __forceinline__ Raw load(const E* p) { return *reinterpret_cast<const Loose*>(p); }
   static __device__ __forceinline__ void widen(Raw w, float* v) {
     if constexpr (sizeof(E) == 2) {
 #pragma unroll
@@ -57,55 +59,43 @@ struct Pack {
       }
     }
   }
-  static __device__ __forceinline__ void get(const E* p, float* v) { widen(load(p), v); }
   static __device__ __forceinline__ void put(E* p, const float* v) {
+    u32x4 w;
     if constexpr (sizeof(E) == 2) {
-      u32x4 w;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         w[i] = (unsigned)__builtin_bit_cast(unsigned short, (__bf16)v[2 * i]) |
                (unsigned)__builtin_bit_cast(unsigned short, (__bf16)v[2 * i + 1]) << 16;
-      *reinterpret_cast<u32x4*>(p) = w;
     } else {
-      const f32x4 w = {v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f32x4*>(p) = w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(unsigned, v[i]);
     }
+    *reinterpret_cast<Loose*>(p) = w;
   }
 };
-template <class E>
-struct Pack<E, 1> {
-  typedef E Raw;
-  static __device__ __forceinline__ Raw load(const E* p) { return *p; }
-  static __device__ __forceinline__ void widen(Raw w, float* v) { v[0] = (float)w; }
-  static __device__ __forceinline__ void get(const E* p, float* v) { v[0] = (float)*p; }
-  static __device__ __forceinline__ void put(E* p, const float* v) { *p = (E)v[0]; }
-};
 
-// VEC values of weight or bias at column c (absent: `none`)
-template <int VEC>
-__device__ __forceinline__ void vector_at(const void* p, int bf16, int vec, float none, int c, float* v) {
+// N values of weight or bias from column c (absent: `none`)
+template <int N>
+__device__ __forceinline__ void vector_at(const void* p, int bf16, float none, int c, float* v) {
   if (!p) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = none;
+    for (int i = 0; i < N; ++i) v[i] = none;
   } else if (bf16) {
     const __bf16* q = static_cast<const __bf16*>(p) + c;
-    if (VEC == 8 && vec) {
-      Pack<__bf16, 8>::get(q, v);
+    if constexpr (N == 8) {
+      Pack<__bf16>::widen(Pack<__bf16>::load(q), v);
     } else {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = (float)q[i];
+      for (int i = 0; i < N; ++i) v[i] = (float)q[i];
     }
   } else {
     const float* q = static_cast<const float*>(p) + c;
-    if (VEC >= 4 && vec) {
+    if constexpr (N >= 4) {
 #pragma unroll
-      for (int i = 0; i < VEC; i += 4) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(q + i);
-        v[i] = w[0], v[i + 1] = w[1], v[i + 2] = w[2], v[i + 3] = w[3];
-      }
+      for (int i = 0; i < N; i += 4) Pack<float>::widen(Pack<float>::load(q + i), v + i);
     } else {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = q[i];
+      for (int i = 0; i < N; ++i) v[i] = q[i];
     }
   }
 }
@@ -133,77 +123,88 @@ __device__ __forceinline__ float2 row_sum(float2 v, float2* sh) {
 
 constexpr int threads_of(int wv) { return wv == 1 ? 256 : wv * 64; }
 
-// The pieces of a thread in row t of an operand.
-template <class E, int VEC, int NV, int WV>
+// The pieces of a thread in a row of n elements: piece i WV 64 + l from its element at(i) on, of which those below skip(i)
+// are another piece's (all of them: no piece).  PART: n is no whole number of pieces; the last one then is the 16 bytes
+// that end with the row, so that every access is whole.  What it shares with the piece before is computed by both
+// alike, and enters sums once.
+template <class E, int NV, int WV, bool PART>
 struct Row {
-  typename Pack<E, VEC>::Raw raw[NV];
-  __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t t, int l, int nv) {
+  static constexpr int kN = Pack<E>::kN;
+  u32x4 raw[NV];
+  static __device__ __forceinline__ int skip(int i, int l, int n) {
+    const int left = n - (i * WV * 64 + l) * kN;
+    if (!PART) return left > 0 ? 0 : kN;
+    return left >= kN ? 0 : (left > 0 ? kN - left : kN);
+  }
+  static __device__ __forceinline__ int at(int i, int l, int n) {
+    const int c = (i * WV * 64 + l) * kN;
+    return PART && c > n - kN ? n - kN : c;
+  }
+  __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t t, int l, int n) {
     const E* p = static_cast<const E*>(base) + t * ld;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = i * WV * 64 + l;
-      if (c < nv) raw[i] = Pack<E, VEC>::load(p + (int64_t)c * VEC);
+      if (skip(i, l, n) < kN) raw[i] = Pack<E>::load(p + at(i, l, n));
+      else raw[i] = u32x4{0u, 0u, 0u, 0u};
     }
   }
 };
 
 // A workgroup walks rows with a stride, weight and bias of its columns in registers; the next row is read while one is
 // normalised.
-template <class E, int VEC, int NV, int WV>
-__global__ void __launch_bounds__(threads_of(WV)) fwd_kernel(Args a) {
-  constexpr int kT = WV * 64, kRows = threads_of(WV) / kT;
+template <class E, int NV, int WV, bool PART>
+__global__ void __launch_bounds__(threads_of(WV), 2) fwd_kernel(Args a) {
+  constexpr int kT = WV * 64, kRows = threads_of(WV) / kT, kN = Pack<E>::kN;
+  typedef Row<E, NV, WV, PART> R;
   __shared__ float2 sh[2][WV];
   const int l = threadIdx.x % kT;
-  const int nv = a.n / VEC;
   const int64_t stride = (int64_t)gridDim.x * kRows;
   int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / kT;
   if (t >= a.T) return;      // whole waves; with WV > 1 a workgroup has one row at a time
-  Row<E, VEC, NV, WV> x;
-  x.load(a.X, a.ldx, t, l, nv);
-  float w[NV][VEC], b[NV][VEC];
+  R x;
+  x.load(a.X, a.ldx, t, l, a.n);
+  float w[NV][kN], b[NV][kN];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = i * kT + l;
-    if (c < nv) {
-      vector_at<VEC>(a.weight, a.w_bf16, a.vec_w, 1.f, c * VEC, w[i]);
-      vector_at<VEC>(a.bias, a.w_bf16, a.vec_w, 0.f, c * VEC, b[i]);
+    if (R::skip(i, l, a.n) < kN) {
+      vector_at<kN>(a.weight, a.w_bf16, 1.f, R::at(i, l, a.n), w[i]);
+      vector_at<kN>(a.bias, a.w_bf16, 0.f, R::at(i, l, a.n), b[i]);
     }
   }
   for (;;) {
-    float v[NV][VEC];
+    float v[NV][kN];
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (i * kT + l < nv) {
-        Pack<E, VEC>::widen(x.raw[i], v[i]);
+    for (int i = 0; i < NV; ++i) {
+      Pack<E>::widen(x.raw[i], v[i]);
+      const int skip = R::skip(i, l, a.n);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) s += v[i][k];
-      }
+      for (int k = 0; k < kN; ++k) s += !PART || k >= skip ? v[i][k] : 0.f;
+    }
     const int64_t next = t + stride;
-    if (next < a.T) x.load(a.X, a.ldx, next, l, nv);
+    if (next < a.T) x.load(a.X, a.ldx, next, l, a.n);
     const float mu = row_sum<WV>(make_float2(s, 0.f), sh[0]).x / (float)a.n;
     float q = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (i * kT + l < nv) {
+    for (int i = 0; i < NV; ++i) {
+      const int skip = R::skip(i, l, a.n);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-          v[i][k] -= mu;
-          q = fmaf(v[i][k], v[i][k], q);
-        }
+      for (int k = 0; k < kN; ++k) {
+        v[i][k] -= mu;
+        q = (PART ? k >= skip : skip == 0) ? fmaf(v[i][k], v[i][k], q) : q;
       }
+    }
     // (the barrier within keeps sh[0] until every wave has read it)
     const float var = row_sum<WV>(make_float2(q, 0.f), sh[1]).x / (float)a.n;
     const float r = 1.f / sqrtf(var + a.eps);
     E* y = static_cast<E*>(a.Y) + t * a.ldy;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = i * kT + l;
-      if (c < nv) {
-        float o[VEC];
+      if (R::skip(i, l, a.n) < kN) {
+        float o[kN];
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) o[k] = fmaf(v[i][k] * r, w[i][k], b[i][k]);
-        Pack<E, VEC>::put(y + (int64_t)c * VEC, o);
+        for (int k = 0; k < kN; ++k) o[k] = fmaf(v[i][k] * r, w[i][k], b[i][k]);
+        Pack<E>::put(y + R::at(i, l, a.n), o);
       }
     }
     if (l == 0) {
@@ -233,8 +234,8 @@ __global__ void __launch_bounds__(1024) fwd_wide_kernel(Args a) {
   const float r = 1.f / sqrtf(row_sum<16>(make_float2(q, 0.f), sh[1]).x / (float)a.n + a.eps);
   for (int c = threadIdx.x; c < a.n; c += 1024) {
     float w, b;
-    vector_at<1>(a.weight, a.w_bf16, 0, 1.f, c, &w);
-    vector_at<1>(a.bias, a.w_bf16, 0, 0.f, c, &b);
+    vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
+    vector_at<1>(a.bias, a.w_bf16, 0.f, c, &b);
     y[c] = (E)fmaf(((float)x[c] - mu) * r, w, b);
   }
   if (threadIdx.x == 0) {
@@ -243,112 +244,120 @@ __global__ void __launch_bounds__(1024) fwd_wide_kernel(Args a) {
   }
 }
 
-template <class E, int VEC, int NV, int WV>
-__global__ void __launch_bounds__(threads_of(WV)) bwd_kernel(Args a) {
-  constexpr int kT = WV * 64, kRows = threads_of(WV) / kT;
+template <class E, int NV, int WV, bool PART>
+__global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
+  constexpr int kT = WV * 64, kRows = threads_of(WV) / kT, kN = Pack<E>::kN;
+  typedef Row<E, NV, WV, PART> R;
   __shared__ float2 sh[2][WV];
-  __shared__ float comb[kRows > 1 ? 2 * NV * VEC * kT : 1];
+  __shared__ float comb[kRows > 1 ? 2 * NV * kN * kT : 1];
   const int l = threadIdx.x % kT, sub = threadIdx.x / kT;
-  const int nv = a.n / VEC;
   const int64_t stride = (int64_t)gridDim.x * kRows;
   int64_t t = (int64_t)blockIdx.x * kRows + sub;
-  Row<E, VEC, NV, WV> x, g;
+  R x, g;
   float mu_next = 0.f, r_next = 0.f;
   auto fetch = [&](int64_t row) {
     if (row >= a.T) return;
-    x.load(a.X, a.ldx, row, l, nv);
-    g.load(a.G, a.ldg, row, l, nv);
+    x.load(a.X, a.ldx, row, l, a.n);
+    g.load(a.G, a.ldg, row, l, a.n);
     mu_next = a.mean[row];
     r_next = a.rstd[row];
   };
   fetch(t);
-  float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
+  float w[NV][kN], dw[NV][kN], db[NV][kN];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = i * kT + l;
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) w[i][k] = dw[i][k] = db[i][k] = 0.f;
-    if (c < nv) vector_at<VEC>(a.weight, a.w_bf16, a.vec_w, 1.f, c * VEC, w[i]);
+    for (int k = 0; k < kN; ++k) w[i][k] = dw[i][k] = db[i][k] = 0.f;
+    if (R::skip(i, l, a.n) < kN) vector_at<kN>(a.weight, a.w_bf16, 1.f, R::at(i, l, a.n), w[i]);
   }
   const float inv_n = 1.f / (float)a.n;
   int turn = 0;
   for (; t < a.T; t += stride, turn ^= 1) {
     const float mu = mu_next, r = r_next;
-    float h[NV][VEC], gg[NV][VEC];
+    float h[NV][kN], gg[NV][kN];
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (i * kT + l < nv) {
-        Pack<E, VEC>::widen(x.raw[i], h[i]);
-        Pack<E, VEC>::widen(g.raw[i], gg[i]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) h[i][k] = mu, gg[i][k] = 0.f;
-      }
+    for (int i = 0; i < NV; ++i) {
+      Pack<E>::widen(x.raw[i], h[i]);
+      Pack<E>::widen(g.raw[i], gg[i]);
+    }
     fetch(t + stride);
+    // a piece that is not there has g = 0, so that nothing comes of it
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      const int skip = R::skip(i, l, a.n);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) {
+      for (int k = 0; k < kN; ++k) {
         h[i][k] = (h[i][k] - mu) * r;
         dw[i][k] = fmaf(gg[i][k], h[i][k], dw[i][k]);
         db[i][k] += gg[i][k];
         gg[i][k] *= w[i][k];
-        s.x += gg[i][k];
-        s.y = fmaf(gg[i][k], h[i][k], s.y);
+        const float q = !PART || k >= skip ? gg[i][k] : 0.f;
+        s.x += q;
+        s.y = fmaf(q, h[i][k], s.y);
       }
+    }
     if (!a.Y) continue;
     s = row_sum<WV>(s, sh[turn]);
     const float ma = s.x * inv_n, mh = s.y * inv_n;
     E* dx = static_cast<E*>(a.Y) + t * a.ldy;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = i * kT + l;
-      if (c < nv) {
-        float o[VEC];
+      const int skip = R::skip(i, l, a.n);
+      if (skip < kN) {
+        E* p = dx + R::at(i, l, a.n);
+        float o[kN];
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) o[k] = r * (gg[i][k] - ma - h[i][k] * mh);
-        if (a.beta != 0.f) {
-          float old[VEC];
-          Pack<E, VEC>::get(dx + (int64_t)c * VEC, old);
+        for (int k = 0; k < kN; ++k) o[k] = r * (gg[i][k] - ma - h[i][k] * mh);
+        if (a.beta == 0.f) {
+          Pack<E>::put(p, o);
+        } else if (!PART || skip == 0) {
+          float old[kN];
+          Pack<E>::widen(Pack<E>::load(p), old);
 #pragma unroll
-          for (int k = 0; k < VEC; ++k) o[k] = fmaf(a.beta, old[k], o[k]);
+          for (int k = 0; k < kN; ++k) o[k] = fmaf(a.beta, old[k], o[k]);
+          Pack<E>::put(p, o);
+        } else {
+          // the shared elements are added to once: this piece writes its own alone
+#pragma unroll
+          for (int k = 0; k < kN; ++k)
+            if (k >= skip) p[k] = (E)fmaf(a.beta, (float)p[k], o[k]);
         }
-        Pack<E, VEC>::put(dx + (int64_t)c * VEC, o);
       }
     }
   }
   if (!a.part) return;
+  float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
   if constexpr (kRows > 1) {
     // the workgroup's rows in turn: a fixed order
-    float* mine = comb + l * VEC;
     for (int q = 0; q < kRows; ++q) {
       if (q == sub)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+          const int skip = R::skip(i, l, a.n);
+          float* p = comb + R::at(i, l, a.n);
 #pragma unroll
-          for (int k = 0; k < VEC; ++k) {
-            float* p = mine + i * kT * VEC + k;
-            p[0] = q ? p[0] + dw[i][k] : dw[i][k];
-            p[NV * VEC * kT] = q ? p[NV * VEC * kT] + db[i][k] : db[i][k];
-          }
+          for (int k = 0; k < kN; ++k)
+            if (k >= skip) {
+              p[k] = q ? p[k] + dw[i][k] : dw[i][k];
+              p[NV * kN * kT + k] = q ? p[NV * kN * kT + k] + db[i][k] : db[i][k];
+            }
+        }
       __syncthreads();
     }
-    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
     for (int c = threadIdx.x; c < a.n; c += threads_of(WV)) {
       part[c] = comb[c];
-      part[a.n + c] = comb[NV * VEC * kT + c];
+      part[a.n + c] = comb[NV * kN * kT + c];
     }
   } else {
-    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = i * kT + l;
-      if (c < nv)
+      const int skip = R::skip(i, l, a.n), c = R::at(i, l, a.n);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-          part[c * VEC + k] = dw[i][k];
-          part[a.n + c * VEC + k] = db[i][k];
+      for (int k = 0; k < kN; ++k)
+        if (k >= skip) {
+          part[c + k] = dw[i][k];
+          part[a.n + c + k] = db[i][k];
         }
     }
   }
@@ -366,7 +375,7 @@ __global__ void __launch_bounds__(1024) bwd_wide_kernel(Args a) {
   float2 s = make_float2(0.f, 0.f);
   for (int c = threadIdx.x; c < a.n; c += 1024) {
     float w;
-    vector_at<1>(a.weight, a.w_bf16, 0, 1.f, c, &w);
+    vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
     w *= (float)g[c];
     s.x += w;
     s.y = fmaf(w, ((float)x[c] - mu) * r, s.y);
@@ -375,7 +384,7 @@ __global__ void __launch_bounds__(1024) bwd_wide_kernel(Args a) {
   const float ma = s.x / (float)a.n, mh = s.y / (float)a.n;
   for (int c = threadIdx.x; c < a.n; c += 1024) {
     float w;
-    vector_at<1>(a.weight, a.w_bf16, 0, 1.f, c, &w);
+    vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
     float o = r * (w * (float)g[c] - ma - ((float)x[c] - mu) * r * mh);
     if (a.beta != 0.f) o = fmaf(a.beta, (float)dx[c], o);
     dx[c] = (E)o;
@@ -421,32 +430,34 @@ __global__ void __launch_bounds__(1024) vector_sum_kernel(const float* part, int
 
 // The instance of a row of n: NV pieces of a thread and WV waves of a row.  A wave takes rows of up to four pieces a
 // lane (bf16: 2048 wide; 2048 wide and 8192 rows, forward / backward: 15 / 21 us against 21 / 24 with four waves), eight
-// waves up to two (8192: 46 / 83 us against 49 / 85 with four waves of four and 51 / 84 with sixteen of one), sixteen
-// waves up to 16384; wider rows are read three times.  Rows that do not start on 16 bytes, or whose width is no
-// whole number of pieces, have pieces of one element.
+// waves up to four (8192 wide, two: 46 / 83 us against 49 / 85 with four waves of four and 51 / 84 with sixteen of one);
+// rows wider than that (bf16 16384, fp32 8192), or narrower than a piece, are read three times.  A backward with a last
+// piece that overlaps keeps to two pieces a lane of one wave: four spill (2047 wide and 8192 rows 47 us).
 struct Shape {
-  int vec, nv, wv;   // wv 0: wide
+  int nv, wv;   // wv 0: wide
+  bool part;    // the last piece is a part
 };
-Shape shape_of(int64_t n, int esz, bool aligned) {
-  const int vec = aligned && n % (16 / esz) == 0 ? 16 / esz : 1;
-  const int64_t p = n / vec;
+Shape shape_of(int64_t n, int esz, bool bwd) {
+  const int per = 16 / esz;
+  const int64_t p = (n + per - 1) / per;
   auto fit = [&](int wv, int limit) -> int {
-    for (int nv : {1, 2, 4, 8, 16})
+    for (int nv : {1, 2, 4})
       if (nv <= limit && p <= (int64_t)nv * wv * 64) return nv;
     return 0;
   };
-  if (int nv = fit(1, vec == 1 ? 16 : 4)) return {vec, nv, 1};
-  if (int nv = fit(8, vec == 1 ? 16 : 2)) return {vec, nv, 8};
-  if (int nv = fit(16, vec == 1 ? 16 : (esz == 4 ? 4 : 2))) return {vec, nv, 16};
-  return {vec, 0, 0};
+  const bool part = n % per != 0;
+  if (n < per) return {0, 0, part};
+  if (int nv = fit(1, bwd && part ? 2 : 4)) return {nv, 1, part};
+  if (int nv = fit(8, 4)) return {nv, 8, part};
+  return {0, 0, part};
 }
 
 // Workgroups of a forward: about two waves more than fill the card (12,608 rows of 768: 9.5 us with 1024 workgroups, 11.6
 // with 512, 10.3 with one per four rows; 8192 of 8192: 46, 48 and 48).
 int64_t fwd_groups(int64_t T, const Shape& s) {
   const int rows = s.wv == 1 ? 4 : 1;
-  const int64_t g = (T + rows - 1) / rows, most = s.wv == 16 ? 512 : 1024;
-  return g < most ? g : most;
+  const int64_t g = (T + rows - 1) / rows;
+  return g < 1024 ? g : 1024;
 }
 // And of a backward, each with a partial row of dw and db to write and add up (12,608 rows of 768: 13.4 us with 512, 17.5
 // with 256, 15.6 with 1024; 8192 of 8192: 83 with 256, 91 with 512).
@@ -457,31 +468,20 @@ int groups_of(int64_t T, int64_t n, const Shape& s) {
   return (int)(g < most ? g : most);
 }
 
-template <class E, int VEC, int NV, int WV>
-void launch(const Args& a, bool bwd, int groups, hipStream_t s) {
+template <class E, int NV, int WV>
+void launch(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t s) {
   const dim3 grid((unsigned)groups), block(threads_of(WV));
-  if (bwd) hipLaunchKernelGGL((bwd_kernel<E, VEC, NV, WV>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((fwd_kernel<E, VEC, NV, WV>), grid, block, 0, s, a);
+  if (bwd && sh.part) hipLaunchKernelGGL((bwd_kernel<E, NV, WV, true>), grid, block, 0, s, a);
+  else if (bwd) hipLaunchKernelGGL((bwd_kernel<E, NV, WV, false>), grid, block, 0, s, a);
+  else if (sh.part) hipLaunchKernelGGL((fwd_kernel<E, NV, WV, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((fwd_kernel<E, NV, WV, false>), grid, block, 0, s, a);
 }
 
-// One-element pieces have instances of four and sixteen a thread, whole ones of one, two and four.
-template <class E, int VEC, int WV>
-void launch_nv(const Args& a, int nv, bool bwd, int groups, hipStream_t s) {
-  if constexpr (VEC == 1) {
-    if (nv <= 4) launch<E, VEC, 4, WV>(a, bwd, groups, s);
-    else launch<E, VEC, 16, WV>(a, bwd, groups, s);
-  } else {
-    if (nv == 1) launch<E, VEC, 1, WV>(a, bwd, groups, s);
-    else if (nv == 2) launch<E, VEC, 2, WV>(a, bwd, groups, s);
-    else if constexpr (WV == 1 || (WV == 16 && sizeof(E) == 4)) launch<E, VEC, 4, WV>(a, bwd, groups, s);
-  }
-}
-
-template <class E, int VEC>
-void launch_wv(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t s) {
-  if (sh.wv == 1) launch_nv<E, VEC, 1>(a, sh.nv, bwd, groups, s);
-  else if (sh.wv == 8) launch_nv<E, VEC, 8>(a, sh.nv, bwd, groups, s);
-  else launch_nv<E, VEC, 16>(a, sh.nv, bwd, groups, s);
+template <class E, int WV>
+void launch_nv(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t s) {
+  if (sh.nv == 1) launch<E, 1, WV>(a, sh, bwd, groups, s);
+  else if (sh.nv == 2) launch<E, 2, WV>(a, sh, bwd, groups, s);
+  else launch<E, 4, WV>(a, sh, bwd, groups, s);
 }
 
 template <class E>
@@ -492,10 +492,10 @@ hipError_t run(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t
     if (bwd && a.part)
       hipLaunchKernelGGL(bwd_wide_vectors_kernel<E>, dim3((unsigned)groups, (unsigned)((a.n + 255) / 256)), dim3(256), 0, s,
                          a);
-  } else if (sh.vec == 1) {
-    launch_wv<E, 1>(a, sh, bwd, groups, s);
+  } else if (sh.wv == 1) {
+    launch_nv<E, 1>(a, sh, bwd, groups, s);
   } else {
-    launch_wv<E, 16 / (int)sizeof(E)>(a, sh, bwd, groups, s);
+    launch_nv<E, 8>(a, sh, bwd, groups, s);
   }
   return hipGetLastError();
 }
@@ -514,8 +514,6 @@ ff_status check_sizes(int64_t T, int64_t n, int act, int w_dtype) {
     return fail(FF_EINVAL, "T=%lld or n=%lld out of range", (long long)T, (long long)n);
   return FF_OK;
 }
-
-bool whole(const void* p, int64_t ld, int esz) { return (uintptr_t)p % 16 == 0 && ld * esz % 16 == 0; }
 
 }  // namespace norm
 }  // namespace ff
@@ -538,8 +536,7 @@ ff_status ff_layernorm_fwd(int64_t T, int64_t n, int act, const void* X, int64_t
   Args a{};
   a.X = X, a.Y = Y, a.ldx = ldx, a.ldy = ldy, a.T = T, a.n = (int)n, a.weight = weight, a.bias = bias;
   a.w_bf16 = w_dtype == FF_BF16, a.eps = eps, a.mean = mean, a.rstd = rstd;
-  a.vec_w = (uintptr_t)weight % 16 == 0 && (uintptr_t)bias % 16 == 0;
-  const Shape sh = shape_of(n, esz, whole(X, ldx, esz) && whole(Y, ldy, esz));
+  const Shape sh = shape_of(n, esz, false);
   const int groups = (int)fwd_groups(T, sh);
   const hipError_t e = act == FF_BF16 ? run<__bf16>(a, sh, false, groups, (hipStream_t)stream)
                                       : run<float>(a, sh, false, groups, (hipStream_t)stream);
@@ -577,7 +574,7 @@ ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t
     if (!mean || !rstd) return ff::fail(FF_EINVAL, "mean or rstd is NULL");
     if ((uintptr_t)weight % wsz || (uintptr_t)mean % 4 || (uintptr_t)rstd % 4)
       return ff::fail(FF_EINVAL, "weight, mean or rstd is misaligned");
-    const Shape sh = shape_of(n, esz, whole(X, ldx, esz) && whole(G, ldg, esz) && (!dX || whole(dX, lddx, esz)));
+    const Shape sh = shape_of(n, esz, true);
     groups = groups_of(T, n, sh);
     if (vectors) {
       if (!workspace || (uintptr_t)workspace % 16) return ff::fail(FF_EINVAL, "the workspace is NULL or not 16-byte aligned");
@@ -589,7 +586,6 @@ ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t
     a.X = X, a.G = G, a.Y = dX, a.ldx = ldx, a.ldg = ldg, a.ldy = lddx, a.T = T, a.n = (int)n, a.weight = weight;
     a.w_bf16 = w_dtype == FF_BF16, a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd), a.beta = beta_dx;
     a.part = vectors ? static_cast<float*>(workspace) : nullptr;
-    a.vec_w = (uintptr_t)weight % 16 == 0;
     const hipError_t e = act == FF_BF16 ? run<__bf16>(a, sh, true, groups, (hipStream_t)stream)
                                         : run<float>(a, sh, true, groups, (hipStream_t)stream);
     if (e != hipSuccess) return ff::fail(FF_EDEVICE, "layer norm backward: %s", hipGetErrorString(e));

@@ -76,7 +76,8 @@ def _close(got, want, bound, what):
 # one row to many, widths of one element, of every instance (one wave with 1, 2 and 4 pieces, 4 and 16 waves), odd ones,
 # and ones read three times
 SIZES = [(1, 1), (3, 2), (7, 64), (1, 768), (513, 768), (130, 1000), (66, 1021), (5, 2048), (9, 2056), (600, 1024), (17, 4096),
-         (33, 8192), (3, 5001), (2, 28672), (2, 32771), (3, 40000)]
+         (33, 8192), (3, 5001), (2, 28672), (2, 32771), (3, 40000),
+         (5, 9), (600, 15), (70, 2047), (40, 1025), (9, 12291), (1, 16384)]
 
 
 @pytest.mark.parametrize("T,n", SIZES)
@@ -205,3 +206,16 @@ def test_refusals(dev):
         ff.layernorm_fwd(X.half())
     with pytest.raises(ff.FrameFTError):
         ff.layernorm_bwd(X, X, w, m, r, workspace=torch.empty(64, dtype=torch.uint8, device=dev))
+
+
+@pytest.mark.parametrize("n", [9, 1021, 2047, 5473])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_odd_widths_in_place(dev, n, dtype):
+    """The last piece of an odd row overlaps the one before it: in place, the same bits as into another tensor."""
+    x, g, w, b = _case(300, n, dtype, n)
+    X, wt, bt = torch_act(x, dtype, dev), torch.from_numpy(w).to(dev), torch.from_numpy(b).to(dev)
+    Y = ff.layernorm_fwd(X, wt, bt)[0]
+    got = X.clone()
+    ff.layernorm_fwd(got, wt, bt, Y=got)
+    torch.cuda.synchronize()
+    assert torch.equal(got, Y)
