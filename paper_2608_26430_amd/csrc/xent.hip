@@ -50,15 +50,12 @@ hipError_t launch_gemm(int layout, int bf16, int tile, const GemmArgs& a, hipStr
 
 namespace {
 
-// Joins the statistics of a token's columns: a workgroup takes TK tokens, its 256 / TK shares of the entries are joined
-// through LDS.
+// Joins the statistics of a token's columns, (maximum, sum of exponentials without the target's): a workgroup takes TK
+// tokens, its 256 / TK shares of the entries are joined through LDS.  The result is that of threads with part 0.
 template <int TK>
-__global__ void __launch_bounds__(256) combine_kernel(const float2* stats, int nstat, int N, const int64_t* target,
-                                                      int64_t vocab, float* zt, float* loss, float* lse) {
+__device__ __forceinline__ float2 join_stats(const float2* stats, int nstat, int N, int t, int part, int tk,
+                                             float2 (&sh)[256 / TK][TK]) {
   constexpr int kShares = 256 / TK;
-  __shared__ float2 sh[kShares][TK];
-  const int tk = threadIdx.x % TK, part = threadIdx.x / TK;
-  const int t = blockIdx.x * TK + tk;
   float top = -INFINITY, sum = 0.f;
   auto join = [&](float2 s) {
     const float m = fmaxf(top, s.x);
@@ -86,18 +83,32 @@ __global__ void __launch_bounds__(256) combine_kernel(const float2* stats, int n
       sh[part][tk] = make_float2(top, sum);
     }
   }
+  return make_float2(top, sum);
+}
+
+// A token's loss and lse, and the target's value of P before its weight.
+struct Token {
+  float lse, loss, own;
+};
+__device__ __forceinline__ Token token_of(float2 joined, int64_t target, int64_t vocab, float z) {
+  const float m = joined.x, others = joined.y;
+  if (target < 0 || target >= vocab) return Token{m + logf(others), 0.f, 0.f};
+  const float total = others + expf(z - m), ls = logf(total);
+  return Token{m + ls, z == m ? log1pf(others) : (m - z) + ls, -others / total};
+}
+
+template <int TK>
+__global__ void __launch_bounds__(256) combine_kernel(const float2* stats, int nstat, int N, const int64_t* target,
+                                                      int64_t vocab, float* zt, float* loss, float* lse) {
+  __shared__ float2 sh[256 / TK][TK];
+  const int tk = threadIdx.x % TK, part = threadIdx.x / TK;
+  const int t = blockIdx.x * TK + tk;
+  const float2 joined = join_stats<TK>(stats, nstat, N, t, part, tk, sh);
   if (part || t >= N) return;
-  const float m = top, others = sum;
-  const int64_t tg = target[t];
-  if (tg >= 0 && tg < vocab) {
-    const float z = zt[t], total = others + expf(z - m), ls = logf(total);
-    lse[t] = m + ls;
-    loss[t] = z == m ? log1pf(others) : (m - z) + ls;
-    zt[t] = -others / total;     // the target's value of P before its weight
-  } else {
-    lse[t] = m + logf(others);
-    loss[t] = 0.f;
-  }
+  const Token k = token_of(joined, target[t], vocab, zt[t]);
+  lse[t] = k.lse;
+  loss[t] = k.loss;
+  zt[t] = k.own;
 }
 
 template <class E>
@@ -135,17 +146,35 @@ struct Piece16<float> {
 
 // e = exp(z - maximum of its columns) -> P, in place; rest: elements from a row to the one that takes what rounding left
 // (0: none).  Bound by memory: P is read and written once (4096 x 32,000 in bf16: 74 us, 7 TB/s out of the last-level cache).
+// JOIN: zt still holds the target's logit, and every workgroup of a token joins its statistics for itself, the first one
+// writing loss and lse: a launch less than with combine_kernel, whose sums these are, where that reads little (12
+// tokens, 1847 entries: 5.3 us for 4.6 + 3.5; 40 of 32,000, 160,000 statistics read: 8.7 for 6.0 + 5.0; 64 of 128,000 in
+// fp32, 8 million: 44 for 11.5 + 10.6).
 constexpr int kRescaleRow = 4;   // pieces per thread
-template <class E>
+template <class E, bool JOIN>
 __global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int64_t rest, int N, int V, const float2* stats, int cols,
-                                                      const int64_t* target, const float* own, const float* lse,
+                                                      const int64_t* target, const float* zt, float* loss, float* lse,
                                                       const float* dloss, float scale) {
   constexpr int kN = Piece16<E>::kN;
   const int t = blockIdx.y;
   const int64_t tg = target[t];
   const bool counted = tg >= 0 && tg < V;
   const float w = counted ? scale * (dloss ? dloss[t] : 1.f) : 0.f;
-  const float ls = lse[t];
+  float ls, own = 0.f;
+  if constexpr (JOIN) {
+    __shared__ float2 sh[256][1];
+    __shared__ Token joined;
+    const float2 s = join_stats<1>(stats, (V + cols - 1) / cols, N, t, threadIdx.x, 0, sh);
+    if (threadIdx.x == 0) {
+      joined = token_of(s, tg, V, counted ? zt[t] : 0.f);
+      if (blockIdx.x == 0) lse[t] = joined.lse, loss[t] = joined.loss;
+    }
+    __syncthreads();
+    ls = joined.lse, own = joined.own;
+  } else {
+    ls = lse[t];
+    if (counted) own = zt[t];
+  }
   E* row = P + (int64_t)t * ldp;
 #pragma unroll
   for (int q = 0; q < kRescaleRow; ++q) {
@@ -159,7 +188,7 @@ __global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int64_t
 #pragma unroll
       for (int i = 0; i < kN; ++i) v[i] *= f;
       if (tg >= c && tg < c + kN) {
-        const float p = own[t] * w;
+        const float p = own * w;
 #pragma unroll
         for (int i = 0; i < kN; ++i) v[i] = tg == c + i ? p : v[i];
       }
@@ -176,16 +205,31 @@ __global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int64_t
   }
 }
 
-// out = beta out + sum over the splits of part: N x M, M a multiple of four.
-template <class E>
+// out = beta out + sum over the splits of part: N x M, M a multiple of four.  SH threads share the splits of four results;
+// their sums are joined in a fixed order.  Few results of many splits are bound by the latency of one load after the
+// other: 8 tokens, 176 wide, 128 sums 33 us with one thread, 3.9 with 16.
+template <class E, int SH>
 __global__ void __launch_bounds__(256) sum_kernel(const float* part, int splits, int64_t N, int M, float beta, E* out,
                                                   int64_t ldo) {
-  const int64_t per = M / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= N * per) return;
+  constexpr int kWide = 256 / SH;
+  __shared__ f32x4 sh[SH][kWide];
+  const int lane = threadIdx.x % kWide, share = threadIdx.x / kWide;
+  const int64_t per = M / 4, id = (int64_t)blockIdx.x * kWide + lane;
   const int64_t row = id / per;
   const int c = (int)(id - row * per) * 4;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) v += load4(part + ((int64_t)s * N + row) * M + c);
+  if (row < N) {
+#pragma unroll 4
+    for (int s = share; s < splits; s += SH) v += load4(part + ((int64_t)s * N + row) * M + c);
+  }
+  if constexpr (SH > 1) {
+    sh[share][lane] = v;
+    __syncthreads();
+    if (share) return;
+#pragma unroll
+    for (int i = 1; i < SH; ++i) v += sh[i][lane];
+  }
+  if (row >= N) return;
   E* p = out + row * ldo + c;
   if (beta != 0.f) v += beta * load4(p);
   store4(p, v);
@@ -211,6 +255,8 @@ __global__ void __launch_bounds__(256) live_rows_kernel(const E* H, int64_t ldh,
 
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // P of one piece
 constexpr int64_t kPairTokens = 128;                  // tokens up to which bf16 P is kept in two terms
+constexpr int64_t kFewTokens = 64;                    // tokens up to which a workgroup joins one token's statistics
+constexpr int64_t kJoinReads = (int64_t)1 << 20;      // statistics up to which the rescaling workgroups join them
 constexpr int64_t kStatBytes = (int64_t)64 << 20;     // statistics of one piece
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -379,7 +425,7 @@ hipError_t run_combine(const Call& c, const Tensors& x, int64_t t0, int64_t N, i
   float* zt = reinterpret_cast<float*>(x.ws + c.off_zt);
   const int nstat = (int)(up(c.V, stat) / stat);
   // few tokens: all threads on one (a token's entries lie N apart, so that many tokens are read side by side)
-  if (N <= 64)
+  if (N <= kFewTokens)
     hipLaunchKernelGGL(combine_kernel<1>, dim3((unsigned)N), dim3(256), 0, x.s, stats, nstat, (int)N, x.target + t0, c.V, zt,
                        x.loss + t0, x.lse + t0);
   else
@@ -388,30 +434,35 @@ hipError_t run_combine(const Call& c, const Tensors& x, int64_t t0, int64_t N, i
   return hipGetLastError();
 }
 
-template <class E>
+template <class E, bool JOIN>
 void rescale(const Call& c, const Tensors& x, int64_t t0, int64_t N, int stat) {
   const int64_t ldp = up(c.V, 64), seg = 256 * kRescaleRow * Piece16<E>::kN;
   // rows in groups that fit the grid's second dimension
   for (int64_t r = 0; r < N; r += 32768) {
     const int64_t rows = N - r < 32768 ? N - r : 32768;
-    hipLaunchKernelGGL(rescale_kernel<E>, dim3((unsigned)((ldp + seg - 1) / seg), (unsigned)rows), dim3(256), 0, x.s,
+    hipLaunchKernelGGL((rescale_kernel<E, JOIN>), dim3((unsigned)((ldp + seg - 1) / seg), (unsigned)rows), dim3(256), 0, x.s,
                        reinterpret_cast<E*>(x.ws + c.off_p) + r * ldp, ldp, c.terms == 2 ? N * ldp : 0, (int)N, (int)c.V,
                        reinterpret_cast<const float2*>(x.ws + c.off_stats) + r, stat, x.target + t0 + r,
-                       reinterpret_cast<const float*>(x.ws + c.off_zt) + r, x.lse + t0 + r, x.dloss ? x.dloss + t0 + r : nullptr, x.scale);
+                       reinterpret_cast<const float*>(x.ws + c.off_zt) + r, x.loss + t0 + r, x.lse + t0 + r,
+                       x.dloss ? x.dloss + t0 + r : nullptr, x.scale);
   }
 }
 
 hipError_t run_sum(const Call& c, const Tensors& x, int splits, int64_t N, int64_t M, float beta, void* out, int64_t ldo) {
   const int64_t threads = N * (M / 4);
   if (threads == 0) return hipSuccess;
-  const dim3 grid((unsigned)((threads + 255) / 256));
   const float* part = reinterpret_cast<const float*>(x.ws + c.off_part);
-  if (c.bf16)
-    hipLaunchKernelGGL(sum_kernel<__bf16>, grid, dim3(256), 0, x.s, part, splits, N, (int)M, beta,
-                       static_cast<__bf16*>(out), ldo);
-  else
-    hipLaunchKernelGGL(sum_kernel<float>, grid, dim3(256), 0, x.s, part, splits, N, (int)M, beta, static_cast<float*>(out),
-                       ldo);
+  const int shares = splits >= 16 && threads <= 65536 ? 16 : 1;
+  const dim3 grid((unsigned)((threads * shares + 255) / 256)), block(256);
+  if (c.bf16) {
+    __bf16* o = static_cast<__bf16*>(out);
+    if (shares > 1) hipLaunchKernelGGL((sum_kernel<__bf16, 16>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo);
+    else hipLaunchKernelGGL((sum_kernel<__bf16, 1>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo);
+  } else {
+    float* o = static_cast<float*>(out);
+    if (shares > 1) hipLaunchKernelGGL((sum_kernel<float, 16>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo);
+    else hipLaunchKernelGGL((sum_kernel<float, 1>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo);
+  }
   return hipGetLastError();
 }
 
@@ -494,9 +545,15 @@ hipError_t run_bwd(const Call& c, const Tensors& x, bool step) {
     const int64_t N = c.T - t0 < c.Tp ? c.T - t0 : c.Tp;
     XENT_TRY(run_logits(c, x, t0, N, 0, c.V, step ? kExp : kGrad, &stat));
     if (step) {
-      XENT_TRY(run_combine(c, x, t0, N, stat));
-      if (c.bf16) rescale<__bf16>(c, x, t0, N, stat);
-      else rescale<float>(c, x, t0, N, stat);
+      const int64_t seg = 256 * kRescaleRow * (16 / c.esz);     // of a workgroup's columns
+      if (N <= kFewTokens && N * (up(c.V, stat) / stat) * (up(c.V, seg) / seg) <= kJoinReads) {
+        if (c.bf16) rescale<__bf16, true>(c, x, t0, N, stat);
+        else rescale<float, true>(c, x, t0, N, stat);
+      } else {
+        XENT_TRY(run_combine(c, x, t0, N, stat));
+        if (c.bf16) rescale<__bf16, false>(c, x, t0, N, stat);
+        else rescale<float, false>(c, x, t0, N, stat);
+      }
       XENT_TRY(hipGetLastError());
     }
     if (c.dh) XENT_TRY(run_dh(c, x, t0, N, 0, c.V, true, true));
