@@ -324,3 +324,24 @@ def test_few_tokens_are_off_by_their_results_rounding_only(dev, T, n, V, dw):
             ([(step[3], ref[3], ref[4][2]), (back[1], ref[3], ref[4][2])] if dw else []):
         bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2.0 ** -14) * sums
         assert np.all(np.abs(to_np(got) - want) <= 1.05 * bound + 1e-37)
+
+
+@pytest.mark.parametrize("T,n,V", [(64, 16, 70001), (65, 16, 3000), (8, 24, 60000), (5, 1000, 4012), (1, 176, 87270), (2, 1208, 86)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_tokens_of_wide_and_narrow_vocabularies(dev, T, n, V, dtype):
+    """Statistics joined by a launch of their own or where P is made, sums of few results over many splits: against the
+    reference, and loss and lse with the bits of the forward alone, whose statistics and sums are the same."""
+    H, W, target, dloss = _case(T, n, V, dtype, 3 * T + V, skip=0.3 if T > 1 else 0.0)
+    ref = TO.xent(H, W, target, dloss, 0.7)
+    Ht, Wt, tt, dt = _dev(dev, dtype, H, W, target, dloss)
+    ws = _garbage(T, n, V, dtype, True, dev)
+    got = ff.xent_step(Ht, Wt, tt, dloss=dt, scale=0.7, want_dw=True, workspace=ws)
+    ws.fill_(255)
+    alone = ff.xent_step(Ht, Wt, tt, dloss=dt, scale=0.7, workspace=ws)
+    ws.fill_(255)
+    loss, lse = ff.xent_fwd(Ht, Wt, tt, workspace=ws)
+    torch.cuda.synchronize()
+    _verify(ref, dict(loss=got[0], lse=got[1], dH=got[2], dW=got[3]), n, V, dtype)
+    _verify(ref, dict(dH=alone[2]), n, V, dtype)
+    for o in (got, alone):
+        assert torch.equal(o[0], loss) and torch.equal(o[1], lse)
