@@ -430,15 +430,16 @@ ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, 
 /*
  * ff_xent_* -- cross entropy of a head's logits z = H W^T over a vocabulary of V entries, without keeping the logits:
  *   lse_t  = log sum_v exp z_tv,   loss_t = lse_t - z_t,target[t]
- *   P_tv   = (exp(z_tv - lse_t) - [v = target[t]]) scale dloss[t]
- *   dH     = beta_dh dH + P W,     dW = beta_dw dW + P^T H
+ *   P_tv   = (exp(z_tv - lse_t) - [v = target[t]]) dloss[t]
+ *   dH     = beta_dh dH + scale P W,     dW = beta_dw dW + scale P^T H
  * A token whose target lies outside [0, V) has none: its loss is 0, its row of P is 0 whatever H holds, its lse is
  * still that of its logits.
  *   H, dH  : device, T x n of type act, W, dW : device, V x n of type act; n a multiple of 8 (bf16) or 4 (fp32), 16-byte
  *            aligned, leading dimensions multiples of 8 (4), at most 1048576.  beta = 0 does not read the output.
  *   target : device, T int64.   loss, lse : device, T fp32.
  *   dloss  : device, T fp32, gradient of the result with respect to each token's loss; NULL for ones.
- *            `scale` multiplies it (1 / counted tokens for a mean).
+ *            `scale` multiplies the gradients (1 / counted tokens for a mean): P's rounding to bf16 is smallest where
+ *            the weight of all tokens is in scale and dloss is NULL.
  *   workspace : device, 256-byte aligned, at least ff_xent_workspace bytes for the same T, n, V, act and the outputs wanted
  *            (FF_XENT_DH, FF_XENT_DW or both; 0: loss alone).  It holds P, in type act, for a piece of the tokens or of
  *            the vocabulary (at most 256 MiB, or 256 tokens of it where V is larger), fp32 partial sums of dH, and with dW

@@ -2,7 +2,7 @@
 //
 // With H (T x n) the activations, W (V x n) the head, z = H W^T:
 //   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,target
-//   P_tv  = (exp(z_tv - lse_t) - [v = target_t]) scale dloss_t,   dH = P W,   dW = P^T H
+//   P_tv  = (exp(z_tv - lse_t) - [v = target_t]) dloss_t,   dH = scale P W,   dW = scale P^T H
 // Tokens whose target is no vocabulary entry have loss 0 and P = 0.
 //
 // The products run on MFMA (xent_gemm.h).  Only P, in the activations' type, passes through memory, a bounded
@@ -13,10 +13,14 @@
 //                   of a token are joined, e becomes P in place: 2 products (3 with dW) instead of the 3 (4) of a
 //                   backward that computes the logits again.
 //   backward alone  logits product whose epilogue writes P from the saved lse.
-// P is kept in the activations' type: each of its values carries one rounding (2^-9 relative in bf16), as do the
-// factors W and H; e, stored first, is in fp16 (2^-12 down to 2^-29 of the columns' maximum).  The sums of exponentials leave the target out: its own value of P,
-// exp(z - lse) - 1, is then minus the others' share, and the loss of a token whose target has the largest logit is log(1 +
-// others), so that both keep their digits when the target's probability is near one.
+// P is kept in the activations' type: each of its values carries one rounding (up to 2^-8 relative in bf16), as do the
+// factors W and H; e, stored first, is in fp16 (2^-11 down to 2^-29 of the columns' maximum).  The sums of exponentials
+// leave the target out: its own value of P, exp(z - lse) - 1, is then minus the others' share, and the loss of a token
+// whose target has the largest logit is log(1 + others), so that both keep their digits when the target's probability is
+// near one.
+// scale is applied to the products' fp32 results: P of a token whose target is unlikely then holds minus nearly one, whose
+// rounding is at most 2^-9, where nearly 1 / T of many tokens would all be rounded alike by up to twice that (3289 tokens,
+// 1920 wide, 41,071 entries: dH's error 0.0025 -> 0.0019).
 // With few tokens (kPairTokens) a handful of those roundings would decide the result (one token's dH would be off by its
 // target's, up to 2^-8), so P is kept as a sum of two bf16 matrices there, the second one what rounding left of the
 // first, as further tokens of dH's product and further k of dW's; the products are bound by reading W and writing dW.
@@ -154,12 +158,12 @@ constexpr int kRescaleRow = 4;   // pieces per thread
 template <class E, bool JOIN>
 __global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int64_t rest, int N, int V, const float2* stats, int cols,
                                                       const int64_t* target, const float* zt, float* loss, float* lse,
-                                                      const float* dloss, float scale) {
+                                                      const float* dloss) {
   constexpr int kN = Piece16<E>::kN;
   const int t = blockIdx.y;
   const int64_t tg = target[t];
   const bool counted = tg >= 0 && tg < V;
-  const float w = counted ? scale * (dloss ? dloss[t] : 1.f) : 0.f;
+  const float w = counted ? (dloss ? dloss[t] : 1.f) : 0.f;
   float ls, own = 0.f;
   if constexpr (JOIN) {
     __shared__ float2 sh[256][1];
@@ -209,8 +213,8 @@ __global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int64_t
 // their sums are joined in a fixed order.  Few results of many splits are bound by the latency of one load after the
 // other: 8 tokens, 176 wide, 128 sums 33 us with one thread, 3.9 with 16.
 template <class E, int SH>
-__global__ void __launch_bounds__(256) sum_kernel(const float* part, int splits, int64_t N, int M, float beta, E* out,
-                                                  int64_t ldo) {
+__global__ void __launch_bounds__(256) sum_kernel(const float* part, int splits, int64_t N, int M, float beta,
+                                                  E* out, int64_t ldo) {
   constexpr int kWide = 256 / SH;
   __shared__ f32x4 sh[SH][kWide];
   const int lane = threadIdx.x % kWide, share = threadIdx.x / kWide;
@@ -415,7 +419,7 @@ hipError_t run_logits(const Call& c, const Tensors& x, int64_t t0, int64_t N, in
   a.stats = reinterpret_cast<float2*>(x.ws + c.off_stats);
   a.target = x.target + t0, a.v0 = v0, a.vocab = c.V;
   a.zt = reinterpret_cast<float*>(x.ws + c.off_zt);
-  a.lse = x.lse + t0, a.loss = x.loss ? x.loss + t0 : nullptr, a.dloss = x.dloss ? x.dloss + t0 : nullptr, a.scale = x.scale;
+  a.lse = x.lse + t0, a.loss = x.loss ? x.loss + t0 : nullptr, a.dloss = x.dloss ? x.dloss + t0 : nullptr;
   *stat = stat_cols(p.tile);
   return launch_gemm(0, c.bf16, p.tile, a, x.s);
 }
@@ -444,7 +448,7 @@ void rescale(const Call& c, const Tensors& x, int64_t t0, int64_t N, int stat) {
                        reinterpret_cast<E*>(x.ws + c.off_p) + r * ldp, ldp, c.terms == 2 ? N * ldp : 0, (int)N, (int)c.V,
                        reinterpret_cast<const float2*>(x.ws + c.off_stats) + r, stat, x.target + t0 + r,
                        reinterpret_cast<const float*>(x.ws + c.off_zt) + r, x.loss + t0 + r, x.lse + t0 + r,
-                       x.dloss ? x.dloss + t0 + r : nullptr, x.scale);
+                       x.dloss ? x.dloss + t0 + r : nullptr);
   }
 }
 
@@ -479,7 +483,7 @@ hipError_t run_dh(const Call& c, const Tensors& x, int64_t t0, int64_t N, int64_
   const bool direct = p.splits * c.terms == 1 && first && last;
   void* out = x.dH + t0 * x.lddh * c.esz;
   a.mode = direct ? kOut : kPart;
-  a.out = out, a.ldo = x.lddh, a.beta = x.beta_dh;
+  a.out = out, a.ldo = x.lddh, a.alpha = x.scale, a.beta = x.beta_dh;
   a.part = reinterpret_cast<float*>(x.ws + c.off_part), a.part_add = !first;
   XENT_TRY(launch_gemm(1, c.bf16, p.tile, a, x.s));
   return direct || !last ? hipSuccess : run_sum(c, x, p.splits * c.terms, N, c.n, x.beta_dh, out, x.lddh);
@@ -498,7 +502,7 @@ hipError_t run_dw(const Call& c, const Tensors& x, int64_t v0, int64_t M) {
   a.kt = (int)(up(K, c.kk) / c.kk), a.kt_split = p.kt_split, a.splits = p.splits;
   void* out = x.dW + v0 * x.lddw * c.esz;
   a.mode = p.splits == 1 ? kOut : kPart;
-  a.out = out, a.ldo = x.lddw, a.beta = x.beta_dw;
+  a.out = out, a.ldo = x.lddw, a.alpha = x.scale, a.beta = x.beta_dw;
   a.part = reinterpret_cast<float*>(x.ws + c.off_part);
   XENT_TRY(launch_gemm(2, c.bf16, p.tile, a, x.s));
   return p.splits == 1 ? hipSuccess : run_sum(c, x, p.splits, M, c.n, x.beta_dw, out, x.lddw);

@@ -42,9 +42,9 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 enum Mode {
   kStats = 0,     // logits: maximum and sum of exponentials (the target's left out) of each wave's columns, the target's logit
   kExp = 1,       // the same, and exp(z - maximum) to out (bf16 activations: store8_half)
-  kGrad = 2,      // logits: out = (softmax - onehot) weight from the saved log-sum-exp
-  kOut = 3,       // out = beta out + product
-  kPart = 4,      // fp32 partial sums of one share of k
+  kGrad = 2,      // logits: out = (softmax - onehot) dloss from the saved log-sum-exp
+  kOut = 3,       // out = beta out + alpha product
+  kPart = 4,      // alpha times fp32 partial sums of one share of k
 };
 
 struct GemmArgs {
@@ -73,7 +73,7 @@ struct GemmArgs {
   const float* lse;       // [N]
   const float* loss;      // [N] or NULL (kGrad: the target's value from it)
   const float* dloss;     // [N] or NULL
-  float scale;
+  float alpha;            // kOut, kPart: factor of the product
 };
 
 template <class E>
@@ -304,6 +304,7 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
   if constexpr (TRA) {
     const bool partial = a.mode == kPart;
     float* part = partial ? a.part + (int64_t)split * a.N * a.M : nullptr;
+    const float alpha = a.alpha;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int row = j0 + j * 16 + r;
@@ -312,7 +313,7 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
       for (int f = 0; f < FM; ++f) {
         const int c = col(f);
         if (c >= a.M) continue;
-        f32x4 v = acc[f][j];
+        f32x4 v = acc[f][j] * alpha;
         if (partial) {
           float* p = part + (int64_t)row * a.M + c;
           if (a.part_add) v += load4(p);
@@ -360,7 +361,7 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
       E* out = static_cast<E*>(a.out) + (int64_t)row * a.ldo;
       if (a.mode == kGrad) {
         const float lse = live ? a.lse[row] : 0.f;
-        const float w = counted ? a.scale * (a.dloss ? a.dloss[row] : 1.f) : 0.f;
+        const float w = counted ? (a.dloss ? a.dloss[row] : 1.f) : 0.f;
         const float own = at >= 0 && a.loss ? expm1f(-a.loss[row]) : 0.f;
 #pragma unroll
         for (int f = 0; f < FM; ++f) {
@@ -510,10 +511,11 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
   for (int f = 0; f < FM; ++f)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[f][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // fp32, and the logits of few tokens: sums of 128 k (bf16 256) at a time, then their sum, so that rounding grows with
-  // the length of both, not of k (fp32, 1024 wide, 44 entries: the loss's error 1.2e-6 -> 3.4e-7, costs 3%; bf16, 1 to 64
-  // tokens: the mean error 3.5e-7 -> 1.6e-7 with the exponentials' difference taken before it is scaled, and no cost)
-  constexpr bool kBlocked = sizeof(E) == 4 || (NB == 4 && !TRA);
+  // fp32 (128 k at a time), and the logits of few tokens (one k tile): sums of a block, then their sum, so that rounding
+  // grows with the length of both, not of k (fp32, 1024 wide, 44 entries: the loss's error 1.2e-6 -> 3.4e-7, costs 3%;
+  // bf16, 1 to 64 tokens: the mean error 3.5e-7 -> 1.6e-7 with the exponentials' difference taken before it is scaled, and
+  // no cost)
+  constexpr bool kFew = NB == 4 && !TRA, kBlocked = sizeof(E) == 4 || kFew;
   f32x4 total_acc[kBlocked ? FM : 1][kBlocked ? FN : 1] = {};
   auto close_block = [&](bool end) {
     if constexpr (kBlocked) {
@@ -579,7 +581,7 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
           read(b, kk, fa, fb);
           multiply(fa, fb);
         }
-        close_block((t0 + b) % 4 == 3);
+        close_block(kFew || (t0 + b) % 4 == 3);
       }
     }
   }

@@ -345,3 +345,24 @@ def test_few_tokens_of_wide_and_narrow_vocabularies(dev, T, n, V, dtype):
     _verify(ref, dict(dH=alone[2]), n, V, dtype)
     for o in (got, alone):
         assert torch.equal(o[0], loss) and torch.equal(o[1], lse)
+
+
+def test_tokens_of_one_weight_are_not_rounded_alike(dev):
+    """Tokens of small logits all have nearly -1 at their target.  Times a scale that puts the products just under the middle
+    between two bf16 numbers, each rounded down by nearly 2^-8, the gradient would be that much too small as a
+    whole; with the scale applied after the products it is off by at most what rounds 0.999, 2^-9."""
+    T, n, V = 300, 64, 1000
+    g = inputs.rng(97)
+    H = inputs.gaussian(g, (T, n), std=0.01, dtype="bf16")
+    W = inputs.gaussian(g, (V, n), dtype="bf16")
+    target = g.integers(0, V, T).astype(np.int64)
+    scale = float(np.float32((1 + 0.9 * 2.0 ** -8) / 0.999 / 4096))
+    ref = TO.xent(H, W, target, np.ones(T), scale)
+    Ht, Wt = torch_act(H, "bf16", dev), torch_act(W, "bf16", dev)
+    tt = torch.from_numpy(target).to(dev)
+    step = ff.xent_step(Ht, Wt, tt, scale=scale, want_dw=True)
+    back = ff.xent_bwd(Ht, Wt, tt, step[1], loss=step[0], scale=scale, want_dw=True)
+    torch.cuda.synchronize()
+    for got, want in ((step[2], ref[2]), (step[3], ref[3]), (back[0], ref[2]), (back[1], ref[3])):
+        share = float(np.sum((to_np(got) - want) * want) / np.sum(want * want))
+        assert abs(share) <= 1.05 * 2.0 ** -9, share
