@@ -454,7 +454,7 @@ ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, 
  * dH == NULL or dW == NULL skips that output.  Arithmetic: products accumulate in fp32, softmax statistics are fp32, P is
  * rounded to type act before the products that read it (in ff_xent_step with bf16, after exp(z - max) was
  * rounded to fp16; up to 128 tokens in bf16, P is kept as the sum of two roundings).
- * With T = 0, dW = beta_dw dW.
+ * With T = 0, dW = beta_dw dW.  V is at most 2^24 for the loss alone, 2^22 with a gradient.
  */
 enum { FF_XENT_DH = 1, FF_XENT_DW = 2 };
 ff_status ff_xent_workspace(int64_t T, int64_t n, int64_t V, int act, int want, int64_t* bytes);

@@ -568,11 +568,11 @@ hipError_t run_bwd(const Call& c, const Tensors& x, bool step) {
 
 // ------------------------------------------------------------------------------------------- argument checks
 
-ff_status check_sizes(int64_t T, int64_t n, int64_t V, int act) {
+ff_status check_sizes(int64_t T, int64_t n, int64_t V, int act, bool grad) {
   if (act != FF_F32 && act != FF_BF16) return fail(FF_EINVAL, "unknown activation dtype %d", act);
   const int64_t mult = act == FF_BF16 ? 8 : 4;
   if (T < 0 || T > ((int64_t)1 << 28)) return fail(FF_EINVAL, "T=%lld out of range", (long long)T);
-  if (V < 1 || V > ((int64_t)1 << 24)) return fail(FF_EINVAL, "V=%lld out of range", (long long)V);
+  if (V < 1 || V > (grad ? kMaxGradVocab : (int64_t)1 << 24)) return fail(FF_EINVAL, "V=%lld out of range", (long long)V);
   if (n < mult || n > ((int64_t)1 << 18) || n % mult)
     return fail(FF_EINVAL, "n=%lld must be a multiple of %lld, at most 262144", (long long)n, (long long)mult);
   return FF_OK;
@@ -581,7 +581,7 @@ ff_status check_sizes(int64_t T, int64_t n, int64_t V, int act) {
 ff_status check_rows(const char* name, const void* p, int64_t ld, int64_t n, int act) {
   const int64_t mult = act == FF_BF16 ? 8 : 4;
   if (!p) return fail(FF_EINVAL, "%s is NULL", name);
-  if (ld < n || ld > ((int64_t)1 << 20) || ld % mult)
+  if (ld < n || ld > kMaxLd || ld % mult)
     return fail(FF_EINVAL, "leading dimension of %s (%lld) must be a multiple of %lld, from %lld to 1048576", name,
                 (long long)ld, (long long)mult, (long long)n);
   if ((uintptr_t)p % 16) return fail(FF_EINVAL, "%s is not 16-byte aligned", name);
@@ -637,7 +637,7 @@ extern "C" {
 
 ff_status ff_xent_workspace(int64_t T, int64_t n, int64_t V, int act, int want, int64_t* bytes) {
   ff::clear_error();
-  XENT_CHECK(ff::xent::check_sizes(T, n, V, act));
+  XENT_CHECK(ff::xent::check_sizes(T, n, V, act, want != 0));
   if (want < 0 || want > (FF_XENT_DH | FF_XENT_DW)) return ff::fail(FF_EINVAL, "unknown outputs %d", want);
   if (!bytes) return ff::fail(FF_EINVAL, "bytes is NULL");
   *bytes = (int64_t)ff::xent::plan(T, n, V, act, want & FF_XENT_DH, want & FF_XENT_DW).bytes;
@@ -648,7 +648,7 @@ ff_status ff_xent_fwd(int64_t T, int64_t n, int64_t V, int act, const void* H, i
                       const int64_t* target, float* loss, float* lse, void* workspace, int64_t workspace_bytes,
                       void* stream) {
   ff::clear_error();
-  XENT_CHECK(ff::xent::check_sizes(T, n, V, act));
+  XENT_CHECK(ff::xent::check_sizes(T, n, V, act, false));
   if (T == 0) return FF_OK;
   const Call c = ff::xent::plan(T, n, V, act, false, false);
   XENT_CHECK(ff::xent::check_rows("H", H, ldh, n, act));
@@ -668,7 +668,7 @@ ff_status ff_xent_bwd(int64_t T, int64_t n, int64_t V, int act, const void* H, i
                       float beta_dh, void* dH, int64_t lddh, float beta_dw, void* dW, int64_t lddw, void* workspace,
                       int64_t workspace_bytes, void* stream) {
   ff::clear_error();
-  XENT_CHECK(ff::xent::check_sizes(T, n, V, act));
+  XENT_CHECK(ff::xent::check_sizes(T, n, V, act, true));
   if (!dH && !dW) return FF_OK;
   const Call c = ff::xent::plan(T, n, V, act, dH != nullptr, dW != nullptr);
   Tensors x{(const char*)H, ldh, (const char*)W, ldw, target, dloss, scale, const_cast<float*>(loss), const_cast<float*>(lse), beta_dh,
@@ -682,7 +682,7 @@ ff_status ff_xent_step(int64_t T, int64_t n, int64_t V, int act, const void* H, 
                        void* dH, int64_t lddh, float beta_dw, void* dW, int64_t lddw, void* workspace,
                        int64_t workspace_bytes, void* stream) {
   ff::clear_error();
-  XENT_CHECK(ff::xent::check_sizes(T, n, V, act));
+  XENT_CHECK(ff::xent::check_sizes(T, n, V, act, dH || dW));
   const Call c = ff::xent::plan(T, n, V, act, dH != nullptr, dW != nullptr);
   Tensors x{(const char*)H, ldh, (const char*)W, ldw, target, dloss, scale, loss, lse, beta_dh, beta_dw, (char*)dH, lddh,
             (char*)dW, lddw, (char*)workspace, (hipStream_t)stream};

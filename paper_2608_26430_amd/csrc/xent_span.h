@@ -15,6 +15,14 @@ namespace xent {
 
 constexpr int kTileBytes = 128;   // of k in a tile of an operand stored along k
 
+// A load's place within its tile's range has 32 bits, of which the highest is set for a place past every range.  The tallest
+// tiles have 256 rows in bf16 and 128 in fp32: the longest rows that H, W, dH and dW may have, and those of P, which has a
+// column per vocabulary entry.
+constexpr int64_t kMaxLd = (int64_t)1 << 20, kMaxGradVocab = (int64_t)1 << 22;
+static_assert(255 * kMaxGradVocab * 2 + kTileBytes < (int64_t)1 << 31 && 127 * kMaxGradVocab * 4 + kTileBytes < (int64_t)1 << 31 &&
+                  kMaxLd <= kMaxGradVocab,
+              "places within a tile fit 31 bits");
+
 // An operand's tile of `bx` along i (or j) from x0 and one k tile: bytes from the operand's first element to the tile's, and
 // the bytes from there on that may be read.  X: extent along i.  along_k: rows of memory run along k, X counts rows, and a
 // row is read to the next whole 16-byte piece of k (H and W: their widths are whole pieces; P: zero padding).  Otherwise
