@@ -217,31 +217,33 @@ __global__ void __launch_bounds__(threads_of(WV), 2) fwd_kernel(Args a) {
   }
 }
 
-// Rows too wide for the registers: read three times.
+// Rows too wide for the registers: read three times.  (sh[0] and sh[1] take turns, so that the barrier of one sum keeps
+// the other's place until every wave has read it, over rows too.)
 template <class E>
 __global__ void __launch_bounds__(1024) fwd_wide_kernel(Args a) {
   __shared__ float2 sh[2][16];
-  const int64_t t = blockIdx.x;
-  const E* x = static_cast<const E*>(a.X) + t * a.ldx;
-  E* y = static_cast<E*>(a.Y) + t * a.ldy;
-  float s = 0.f;
-  for (int c = threadIdx.x; c < a.n; c += 1024) s += (float)x[c];
-  const float mu = row_sum<16>(make_float2(s, 0.f), sh[0]).x / (float)a.n;
-  float q = 0.f;
-  for (int c = threadIdx.x; c < a.n; c += 1024) {
-    const float d = (float)x[c] - mu;
-    q = fmaf(d, d, q);
-  }
-  const float r = 1.f / sqrtf(row_sum<16>(make_float2(q, 0.f), sh[1]).x / (float)a.n + a.eps);
-  for (int c = threadIdx.x; c < a.n; c += 1024) {
-    float w, b;
-    vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
-    vector_at<1>(a.bias, a.w_bf16, 0.f, c, &b);
-    y[c] = (E)fmaf(((float)x[c] - mu) * r, w, b);
-  }
-  if (threadIdx.x == 0) {
-    if (a.mean) a.mean[t] = mu;
-    if (a.rstd) a.rstd[t] = r;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const E* x = static_cast<const E*>(a.X) + t * a.ldx;
+    E* y = static_cast<E*>(a.Y) + t * a.ldy;
+    float s = 0.f;
+    for (int c = threadIdx.x; c < a.n; c += 1024) s += (float)x[c];
+    const float mu = row_sum<16>(make_float2(s, 0.f), sh[0]).x / (float)a.n;
+    float q = 0.f;
+    for (int c = threadIdx.x; c < a.n; c += 1024) {
+      const float d = (float)x[c] - mu;
+      q = fmaf(d, d, q);
+    }
+    const float r = 1.f / sqrtf(row_sum<16>(make_float2(q, 0.f), sh[1]).x / (float)a.n + a.eps);
+    for (int c = threadIdx.x; c < a.n; c += 1024) {
+      float w, b;
+      vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
+      vector_at<1>(a.bias, a.w_bf16, 0.f, c, &b);
+      y[c] = (E)fmaf(((float)x[c] - mu) * r, w, b);
+    }
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[t] = mu;
+      if (a.rstd) a.rstd[t] = r;
+    }
   }
 }
 
@@ -367,44 +369,46 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
 // Rows too wide for the registers: dx row by row.
 template <class E>
 __global__ void __launch_bounds__(1024) bwd_wide_kernel(Args a) {
-  __shared__ float2 sh[16];
-  const int64_t t = blockIdx.x;
-  const E* x = static_cast<const E*>(a.X) + t * a.ldx;
-  const E* g = static_cast<const E*>(a.G) + t * a.ldg;
-  E* dx = static_cast<E*>(a.Y) + t * a.ldy;
-  const float mu = a.mean[t], r = a.rstd[t];
-  float2 s = make_float2(0.f, 0.f);
-  for (int c = threadIdx.x; c < a.n; c += 1024) {
-    float w;
-    vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
-    w *= (float)g[c];
-    s.x += w;
-    s.y = fmaf(w, ((float)x[c] - mu) * r, s.y);
-  }
-  s = row_sum<16>(s, sh);
-  const float ma = s.x / (float)a.n, mh = s.y / (float)a.n;
-  for (int c = threadIdx.x; c < a.n; c += 1024) {
-    float w;
-    vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
-    float o = r * (w * (float)g[c] - ma - ((float)x[c] - mu) * r * mh);
-    if (a.beta != 0.f) o = fmaf(a.beta, (float)dx[c], o);
-    dx[c] = (E)o;
+  __shared__ float2 sh[2][16];
+  int turn = 0;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x, turn ^= 1) {
+    const E* x = static_cast<const E*>(a.X) + t * a.ldx;
+    const E* g = static_cast<const E*>(a.G) + t * a.ldg;
+    E* dx = static_cast<E*>(a.Y) + t * a.ldy;
+    const float mu = a.mean[t], r = a.rstd[t];
+    float2 s = make_float2(0.f, 0.f);
+    for (int c = threadIdx.x; c < a.n; c += 1024) {
+      float w;
+      vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
+      w *= (float)g[c];
+      s.x += w;
+      s.y = fmaf(w, ((float)x[c] - mu) * r, s.y);
+    }
+    s = row_sum<16>(s, sh[turn]);
+    const float ma = s.x / (float)a.n, mh = s.y / (float)a.n;
+    for (int c = threadIdx.x; c < a.n; c += 1024) {
+      float w;
+      vector_at<1>(a.weight, a.w_bf16, 1.f, c, &w);
+      float o = r * (w * (float)g[c] - ma - ((float)x[c] - mu) * r * mh);
+      if (a.beta != 0.f) o = fmaf(a.beta, (float)dx[c], o);
+      dx[c] = (E)o;
+    }
   }
 }
-// and dw, db: a workgroup takes 256 columns of a share of the rows
+// and dw, db: a workgroup takes 256 columns at a time of a share of the rows
 template <class E>
 __global__ void __launch_bounds__(256) bwd_wide_vectors_kernel(Args a) {
-  const int c = blockIdx.y * 256 + threadIdx.x;
-  if (c >= a.n) return;
-  float dw = 0.f, db = 0.f;
-  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-    const float g = (float)(static_cast<const E*>(a.G) + t * a.ldg)[c];
-    dw = fmaf(g, ((float)(static_cast<const E*>(a.X) + t * a.ldx)[c] - a.mean[t]) * a.rstd[t], dw);
-    db += g;
+  for (int c = blockIdx.y * 256 + threadIdx.x; c < a.n; c += gridDim.y * 256) {
+    float dw = 0.f, db = 0.f;
+    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+      const float g = (float)(static_cast<const E*>(a.G) + t * a.ldg)[c];
+      dw = fmaf(g, ((float)(static_cast<const E*>(a.X) + t * a.ldx)[c] - a.mean[t]) * a.rstd[t], dw);
+      db += g;
+    }
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+    part[c] = dw;
+    part[a.n + c] = db;
   }
-  float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
-  part[c] = dw;
-  part[a.n + c] = db;
 }
 
 // out (dw then db) = [out +] sum over the partial rows: 32 columns x 32 shares of the rows per workgroup.
@@ -488,11 +492,12 @@ void launch_nv(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t
 template <class E>
 hipError_t run(const Args& a, const Shape& sh, bool bwd, int groups, hipStream_t s) {
   if (sh.wv == 0) {
-    if (!bwd) hipLaunchKernelGGL(fwd_wide_kernel<E>, dim3((unsigned)a.T), dim3(1024), 0, s, a);
-    if (bwd && a.Y) hipLaunchKernelGGL(bwd_wide_kernel<E>, dim3((unsigned)a.T), dim3(1024), 0, s, a);
-    if (bwd && a.part)
-      hipLaunchKernelGGL(bwd_wide_vectors_kernel<E>, dim3((unsigned)groups, (unsigned)((a.n + 255) / 256)), dim3(256), 0, s,
-                         a);
+    // a launch has fewer than 2^32 threads
+    const dim3 rows((unsigned)(a.T < (1 << 20) ? a.T : (1 << 20)));
+    const dim3 columns((unsigned)groups, (unsigned)(a.n < (1 << 20) ? (a.n + 255) / 256 : 4096));
+    if (!bwd) hipLaunchKernelGGL(fwd_wide_kernel<E>, rows, dim3(1024), 0, s, a);
+    if (bwd && a.Y) hipLaunchKernelGGL(bwd_wide_kernel<E>, rows, dim3(1024), 0, s, a);
+    if (bwd && a.part) hipLaunchKernelGGL(bwd_wide_vectors_kernel<E>, columns, dim3(256), 0, s, a);
   } else if (sh.wv == 1) {
     launch_nv<E, 1>(a, sh, bwd, groups, s);
   } else {

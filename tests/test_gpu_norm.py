@@ -219,3 +219,29 @@ def test_odd_widths_in_place(dev, n, dtype):
     ff.layernorm_fwd(got, wt, bt, Y=got)
     torch.cuda.synchronize()
     assert torch.equal(got, Y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_rows_than_one_launch_has_workgroups_for(dev, dtype):
+    """Rows narrower than a 16-byte piece, 2^22 and a few of them: a workgroup each would be more threads than a launch can
+    have."""
+    T, n = (1 << 22) + 5, 3
+    x, g, w, b = _case(T, n, dtype, 11)
+    X, G = torch_act(x, dtype, dev), torch_act(g, dtype, dev)
+    wt, bt = torch.from_numpy(w).to(dev), torch.from_numpy(b).to(dev)
+    Y, m, r = ff.layernorm_fwd(X, wt, bt)
+    dX, dw, db = ff.layernorm_bwd(X, G, wt, m, r)
+    torch.cuda.synchronize()
+    rows = np.r_[0:500, (1 << 20) - 250:(1 << 20) + 250, (1 << 21) - 5:(1 << 21) + 5, T - 500:T]
+    y, ey, dx, edx, _, _, mean, em, rstd, er = _bounds(x[rows], g[rows], w, b, U[dtype])
+    at = torch.from_numpy(rows).to(dev)
+    for got, want, bound, what in ((Y, y, ey, "y"), (m, mean, em, "mean"), (r, rstd, er, "rstd"), (dX, dx, edx, "dx")):
+        _close(to_np(got[at]), want, bound, what)
+    assert bool(torch.isfinite(Y).all()) and bool(torch.isfinite(dX).all())
+    # at most T / 256 terms a workgroup's thread adds, then the partial rows: below (T / 256 + 1024) v of the absolute sums
+    y64, mean64, rstd64 = TO.layernorm_fwd(x, w, b)
+    h = (x.astype(np.float64) - mean64[:, None]) * rstd64[:, None]
+    eh = 2 * 64 * V32 * (np.abs(h) + rstd64[:, None] * (np.abs(x) + np.abs(x).mean(axis=1, keepdims=True)))
+    terms = (T / 256 + 1024) * V32
+    _close(to_np(dw), (g * h).sum(axis=0), terms * np.abs(g * h).sum(axis=0) + (np.abs(g) * eh).sum(axis=0), "dweight")
+    _close(to_np(db), g.astype(np.float64).sum(axis=0), terms * np.abs(g).astype(np.float64).sum(axis=0), "dbias")
