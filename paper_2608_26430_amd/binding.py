@@ -643,7 +643,7 @@ def _rows(t, name, like):
         raise ValueError(f"{name} must be a {like.shape[0]} x {like.shape[1]} {like.dtype} tensor with unit column stride "
                          f"on {like.device}")
     # the stride of a single row says nothing
-    return t.data_ptr(), max(st[0], t.shape[1]) if t.shape[0] < 2 else st[0]
+    return t.data_ptr(), t.shape[1] if t.shape[0] < 2 else st[0]
 
 
 def _input(t, name):
@@ -655,7 +655,7 @@ def _input(t, name):
     T, n = t.shape
     if st[1] != 1 and n != 1:
         raise ValueError(f"{name} must be a 2-D device tensor with unit column stride")
-    return t.data_ptr(), (max(st[0], n) if T < 2 else st[0]), T, n, dev
+    return t.data_ptr(), (n if T < 2 else st[0]), T, n, dev
 
 
 def _array(t, name, n, dtype, dev):

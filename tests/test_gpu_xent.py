@@ -366,3 +366,22 @@ def test_tokens_of_one_weight_are_not_rounded_alike(dev):
     for got, want in ((step[2], ref[2]), (step[3], ref[3]), (back[0], ref[2]), (back[1], ref[3])):
         share = float(np.sum((to_np(got) - want) * want) / np.sum(want * want))
         assert abs(share) <= 1.05 * 2.0 ** -9, share
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_row_of_any_stride(dev, dtype):
+    """The last position of one long sequence, and a row out of wider ones whose stride is no whole number of pieces: the
+    stride of a single row says nothing."""
+    n, V = 256, 1000
+    Ht, Wt, tt, _ = _dev(dev, dtype, *_case(1, n, V, dtype, 5, skip=0.0))
+    want = ff.xent_step(Ht, Wt, tt, want_dw=True)
+    states = torch.full((1, 8192, n), float("nan"), device=dev, dtype=Ht.dtype)
+    grads = torch.zeros_like(states)
+    states[:, -1] = Ht
+    wider = torch.full((1, n + 3), float("nan"), device=dev, dtype=Ht.dtype)
+    wider[:, :n] = Ht
+    for view, dH in ((states[:, -1], grads[:, -1]), (wider[:, :n], None)):
+        got = ff.xent_step(view, Wt, tt, dH=dH, want_dw=True)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(grads[:, -1], want[2]) and not bool(grads[:, :-1].any())
