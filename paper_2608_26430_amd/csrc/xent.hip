@@ -9,15 +9,15 @@
 // piece of it at a time:
 //   loss alone      logits product whose epilogue leaves (maximum, sum of exponentials) per token and wave's columns
 //                   and the target's logit; nothing of the logits is written.
-//   loss + gradient the same product also writes e = exp(z - maximum of the wave's columns); when the statistics
+//   loss + gradient the same product also writes e = exp(z - maximum of the wave's other columns); when the statistics
 //                   of a token are joined, e becomes P in place: 2 products (3 with dW) instead of the 3 (4) of a
 //                   backward that computes the logits again.
 //   backward alone  logits product whose epilogue writes P from the saved lse.
 // P is kept in the activations' type: each of its values carries one rounding (up to 2^-8 relative in bf16), as do the
-// factors W and H; e, stored first, is in fp16 (2^-11 down to 2^-29 of the columns' maximum).  The sums of exponentials
-// leave the target out: its own value of P, exp(z - lse) - 1, is then minus the others' share, and the loss of a token
-// whose target has the largest logit is log(1 + others), so that both keep their digits when the target's probability is
-// near one.
+// factors W and H; e, stored first, is in fp16 (2^-11 down to 2^-29 of the columns' maximum).  Maxima and sums leave the
+// target out: its own value of P, exp(z - lse) - 1, is then minus the others' share, the loss of a token whose target
+// has the largest logit is log(1 + others), and the others' exponentials are in fp16's range however far the target is
+// above them, so that all keep their digits when the target's probability is near one.
 // scale is applied to the products' fp32 results: P of a token whose target is unlikely then holds minus nearly one, whose
 // rounding is at most 2^-9, where nearly 1 / T of many tokens would all be rounded alike by up to twice that (3289 tokens,
 // 1920 wide, 41,071 entries: dH's error 0.0025 -> 0.0019).
@@ -54,7 +54,7 @@ hipError_t launch_gemm(int layout, int bf16, int tile, const GemmArgs& a, hipStr
 
 namespace {
 
-// Joins the statistics of a token's columns, (maximum, sum of exponentials without the target's): a workgroup takes TK
+// Joins the statistics of a token's columns, (maximum, sum of exponentials), both without the target: a workgroup takes TK
 // tokens, its 256 / TK shares of the entries are joined through LDS.  The result is that of threads with part 0.
 template <int TK>
 __device__ __forceinline__ float2 join_stats(const float2* stats, int nstat, int N, int t, int part, int tk,
@@ -97,8 +97,12 @@ struct Token {
 __device__ __forceinline__ Token token_of(float2 joined, int64_t target, int64_t vocab, float z) {
   const float m = joined.x, others = joined.y;
   if (target < 0 || target >= vocab) return Token{m + logf(others), 0.f, 0.f};
+  if (z >= m) {
+    const float rest = others * expf(m - z), ls = log1pf(rest) + (z - z);     // (an infinite z: NaN)
+    return Token{z + ls, ls, -rest / (1.f + rest)};
+  }
   const float total = others + expf(z - m), ls = logf(total);
-  return Token{m + ls, z == m ? log1pf(others) : (m - z) + ls, -others / total};
+  return Token{m + ls, (m - z) + ls, -others / total};
 }
 
 template <int TK>
@@ -148,7 +152,7 @@ struct Piece16<float> {
   }
 };
 
-// e = exp(z - maximum of its columns) -> P, in place; rest: elements from a row to the one that takes what rounding left
+// e = exp(z - maximum of its columns but the target) -> P, in place; rest: elements from a row to the one that takes what rounding left
 // (0: none).  Bound by memory: P is read and written once (4096 x 32,000 in bf16: 74 us, 7 TB/s out of the last-level cache).
 // JOIN: zt still holds the target's logit, and every workgroup of a token joins its statistics for itself, the first one
 // writing loss and lse: a launch less than with combine_kernel, whose sums these are, where that reads little (12

@@ -40,7 +40,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 enum Mode {
-  kStats = 0,     // logits: maximum and sum of exponentials (the target's left out) of each wave's columns, the target's logit
+  kStats = 0,     // logits: maximum and sum of exponentials of each wave's columns, the target left out, and its logit
   kExp = 1,       // the same, and exp(z - maximum) to out (bf16 activations: store8_half)
   kGrad = 2,      // logits: out = (softmax - onehot) dloss from the saved log-sum-exp
   kOut = 3,       // out = beta out + alpha product
@@ -65,7 +65,7 @@ struct GemmArgs {
   float* part;            // [splits][N][M] fp32
   int part_add;           // 1: added to what is there (an earlier piece of the vocabulary)
   // logits
-  float2* stats;          // [wave columns][N] (maximum, sum of exponentials)
+  float2* stats;          // [wave columns][N] (maximum, sum of exponentials), the target left out
   const int64_t* target;  // [N]
   int64_t v0;             // first vocabulary entry of A
   int64_t vocab;          // entries of the whole vocabulary
@@ -263,7 +263,7 @@ __device__ __forceinline__ void store8(__bf16* p, f32x4 v, f32x4 w) {
   *reinterpret_cast<u32x4*>(p) = x;
 }
 // and eight exponentials of kExp, times 2^kExpShift, in fp16: its 11 bits leave the rounding of P to bf16 nearly the only
-// one, and the shift keeps them down to 2^-29 of the columns' maximum
+// one, and the shift keeps them down to 2^-29 of the columns' maximum (the target, which may be far above, left out)
 constexpr int kExpShift = 15;
 __device__ __forceinline__ void store8_half(void* p, f32x4 v, f32x4 w) {
   typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -392,6 +392,18 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
           for (int i = 0; i < 4; ++i)
             if (col(f) + i >= a.M) acc[f][j][i] = -INFINITY;
       }
+      // the target stays out of the maximum as well as of the sum: the others' exponentials would leave fp16's range
+      // where its logit is far above theirs
+      if (hit) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (col(f) + i == at) {
+              a.zt[row] = acc[f][j][i];
+              acc[f][j][i] = -INFINITY;
+            }
+      }
       float top = -INFINITY;
 #pragma unroll
       for (int f = 0; f < FM; ++f)
@@ -404,20 +416,11 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[FM][FN], 
       float sum = 0.f;
 #pragma unroll
       for (int f = 0; f < FM; ++f) {
-        const int c = col(f);
         f32x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           v[i] = sizeof(E) == 2 ? exp2_fast(fmaf(acc[f][j][i] - ref, kLog2e, (float)kExpShift)) : expf(acc[f][j][i] - ref);
         if (a.mode == kExp) put(out, f, v, live);
-        if (hit) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (c + i == at) {
-              a.zt[row] = acc[f][j][i];
-              v[i] = 0.f;
-            }
-        }
         sum += (v[0] + v[1]) + (v[2] + v[3]);
       }
       sum += __shfl_xor(sum, 16);

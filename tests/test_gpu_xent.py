@@ -385,3 +385,51 @@ def test_one_row_of_any_stride(dev, dtype):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert torch.equal(grads[:, -1], want[2]) and not bool(grads[:, :-1].any())
+
+
+@pytest.mark.parametrize("T,V", [(64, 2), (300, 2), (300, 700), (2000, 3000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_other_entries_of_confident_tokens_keep_their_gradient(dev, T, V, dtype):
+    """The target's logit up to 60 above all others, which are 0: every other entry has P = exp(-60), and column c >= 1 of dH
+    sums that over the entries with c - 1 = v mod 7, column 0 is minus the sum over all.  All terms of a sum have one sign, so
+    each result is off by its own and P's rounding (fp16 2^-11, bf16 2^-9 each), in all below 4 x 2^-8; fp32: lse's rounding 60
+    v, the exponentials' arguments 64 v, and V / 16 + 48 steps of 2 v, below (256 + V / 8) v."""
+    n = 64
+    z = np.linspace(1, 60, T)
+    H = np.zeros((T, n), dtype=np.float32)
+    H[:, 0] = z
+    H = inputs.bf16_round(H)
+    W = np.zeros((V, n), dtype=np.float32)
+    W[np.arange(V), 1 + np.arange(V) % 7] = 1.0
+    W[1] = 0.0
+    W[1, 0] = 1.0
+    target = np.ones(T, dtype=np.int64)
+    ref = TO.xent(H, W, target)
+    Ht, Wt, tt, _ = _dev(dev, dtype, H, W, target, np.ones(T, dtype=np.float32))
+    loss, lse, dH, _ = ff.xent_step(Ht, Wt, tt)
+    back = ff.xent_bwd(Ht, Wt, tt, lse, loss=loss)[0]
+    torch.cuda.synchronize()
+    tol = 4 * 2.0 ** -8 if dtype == "bf16" else (256 + V / 8) * V32
+    used = 1 + min(V, 7)
+    exact = np.log1p((V - 1) * np.exp(-H[:, 0].astype(np.float64)))      # lse - z would cancel in float64 as well
+    assert np.all(np.abs(to_np(loss) - exact) <= (64 + V / 16) * V32 * exact)
+    for got in (dH, back):
+        assert np.all(np.abs(to_np(got)[:, :used] - ref[2][:, :used]) <= tol * np.abs(ref[2][:, :used]))
+        assert bool((got[:, used:] == 0).all())
+
+
+@pytest.mark.parametrize("V", [1, 2, 300])
+def test_a_target_that_all_others_are_far_below(dev, V):
+    """Logits so far apart that the others' exponentials are below fp32: loss and gradient are zero, not NaN; an infinite
+    logit gives NaN."""
+    n = 8
+    H = torch.zeros((3, n), device=dev)
+    H[:, 0] = torch.tensor([200.0, 3e38, float("inf")], device=dev)
+    W = torch.zeros((V, n), device=dev)
+    W[0, 0] = 1.0
+    W[1:, 1] = 1.0
+    for dt in (torch.float32, torch.bfloat16):
+        loss, lse, dH, _ = ff.xent_step(H.to(dt), W.to(dt), torch.zeros(3, dtype=torch.int64, device=dev))
+        torch.cuda.synchronize()
+        assert bool((loss[:2] == 0).all()) and bool((dH[:2] == 0).all()) and torch.equal(lse[:2], H[:2, 0].to(dt).float())
+        assert bool(torch.isnan(loss[2])) and bool(torch.isnan(lse[2]))
