@@ -213,16 +213,16 @@ __global__ void __launch_bounds__(256) rescale_kernel(E* P, int64_t ldp, int64_t
   }
 }
 
-// out = beta out + sum over the splits of part: N x M, M a multiple of four.  SH threads share the splits of four results;
+// out = beta out + sum over the splits of part: N x M, M a multiple of four, from group `first` of four results on.  SH threads share the splits of four results;
 // their sums are joined in a fixed order.  Few results of many splits are bound by the latency of one load after the
 // other: 8 tokens, 176 wide, 128 sums 33 us with one thread, 3.9 with 16.
 template <class E, int SH>
 __global__ void __launch_bounds__(256) sum_kernel(const float* part, int splits, int64_t N, int M, float beta,
-                                                  E* out, int64_t ldo) {
+                                                  E* out, int64_t ldo, int64_t first) {
   constexpr int kWide = 256 / SH;
   __shared__ f32x4 sh[SH][kWide];
   const int lane = threadIdx.x % kWide, share = threadIdx.x / kWide;
-  const int64_t per = M / 4, id = (int64_t)blockIdx.x * kWide + lane;
+  const int64_t per = M / 4, id = first + (int64_t)blockIdx.x * kWide + lane;
   const int64_t row = id / per;
   const int c = (int)(id - row * per) * 4;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -244,12 +244,12 @@ __global__ void __launch_bounds__(256) sum_kernel(const float* part, int splits,
 }
 
 // Rows of H with a target; zeros elsewhere, so that nothing a skipped token holds (NaN, infinities) reaches dW, where
-// its zero of P would be multiplied by it.
+// its zero of P would be multiplied by it.  From piece `first` on.
 template <class E>
 __global__ void __launch_bounds__(256) live_rows_kernel(const E* H, int64_t ldh, int64_t T, int n, const int64_t* target,
-                                                        int64_t vocab, int copies, E* out) {
+                                                        int64_t vocab, int copies, E* out, int64_t first) {
   constexpr int kN = Piece16<E>::kN;
-  const int64_t per = n / kN, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t per = n / kN, id = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= T * per) return;
   const int64_t t = id / per;
   const int c = (int)(id - t * per) * kN;
@@ -402,6 +402,8 @@ struct Tensors {
   hipStream_t s;
 };
 
+constexpr int64_t kLaunchItems = (int64_t)1 << 28;   // threads of one launch of sums or copies: it must have fewer than 2^32
+
 #define XENT_TRY(call)                   \
   do {                                   \
     const hipError_t e_ = (call);        \
@@ -458,20 +460,23 @@ void rescale(const Call& c, const Tensors& x, int64_t t0, int64_t N, int stat) {
 
 hipError_t run_sum(const Call& c, const Tensors& x, int splits, int64_t N, int64_t M, float beta, void* out, int64_t ldo) {
   const int64_t threads = N * (M / 4);
-  if (threads == 0) return hipSuccess;
   const float* part = reinterpret_cast<const float*>(x.ws + c.off_part);
   const int shares = splits >= 16 && threads <= 65536 ? 16 : 1;
-  const dim3 grid((unsigned)((threads * shares + 255) / 256)), block(256);
-  if (c.bf16) {
-    __bf16* o = static_cast<__bf16*>(out);
-    if (shares > 1) hipLaunchKernelGGL((sum_kernel<__bf16, 16>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo);
-    else hipLaunchKernelGGL((sum_kernel<__bf16, 1>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo);
-  } else {
-    float* o = static_cast<float*>(out);
-    if (shares > 1) hipLaunchKernelGGL((sum_kernel<float, 16>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo);
-    else hipLaunchKernelGGL((sum_kernel<float, 1>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo);
+  for (int64_t first = 0; first < threads; first += kLaunchItems) {
+    const int64_t items = threads - first < kLaunchItems ? threads - first : kLaunchItems;
+    const dim3 grid((unsigned)((items * shares + 255) / 256)), block(256);
+    if (c.bf16) {
+      __bf16* o = static_cast<__bf16*>(out);
+      if (shares > 1) hipLaunchKernelGGL((sum_kernel<__bf16, 16>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo, first);
+      else hipLaunchKernelGGL((sum_kernel<__bf16, 1>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo, first);
+    } else {
+      float* o = static_cast<float*>(out);
+      if (shares > 1) hipLaunchKernelGGL((sum_kernel<float, 16>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo, first);
+      else hipLaunchKernelGGL((sum_kernel<float, 1>), grid, block, 0, x.s, part, splits, N, (int)M, beta, o, ldo, first);
+    }
+    XENT_TRY(hipGetLastError());
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 // dH of tokens t0 .. from P of vocabulary entries v0 ..; first / last piece of the vocabulary
@@ -514,14 +519,18 @@ hipError_t run_dw(const Call& c, const Tensors& x, int64_t v0, int64_t M) {
 
 hipError_t run_live_rows(const Call& c, const Tensors& x) {
   const int64_t threads = c.T * (c.n * c.esz / 16);
-  const dim3 grid((unsigned)((threads + 255) / 256));
-  if (c.bf16)
-    hipLaunchKernelGGL(live_rows_kernel<__bf16>, grid, dim3(256), 0, x.s, reinterpret_cast<const __bf16*>(x.H), x.ldh,
-                       c.T, (int)c.n, x.target, c.V, c.terms, reinterpret_cast<__bf16*>(x.ws + c.off_live));
-  else
-    hipLaunchKernelGGL(live_rows_kernel<float>, grid, dim3(256), 0, x.s, reinterpret_cast<const float*>(x.H), x.ldh, c.T,
-                       (int)c.n, x.target, c.V, c.terms, reinterpret_cast<float*>(x.ws + c.off_live));
-  return hipGetLastError();
+  for (int64_t first = 0; first < threads; first += kLaunchItems) {
+    const int64_t items = threads - first < kLaunchItems ? threads - first : kLaunchItems;
+    const dim3 grid((unsigned)((items + 255) / 256));
+    if (c.bf16)
+      hipLaunchKernelGGL(live_rows_kernel<__bf16>, grid, dim3(256), 0, x.s, reinterpret_cast<const __bf16*>(x.H), x.ldh,
+                         c.T, (int)c.n, x.target, c.V, c.terms, reinterpret_cast<__bf16*>(x.ws + c.off_live), first);
+    else
+      hipLaunchKernelGGL(live_rows_kernel<float>, grid, dim3(256), 0, x.s, reinterpret_cast<const float*>(x.H), x.ldh, c.T,
+                         (int)c.n, x.target, c.V, c.terms, reinterpret_cast<float*>(x.ws + c.off_live), first);
+    XENT_TRY(hipGetLastError());
+  }
+  return hipSuccess;
 }
 
 hipError_t run_fwd(const Call& c, const Tensors& x) {

@@ -433,3 +433,54 @@ def test_a_target_that_all_others_are_far_below(dev, V):
         torch.cuda.synchronize()
         assert bool((loss[:2] == 0).all()) and bool((dH[:2] == 0).all()) and torch.equal(lse[:2], H[:2, 0].to(dt).float())
         assert bool(torch.isnan(loss[2])) and bool(torch.isnan(lse[2]))
+
+
+def _room(dev, gib):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info(dev)[0] < gib * 2 ** 30:
+        pytest.skip(f"needs {gib} GiB of free memory")
+
+
+def test_no_tokens_of_a_head_of_more_pieces_than_a_launch_has_threads(dev):
+    """2^22 entries, 4096 wide: scaling dW takes a thread for four elements, 2^32 of them, more than one launch can have."""
+    _room(dev, 40)
+    V, n = 1 << 22, 4096
+    dW = torch.full((V, n), 2.0, dtype=torch.bfloat16, device=dev)
+    W, H = dW[:V], torch.empty((0, n), dtype=torch.bfloat16, device=dev)
+    ff.xent_step(H, W, torch.empty((0,), dtype=torch.int64, device=dev), dW=dW, beta_dw=0.5, want_dh=False, want_dw=True)
+    torch.cuda.synchronize()
+    for v in range(0, V, 1 << 18):
+        assert bool((dW[v:v + (1 << 18)] == 1).all()), v
+
+
+def test_copy_of_more_pieces_than_a_launch_has_threads(dev):
+    """2^23 tokens, 4096 wide: dW's copy of H takes a thread for eight elements, 2^32 of them.  Tokens repeat with a period
+    of 1000, every tenth without a target and of NaN; the workspace is full of NaN, so that a row which is not copied shows.
+    Bounds as at the head of this file, dW's with T terms; the last period is not whole, 608 of 8,388,608 tokens."""
+    _room(dev, 170)
+    T, n, V = 1 << 23, 4096, 2
+    g = inputs.rng(3)
+    H0 = torch_act(inputs.gaussian(g, (1000, n), dtype="bf16"), "bf16", dev)
+    t0 = torch.from_numpy(g.integers(0, V, 1000)).to(dev)
+    t0[::10] = -1
+    H0[::10] = float("nan")
+    H = torch.empty((T, n), dtype=torch.bfloat16, device=dev)
+    whole = T // 1000 * 1000
+    H[:whole].view(-1, 1000, n).copy_(H0.expand(T // 1000, 1000, n))
+    H[whole:] = H0[:T - whole]
+    target = t0.repeat(T // 1000 + 1)[:T]
+    W = torch_act(inputs.gaussian(g, (V, n), std=2 / np.sqrt(n), dtype="bf16"), "bf16", dev)
+    ws = ff.xent_workspace(T, n, V, torch.bfloat16, want_dw=True, device=dev)
+    ws.fill_(255)
+    loss, _, _, dW = ff.xent_step(H, W, target, scale=1.0 / T, want_dh=False, want_dw=True, workspace=ws)
+    torch.cuda.synchronize()
+    ref = TO.xent(np.nan_to_num(to_np(H0)), to_np(W), t0.cpu().numpy(), None, 1.0 / 1000)
+    assert bool(torch.isfinite(dW).all())
+    Ez = (n / 16 + 48) * 2 * V32 * ref[4][0].max()
+    tol = (2 * Ez + 3 * U["bf16"] + (32 + 64 * 90) * V32) + (T / 16 + 48) * 2 * V32 + U["bf16"] + 2 * 608 / T
+    assert np.all(np.abs(to_np(dW) - ref[3]) <= tol * ref[4][2])
+    live = (t0 >= 0).cpu().numpy()
+    El = 2 * Ez + 16 * V32 * (1 + np.abs(ref[1]) + ref[4][0]) + 65 * V32
+    for at in (0, whole // 2000 * 1000, whole - 1000):
+        got = to_np(loss[at:at + 1000])
+        assert np.all(np.abs(got - ref[0])[live] <= El[live]) and np.all(got[~live] == 0)
