@@ -420,6 +420,7 @@ ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t
  *                replayed draws another mask when the program changes that value.
  *   R          : device, T x n of type act, added after scaling, or NULL.
  *   X, Y, R    : element alignment, any leading dimension >= n; Y may be X or R.
+ * T is at most 2^40, n at most 2^28, T ceil(n / 8) at most 2^44.
  * The mask: block b = t ceil(n / 8) + i / 8 of eight elements of row t takes the four 32-bit words of Philox 4x32-10 with
  * counter (b, offset), low words first, and key seed; element i takes the 16 bits number i mod 8 of them, the low half
  * of a word first, and is dropped where they are below D.

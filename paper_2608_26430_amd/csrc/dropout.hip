@@ -165,6 +165,9 @@ extern "C" ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, in
   if (act != FF_F32 && act != FF_BF16) return ff::fail(FF_EINVAL, "unknown activation dtype %d", act);
   if (T < 0 || T > ((int64_t)1 << 40) || n < 1 || n > ((int64_t)1 << 28))
     return ff::fail(FF_EINVAL, "T=%lld or n=%lld out of range", (long long)T, (long long)n);
+  // no card holds so many; the blocks' numbers and places stay within 64 bits
+  const int64_t nb = (n + 7) / 8;
+  if (T > ((int64_t)1 << 44) / nb) return ff::fail(FF_EINVAL, "T=%lld rows of n=%lld: too many", (long long)T, (long long)n);
   if (!(p >= 0.0 && p <= 1.0)) return ff::fail(FF_EINVAL, "p=%g outside [0, 1]", p);
   if (T == 0) return FF_OK;
   const int esz = act == FF_BF16 ? 2 : 4;
@@ -174,9 +177,8 @@ extern "C" ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, in
   if (R && (st = ff::check_rows("R", R, ldr, n, esz)) != FF_OK) return st;
   if ((uintptr_t)offset_dev % 8) return ff::fail(FF_EINVAL, "offset_dev is not 8-byte aligned");
   const unsigned drop = p < 1.0 ? (unsigned)std::fmin(std::nearbyint(p * 65536.0), 65535.0) : 65536u;
-  ff::DropArgs a{X, R, Y, ldx, R ? ldr : 0, ldy, T, 0, (int)n, (int)((n + 7) / 8), (int64_t)seed, offset, offset_dev, drop,
+  ff::DropArgs a{X, R, Y, ldx, R ? ldr : 0, ldy, T, T * nb, (int)n, (int)nb, (int64_t)seed, offset, offset_dev, drop,
                  drop < 65536u ? 65536.f / (float)(65536u - drop) : 0.f};
-  a.blocks = T * a.nb;
   if (act == FF_BF16) ff::launch<__bf16>(a, (hipStream_t)stream);
   else ff::launch<float>(a, (hipStream_t)stream);
   const hipError_t e = hipGetLastError();
