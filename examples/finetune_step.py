@@ -58,8 +58,10 @@ class Layer:
         x2 = ff.dropout(y, p, seed, 2 * draw + 1, residual=x, Y=y)
         h2, m2, r2 = ff.layernorm_fwd(x2, q["norm2.weight"], q["norm2.bias"])
         counted = ((target >= 0) & (target < self.head.shape[0])).sum().clamp(min=1)
-        share = (1.0 / counted.float()).expand(x.shape[0]).contiguous()
-        loss, _, dh2, _ = ff.xent_step(h2, self.head, target, dloss=share, workspace=self.ws_loss)
+        share = 1.0 / counted.float()
+        # Gradients of the tokens' sum: the mean's factor is known on the device only, and goes onto the fp32 results below.
+        # As a weight of every token (dloss) it would be rounded to bf16 with the softmax, alike for all of them.
+        loss, _, dh2, _ = ff.xent_step(h2, self.head, target, workspace=self.ws_loss)
 
         grads = {}
         dx2, grads["norm2.weight"], grads["norm2.bias"] = ff.layernorm_bwd(
@@ -71,7 +73,9 @@ class Layer:
         # (an earlier layer would also take dx = dx2 + the norm's dX, with beta_dx = 1)
         _, grads["norm1.weight"], grads["norm1.bias"] = ff.layernorm_bwd(
             x, dh1, q["norm1.weight"], m1, r1, want_dx=False, workspace=self.ws_norm)
-        return (loss * share).sum(), grads
+        for g in grads.values():
+            g.mul_(share)
+        return loss.sum() * share, grads
 
     def step(self, x, target, lr):
         loss, grads = self.gradients(x, target, self.steps)

@@ -112,3 +112,23 @@ def test_gradients_are_the_differences(example):
         got, want = float((grads[k] * d).sum()), (up - down) / (2 * h)
         # fp32 losses near 5: 2^-24 x 5 x about 30 operations over 2 h = 1e-4; third derivatives times h^2 / 6: 4e-4 of their size
         assert abs(got - want) <= 1e-4 + 5e-3 * abs(want) + 4e-4, (k, got, want)
+
+
+def test_the_mean_over_tokens_is_not_rounded_alike(example):
+    """Gradient at most targets is nearly minus one.  Over 510 counted tokens the mean's share of it lies just under the
+    middle between two bf16 numbers (512 / 510 x 0.9995 = 1.0034 between 1 and 1.0078), so that rounding it would make all
+    gradients 0.3% too small as a whole.  Rounded near one it is off by at most 2^-9 (0.9995 -> 1); what the other roundings
+    leave is independent between elements and nearly cancels in this projection."""
+    width, vocab, T, nnz, rho = 256, 1000, 512, 900, 16
+    layer = example.Layer(width, vocab, T, nnz, rho=rho, p=0.1, seed=5)
+    layer.support = inputs.support(inputs.rng(5), width, width, nnz)
+    g = inputs.rng(8)
+    x = torch.from_numpy(inputs.gaussian(g, (T, width), dtype="bf16")).to("cuda", torch.bfloat16)
+    target = torch.from_numpy(g.integers(0, vocab, T)).cuda()
+    target[:2] = -100
+    _, grads = layer.gradients(x, target, draw=0)
+    torch.cuda.synchronize()
+    _, ref = _float64(layer, x, target, 0, width, rho)
+    for k in ("norm2.weight", "norm2.bias"):
+        share = float(np.sum((to_np(grads[k]) - ref[k]) * ref[k]) / np.sum(ref[k] ** 2))
+        assert abs(share) <= 1.05 * 2.0 ** -9, (k, share)
