@@ -144,3 +144,39 @@ def test_refusals(dev):
         with pytest.raises(ff.FrameFTError):
             ff.dropout(X, p, 1)
     assert ff.dropout(X[:0], 0.1, 1).shape == (0, 64)
+
+
+@pytest.mark.parametrize("T,n,dtype,residual", [(2100, 28675, "bf16", True), (2100, 28675, "f32", False), (1 << 20, 17, "f32", True),
+                                                (1 << 20, 17, "bf16", False), (70_000, 500, "bf16", True)])
+def test_more_blocks_than_threads(dev, T, n, dtype, residual):
+    """More than 2^21 blocks of eight: a thread takes several, carrying row and column along.  Rows from the start, around
+    every seam between two turns, some in between and the end, against the reference."""
+    nb = -(-n // 8)
+    assert T * nb > 1 << 21
+    g = inputs.rng(T + n)
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(n)
+    X = (torch.rand((T, n), generator=gen, device=dev) + 0.5).to(tdt)
+    R = torch.randn((T, n), generator=gen, device=dev).to(tdt) if residual else None
+    Y = ff.dropout(X, 0.3, SEED, 5, residual=R)
+    torch.cuda.synchronize()
+    seams = [k * (1 << 21) // nb for k in range(1, T * nb // (1 << 21) + 1)]
+    rows = np.unique(np.clip(np.r_[0:3, [s + d for s in seams for d in (-1, 0, 1)], g.integers(0, T, 30), T - 3:T], 0, T - 1))
+    block = rows[:, None].astype(np.uint64) * np.uint64(nb) + np.arange(nb, dtype=np.uint64)
+    counter = np.zeros(block.shape + (4,), dtype=np.uint64)
+    counter[..., 0], counter[..., 1], counter[..., 2] = block & np.uint64(0xFFFFFFFF), block >> np.uint64(32), 5
+    words = TO.philox4x32(counter, (SEED & 0xFFFFFFFF, SEED >> 32)).astype(np.int64)
+    draws = np.stack([words & 0xFFFF, words >> 16], axis=-1).reshape(len(rows), nb * 8)[:, :n]
+    drop = TO.dropout_draws(0.3)
+    at = torch.from_numpy(rows).to(dev)
+    scaled = np.where(draws >= drop, to_np(X[at]) * (65536 / (65536 - drop)), 0.0)
+    want = scaled + (to_np(R[at]) if residual else 0.0)
+    bound = U[dtype] * np.abs(want) + 4 * V32 * (scaled + (np.abs(to_np(R[at])) if residual else 0.0))
+    got = to_np(Y[at])
+    assert np.all(np.abs(got - want) <= bound)
+    if not residual:
+        np.testing.assert_array_equal(got != 0, draws >= drop)
+        # the whole result: the share that is kept, within six standard deviations
+        kept = float((Y != 0).double().mean())
+        assert abs(kept - (1 - drop / 65536)) <= 6 * (0.21 / (T * n)) ** 0.5

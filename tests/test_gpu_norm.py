@@ -245,3 +245,45 @@ def test_more_rows_than_one_launch_has_workgroups_for(dev, dtype):
     terms = (T / 256 + 1024) * V32
     _close(to_np(dw), (g * h).sum(axis=0), terms * np.abs(g * h).sum(axis=0) + (np.abs(g) * eh).sum(axis=0), "dweight")
     _close(to_np(db), g.astype(np.float64).sum(axis=0), terms * np.abs(g).astype(np.float64).sum(axis=0), "dbias")
+
+
+# more rows than the kernels have places for at once, three times over and a few: rows of one wave (4096 places forward, 2048
+# backward) and of eight (1024; 512, above 4096 wide 256), whole pieces and a last one that overlaps
+@pytest.mark.parametrize("T,n", [(12609, 768), (12609, 1021), (12300, 2047), (3100, 2056), (3100, 8192), (3100, 5473)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_workgroups_walk_over_rows(dev, T, n, dtype):
+    """Every row of a long call has the bits that it has in a short one, whose workgroups take one row each; in place, added to
+    an old gradient; dw and db, kept over the rows of a workgroup, against the reference: at most T / 256 rows a thread, 4 waves,
+    then 16 partial rows a thread and 32 of those, below (T / 256 + 128) v of the absolute sums and what h is off."""
+    x, g, w, b = _case(T, n, dtype, T + n)
+    X, G = torch_act(x, dtype, dev), torch_act(g, dtype, dev)
+    wt, bt = torch.from_numpy(w).to(dev), torch.from_numpy(b).to(dev)
+    old = torch_act(inputs.gaussian(inputs.rng(n), (T, n), dtype=dtype), dtype, dev)
+    Y, m, r = ff.layernorm_fwd(X, wt, bt)
+    inplace = X.clone()
+    _, m2, r2 = ff.layernorm_fwd(inplace, wt, bt, Y=inplace)
+    dX, dw, db = ff.layernorm_bwd(X, G, wt, m, r)
+    onto = old.clone()
+    dw2, db2 = dw.clone(), db.clone()
+    ff.layernorm_bwd(X, G, wt, m, r, dX=onto, dweight=dw2, dbias=db2, beta_dx=0.5, accumulate=True)
+    torch.cuda.synchronize()
+    assert torch.equal(inplace, Y) and torch.equal(m2, m) and torch.equal(r2, r)
+    assert torch.equal(dw2, 2 * dw) and torch.equal(db2, 2 * db)
+    for t in range(0, T, 250):
+        s = slice(t, min(T, t + 250))
+        y, ms, rs = ff.layernorm_fwd(X[s], wt, bt)
+        dx = ff.layernorm_bwd(X[s], G[s], wt, ms, rs, want_dw=False)[0]
+        dx2 = ff.layernorm_bwd(X[s], G[s], wt, ms, rs, dX=old[s].clone(), beta_dx=0.5, want_dw=False)[0]
+        for short, long in ((y, Y), (ms, m), (rs, r), (dx, dX), (dx2, onto)):
+            assert torch.equal(short, long[s]), t
+    y, mean, rstd = TO.layernorm_fwd(x, w, b)
+    h = (x.astype(np.float64) - mean[:, None]) * rstd[:, None]
+    eh = 2 * 64 * V32 * (np.abs(h) + rstd[:, None] * (np.abs(x) + np.abs(x).mean(axis=1, keepdims=True)))
+    terms = (T / 256 + 128) * V32
+    _close(to_np(dw), (g * h).sum(axis=0), terms * np.abs(g * h).sum(axis=0) + (np.abs(g) * eh).sum(axis=0), "dweight")
+    _close(to_np(db), g.astype(np.float64).sum(axis=0), terms * np.abs(g).astype(np.float64).sum(axis=0), "dbias")
+    rows = np.r_[0:40, T // 2:T // 2 + 40, T - 40:T]
+    y, ey, dx, edx, _, _, mean, em, rstd, er = _bounds(x[rows], g[rows], w, b, U[dtype])
+    at = torch.from_numpy(rows).to(dev)
+    for got, want, bound, what in ((Y, y, ey, "y"), (m, mean, em, "mean"), (r, rstd, er, "rstd"), (dX, dx, edx, "dx")):
+        _close(to_np(got[at]), want, bound, what)
