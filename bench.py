@@ -31,7 +31,7 @@ CSRC = os.path.join(ROOT, "paper_2608_26430_amd", "csrc")
 
 
 # sources of the operators beside the adapter (layer norm, dropout, loss), which no workload here runs
-OTHER_SOURCES = ("norm.hip", "dropout.hip", "xent.hip", "xent_gemm.h", "xent_inst.hip", "xent_span.h")
+OTHER_SOURCES = ("norm.hip", "dropout.hip", "xent.hip", "xent_gemm.h", "xent_inst.hip", "xent_plan.h", "xent_span.h")
 
 
 def kernel_hash() -> str:

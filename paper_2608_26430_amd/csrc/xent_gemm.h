@@ -27,6 +27,7 @@
 #pragma once
 
 #include "ff_internal.h"
+#include "xent_plan.h"
 #include "xent_span.h"
 
 namespace ff {
@@ -608,16 +609,6 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gemm_kernel(GemmArgs a) {
   // no direct load may be in flight when the workgroup's LDS is given to another one
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
-
-// Tile sizes of the instances: large (256 x 256, wave 128 x 64; bf16 only), medium (128 x 128, wave 64 x 64), small (128 x
-// 32, wave 32 x 32), and tiny (32 x 32, wave 16 x 16) for the logits of a few classes.
-enum Tile { kLarge = 0, kMedium = 1, kSmall = 2, kTiny = 3 };
-constexpr int tile_m(int t) { return t == kLarge ? 256 : (t == kTiny ? 32 : 128); }
-constexpr int tile_n(int t) { return t == kLarge ? 256 : (t == kMedium ? 128 : 32); }
-// columns of one entry of the logits' statistics
-constexpr int stat_cols(int t) { return t == kLarge ? 128 : (t == kMedium ? 64 : (t == kSmall ? 32 : 16)); }
-
-constexpr int kCUs = 256;
 
 // layout 0: logits, 1: dH, 2: dW
 hipError_t launch_gemm(int layout, int bf16, int tile, const GemmArgs& a, hipStream_t s);
