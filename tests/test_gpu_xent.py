@@ -52,7 +52,7 @@ def _garbage(T, n, V, dtype, dw, dev, dh=True):
     return ws.fill_(255)
 
 
-def _verify(ref, got, n, V, dtype, old=None, beta=0.0):
+def _verify(ref, got, n, V, dtype, old=None, beta=0.0, normwise=True):
     """got: dict of loss, lse, dH, dW (any may be missing)."""
     loss, lse, dH, dW, (zabs, dHa, dWa) = ref
     u, T = U[dtype], len(loss)
@@ -77,7 +77,7 @@ def _verify(ref, got, n, V, dtype, old=None, beta=0.0):
         total = want if old is None else want + beta * old[name]
         bound = bound + u * np.abs(total) + (0 if old is None else 4 * V32 * np.abs(old[name]))
         close(name, total, bound)
-        if np.linalg.norm(total) > 0 and V > 1 and dtype in TOL:
+        if normwise and np.linalg.norm(total) > 0 and V > 1 and dtype in TOL:
             assert rel(fl[name], total) <= TOL[dtype], (name, rel(fl[name], total))
 
 
@@ -484,3 +484,73 @@ def test_copy_of_more_pieces_than_a_launch_has_threads(dev):
     for at in (0, whole // 2000 * 1000, whole - 1000):
         got = to_np(loss[at:at + 1000])
         assert np.all(np.abs(got - ref[0])[live] <= El[live]) and np.all(got[~live] == 0)
+
+
+@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_logits_through_the_gradients(dev, T, dtype):
+    """Logits of +-2000 through the step and the backward.  No target is its token's largest logit (lse - z of the reference
+    would cancel to zero).  fp32 has the bounds per element alone: lse's rounding at 2000 is 6e-5 of P, past TOL."""
+    n, V = 16, 400
+    g = inputs.rng(13)
+    H, W = inputs.gaussian(g, (T, n), dtype=dtype), inputs.gaussian(g, (V, n), std=150.0, dtype=dtype)
+    target = g.integers(0, V, T).astype(np.int64)
+    top = (H.astype(np.float64) @ W.astype(np.float64).T).argmax(axis=1)
+    target = np.where(target == top, (target + 1) % V, target)
+    ref = TO.xent(H, W, target)
+    Ht, Wt, tt, _ = _dev(dev, dtype, H, W, target, np.ones(T, dtype=np.float32))
+    loss, lse, dH, dW = ff.xent_step(Ht, Wt, tt, want_dw=True)
+    dH2, dW2 = ff.xent_bwd(Ht, Wt, tt, lse, loss=loss, want_dw=True)
+    torch.cuda.synchronize()
+    normwise = dtype == "bf16"
+    _verify(ref, dict(loss=loss, lse=lse, dH=dH, dW=dW), n, V, dtype, normwise=normwise)
+    _verify(ref, dict(dH=dH2, dW=dW2), n, V, dtype, normwise=normwise)
+
+
+OFF = np.r_[3, 128:256, 300:310, 384:512, 640]      # with all columns of some waves
+
+
+@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_entries_switched_off_by_the_lowest_value(dev, T, dtype):
+    """Entries whose logit is the type's lowest value or overflows to minus infinity take no probability and get no
+    gradient: as if they were not there."""
+    n, V = 24, 700
+    H, W, _, dloss = _case(T, n, V, dtype, 21)
+    H[:, 0] = np.where(np.arange(T) % 2, 0.5, 4.0)
+    W[OFF, 0] = inputs.bf16_round(np.full(1, -3.38e38, dtype=np.float32))[0]
+    keep = np.setdiff1d(np.arange(V), OFF)
+    at = inputs.rng(22).integers(0, len(keep), T)
+    ref = TO.xent(H, W[keep], at, dloss, 1.0)
+    Ht, Wt, tt, dt = _dev(dev, dtype, H, W, keep[at].astype(np.int64), dloss)
+    loss, lse, dH, dW = ff.xent_step(Ht, Wt, tt, dloss=dt, want_dw=True)
+    alone = ff.xent_fwd(Ht, Wt, tt)
+    dH2, dW2 = ff.xent_bwd(Ht, Wt, tt, lse, loss=loss, dloss=dt, want_dw=True)
+    torch.cuda.synchronize()
+    assert torch.equal(alone[0], loss) and torch.equal(alone[1], lse)
+    for a, b in ((dH, dW), (dH2, dW2)):
+        _verify(ref, dict(loss=loss, lse=lse, dH=a, dW=b[keep]), n, V, dtype)
+        assert bool((b[OFF] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_entries_of_minus_infinity_in_the_loss_alone(dev, dtype):
+    """Minus infinity in the head, under activations that are positive there, takes no probability; a token whose target it is
+    has an infinite loss.  (The gradients multiply the head by P: they need it finite.)"""
+    T, n, V = 150, 24, 700
+    H, W, _, _ = _case(T, n, V, dtype, 23)
+    H[:, 0] = np.abs(H[:, 0]) + 1
+    H = inputs.bf16_round(H) if dtype == "bf16" else H      # what the device holds
+    W[OFF, 0] = -np.inf
+    keep = np.setdiff1d(np.arange(V), OFF)
+    at = inputs.rng(24).integers(0, len(keep), T)
+    loss64, lse64, _, _, sums = TO.xent(H, W[keep], at)
+    target = keep[at].astype(np.int64)
+    target[5] = OFF[7]
+    Ht, Wt, tt, _ = _dev(dev, dtype, H, W, target, np.ones(T, dtype=np.float32))
+    loss, lse = ff.xent_fwd(Ht, Wt, tt)
+    torch.cuda.synchronize()
+    assert float(loss[5]) == np.inf
+    others = np.setdiff1d(np.arange(T), 5)
+    El = 2 * (n / 16 + 48) * 2 * V32 * sums[0] + 16 * V32 * (1 + np.abs(lse64) + sums[0]) + (V / 64 + 64) * V32
+    assert np.all(np.abs(to_np(lse) - lse64) <= 1.05 * El) and np.all((np.abs(to_np(loss) - loss64) <= 1.05 * El)[others])
