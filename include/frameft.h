@@ -378,10 +378,11 @@ double ff_lr_linear_warmup(int64_t step, int64_t warmup, int64_t total, double b
 /*
  * Operators around the adapter in a training step: layer norm, dropout and the loss of the head.  They need no
  * frame and no plan.  Activations are T rows of n elements of type `act` as above, row t at X + t ldx.  The calls are
- * asynchronous on `stream`, allocate nothing, synchronise nothing, may be captured into a graph, and write nothing
- * when they return an error (FF_EINVAL, or FF_EDEVICE on a failed launch).  Equal inputs give equal bits.  A
- * workspace belongs to the call until it has run: calls that overlap in time need one each.  Outputs must not
- * overlap inputs or the workspace except where it is said.
+ * asynchronous on `stream`, allocate nothing, synchronise nothing and may be captured into a graph.  A call that returns
+ * FF_EINVAL has written nothing; after FF_EDEVICE (a launch failed) the layer norm's backward and the loss, which
+ * launch several kernels, may have written some of their outputs.  Equal inputs give equal bits.  A workspace belongs to
+ * the call until it has run: calls that overlap in time need one each.  Outputs must not overlap inputs or the
+ * workspace except where it is said.
  */
 
 /*
@@ -437,14 +438,17 @@ ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, 
  * still that of its logits.
  *   H, dH  : device, T x n of type act, W, dW : device, V x n of type act; n a multiple of 8 (bf16) or 4 (fp32), 16-byte
  *            aligned, leading dimensions multiples of 8 (4), at most 1048576.  beta = 0 does not read the output.
+ *            The gradients multiply W by P and need it finite: an entry is switched off by a logit of the type's lowest
+ *            value; minus infinity works for the loss alone.
  *   target : device, T int64.   loss, lse : device, T fp32.
  *   dloss  : device, T fp32, gradient of the result with respect to each token's loss; NULL for ones.
  *            `scale` multiplies the gradients (1 / counted tokens for a mean): P's rounding to bf16 is smallest where
- *            the weight of all tokens is in scale and dloss is NULL.
+ *            the weight of all tokens is in scale, or in a factor on the results, and dloss is NULL.
  *   workspace : device, 256-byte aligned, at least ff_xent_workspace bytes for the same T, n, V, act and the outputs wanted
  *            (FF_XENT_DH, FF_XENT_DW or both; 0: loss alone).  It holds P, in type act, for a piece of the tokens or of
- *            the vocabulary (at most 256 MiB, or 256 tokens of it where V is larger), fp32 partial sums of dH, and with dW
- *            a copy of H (two up to 128 tokens in bf16).
+ *            the vocabulary (at most 256 MiB, or 256 tokens where a longer piece of them is larger; with dW, 256 entries
+ *            of all tokens where that is larger), fp32 partial sums of dH, and with dW a copy of H (two up to 128 tokens
+ *            in bf16).
  * ff_xent_fwd  : loss and lse.
  * ff_xent_step : loss, lse and the gradients in one call, which computes the logits once (twice with dW where P does not
  *                fit one piece).

@@ -841,7 +841,8 @@ def xent_bwd(H, W, target, lse, dloss=None, scale: float = 1.0, dH=None, dW=None
 def xent_step(H, W, target, dloss=None, scale: float = 1.0, loss=None, lse=None, dH=None, dW=None, beta_dh: float = 0.0,
               beta_dw: float = 0.0, want_dh: bool = True, want_dw: bool = False, workspace=None, stream=None):
     """xent_fwd and xent_bwd in one call, which computes the logits once: returns (loss, lse, dH, dW), dH and dW the
-    gradients of sum_t scale dloss[t] loss[t] (None where not wanted; ff_xent_step)."""
+    gradients of sum_t scale dloss[t] loss[t] (None where not wanted; ff_xent_step).  A weight that all tokens share belongs
+    in scale or on the results: in dloss it is rounded to bf16 with the softmax."""
     f32 = (_T or _torch()).float32
     T, n, V, act, hp, ldh, wp, ldw, tp, dev = _head(H, W, target)
     if _elsewhere(dev):

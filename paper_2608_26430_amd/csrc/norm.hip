@@ -5,11 +5,11 @@
 // Every sum is in fp32; the variance is that of the centred row, which stays in registers, so that a large mean costs
 // no digits.  A row belongs to WV waves (1 or 8) whose threads hold NV pieces of 16 bytes each;
 // rows wider than that are read three times.  Workgroups walk the rows with a stride, the vectors of their columns in
-// registers (fp32 weight and bias read for every row were twice a bf16 row's own bytes: 8192 x 8192 forward 67 -> 46
+// registers (fp32 weight and bias read for every row were twice a bf16 row's own bytes: 8192 x 8192 forward 67 -> 52
 // us), reading the next row under the arithmetic of one.  The backward's also keep dw and db of their columns and leave one
 // partial row each, added up in a fixed order by a second kernel: the same inputs give the same bits.  Bound by
-// memory: forward 2 T n, backward 3 T n elements; 8192 x 8192 in bf16 50 and 83 + 5 us, 5.3 and 4.8 TB/s, where a large
-// copy has 5.2; 12,608 x 768 11.7 and 14.7 + 3.8 us, of which a launch and the first row's latency are 4 each.
+// memory: forward 2 T n, backward 3 T n elements; 8192 x 8192 in bf16 52 and 84 + 5 us, 5.1 and 4.8 TB/s, where a large
+// copy has 5.2; 12,608 x 768 11.8 and 14.7 + 3.9 us, of which a launch and the first row's latency are 4 each.
 #include <cmath>
 
 #include "ff_internal.h"
@@ -434,8 +434,9 @@ __global__ void __launch_bounds__(1024) vector_sum_kernel(const float* part, int
 // ------------------------------------------------------------------------------------------- dispatch
 
 // The instance of a row of n: NV pieces of a thread and WV waves of a row.  A wave takes rows of up to four pieces a
-// lane (bf16: 2048 wide; 2048 wide and 8192 rows, forward / backward: 15 / 21 us against 21 / 24 with four waves), eight
-// waves up to four (8192 wide, two: 46 / 83 us against 49 / 85 with four waves of four and 51 / 84 with sixteen of one);
+// lane (bf16: 2048 wide; 2048 wide and 8192 rows, forward / backward: 14.6 / 20.8 us against 17.4 / 26.8 with four waves),
+// eight waves up to four (8192 wide, two: 50.6 / 87 us against 51.1 / 94 with four waves of four and 65 / 90 with sixteen of
+// one);
 // rows wider than that (bf16 16384, fp32 8192), or narrower than a piece, are read three times.  A backward with a last
 // piece that overlaps keeps to two pieces a lane of one wave: four spill (2047 wide and 8192 rows 47 us).
 struct Shape {
@@ -457,15 +458,15 @@ Shape shape_of(int64_t n, int esz, bool bwd) {
   return {0, 0, part};
 }
 
-// Workgroups of a forward: about two waves more than fill the card (12,608 rows of 768: 9.5 us with 1024 workgroups, 11.6
-// with 512, 10.3 with one per four rows; 8192 of 8192: 46, 48 and 48).
+// Workgroups of a forward: four of one-wave rows per CU (12,608 rows of 768: 11.8 us with 1024 workgroups, 13.1 with 512, 11.9
+// with one per four rows; 8192 of 8192: 52, 50 and, one row each, 67).
 int64_t fwd_groups(int64_t T, const Shape& s) {
   const int rows = s.wv == 1 ? 4 : 1;
   const int64_t g = (T + rows - 1) / rows;
   return g < 1024 ? g : 1024;
 }
-// And of a backward, each with a partial row of dw and db to write and add up (12,608 rows of 768: 13.4 us with 512, 17.5
-// with 256, 15.6 with 1024; 8192 of 8192: 83 with 256, 91 with 512).
+// And of a backward, each with a partial row of dw and db to write and add up (12,608 rows of 768: 14.8 us with 512, 18.6
+// with 256, 16.9 with 1024; 8192 of 8192: 83 with 256, 92 with 512, 107 with 128).
 constexpr int kGroups = 512;
 int groups_of(int64_t T, int64_t n, const Shape& s) {
   const int rows = s.wv == 1 ? 4 : 1;
