@@ -221,7 +221,7 @@ def prepare(case, seed):
                 if case["states"] == "8bit":
                     s.m_exp[i].copy_(st["mx"][i])
                     s.v_exp[i].copy_(st["vx"][i])
-            st["set"] = s
+            st["set"], st["grads"] = s, s.grads(st["g"])
             for k in ("m_all", "m", "mx", "v_all", "v", "vx"):
                 del st[k]
         return st
@@ -244,7 +244,7 @@ def _run_own(st):
     kind = case["kind"]
     if kind == "adamw":
         h, s = _HYPER, st["set"]
-        s.step(st["g"], h["lr"], h["step"], grad_scale=h["scale"])
+        s.step(st["grads"], h["lr"], h["step"], grad_scale=h["scale"])
         m, v = s.read()
         return [t for t in (st["c_all"], st["w_all"], m, v) if t is not None]
     if kind == "glu":
@@ -355,7 +355,7 @@ def _run_join(st):
 # States of 8 bits: blocks of 256 values share a unit 2^k; a code c stands for c units below 16 and (8 + c % 8) 2^(c / 8 - 1)
 # from there on.  m has a sign in bit 7 and 7 bits of code (up to 15 x 2^14 units), v 8 bits (up to 15 x 2^30).  k is the
 # least that holds the block's largest value, at least -120.  Values are rounded up where a random fraction (16 bits and a
-# half) carries theirs over the next code; a positive v has a code of 1 at least, a moment that is not finite the code 0.
+# half) carries theirs over the next code; a positive v has a code of 1 at least; where a moment is not finite, both have the code 0.
 # (The half: moments of short gradients and codes often lie on multiples of 2^-16 of a step, where the last bit of the
 # 64 would decide.)
 
@@ -436,7 +436,7 @@ def _run_adamw(st):
         if eight:
             words = torch.stack(_philox(torch.arange((n + 3) // 4, device="cuda"), h["step"], i, st["seed"]), dim=1).view(-1)[:n]
             for x, codes, exps, top, shift, values in ((m, "m", "mx", 14, 0, ms), (v, "v", "vx", 30, 16, vs)):
-                xb = _blocks(torch.where(x.abs().float().isfinite(), x, torch.zeros_like(x)))
+                xb = _blocks(torch.where(m32.isfinite() & v32.isfinite(), x, torch.zeros_like(x)))
                 k = _unit(xb, top)
                 code = _encode(xb, k, _blocks(((words >> shift & 0xFFFF).double() + 0.5) / 65536.0), top)
                 st[codes][i].copy_(code.view(-1)[:n])
@@ -558,12 +558,12 @@ def _powers(k):
     return torch.tensor([2.0 ** i for i in range(-250, 251)], dtype=torch.float64, device="cuda")[k.long() + 250]
 
 
-def _exact_state(x, draws, top):
+def _exact_state(x, finite, draws, top):
     """The values that a moment x (float64) has after its rounding to 8 bits; draws: 16 random bits for each."""
     n, grid = x.numel(), _values(top)
     rows = -(-n // 256)
     full = torch.zeros((rows * 256,), dtype=torch.float64, device="cuda")
-    full[:n] = torch.where(x.abs() <= torch.finfo(torch.float32).max, x, torch.zeros_like(x))
+    full[:n] = torch.where(finite, x, torch.zeros_like(x))
     full = full.view(rows, 256)
     # the least power of two for which the block's largest value, in fp32, is one of the codes' values or below
     big = full.abs().max(dim=1).values.float().double()
@@ -612,7 +612,8 @@ def _exact_adamw(case, seed):
                 q = [hi1 ^ q[1] ^ (key[0] + r * 0x9E3779B9) % 2 ** 32, lo1,
                      hi0 ^ q[3] ^ (key[1] + r * 0xBB67AE85) % 2 ** 32, lo0]
             word = torch.where(e % 4 < 2, torch.where(e % 2 == 0, q[0], q[1]), torch.where(e % 2 == 0, q[2], q[3]))
-            m, v = _exact_state(m, word % 65536, 14), _exact_state(v, word // 65536, 30)
+            finite = (m.abs() <= torch.finfo(torch.float32).max) & (v <= torch.finfo(torch.float32).max)
+            m, v = _exact_state(m, finite, word % 65536, 14), _exact_state(v, finite, word // 65536, 30)
         ms[i].copy_(m)
         vs[i].copy_(v)
     return [c_all] + ([c_all.clone()] if case["copies"] else []) + [m_all, v_all]
