@@ -370,6 +370,53 @@ ff_status ff_adamw_step(int64_t n, float* c, const float* g, float* m, float* v,
 ff_status ff_adamw_step_batched(int64_t count, int64_t n, float* const* c, const float* const* g,
                                 float* const* m, float* const* v, float lr, float beta1, float beta2,
                                 float eps, float weight_decay, int64_t step, void* stream);
+/*
+ * ff_adamw_set -- the same step for tensors of any lengths at once (adapters with supports of their own, norm vectors, whole
+ * weights), with gradients in fp32 or bf16, a decay for each tensor, and the moments in fp32 or in 8 bits.
+ *   ff_adamw_set_create : a set of `count` tensors (at most 2^20); every array is a HOST array of `count` entries, read in the call.
+ *     n            : lengths, 0 <= n[i] <= 2^40.
+ *     c            : device, fp32 parameters, n[i] each, 4-byte aligned.
+ *     copy         : device, bf16 copies of the parameters that a step writes (rounded to nearest), 2-byte aligned; the array or
+ *                    entries of it may be NULL.
+ *     m, v         : device, moments: n[i] fp32, 4-byte aligned (FF_STATES_F32), or n[i] bytes (FF_STATES_8BIT).
+ *     m_exp, v_exp : device, ceil(n[i] / 256) bytes each (FF_STATES_8BIT; else NULL).
+ *     All zeros are the states of a first step, of either kind.  The memory stays the caller's and must outlive the set.
+ *     weight_decay : host, per tensor, or NULL for zeros.
+ *     Allocates a table on the current device (88 bytes a tensor, 8 for 4096 elements); on error *out is NULL.
+ *   ff_adamw_set_step : one step of every tensor whose gradient is not NULL.
+ *     g : HOST array of `count` device pointers, gradients of type g_dtype, element aligned; read in the call, so that a captured
+ *         step keeps the addresses of its capture.
+ *     The hyperparameters are those of ff_adamw_step; gradients are multiplied by grad_scale.  lr_dev, grad_scale_dev (fp32)
+ *     and step_dev (int64) are NULL or one device value each, read when the call runs: factors of lr and grad_scale, and an
+ *     addend of step (the sum must be at least 1), for captured steps that are replayed.
+ *   ff_adamw_set_read : the values of 8-bit moments in bf16, which holds them exactly: m[i], v[i] (HOST arrays of device
+ *     pointers, NULL to skip one) receive n[i] values and zeros up to the next multiple of 256.
+ * 8-bit moments: each block of 256 elements of a tensor has a unit 2^(m_exp - 120); the code a (of v: the byte; of m: its low 7
+ * bits, bit 7 the sign) stands for a units below 16 and (8 + a mod 8) 2^(a div 8 - 1) from there on.  A step takes the block's
+ * exponent as small as its largest new moment (in fp32) allows, at least 0, and rounds each moment up or down at random, with
+ * probabilities in proportion, where a random fraction carries it over the next code: (h + 1/2) / 65536 with h the low (m) or high
+ * (v) half of word i mod 4 of Philox 4x32-10 with counter (i / 4 (64 bits), low 32 bits of step, number of the tensor) and key seed.
+ * A v > 0 has a code of at least 1; where a moment is not finite in fp32, both of the element become 0.  The parameters are stepped with the
+ * moments before their rounding; moments and their place between codes are computed in fp64.
+ * Calls on one set must be ordered.  Steps and reads are asynchronous on `stream` and allocate nothing; equal inputs give equal bits.
+ * Errors: FF_EINVAL, FF_ENOMEM, FF_EDEVICE; after FF_EDEVICE some tensors may have been stepped.
+ */
+enum { FF_STATES_F32 = 0, FF_STATES_8BIT = 1 };
+typedef struct ff_adamw_set ff_adamw_set;
+typedef struct ff_adamw_hyper {
+    double lr, beta1, beta2, eps, grad_scale;
+    int64_t step;
+    uint64_t seed;
+    const float* lr_dev;
+    const float* grad_scale_dev;
+    const int64_t* step_dev;
+} ff_adamw_hyper;
+ff_status ff_adamw_set_create(int64_t count, const int64_t* n, int states, int g_dtype, float* const* c, void* const* copy,
+                              void* const* m, void* const* v, uint8_t* const* m_exp, uint8_t* const* v_exp,
+                              const double* weight_decay, ff_adamw_set** out);
+void ff_adamw_set_destroy(ff_adamw_set* s);
+ff_status ff_adamw_set_step(const ff_adamw_set* s, const void* const* g, const ff_adamw_hyper* h, void* stream);
+ff_status ff_adamw_set_read(const ff_adamw_set* s, void* const* m, void* const* v, void* stream);
 /* Learning rate of optimizer step `step` (0 for the first) under the linear schedule
  * with warmup of Appendix G: base_lr * step / warmup during the warmup, then falling
  * linearly to 0 at step `total`.  Host function. */

@@ -75,6 +75,10 @@ def _load():
         "ff_adamw_step": (i32, [i64, vp, vp, vp, vp, f32, f32, f32, f32, f32, i64, vp]),
         "ff_adamw_step_batched": (i32, [i64, i64, vp, vp, vp, vp, f32, f32, f32, f32, f32, i64, vp]),
         "ff_lr_linear_warmup": (ctypes.c_double, [i64, i64, i64, ctypes.c_double]),
+        "ff_adamw_set_create": (i32, [i64, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(vp)]),
+        "ff_adamw_set_destroy": (None, [vp]),
+        "ff_adamw_set_step": (i32, [vp, vp, vp, vp]),
+        "ff_adamw_set_read": (i32, [vp, vp, vp, vp]),
         "ff_coef_to_plan": (i32, [vp, vp, vp, vp]),
         "ff_coef_to_user": (i32, [vp, vp, vp, i32, vp]),
         "ff_layernorm_fwd": (i32, [i64, i64, i32, vp, i64, i32, vp, vp, f32, vp, i64, vp, vp, vp]),
@@ -431,6 +435,144 @@ def adamw_step_batched(cs: Sequence, gs: Sequence, ms: Sequence, vs: Sequence, l
     _check(_load().ff_adamw_step_batched(len(cs), n, *[p.data_ptr() for p in ptrs], lr, beta1, beta2, eps,
                                          weight_decay, step, _stream(stream)))
     return cs
+
+
+class _AdamWHyper(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("lr_dev", ctypes.c_void_p), ("grad_scale_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p)]
+
+
+class _Grads:
+    """Gradients of an AdamWSet: the tensors, kept alive, and their addresses."""
+
+    def __init__(self, tensors, ptrs):
+        self.tensors, self.ptrs = tensors, ptrs
+
+
+class AdamWSet:
+    """AdamW over tensors of any lengths in one launch (ff_adamw_set_*).
+
+    params: contiguous fp32 device tensors, stepped in place.  weight_decay: one number or one for each tensor.  states: "f32"
+    or "8bit".  copies: None, or bf16 tensors (None for some) that every step writes the parameters to.  seed: of the random
+    rounding of 8-bit states.  The states are made here, zero: flat arrays (m_all, v_all) that hold tensor i from element
+    offsets[i], a multiple of 256, on; m, v (and m_exp, v_exp, exponents of the blocks of 8-bit states) are the tensors'
+    views of them, 1-D, to be saved and restored as they are."""
+
+    def __init__(self, params: Sequence, weight_decay=0.0, states: str = "f32", copies: Optional[Sequence] = None,
+                 grad_dtype=None, betas=(0.9, 0.999), eps: float = 1e-8, seed: int = 0):
+        self._h = ctypes.c_void_p()
+        torch = _torch()
+        params = list(params)
+        if not params:
+            raise ValueError("a set needs at least one tensor")
+        if states not in ("f32", "8bit"):
+            raise ValueError(f"unknown states {states!r}: 'f32' or '8bit'")
+        grad_dtype = torch.float32 if grad_dtype is None else grad_dtype
+        if grad_dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"unsupported gradient dtype {grad_dtype}")
+        self.device = params[0].device
+        for i, t in enumerate(params):
+            if t.dtype is not torch.float32 or t.device != self.device or not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"parameter {i} must be a contiguous fp32 tensor on one device with the others")
+        decay = [float(weight_decay)] * len(params) if isinstance(weight_decay, (int, float)) else [float(x) for x in weight_decay]
+        copies = None if copies is None else list(copies)
+        if len(decay) != len(params) or (copies is not None and len(copies) != len(params)):
+            raise ValueError("weight_decay and copies need one entry for each tensor")
+        for i, w in enumerate(copies or []):
+            if w is not None and (w.dtype is not torch.bfloat16 or w.numel() != params[i].numel() or w.device != self.device
+                                  or not w.is_contiguous()):
+                raise ValueError(f"copy {i} must be a contiguous bf16 tensor as long as its parameter, on {self.device}")
+        self.params, self.copies, self.states, self.grad_dtype = params, copies, states, grad_dtype
+        self.betas, self.eps, self.seed = (float(betas[0]), float(betas[1])), float(eps), int(seed)
+        self.lengths = [t.numel() for t in params]
+        self.offsets = [0]
+        for n in self.lengths:
+            self.offsets.append(self.offsets[-1] + (n + 255) // 256 * 256)
+        total, eight = self.offsets.pop(), states == "8bit"
+        dt = torch.uint8 if eight else torch.float32
+        self.m_all, self.v_all = (torch.zeros((total,), dtype=dt, device=self.device) for _ in range(2))
+        self.m, self.v = self.views(self.m_all), self.views(self.v_all)
+        self.m_exp = self.v_exp = None
+        if eight:
+            self.m_exp_all, self.v_exp_all = (torch.zeros((total // 256,), dtype=dt, device=self.device) for _ in range(2))
+            self.m_exp, self.v_exp = ([x[o // 256:o // 256 + (n + 255) // 256] for o, n in zip(self.offsets, self.lengths)]
+                                      for x in (self.m_exp_all, self.v_exp_all))
+        count = len(params)
+
+        def ptrs(ts):
+            return (ctypes.c_void_p * count)(*[None if t is None or t.numel() == 0 else t.data_ptr() for t in ts]) if ts else None
+
+        with torch.cuda.device(self.device):
+            _check(_load().ff_adamw_set_create(
+                count, (ctypes.c_int64 * count)(*self.lengths), int(eight), FF_BF16 if grad_dtype is torch.bfloat16 else FF_F32,
+                ptrs(params), ptrs(copies), ptrs(self.m), ptrs(self.v), ptrs(self.m_exp), ptrs(self.v_exp),
+                (ctypes.c_double * count)(*decay), ctypes.byref(self._h)))
+
+    def views(self, flat):
+        """The tensors' parts of an array laid out as m_all and v_all are."""
+        return [flat[o:o + n] for o, n in zip(self.offsets, self.lengths)]
+
+    def grads(self, tensors: Sequence) -> _Grads:
+        """Checked gradients for step(): contiguous tensors of grad_dtype, None for a tensor that is not to be stepped.  For
+        programs whose gradients stay in the same memory; step() takes a list as well."""
+        if len(tensors) != len(self.params):
+            raise ValueError(f"{len(tensors)} gradients for {len(self.params)} tensors")
+        out = []
+        for i, (g, n) in enumerate(zip(tensors, self.lengths)):
+            if g is None or n == 0:
+                out.append(None)
+                continue
+            if g.dtype is not self.grad_dtype or g.numel() != n or g.device != self.device or not g.is_contiguous():
+                raise ValueError(f"gradient {i} must be a contiguous {self.grad_dtype} tensor of {n} elements on {self.device}")
+            out.append(g.data_ptr())
+        return _Grads(list(tensors), (ctypes.c_void_p * len(out))(*out))
+
+    def step(self, grads, lr: float, step: int, grad_scale: float = 1.0, lr_dev=None, grad_scale_dev=None, step_dev=None,
+             stream=None):
+        """Step number `step` (1 for the first) of every tensor that has a gradient (ff_adamw_set_step).  lr_dev, grad_scale_dev
+        (fp32) and step_dev (int64): device tensors of one element, read when the call runs: factors of lr and grad_scale, an
+        addend of step."""
+        torch = _T or _torch()
+        dev = self.device.index
+        if _elsewhere(dev):
+            with torch.cuda.device(dev):
+                return self.step(grads, lr, step, grad_scale, lr_dev, grad_scale_dev, step_dev, stream)
+        if not isinstance(grads, _Grads):
+            grads = self.grads(grads)
+
+        def one(t, name, dtype):
+            return None if t is None else _array(t.view(1), name, 1, dtype, dev)
+
+        h = _AdamWHyper(lr, self.betas[0], self.betas[1], self.eps, grad_scale, step, self.seed & (1 << 64) - 1,
+                        one(lr_dev, "lr_dev", torch.float32), one(grad_scale_dev, "grad_scale_dev", torch.float32),
+                        one(step_dev, "step_dev", torch.int64))
+        _check((_lib or _load()).ff_adamw_set_step(self._h, grads.ptrs, ctypes.byref(h), _stream(stream)))
+
+    def read(self, stream=None):
+        """(m, v), laid out as m_all and v_all: the values of the moments, in bf16 for 8-bit states (ff_adamw_set_read), the states
+        themselves for fp32 ones."""
+        if self.states == "f32":
+            return self.m_all, self.v_all
+        torch = _T or _torch()
+        if _elsewhere(self.device.index):
+            with torch.cuda.device(self.device):
+                return self.read(stream)
+        m, v = (_new(self.m_all.shape, torch.bfloat16, self.device, stream) for _ in range(2))
+        pm, pv = ((ctypes.c_void_p * len(self.offsets))(*[t.data_ptr() + 2 * o for o in self.offsets]) for t in (m, v))
+        _check((_lib or _load()).ff_adamw_set_read(self._h, pm, pv, _stream(stream)))
+        return m, v
+
+    def close(self):
+        if self._h:
+            _load().ff_adamw_set_destroy(self._h)
+            self._h = ctypes.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def lr_linear_warmup(step: int, warmup: int, total: int, base_lr: float) -> float:

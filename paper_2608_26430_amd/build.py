@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libframeft.so")
 # each, compiled once per variant, so that their long compiles run in parallel
 SOURCES = [("capi.cpp", "capi.cpp.o", []), ("framegen.cpp", "framegen.cpp.o", []), ("plan.cpp", "plan.cpp.o", []),
            ("kernels.hip", "kernels.hip.o", []), ("kernels_w128.hip", "kernels_w128.hip.o", []),
-           ("optim.hip", "optim.hip.o", []), ("group.cpp", "group.cpp.o", []),
+           ("optim.hip", "optim.hip.o", []), ("optim_set.hip", "optim_set.hip.o", []), ("group.cpp", "group.cpp.o", []),
            ("lift.hip", "lift.hip.o", []), ("slab.hip", "slab.hip.o", []),
            ("slab_ms.hip", "slab_ms.hip.o", []), ("norm.hip", "norm.hip.o", []), ("dropout.hip", "dropout.hip.o", []),
            ("xent.hip", "xent.hip.o", [])] + [
