@@ -458,6 +458,50 @@ ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t
                            int64_t workspace_bytes, void* stream);
 
 /*
+ * ff_resnorm_* -- what stands between two blocks: the residual stream r takes a block's output b, through a norm after the block,
+ * a gate and the scales of both, and the next block's norm reads the result, in one pass:
+ *   p = post(b),   x = res_scale r + block_scale gate p,   y = norm(x)
+ *   post, norm : FF_NORM_NONE, FF_NORM_RMS (v / sqrt(mean v^2 + eps)) or FF_NORM_LAYER (as ff_layernorm_fwd), each times its
+ *                weight plus its bias (post_weight, post_bias; weight, bias: device, n elements of type w_dtype, NULL for ones /
+ *                zeros; those of a norm that is not there are not looked at).
+ *   gate       : device, `groups` rows of n elements of type gate_dtype, leading dimension ldgate (not looked at with one row);
+ *                row i holds for the rows i T / groups to (i + 1) T / groups - 1, groups divides T.  NULL: ones (groups is not
+ *                looked at).
+ * ff_resnorm_fwd : R, B -> X (x; may be R) and Y (y; NULL without a norm).  stats: device, 16-byte aligned, T x 4 fp32 for the
+ *   backward (mean and 1 / deviation of b, then of x; the mean of an RMS norm is 0, and both of a norm that is not there);
+ *   NULL where not wanted.  y is that of x before its rounding.  T = 0 is a no-op.
+ * ff_resnorm_bwd : from R and B as the forward read them (x is made again), the gradient dX of x from what else reads the stream
+ *   (NULL: zero) and dY of y (not looked at without a norm), with D = dX + the norm's gradient of x:
+ *     dR = res_scale D,   dB = gradient of p = block_scale gate D through post   (NULL to skip one; each may be any of R, B, dX,
+ *                         dY with its leading dimension, but not both the same)
+ *     dgate        = [dgate +] block_scale sum over a gate row's rows of D p     (fp32, groups x n, contiguous)
+ *     dpost_weight, dpost_bias, dweight, dbias = [... +] the norms' vectors' gradients   (fp32, n each)
+ *   Any of the five may be NULL; they are added to what is there when accumulate != 0.  With T = 0 they become zero (or stay).
+ *   workspace : device, 256-byte aligned, at least ff_resnorm_workspace bytes for the same T, n and groups (1 without a gate).
+ * X, Y, R, B, dX, dY, dR, dB: element alignment, any leading dimension >= n.  Sums and statistics are fp32.
+ */
+enum { FF_NORM_NONE = 0, FF_NORM_RMS = 1, FF_NORM_LAYER = 2 };
+typedef struct ff_resnorm {
+    int64_t T, n;
+    int act, w_dtype, gate_dtype;
+    int post, norm;
+    const void* post_weight;
+    const void* post_bias;
+    const void* weight;
+    const void* bias;
+    const void* gate;
+    int64_t ldgate, groups;
+    float res_scale, block_scale, post_eps, eps;
+} ff_resnorm;
+ff_status ff_resnorm_fwd(const ff_resnorm* d, const void* R, int64_t ldr, const void* B, int64_t ldb, void* X, int64_t ldx,
+                         void* Y, int64_t ldy, float* stats, void* stream);
+ff_status ff_resnorm_workspace(int64_t T, int64_t n, int64_t groups, int64_t* bytes);
+ff_status ff_resnorm_bwd(const ff_resnorm* d, const void* R, int64_t ldr, const void* B, int64_t ldb, const void* dX,
+                         int64_t lddx, const void* dY, int64_t lddy, const float* stats, void* dR, int64_t lddr, void* dB,
+                         int64_t lddb, int accumulate, float* dgate, float* dpost_weight, float* dpost_bias, float* dweight,
+                         float* dbias, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * ff_dropout -- y = [r +] m x / (1 - p') for each element, m in {0, 1} from a counter-based generator: a function of
  * (seed, offset, row, column, n) alone, so that the mask is never stored and the backward pass is this call on the
  * gradient with the same seed and offset (R then the gradient of another path, or NULL).

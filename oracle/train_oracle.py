@@ -118,3 +118,55 @@ def xent(H, W, target, dloss=None, scale=1.0, rows=64):
         dHa[s] = np.abs(P) @ Wa
         dWa += np.abs(P).T @ np.abs(live)
     return loss, lse, dH, dW, (zabs, dHa, dWa)
+
+
+# ------------------------------------------------------------------ join of two blocks
+
+def _norm(kind, v, eps):
+    """(normalised rows, mean, 1 / deviation); zeros where there is no norm."""
+    zero = np.zeros((v.shape[0], 1))
+    if kind == "none":
+        return v, zero, zero
+    mean = v.mean(axis=1, keepdims=True) if kind == "layer" else zero
+    rstd = 1.0 / np.sqrt(((v - mean) ** 2).mean(axis=1, keepdims=True) + eps)
+    return (v - mean) * rstd, mean, rstd
+
+
+def _norm_grad(kind, h, rstd, a):
+    d = a - h * (a * h).mean(axis=1, keepdims=True)
+    return rstd * (d - a.mean(axis=1, keepdims=True) if kind == "layer" else d)
+
+
+def resnorm(r, b, gate=None, post="none", pw=None, pb=None, norm="rms", w=None, bias=None, res=1.0, block=1.0, eps=1e-5,
+            dx=None, dy=None):
+    """The join x = res r + block gate post(b), y = norm(x) and, from dx and dy, its backward.  gate: None, n elements or rows of n
+    for equal shares of the rows.  Returns a dict with all values and, with dx or dy, all gradients."""
+    r, b = np.asarray(r, dtype=np.float64), np.asarray(b, dtype=np.float64)
+    T, n = r.shape
+    one, zero = np.ones(n), np.zeros(n)
+    pw, w = (one if v is None else np.asarray(v, dtype=np.float64) for v in (pw, w))
+    pb, bias = (zero if v is None else np.asarray(v, dtype=np.float64) for v in (pb, bias))
+    g = np.ones((1, n)) if gate is None else np.atleast_2d(np.asarray(gate, dtype=np.float64))
+    rows = T // g.shape[0]
+    G = np.repeat(g, rows, axis=0)
+    o = dict(G=G, pw=pw, w=w, pb=pb, bias=bias)
+    o["hp"], o["mp"], o["rp"] = _norm(post, b, eps)
+    o["p"] = o["hp"] * pw + pb if post != "none" else b
+    o["x"] = res * r + block * G * o["p"]
+    o["h"], o["m"], o["q"] = _norm(norm, o["x"], eps)
+    if norm != "none":
+        o["y"] = o["h"] * w + bias
+    if dx is None and dy is None:
+        return o
+    D = np.zeros((T, n)) if dx is None else np.asarray(dx, dtype=np.float64)
+    if norm != "none":
+        dy = np.asarray(dy, dtype=np.float64)
+        D = D + _norm_grad(norm, o["h"], o["q"], dy * w)
+        o["dw"], o["dbias"] = (dy * o["h"]).sum(axis=0), dy.sum(axis=0)
+    o["D"], o["dr"], o["e"] = D, res * D, block * G * D
+    o["dgate"] = (block * D * o["p"]).reshape(g.shape[0], rows, n).sum(axis=1)
+    o["db"] = o["e"]
+    if post != "none":
+        o["dpw"], o["dpb"] = (o["e"] * o["hp"]).sum(axis=0), o["e"].sum(axis=0)
+        o["db"] = _norm_grad(post, o["hp"], o["rp"], o["e"] * pw)
+    return o

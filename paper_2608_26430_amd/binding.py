@@ -85,6 +85,10 @@ def _load():
         "ff_layernorm_workspace": (i32, [i64, i64, pi64]),
         "ff_layernorm_bwd": (i32, [i64, i64, i32, vp, i64, vp, i64, i32, vp, vp, vp, f32, vp, i64, i32, vp, vp, vp, i64,
                                    vp]),
+        "ff_resnorm_fwd": (i32, [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
+        "ff_resnorm_workspace": (i32, [i64, i64, i64, pi64]),
+        "ff_resnorm_bwd": (i32, [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, i32, vp, vp, vp, vp, vp, vp, i64,
+                                 vp]),
         "ff_dropout": (i32, [i64, i64, i32, vp, i64, f64, u64, u64, vp, vp, i64, vp, i64, vp]),
         "ff_xent_workspace": (i32, [i64, i64, i64, i32, i32, pi64]),
         "ff_xent_fwd": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp]),
@@ -889,6 +893,150 @@ def layernorm_bwd(X, G, weight, mean, rstd, dX=None, dweight=None, dbias=None, b
         _norm_vector(weight, "weight", n, dev), _array(mean, "mean", T, f32, dev), _array(rstd, "rstd", T, f32, dev),
         beta_dx, dxp, lddx, int(accumulate), dwp, dbp, wsp, wsn, _stream(stream)))
     return (dX if want_dx else None), (dweight if want_dw else None), (dbias if want_dw else None)
+
+
+class _Resnorm(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("n", ctypes.c_int64), ("act", ctypes.c_int), ("w_dtype", ctypes.c_int),
+                ("gate_dtype", ctypes.c_int), ("post", ctypes.c_int), ("norm", ctypes.c_int), ("post_weight", ctypes.c_void_p),
+                ("post_bias", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("ldgate", ctypes.c_int64), ("groups", ctypes.c_int64),
+                ("res_scale", ctypes.c_float), ("block_scale", ctypes.c_float), ("post_eps", ctypes.c_float),
+                ("eps", ctypes.c_float)]
+
+
+_NORMS = {"none": 0, None: 0, "rms": 1, "layer": 2}
+
+
+def _resnorm(T, n, act, dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps, post_eps):
+    """The description of a join, and the number of its gate rows."""
+    torch = _T or _torch()
+    f32, bf16 = torch.float32, torch.bfloat16
+    if post not in _NORMS or norm not in _NORMS:
+        raise ValueError(f"unknown norms {post!r}, {norm!r}: 'none', 'rms' or 'layer'")
+    wt = None
+    for v, name, there in ((post_weight, "post_weight", _NORMS[post]), (post_bias, "post_bias", _NORMS[post]),
+                           (weight, "weight", _NORMS[norm]), (bias, "bias", _NORMS[norm])):
+        if v is None:
+            continue
+        if not there:
+            raise ValueError(f"{name} of a norm that is not there")
+        if v.dtype not in (f32, bf16) or (wt is not None and v.dtype is not wt):
+            raise ValueError("the norms' vectors must all be fp32 or all bf16")
+        wt = v.dtype
+    groups, gp, ldgate, gdt = 1, None, n, 0
+    if gate is not None:
+        if gate.dtype not in (f32, bf16):
+            raise ValueError("gate must be fp32 or bf16")
+        g2 = gate if gate.dim() == 2 else gate.view(1, -1)
+        groups = g2.shape[0]
+        if g2.shape[1] != n or g2.get_device() != dev or (n != 1 and g2.stride(1) != 1) or groups < 1 or T % groups:
+            raise ValueError(f"gate must have {n} elements, or rows of {n} whose number divides {T}, on device {dev}")
+        gp, ldgate, gdt = g2.data_ptr(), (n if groups < 2 else g2.stride(0)), int(gate.dtype is bf16)
+    return _Resnorm(T, n, act, int(wt is bf16), gdt, _NORMS[post], _NORMS[norm], _norm_vector(post_weight, "post_weight", n, dev),
+                    _norm_vector(post_bias, "post_bias", n, dev), _norm_vector(weight, "weight", n, dev),
+                    _norm_vector(bias, "bias", n, dev), gp, ldgate, groups, res_scale, block_scale,
+                    eps if post_eps is None else post_eps, eps), groups
+
+
+def resnorm_fwd(R, B, gate=None, post="none", post_weight=None, post_bias=None, norm="rms", weight=None, bias=None,
+                res_scale: float = 1.0, block_scale: float = 1.0, eps: float = 1e-5, post_eps: Optional[float] = None, X=None,
+                Y=None, stats=None, want_stats: bool = True, stream=None):
+    """The join of two blocks: x = res_scale R + block_scale gate post(B), y = norm(x); returns (X, Y, stats), Y None without a norm,
+    stats (T x 4, fp32) for resnorm_bwd (ff_resnorm_fwd).  post, norm: "none", "rms" or "layer", with vectors in fp32 or
+    bf16, all of one type.  gate: n elements, or rows of n, each for an equal share of the rows.  X may be R."""
+    torch = _T or _torch()
+    rp, ldr, T, n, dev = _input(R, "R")
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return resnorm_fwd(R, B, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps,
+                               post_eps, X, Y, stats, want_stats, stream)
+    bp, ldb = _rows(B, "B", R)
+    d, _ = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps,
+                    post_eps)
+    X, xp, ldx = _out_rows(X, "X", R, stream)
+    yp, ldy, sp = None, n, None
+    if d.norm:
+        Y, yp, ldy = _out_rows(Y, "Y", R, stream)
+    if stats is not None:
+        sp = _stats(stats, T, dev)
+    elif want_stats:
+        stats = _new((T, 4), torch.float32, R.device, stream)
+        sp = stats.data_ptr()
+    _check((_lib or _load()).ff_resnorm_fwd(ctypes.byref(d), rp, ldr, bp, ldb, xp, ldx, yp, ldy, sp, _stream(stream)))
+    return X, (Y if d.norm else None), stats
+
+
+def _stats(t, T, dev):
+    if t.dtype is not (_T or _torch()).float32 or t.shape != (T, 4) or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"stats must be a contiguous {T} x 4 fp32 tensor on device {dev}")
+    return t.data_ptr()
+
+
+def _resnorm_bytes(T, n, groups):
+    v = ctypes.c_int64()
+    _check((_lib or _load()).ff_resnorm_workspace(T, n, groups, ctypes.byref(v)))
+    return v.value
+
+
+def resnorm_workspace(T: int, n: int, groups: int = 1, device="cuda"):
+    """A workspace for resnorm_bwd calls of T rows of n with `groups` gate rows (1 without a gate), one such call at a time."""
+    return _torch().empty((_resnorm_bytes(T, n, groups),), dtype=_torch().uint8, device=device)
+
+
+def resnorm_bwd(R, B, dX, dY, stats, gate=None, post="none", post_weight=None, post_bias=None, norm="rms", weight=None,
+                bias=None, res_scale: float = 1.0, block_scale: float = 1.0, eps: float = 1e-5, post_eps: Optional[float] = None,
+                dR=None, dB=None, dgate=None, dpost_weight=None, dpost_bias=None, dweight=None, dbias=None,
+                accumulate: bool = False, want_dr: bool = True, want_db: bool = True, want_vectors: bool = True, workspace=None,
+                stream=None):
+    """Backward of resnorm_fwd from the gradients dX (None: zero) and dY (None without a norm): returns (dR, dB, dgate,
+    dpost_weight, dpost_bias, dweight, dbias), the last five fp32 and, with want_vectors, those of the gate and of the vectors that
+    were given (and of given outputs); None for the others (ff_resnorm_bwd).  accumulate: the five are added to the given ones.  dR and dB may
+    be any of the inputs."""
+    torch = _T or _torch()
+    f32 = torch.float32
+    rp, ldr, T, n, dev = _input(R, "R")
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return resnorm_bwd(R, B, dX, dY, stats, gate, post, post_weight, post_bias, norm, weight, bias, res_scale,
+                               block_scale, eps, post_eps, dR, dB, dgate, dpost_weight, dpost_bias, dweight, dbias, accumulate,
+                               want_dr, want_db, want_vectors, workspace, stream)
+    bp, ldb = _rows(B, "B", R)
+    d, groups = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale,
+                         eps, post_eps)
+    dxp, lddx = _rows(dX, "dX", R) if dX is not None else (None, n)
+    if d.norm and dY is None:
+        raise ValueError("a norm needs dY")
+    dyp, lddy = _rows(dY, "dY", R) if d.norm else (None, n)
+    drp = dbp = None
+    lddr = lddb = n
+    if want_dr:
+        dR, drp, lddr = _out_rows(dR, "dR", R, stream)
+    if want_db:
+        dB, dbp, lddb = _out_rows(dB, "dB", R, stream)
+    outs, ptrs = [], []
+    for given, out, name in ((post_weight, dpost_weight, "dpost_weight"), (post_bias, dpost_bias, "dpost_bias"),
+                             (weight, dweight, "dweight"), (bias, dbias, "dbias")):
+        p = None
+        if out is not None or (want_vectors and given is not None):
+            if accumulate and out is None:
+                raise ValueError(f"accumulate needs an existing {name}")
+            out, p = _out_array(out, name, n, R.device, stream)
+        outs.append(out)
+        ptrs.append(p)
+    gp = None
+    if dgate is not None or (want_vectors and gate is not None):
+        if gate is None or (accumulate and dgate is None):
+            raise ValueError("dgate needs a gate, and accumulate an existing dgate")
+        if dgate is None:
+            dgate = _new(gate.shape, f32, R.device, stream)
+        elif dgate.dtype is not f32 or dgate.shape != gate.shape or dgate.get_device() != dev or not dgate.is_contiguous():
+            raise ValueError("dgate must be a contiguous fp32 tensor of the gate's shape")
+        gp = dgate.data_ptr()
+    workspace = _workspace(workspace, _resnorm_bytes(T, n, groups) if workspace is None else 0, R.device, stream)
+    _check((_lib or _load()).ff_resnorm_bwd(
+        ctypes.byref(d), rp, ldr, bp, ldb, dxp, lddx, dyp, lddy, _stats(stats, T, dev), drp, lddr, dbp, lddb, int(accumulate), gp,
+        *ptrs, workspace.data_ptr(), workspace.nbytes, _stream(stream)))
+    return ((dR if want_dr else None), (dB if want_db else None), dgate, *outs)
 
 
 def dropout(X, p: float, seed: int, offset: int = 0, residual=None, Y=None, offset_dev=None, stream=None):

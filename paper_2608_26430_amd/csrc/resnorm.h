@@ -1,0 +1,385 @@
+// Join of two blocks, forward and backward (kernels; resnorm.hip has the calls, resnorm_inst.hip the backward's instances).
+//
+//   p = post(b) = wp hp + bp, hp = (b - mp) rp;   x = c r + s gate p;   y = w h + bias, h = (x - m) q
+// with the mean 0 for an RMS norm, and 1 / r, 1 / q the root of the centred row's mean square plus eps.  Backward, from dx
+// of the stream and dy of the norm's result:
+//   a = w dy;  D = dx + q (a - mean a - h mean(a h))      (the mean of a for a layer norm alone)
+//   dr = c D;  dgate = s sum D p;  e = s gate D;  dwp = sum e hp, dbp = sum e;  f = wp e
+//   db = rp (f - mean f - hp mean(f hp));  dw = sum dy h, dbias = sum dy
+// Both passes read every row once and keep it in registers; x is made again in the backward from r and b in fp32, as the
+// forward had it before its rounding, so that y's gradient is that of the y that was returned.  Sums and statistics are
+// fp32.  Bound by memory: forward 4 T n, backward 6 T n elements moved.
+//
+// A row belongs to WV waves (1, 4 or 8) whose threads hold 8 or 16 elements.  Workgroups walk the rows with a stride, the
+// vectors of their columns in registers, the next row read under the arithmetic of one.  The backward's walk a slice of the
+// rows of one gate row at a time and leave one partial row of each vector's gradient, added up in a fixed order by a second
+// launch: the same inputs give the same bits.
+#pragma once
+
+#include "rows.h"
+
+namespace ff {
+namespace resnorm {
+
+using norm::Pack;
+using norm::Row;
+using norm::row_sum;
+using norm::threads_of;
+using norm::vector_at;
+
+enum Kind { kNone = 0, kRms = 1, kLayer = 2 };
+
+struct Args {
+  const void* R;
+  const void* B;
+  const void* dX;        // backward; NULL: zero
+  const void* dY;        // backward, with a norm
+  void* X;               // forward: x, backward: dr (NULL: not wanted)
+  void* Y;               // forward: y, backward: db (NULL: not wanted)
+  int64_t ldr, ldb, lddx, lddy, ldx, ldy;
+  int64_t T;
+  int n;
+  int post, norm;        // Kind
+  const void* pw;        // NULL: ones
+  const void* pb;        // NULL: zeros
+  const void* w;
+  const void* b;
+  int w_bf16;
+  const void* gate;      // NULL: ones
+  int64_t ldgate;
+  int gate_bf16;
+  unsigned group_rows;   // rows of one gate row
+  unsigned groups;
+  float res, block, post_eps, eps;
+  float4* stats;         // [T] (mp, rp, m, q); forward: NULL if not wanted
+  // backward
+  unsigned slices;       // of all groups; of one: slices / groups
+  float* part;           // [workgroups][4][n]: dwp, dbp, dw, dbias of a workgroup's rows (NULL: not wanted)
+  float* gate_part;      // [slices][n] (NULL: not wanted)
+  float* gate_out;       // dgate itself, where a group is one slice
+  int gate_add;
+  float4* sums;          // rows too wide for the registers: [T] mean a, mean a h, mean f, mean f hp
+};
+
+template <int NV, int KN>
+__device__ __forceinline__ void fill(float (&v)[NV][KN], float x) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int k = 0; k < KN; ++k) v[i][k] = x;
+}
+
+// Vector p (absent: none) of a thread's columns; zero where it has no piece.
+template <class R, int NV, int KN>
+__device__ __forceinline__ void columns(const void* p, int bf16, float none, int l, int n, float (&v)[NV][KN]) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (R::skip(i, l, n) < KN) {
+      vector_at<KN>(p, bf16, none, R::at(i, l, n), v[i]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < KN; ++k) v[i][k] = 0.f;
+    }
+  }
+}
+
+__device__ __forceinline__ const void* gate_row(const Args& a, int64_t group) {
+  return a.gate ? static_cast<const char*>(a.gate) + group * a.ldgate * (a.gate_bf16 ? 2 : 4) : nullptr;
+}
+
+// (mean, 1 / deviation) of the values v, which become v - mean.
+template <class R, int WV, bool PART, int NV, int KN>
+__device__ __forceinline__ float2 centre(float (&v)[NV][KN], int kind, float eps, int l, int n, float2* sh0, float2* sh1) {
+  float mean = 0.f;
+  if (kind == kLayer) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int skip = R::skip(i, l, n);
+#pragma unroll
+      for (int k = 0; k < KN; ++k) s += (PART ? k >= skip : skip == 0) ? v[i][k] : 0.f;
+    }
+    mean = row_sum<WV>(make_float2(s, 0.f), sh0).x / (float)n;
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int skip = R::skip(i, l, n);
+#pragma unroll
+    for (int k = 0; k < KN; ++k) {
+      v[i][k] -= mean;
+      q = (PART ? k >= skip : skip == 0) ? fmaf(v[i][k], v[i][k], q) : q;
+    }
+  }
+  const float var = row_sum<WV>(make_float2(q, 0.f), sh1).x / (float)n;
+  return make_float2(mean, 1.f / sqrtf(var + eps));
+}
+
+template <class E, int NV, int WV, bool PART>
+__global__ void __launch_bounds__(threads_of(WV), 2) fwd_kernel(Args a) {
+  constexpr int kT = WV * 64, kRows = threads_of(WV) / kT, kN = Pack<E>::kN;
+  typedef Row<E, NV, WV, PART> Rw;
+  __shared__ float2 sh[2][4][WV];
+  const int l = threadIdx.x % kT;
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / kT;
+  if (t >= a.T) return;      // whole waves; with WV > 1 a workgroup has one row at a time
+  Rw r, b;
+  r.load(a.R, a.ldr, t, l, a.n);
+  b.load(a.B, a.ldb, t, l, a.n);
+  float pw[NV][kN], pb[NV][kN], w[NV][kN], bias[NV][kN], gt[NV][kN];
+  if (a.post) {
+    columns<Rw>(a.pw, a.w_bf16, 1.f, l, a.n, pw);
+    columns<Rw>(a.pb, a.w_bf16, 0.f, l, a.n, pb);
+  }
+  if (a.norm) {
+    columns<Rw>(a.w, a.w_bf16, 1.f, l, a.n, w);
+    columns<Rw>(a.b, a.w_bf16, 0.f, l, a.n, bias);
+  }
+  const bool grouped = a.gate && a.groups > 1;
+  if (!grouped) columns<Rw>(a.gate, a.gate_bf16, 1.f, l, a.n, gt);
+  for (int turn = 0;; turn ^= 1) {
+    if (grouped) columns<Rw>(gate_row(a, (unsigned)t / a.group_rows), a.gate_bf16, 1.f, l, a.n, gt);
+    float x[NV][kN], p[NV][kN];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      Pack<E>::widen(r.raw[i], x[i]);
+      Pack<E>::widen(b.raw[i], p[i]);
+    }
+    const int64_t next = t + stride;
+    if (next < a.T) {
+      r.load(a.R, a.ldr, next, l, a.n);
+      b.load(a.B, a.ldb, next, l, a.n);
+    }
+    float2 ps = make_float2(0.f, 0.f), ns = make_float2(0.f, 0.f);
+    if (a.post) {
+      ps = centre<Rw, WV, PART>(p, a.post, a.post_eps, l, a.n, sh[turn][0], sh[turn][1]);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < kN; ++k) p[i][k] = fmaf(p[i][k] * ps.y, pw[i][k], pb[i][k]);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < kN; ++k) x[i][k] = fmaf(a.block * gt[i][k], p[i][k], a.res * x[i][k]);
+    // without a sum over the row, nothing else keeps a wave's results from a wave that has yet to read the elements that
+    // both of their pieces hold (x may be r)
+    if (PART && WV > 1 && !a.post && !a.norm) __syncthreads();
+    E* xo = static_cast<E*>(a.X) + t * a.ldx;
+    float y[NV][kN];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < kN; ++k) y[i][k] = x[i][k];
+    if (a.norm) ns = centre<Rw, WV, PART>(y, a.norm, a.eps, l, a.n, sh[turn][2], sh[turn][3]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (Rw::skip(i, l, a.n) < kN) Pack<E>::put(xo + Rw::at(i, l, a.n), x[i]);
+    if (a.norm) {
+      E* yo = static_cast<E*>(a.Y) + t * a.ldy;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (Rw::skip(i, l, a.n) < kN) {
+#pragma unroll
+          for (int k = 0; k < kN; ++k) y[i][k] = fmaf(y[i][k] * ns.y, w[i][k], bias[i][k]);
+          Pack<E>::put(yo + Rw::at(i, l, a.n), y[i]);
+        }
+      }
+    }
+    if (l == 0 && a.stats) a.stats[t] = make_float4(ps.x, ps.y, ns.x, ns.y);
+    if (next >= a.T) break;
+    t = next;
+  }
+}
+
+// POST, NORM: there is such a norm.  BIAS: one of them may be a layer norm or have a bias (else both are RMS norms without;
+// their code and the sums' registers are left out).
+template <class E, int NV, int WV, bool PART, bool POST, bool NORM, bool BIAS>
+__global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
+  constexpr int kT = WV * 64, kThreads = threads_of(WV), kRows = kThreads / kT, kN = Pack<E>::kN;
+  typedef Row<E, NV, WV, PART> Rw;
+  __shared__ float2 sh[2][2][WV];
+  __shared__ float comb[kRows > 1 ? NV * kN * kT : 1];
+  const int l = threadIdx.x % kT, sub = threadIdx.x / kT;
+  const float inv_n = 1.f / (float)a.n;
+  const unsigned per_group = a.slices / a.groups;
+  float pw[NV][kN], pb[NV][kN], w[NV][kN], gt[NV][kN];
+  if constexpr (POST) {
+    columns<Rw>(a.pw, a.w_bf16, 1.f, l, a.n, pw);
+    if constexpr (BIAS) columns<Rw>(a.pb, a.w_bf16, 0.f, l, a.n, pb);
+  }
+  if constexpr (NORM) columns<Rw>(a.w, a.w_bf16, 1.f, l, a.n, w);
+  float dpw[NV][kN], dpb[NV][kN], dw[NV][kN], db[NV][kN], dg[NV][kN];
+  if constexpr (POST) fill(dpw, 0.f);
+  if constexpr (POST && BIAS) fill(dpb, 0.f);
+  if constexpr (NORM) fill(dw, 0.f);
+  if constexpr (NORM && BIAS) fill(db, 0.f);
+  // a thread's sums of its columns, over the workgroup's rows in a fixed order, to out[n]
+  auto flush = [&](const float (&v)[NV][kN], float* out, int add) {
+    if constexpr (kRows > 1) {
+      for (int q = 0; q < kRows; ++q) {
+        if (q == sub) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const int skip = Rw::skip(i, l, a.n);
+            float* p = comb + Rw::at(i, l, a.n);
+#pragma unroll
+            for (int k = 0; k < kN; ++k)
+              if (k >= skip) p[k] = q ? p[k] + v[i][k] : v[i][k];
+          }
+        }
+        __syncthreads();
+      }
+      for (int c = threadIdx.x; c < a.n; c += kThreads) out[c] = add ? out[c] + comb[c] : comb[c];
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int skip = Rw::skip(i, l, a.n), c = Rw::at(i, l, a.n);
+#pragma unroll
+        for (int k = 0; k < kN; ++k)
+          if (k >= skip) out[c + k] = add ? out[c + k] + v[i][k] : v[i][k];
+      }
+    }
+  };
+  int turn = 0;
+  for (unsigned slice = blockIdx.x; slice < a.slices; slice += gridDim.x) {
+    const unsigned group = slice / per_group;
+    columns<Rw>(gate_row(a, group), a.gate_bf16, 1.f, l, a.n, gt);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < kN; ++k) gt[i][k] *= a.block;
+    fill(dg, 0.f);
+    const int64_t first = (int64_t)group * a.group_rows, end = first + a.group_rows;
+    const int64_t stride = (int64_t)per_group * kRows;
+    int64_t t = first + (int64_t)(slice - group * per_group) * kRows + sub;
+    Rw r, b, dx, dy;
+    float4 st_next = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto fetch = [&](int64_t row) {
+      if (row >= end) return;
+      r.load(a.R, a.ldr, row, l, a.n);
+      b.load(a.B, a.ldb, row, l, a.n);
+      if (a.dX) dx.load(a.dX, a.lddx, row, l, a.n);
+      if constexpr (NORM) dy.load(a.dY, a.lddy, row, l, a.n);
+      st_next = a.stats[row];
+    };
+    fetch(t);
+    for (; t < end; t += stride, turn ^= 1) {
+      const float4 st = st_next;
+      float hp[NV][kN], h[NV][kN], D[NV][kN], f[NV][kN];
+      float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        Pack<E>::widen(b.raw[i], hp[i]);
+        Pack<E>::widen(r.raw[i], h[i]);
+        if (a.dX) {
+          Pack<E>::widen(dx.raw[i], D[i]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < kN; ++k) D[i][k] = 0.f;
+        }
+        if constexpr (NORM) Pack<E>::widen(dy.raw[i], f[i]);
+      }
+      fetch(t + stride);
+      auto p_of = [&](int i, int k) {
+        if constexpr (!POST) return hp[i][k];
+        else if constexpr (BIAS) return fmaf(hp[i][k], pw[i][k], pb[i][k]);
+        else return hp[i][k] * pw[i][k];
+      };
+      if constexpr (POST) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int k = 0; k < kN; ++k) hp[i][k] = BIAS ? (hp[i][k] - st.x) * st.y : hp[i][k] * st.y;
+      }
+      if constexpr (NORM) {
+        // a piece that is not there has dy = 0 and zero vectors, so that nothing comes of it
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int skip = Rw::skip(i, l, a.n);
+#pragma unroll
+          for (int k = 0; k < kN; ++k) {
+            const float x = fmaf(gt[i][k], p_of(i, k), a.res * h[i][k]);
+            h[i][k] = (BIAS ? x - st.z : x) * st.w;
+            dw[i][k] = fmaf(f[i][k], h[i][k], dw[i][k]);
+            if constexpr (BIAS) db[i][k] += f[i][k];
+            f[i][k] *= w[i][k];
+            const float q = !PART || k >= skip ? f[i][k] : 0.f;
+            s.x += q;
+            s.y = fmaf(q, h[i][k], s.y);
+          }
+        }
+        s = row_sum<WV>(s, sh[turn][0]);
+        const float ma = BIAS && a.norm == kLayer ? s.x * inv_n : 0.f, mh = s.y * inv_n;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int k = 0; k < kN; ++k) D[i][k] = fmaf(st.w, f[i][k] - ma - h[i][k] * mh, D[i][k]);
+      }
+      float mf = 0.f, mp = 0.f;
+      s = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int skip = Rw::skip(i, l, a.n);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+          dg[i][k] = fmaf(a.block * D[i][k], p_of(i, k), dg[i][k]);
+          const float e = gt[i][k] * D[i][k];
+          f[i][k] = e;
+          if constexpr (POST) {
+            dpw[i][k] = fmaf(e, hp[i][k], dpw[i][k]);
+            if constexpr (BIAS) dpb[i][k] += e;
+            f[i][k] = e * pw[i][k];
+            const float q = !PART || k >= skip ? f[i][k] : 0.f;
+            s.x += q;
+            s.y = fmaf(q, hp[i][k], s.y);
+          }
+        }
+      }
+      if constexpr (POST) {
+        s = row_sum<WV>(s, sh[turn][1]);
+        mf = BIAS && a.post == kLayer ? s.x * inv_n : 0.f;
+        mp = s.y * inv_n;
+      }
+      if (PART && WV > 1 && !POST && !NORM) __syncthreads();   // as in the forward
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (Rw::skip(i, l, a.n) < kN) {
+          const int c = Rw::at(i, l, a.n);
+          float o[kN];
+          if (a.X) {
+#pragma unroll
+            for (int k = 0; k < kN; ++k) o[k] = a.res * D[i][k];
+            Pack<E>::put(static_cast<E*>(a.X) + t * a.ldx + c, o);
+          }
+          if (a.Y) {
+#pragma unroll
+            for (int k = 0; k < kN; ++k) o[k] = POST ? st.y * (f[i][k] - mf - hp[i][k] * mp) : f[i][k];
+            Pack<E>::put(static_cast<E*>(a.Y) + t * a.ldy + c, o);
+          }
+        }
+      }
+    }
+    if (a.gate_out) flush(dg, a.gate_out + (int64_t)group * a.n, a.gate_add);
+    else if (a.gate_part) flush(dg, a.gate_part + (int64_t)slice * a.n, 0);
+  }
+  if (!a.part) return;
+  float* part = a.part + (int64_t)blockIdx.x * 4 * a.n;
+  if constexpr (POST) flush(dpw, part, 0);
+  if constexpr (POST && BIAS) flush(dpb, part + a.n, 0);
+  if constexpr (NORM) flush(dw, part + 2 * (int64_t)a.n, 0);
+  if constexpr (NORM && BIAS) flush(db, part + 3 * (int64_t)a.n, 0);
+}
+
+// The instance of a row of n: 16-byte pieces of a thread, waves of a row (0: rows are read several times), overlapping last
+// piece.
+struct Shape {
+  int nv, wv;
+  bool part;
+};
+
+
+}  // namespace resnorm
+}  // namespace ff

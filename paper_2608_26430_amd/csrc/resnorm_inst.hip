@@ -1,0 +1,39 @@
+// Instances of the backward of the join of two blocks (resnorm.h), compiled once per element type and kind of norms:
+// -DRESNORM_BF16=0/1, -DRESNORM_COMBO=0..5.
+#include "resnorm.h"
+
+#if !defined(RESNORM_BF16) || !defined(RESNORM_COMBO)
+#error "RESNORM_BF16 and RESNORM_COMBO select the instances"
+#endif
+
+namespace ff {
+namespace resnorm {
+
+#if RESNORM_BF16
+typedef __bf16 E;
+#else
+typedef float E;
+#endif
+
+template <int NV, int WV>
+static void go(const Args& a, const Shape& sh, unsigned groups, hipStream_t s) {
+  constexpr bool P = RESNORM_COMBO < 2 || RESNORM_COMBO == 4, N = RESNORM_COMBO < 4, B = RESNORM_COMBO % 2 == 1 || RESNORM_COMBO == 4;
+  const dim3 grid(groups), block(threads_of(WV));
+  if (sh.part) hipLaunchKernelGGL((bwd_kernel<E, NV, WV, true, P, N, B>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((bwd_kernel<E, NV, WV, false, P, N, B>), grid, block, 0, s, a);
+}
+
+#define RESNORM_NAME2(c, b) launch_bwd_##c##_##b
+#define RESNORM_NAME(c, b) RESNORM_NAME2(c, b)
+
+hipError_t RESNORM_NAME(RESNORM_COMBO, RESNORM_BF16)(const Args& a, const Shape& sh, unsigned groups, hipStream_t s) {
+  constexpr int k = 16 / Pack<E>::kN;      // pieces of 16 elements
+  if (sh.wv == 1 && sh.nv < k) go<k / 2, 1>(a, sh, groups, s);
+  else if (sh.wv == 1) go<k, 1>(a, sh, groups, s);
+  else if (sh.wv == 4) go<k, 4>(a, sh, groups, s);
+  else go<k, 8>(a, sh, groups, s);
+  return hipGetLastError();
+}
+
+}  // namespace resnorm
+}  // namespace ff
