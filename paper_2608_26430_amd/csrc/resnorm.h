@@ -193,46 +193,80 @@ __global__ void __launch_bounds__(threads_of(WV), 2) fwd_kernel(Args a) {
   }
 }
 
+// Vectors of a thread's columns in LDS, in the order in which its row's waves read them back: [piece][quarter of a piece][thread]
+// of four floats each.  In registers they cost 16 a vector, and the backward of both norms spilled (8192 x 8192, 590 us for both
+// passes).
+template <class R, int NV, int KN, int T>
+struct Kept {
+  static constexpr int kFloats = NV * KN * T;
+  float* at;
+  __device__ __forceinline__ void put(const void* p, int bf16, float none, float factor, int l, int n) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float v[KN];
+#pragma unroll
+      for (int k = 0; k < KN; ++k) v[k] = 0.f;      // zero where there is no piece
+      if (R::skip(i, l, n) < KN) vector_at<KN>(p, bf16, none, R::at(i, l, n), v);
+#pragma unroll
+      for (int k = 0; k < KN; k += 4)
+        *reinterpret_cast<float4*>(at + ((i * KN + k) * T + 4 * l)) =
+            make_float4(v[k] * factor, v[k + 1] * factor, v[k + 2] * factor, v[k + 3] * factor);
+    }
+  }
+  __device__ __forceinline__ void get(int i, int l, float (&v)[KN]) const {
+#pragma unroll
+    for (int k = 0; k < KN; k += 4) {
+      const float4 q = *reinterpret_cast<const float4*>(at + ((i * KN + k) * T + 4 * l));
+      v[k] = q.x, v[k + 1] = q.y, v[k + 2] = q.z, v[k + 3] = q.w;
+    }
+  }
+};
+
 // POST, NORM: there is such a norm.  BIAS: one of them may be a layer norm or have a bias (else both are RMS norms without;
-// their code and the sums' registers are left out).
-template <class E, int NV, int WV, bool PART, bool POST, bool NORM, bool BIAS>
+// their code and the sums' registers are left out).  GATE: there is a gate.
+template <class E, int NV, int WV, bool PART, bool POST, bool NORM, bool BIAS, bool GATE>
 __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
   constexpr int kT = WV * 64, kThreads = threads_of(WV), kRows = kThreads / kT, kN = Pack<E>::kN;
   typedef Row<E, NV, WV, PART> Rw;
+  typedef Kept<Rw, NV, kN, kT> Vec;
+  constexpr int kVecs = (POST ? (BIAS ? 2 : 1) : 0) + (NORM ? 1 : 0) + (GATE ? 1 : 0);
   __shared__ float2 sh[2][2][WV];
-  __shared__ float comb[kRows > 1 ? NV * kN * kT : 1];
+  constexpr int kPlace = NV * kN * kT;
+  __shared__ float comb[kRows > 1 ? 2 * kRows * kPlace : 1];
+  int side = 0;
+  __shared__ __align__(16) float kept[kVecs ? kVecs * Vec::kFloats : 4];
   const int l = threadIdx.x % kT, sub = threadIdx.x / kT;
   const float inv_n = 1.f / (float)a.n;
   const unsigned per_group = a.slices / a.groups;
-  float pw[NV][kN], pb[NV][kN], w[NV][kN], gt[NV][kN];
-  if constexpr (POST) {
-    columns<Rw>(a.pw, a.w_bf16, 1.f, l, a.n, pw);
-    if constexpr (BIAS) columns<Rw>(a.pb, a.w_bf16, 0.f, l, a.n, pb);
-  }
-  if constexpr (NORM) columns<Rw>(a.w, a.w_bf16, 1.f, l, a.n, w);
-  float dpw[NV][kN], dpb[NV][kN], dw[NV][kN], db[NV][kN], dg[NV][kN];
-  if constexpr (POST) fill(dpw, 0.f);
-  if constexpr (POST && BIAS) fill(dpb, 0.f);
+  const Vec pw{kept}, w{kept + (POST ? 1 : 0) * Vec::kFloats}, gt{kept + ((POST ? 1 : 0) + (NORM ? 1 : 0)) * Vec::kFloats},
+      pb{kept + (kVecs - 1) * Vec::kFloats};
+  // (the waves of several rows write the same values)
+  if constexpr (POST) Vec(pw).put(a.pw, a.w_bf16, 1.f, 1.f, l, a.n);
+  if constexpr (POST && BIAS) Vec(pb).put(a.pb, a.w_bf16, 0.f, 1.f, l, a.n);
+  if constexpr (NORM) Vec(w).put(a.w, a.w_bf16, 1.f, 1.f, l, a.n);
+  // The gate is one row in a slice, so that sums of D hp and of D give its gradient and those of post's vectors.
+  float sdh[NV][kN], sd[NV][kN], dw[NV][kN], db[NV][kN];
   if constexpr (NORM) fill(dw, 0.f);
   if constexpr (NORM && BIAS) fill(db, 0.f);
   // a thread's sums of its columns, over the workgroup's rows in a fixed order, to out[n]
   auto flush = [&](const float (&v)[NV][kN], float* out, int add) {
     if constexpr (kRows > 1) {
-      for (int q = 0; q < kRows; ++q) {
-        if (q == sub) {
+      // each row's waves their own place; two places in turn, so that a barrier a vector is enough
+      float* p = comb + (side ^= 1) * kRows * kPlace;
 #pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            const int skip = Rw::skip(i, l, a.n);
-            float* p = comb + Rw::at(i, l, a.n);
+      for (int i = 0; i < NV; ++i) {
+        const int skip = Rw::skip(i, l, a.n);
 #pragma unroll
-            for (int k = 0; k < kN; ++k)
-              if (k >= skip) p[k] = q ? p[k] + v[i][k] : v[i][k];
-          }
-        }
-        __syncthreads();
+        for (int k = 0; k < kN; ++k)
+          if (k >= skip) p[sub * kPlace + Rw::at(i, l, a.n) + k] = v[i][k];
       }
-      for (int c = threadIdx.x; c < a.n; c += kThreads) out[c] = add ? out[c] + comb[c] : comb[c];
       __syncthreads();
+      for (int c = threadIdx.x; c < a.n; c += kThreads) {
+        float x = p[c];
+#pragma unroll
+        for (int q = 1; q < kRows; ++q) x += p[q * kPlace + c];
+        out[c] = add ? out[c] + x : x;
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -246,12 +280,12 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
   int turn = 0;
   for (unsigned slice = blockIdx.x; slice < a.slices; slice += gridDim.x) {
     const unsigned group = slice / per_group;
-    columns<Rw>(gate_row(a, group), a.gate_bf16, 1.f, l, a.n, gt);
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int k = 0; k < kN; ++k) gt[i][k] *= a.block;
-    fill(dg, 0.f);
+    if constexpr (GATE) {
+      if (kRows > 1 && slice != blockIdx.x) __syncthreads();      // every wave is done with the last slice's gate
+      Vec(gt).put(gate_row(a, group), a.gate_bf16, 1.f, a.block, l, a.n);
+    }
+    if constexpr (POST || GATE) fill(sdh, 0.f);
+    if constexpr (POST && BIAS) fill(sd, 0.f);
     const int64_t first = (int64_t)group * a.group_rows, end = first + a.group_rows;
     const int64_t stride = (int64_t)per_group * kRows;
     int64_t t = first + (int64_t)(slice - group * per_group) * kRows + sub;
@@ -259,7 +293,7 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
     float4 st_next = make_float4(0.f, 0.f, 0.f, 0.f);
     auto fetch = [&](int64_t row) {
       if (row >= end) return;
-      r.load(a.R, a.ldr, row, l, a.n);
+      if constexpr (NORM) r.load(a.R, a.ldr, row, l, a.n);
       b.load(a.B, a.ldb, row, l, a.n);
       if (a.dX) dx.load(a.dX, a.lddx, row, l, a.n);
       if constexpr (NORM) dy.load(a.dY, a.lddy, row, l, a.n);
@@ -267,26 +301,44 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
     };
     fetch(t);
     for (; t < end; t += stride, turn ^= 1) {
+      asm volatile("" ::: "memory");       // the vectors are read for every row, not kept in registers over all
       const float4 st = st_next;
       float hp[NV][kN], h[NV][kN], D[NV][kN], f[NV][kN];
       float2 s = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         Pack<E>::widen(b.raw[i], hp[i]);
-        Pack<E>::widen(r.raw[i], h[i]);
         if (a.dX) {
           Pack<E>::widen(dx.raw[i], D[i]);
         } else {
 #pragma unroll
           for (int k = 0; k < kN; ++k) D[i][k] = 0.f;
         }
-        if constexpr (NORM) Pack<E>::widen(dy.raw[i], f[i]);
+        if constexpr (NORM) {
+          Pack<E>::widen(r.raw[i], h[i]);
+          Pack<E>::widen(dy.raw[i], f[i]);
+        }
       }
       fetch(t + stride);
-      auto p_of = [&](int i, int k) {
-        if constexpr (!POST) return hp[i][k];
-        else if constexpr (BIAS) return fmaf(hp[i][k], pw[i][k], pb[i][k]);
-        else return hp[i][k] * pw[i][k];
+      // p and block gate of piece i
+      auto p_of = [&](int i, float (&p)[kN]) {
+        float q[kN], c[kN];
+        if constexpr (POST) pw.get(i, l, q);
+        if constexpr (POST && BIAS) pb.get(i, l, c);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+          if constexpr (!POST) p[k] = hp[i][k];
+          else if constexpr (BIAS) p[k] = fmaf(hp[i][k], q[k], c[k]);
+          else p[k] = hp[i][k] * q[k];
+        }
+      };
+      auto gate_of = [&](int i, float (&g)[kN]) {
+        if constexpr (GATE) gt.get(i, l, g);
+        else {
+          const float one = Rw::skip(i, l, a.n) < kN ? a.block : 0.f;
+#pragma unroll
+          for (int k = 0; k < kN; ++k) g[k] = one;
+        }
       };
       if constexpr (POST) {
 #pragma unroll
@@ -299,15 +351,19 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           const int skip = Rw::skip(i, l, a.n);
+          float p[kN], g[kN], wv[kN];
+          p_of(i, p);
+          gate_of(i, g);
+          w.get(i, l, wv);
 #pragma unroll
           for (int k = 0; k < kN; ++k) {
-            const float x = fmaf(gt[i][k], p_of(i, k), a.res * h[i][k]);
+            const float x = fmaf(g[k], p[k], a.res * h[i][k]);
             h[i][k] = (BIAS ? x - st.z : x) * st.w;
             dw[i][k] = fmaf(f[i][k], h[i][k], dw[i][k]);
             if constexpr (BIAS) db[i][k] += f[i][k];
-            f[i][k] *= w[i][k];
+            f[i][k] *= wv[k];
             const float q = !PART || k >= skip ? f[i][k] : 0.f;
-            s.x += q;
+            if constexpr (BIAS) s.x += q;
             s.y = fmaf(q, h[i][k], s.y);
           }
         }
@@ -316,25 +372,26 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-          for (int k = 0; k < kN; ++k) D[i][k] = fmaf(st.w, f[i][k] - ma - h[i][k] * mh, D[i][k]);
+          for (int k = 0; k < kN; ++k) D[i][k] = fmaf(st.w, (BIAS ? f[i][k] - ma : f[i][k]) - h[i][k] * mh, D[i][k]);
       }
       float mf = 0.f, mp = 0.f;
       s = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int skip = Rw::skip(i, l, a.n);
+        float g[kN], q[kN];
+        gate_of(i, g);
+        if constexpr (POST) pw.get(i, l, q);
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
-          dg[i][k] = fmaf(a.block * D[i][k], p_of(i, k), dg[i][k]);
-          const float e = gt[i][k] * D[i][k];
-          f[i][k] = e;
+          if constexpr (POST || GATE) sdh[i][k] = fmaf(D[i][k], hp[i][k], sdh[i][k]);
+          if constexpr (POST && BIAS) sd[i][k] += D[i][k];
+          f[i][k] = g[k] * D[i][k];
           if constexpr (POST) {
-            dpw[i][k] = fmaf(e, hp[i][k], dpw[i][k]);
-            if constexpr (BIAS) dpb[i][k] += e;
-            f[i][k] = e * pw[i][k];
-            const float q = !PART || k >= skip ? f[i][k] : 0.f;
-            s.x += q;
-            s.y = fmaf(q, hp[i][k], s.y);
+            f[i][k] *= q[k];
+            const float c = !PART || k >= skip ? f[i][k] : 0.f;
+            if constexpr (BIAS) s.x += c;
+            s.y = fmaf(c, hp[i][k], s.y);
           }
         }
       }
@@ -362,13 +419,48 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
         }
       }
     }
-    if (a.gate_out) flush(dg, a.gate_out + (int64_t)group * a.n, a.gate_add);
-    else if (a.gate_part) flush(dg, a.gate_part + (int64_t)slice * a.n, 0);
+    // the sums of the slice: a workgroup's first slice writes its partial rows, later ones (where there are more gate rows than
+    // workgroups) add to them
+    float* part = a.part + (int64_t)blockIdx.x * 4 * a.n;
+    const int later = slice != blockIdx.x;
+    if constexpr (GATE) {
+      if (a.gate_out || a.gate_part) {
+        float dg[NV][kN];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float q[kN], c[kN];
+          if constexpr (POST) pw.get(i, l, q);
+          if constexpr (POST && BIAS) pb.get(i, l, c);
+#pragma unroll
+          for (int k = 0; k < kN; ++k) {
+            dg[i][k] = POST ? q[k] * sdh[i][k] : sdh[i][k];
+            if constexpr (POST && BIAS) dg[i][k] = fmaf(c[k], sd[i][k], dg[i][k]);
+            dg[i][k] *= a.block;
+          }
+        }
+        if (a.gate_out) flush(dg, a.gate_out + (int64_t)group * a.n, a.gate_add);
+        else flush(dg, a.gate_part + (int64_t)slice * a.n, 0);
+      }
+    }
+    if constexpr (POST) {
+      if (a.part) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float g[kN];
+          if constexpr (GATE) gt.get(i, l, g);
+#pragma unroll
+          for (int k = 0; k < kN; ++k) {
+            sdh[i][k] *= GATE ? g[k] : a.block;
+            if constexpr (BIAS) sd[i][k] *= GATE ? g[k] : a.block;
+          }
+        }
+        flush(sdh, part, later);
+        if constexpr (BIAS) flush(sd, part + a.n, later);
+      }
+    }
   }
   if (!a.part) return;
   float* part = a.part + (int64_t)blockIdx.x * 4 * a.n;
-  if constexpr (POST) flush(dpw, part, 0);
-  if constexpr (POST && BIAS) flush(dpb, part + a.n, 0);
   if constexpr (NORM) flush(dw, part + 2 * (int64_t)a.n, 0);
   if constexpr (NORM && BIAS) flush(db, part + 3 * (int64_t)a.n, 0);
 }

@@ -1,5 +1,5 @@
 // Instances of the backward of the join of two blocks (resnorm.h), compiled once per element type and kind of norms:
-// -DRESNORM_BF16=0/1, -DRESNORM_COMBO=0..5.
+// -DRESNORM_BF16=0/1, -DRESNORM_COMBO=0..5; with and without a gate.
 #include "resnorm.h"
 
 #if !defined(RESNORM_BF16) || !defined(RESNORM_COMBO)
@@ -19,8 +19,13 @@ template <int NV, int WV>
 static void go(const Args& a, const Shape& sh, unsigned groups, hipStream_t s) {
   constexpr bool P = RESNORM_COMBO < 2 || RESNORM_COMBO == 4, N = RESNORM_COMBO < 4, B = RESNORM_COMBO % 2 == 1 || RESNORM_COMBO == 4;
   const dim3 grid(groups), block(threads_of(WV));
-  if (sh.part) hipLaunchKernelGGL((bwd_kernel<E, NV, WV, true, P, N, B>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((bwd_kernel<E, NV, WV, false, P, N, B>), grid, block, 0, s, a);
+  if (a.gate) {
+    if (sh.part) hipLaunchKernelGGL((bwd_kernel<E, NV, WV, true, P, N, B, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((bwd_kernel<E, NV, WV, false, P, N, B, true>), grid, block, 0, s, a);
+  } else {
+    if (sh.part) hipLaunchKernelGGL((bwd_kernel<E, NV, WV, true, P, N, B, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((bwd_kernel<E, NV, WV, false, P, N, B, false>), grid, block, 0, s, a);
+  }
 }
 
 #define RESNORM_NAME2(c, b) launch_bwd_##c##_##b
