@@ -423,11 +423,12 @@ ff_status ff_adamw_set_read(const ff_adamw_set* s, void* const* m, void* const* 
 double ff_lr_linear_warmup(int64_t step, int64_t warmup, int64_t total, double base_lr);
 
 /*
- * Operators around the adapter in a training step: layer norm, dropout and the loss of the head.  They need no
+ * Operators around the adapter in a training step: layer norm, the join of two blocks, dropout, the gated feed-forward and the
+ * loss of the head.  They need no
  * frame and no plan.  Activations are T rows of n elements of type `act` as above, row t at X + t ldx.  The calls are
  * asynchronous on `stream`, allocate nothing, synchronise nothing and may be captured into a graph.  A call that returns
- * FF_EINVAL has written nothing; after FF_EDEVICE (a launch failed) the layer norm's backward and the loss, which
- * launch several kernels, may have written some of their outputs.  Equal inputs give equal bits.  A workspace belongs to
+ * FF_EINVAL has written nothing; after FF_EDEVICE (a launch failed) calls that launch several kernels (the backwards and the
+ * loss) may have written some of their outputs.  Equal inputs give equal bits.  A workspace belongs to
  * the call until it has run: calls that overlap in time need one each.  Outputs must not overlap inputs or the
  * workspace except where it is said.
  */
@@ -519,6 +520,39 @@ ff_status ff_resnorm_bwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
  */
 ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, double p, uint64_t seed, uint64_t offset,
                      const uint64_t* offset_dev, const void* R, int64_t ldr, void* Y, int64_t ldy, void* stream);
+
+/*
+ * ff_glu_* -- a gated feed-forward block up to its down projection, both projections, the function and the product in one kernel:
+ *   G = X Wg^T [+ Ag],   U = X Wu^T [+ Au],   H = f(G) U
+ *   fn     : f, FF_GLU_SILU (g / (1 + exp -g)), FF_GLU_GELU (g times the normal distribution's integral up to g) or FF_GLU_GELU_TANH
+ *            (g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2).
+ *   X      : device, T x n;  Wg, Wu : device, F x n, one leading dimension ldw (halves of one weight, or two);
+ *   Ag, Au : device, T x F, one leading dimension lda: what adapters on the projections add (ff_adapter_fwd on X); each may be NULL.
+ *   H      : device, T x F.   G, U : device, T x F, one leading dimension ldg, kept for the backward; NULL to keep nothing.
+ * ff_glu_bwd, from the gradient dH (T x F) of H:
+ *   dU = dH f(G),   dG = dH U f'(G)                (T x F, one leading dimension lddg; also what the adapters' backwards take)
+ *   dX = beta_dx dX + dG Wg + dU Wu                (skipped if NULL)
+ *   dWg = beta_dw dWg + dG^T X,   dWu likewise     (F x n, one leading dimension lddw; skipped if both are NULL)
+ *   G, U : as the forward kept them; X is then read for dWg and dWu alone, the weights for dX.  Without them (NULL) G and U
+ *          are made again from X, the weights, Ag and Au, as the forward had them before their rounding.
+ *   dG or dU may be dH, and dG may be G, dU may be U, with the same leading dimension.  beta = 0 does not read the output.
+ *   workspace : device, 256-byte aligned, at least ff_glu_workspace bytes for the same T, n, F, act and the outputs wanted
+ *          (FF_GLU_DX, FF_GLU_DW or both); not looked at without them.  It holds fp32 partial sums of products with few results.
+ * All matrices of type act; n and F multiples of 8 (bf16) or 4 (fp32), at most 262144, T at most 2^28; 16-byte aligned, leading
+ * dimensions multiples of 8 (4), at most 1048576.  Products accumulate in fp32; H, G, U, dG, dU, dX and the weights' gradients are
+ * rounded once each, and the products of the backward read dG and dU so.  Weights, X, dH and what is kept must be finite.
+ * T = 0 writes nothing but dWg = beta_dw dWg and dWu.
+ */
+enum { FF_GLU_SILU = 0, FF_GLU_GELU = 1, FF_GLU_GELU_TANH = 2 };
+enum { FF_GLU_DX = 1, FF_GLU_DW = 2 };
+ff_status ff_glu_fwd(int64_t T, int64_t n, int64_t F, int act, int fn, const void* X, int64_t ldx, const void* Wg,
+                     const void* Wu, int64_t ldw, const void* Ag, const void* Au, int64_t lda, void* H, int64_t ldh, void* G,
+                     void* U, int64_t ldg, void* stream);
+ff_status ff_glu_workspace(int64_t T, int64_t n, int64_t F, int act, int want, int64_t* bytes);
+ff_status ff_glu_bwd(int64_t T, int64_t n, int64_t F, int act, int fn, const void* dH, int64_t lddh, const void* X, int64_t ldx,
+                     const void* Wg, const void* Wu, int64_t ldw, const void* Ag, const void* Au, int64_t lda, const void* G,
+                     const void* U, int64_t ldg, void* dG, void* dU, int64_t lddg, float beta_dx, void* dX, int64_t lddx,
+                     float beta_dw, void* dWg, void* dWu, int64_t lddw, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * ff_xent_* -- cross entropy of a head's logits z = H W^T over a vocabulary of V entries, without keeping the logits:

@@ -10,4 +10,5 @@ from .binding import (  # noqa: F401
     coef_to_user, adamw_step, adamw_step_batched, lr_linear_warmup, PlanGroup, plan_group, adapter_fwd_group,
     adapter_bwd_group, library_path, layernorm_fwd, layernorm_bwd, layernorm_workspace, dropout, xent_fwd, xent_bwd,
     xent_step, xent_workspace, AdamWSet, resnorm_fwd, resnorm_bwd, resnorm_workspace,
+    glu_fwd, glu_bwd, glu_workspace,
 )

@@ -89,6 +89,10 @@ def _load():
         "ff_resnorm_workspace": (i32, [i64, i64, i64, pi64]),
         "ff_resnorm_bwd": (i32, [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, i32, vp, vp, vp, vp, vp, vp, i64,
                                  vp]),
+        "ff_glu_fwd": (i32, [i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp]),
+        "ff_glu_workspace": (i32, [i64, i64, i64, i32, i32, pi64]),
+        "ff_glu_bwd": (i32, [i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, vp, i64, vp, vp, i64, f32,
+                             vp, i64, f32, vp, vp, i64, vp, i64, vp]),
         "ff_dropout": (i32, [i64, i64, i32, vp, i64, f64, u64, u64, vp, vp, i64, vp, i64, vp]),
         "ff_xent_workspace": (i32, [i64, i64, i64, i32, i32, pi64]),
         "ff_xent_fwd": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp]),
@@ -1055,6 +1059,126 @@ def dropout(X, p: float, seed: int, offset: int = 0, residual=None, Y=None, offs
     _check((_lib or _load()).ff_dropout(T, n, act, xp, ldx, p, seed & (1 << 64) - 1, offset & (1 << 64) - 1, op, rp, ldr,
                                         yp, ldy, _stream(stream)))
     return Y
+
+
+_GLU = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+def _glu_fn(fn):
+    if fn not in _GLU:
+        raise ValueError(f"unknown function {fn!r}: 'silu', 'gelu' or 'gelu_tanh'")
+    return _GLU[fn]
+
+
+def _glu_weights(X, Wg, Wu):
+    """Sizes, activation code, pointers and leading dimensions of X and the two weights."""
+    xp, ldx, T, n, dev = _input(X, "X")
+    gp, ldw, F, nw, wdev = _input(Wg, "Wg")
+    if nw != n or Wg.dtype is not X.dtype or wdev != dev:
+        raise ValueError(f"Wg must be an F x {n} {X.dtype} tensor on {X.device}")
+    up, ldu = _rows(Wu, "Wu", Wg)
+    return T, n, F, _act_code(X), xp, ldx, gp, up, _pair(ldw, ldu, "Wg and Wu"), dev
+
+
+def _pair(ld, other, names):
+    if ld != other:
+        raise ValueError(f"{names} must have one row stride")
+    return ld
+
+
+def _hidden(t, name, X, T, F):
+    """Pointer and leading dimension of a T x F tensor of X's type and device."""
+    st = t.stride()
+    if t.dtype is not X.dtype or t.shape != (T, F) or t.get_device() != X.get_device() or (st[1] != 1 and F != 1):
+        raise ValueError(f"{name} must be a {T} x {F} {X.dtype} tensor with unit column stride on {X.device}")
+    return t.data_ptr(), F if T < 2 else st[0]
+
+
+def _hidden_pair(a, b, names, X, T, F):
+    """The pointers of two T x F tensors, either of which may be None, and their leading dimension."""
+    pa, la = _hidden(a, names[0], X, T, F) if a is not None else (None, None)
+    pb, lb = _hidden(b, names[1], X, T, F) if b is not None else (None, None)
+    if la is not None and lb is not None:
+        _pair(la, lb, f"{names[0]} and {names[1]}")
+    return pa, pb, la if la is not None else (lb if lb is not None else F)
+
+
+def glu_fwd(X, Wg, Wu, fn: str = "silu", Ag=None, Au=None, H=None, G=None, U=None, save: bool = False, stream=None):
+    """H = f(X Wg^T [+ Ag]) * (X Wu^T [+ Au]), fn "silu", "gelu" or "gelu_tanh": returns H, with `save` (H, G, U), the last two what f
+    and the product were taken of, for glu_bwd (ff_glu_fwd).  Wg and Wu: F x n with one row stride, e.g. halves of one weight."""
+    torch = _T or _torch()
+    T, n, F, act, xp, ldx, wg, wu, ldw, dev = _glu_weights(X, Wg, Wu)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return glu_fwd(X, Wg, Wu, fn, Ag, Au, H, G, U, save, stream)
+    f = _glu_fn(fn)
+    ap, bp, lda = _hidden_pair(Ag, Au, ("Ag", "Au"), X, T, F)
+    if H is None:
+        H = _new((T, F), X.dtype, X.device, stream)
+        hp, ldh = H.data_ptr(), F
+    else:
+        hp, ldh = _hidden(H, "H", X, T, F)
+    gp = up = None
+    ldg = F
+    if save:
+        G = _new((T, F), X.dtype, X.device, stream) if G is None else G
+        U = _new((T, F), X.dtype, X.device, stream) if U is None else U
+        gp, up, ldg = _hidden_pair(G, U, ("G", "U"), X, T, F)
+    _check((_lib or _load()).ff_glu_fwd(T, n, F, act, f, xp, ldx, wg, wu, ldw, ap, bp, lda, hp, ldh, gp, up, ldg, _stream(stream)))
+    return (H, G, U) if save else H
+
+
+def _glu_bytes(T, n, F, act, want):
+    v = ctypes.c_int64()
+    _check((_lib or _load()).ff_glu_workspace(T, n, F, act, want, ctypes.byref(v)))
+    return v.value
+
+
+def glu_workspace(T: int, n: int, F: int, dtype, want_dx: bool = True, want_dw: bool = False, device="cuda"):
+    """A workspace for glu_bwd calls of these sizes and outputs, one such call at a time."""
+    torch = _torch()
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported activation dtype {dtype}")
+    nbytes = _glu_bytes(T, n, F, FF_BF16 if dtype is torch.bfloat16 else FF_F32, int(want_dx) + 2 * int(want_dw))
+    return torch.empty((nbytes,), dtype=torch.uint8, device=device)
+
+
+def glu_bwd(dH, X, Wg, Wu, fn: str = "silu", G=None, U=None, Ag=None, Au=None, dG=None, dU=None, dX=None, dWg=None, dWu=None,
+            beta_dx: float = 0.0, beta_dw: float = 0.0, want_dx: bool = True, want_dw: bool = False, workspace=None, stream=None):
+    """Backward of glu_fwd from the gradient dH of H: returns (dG, dU, dX, dWg, dWu), the last three None where not wanted
+    (ff_glu_bwd).  G, U: kept by the forward; without them they are made again, and Ag and Au are what the forward added.  dG and dU
+    are also the gradients of what adapters added; dG or dU may be dH, dG may be G, dU may be U."""
+    torch = _T or _torch()
+    T, n, F, act, xp, ldx, wg, wu, ldw, dev = _glu_weights(X, Wg, Wu)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return glu_bwd(dH, X, Wg, Wu, fn, G, U, Ag, Au, dG, dU, dX, dWg, dWu, beta_dx, beta_dw, want_dx, want_dw, workspace,
+                           stream)
+    f = _glu_fn(fn)
+    if (G is None) != (U is None):
+        raise ValueError("G and U are kept together")
+    dhp, lddh = _hidden(dH, "dH", X, T, F)
+    gp, up, ldg = _hidden_pair(G, U, ("G", "U"), X, T, F)
+    ap, bp, lda = _hidden_pair(Ag, Au, ("Ag", "Au"), X, T, F)
+    dG = _new((T, F), X.dtype, X.device, stream) if dG is None else dG
+    dU = _new((T, F), X.dtype, X.device, stream) if dU is None else dU
+    dgp, dup, lddg = _hidden_pair(dG, dU, ("dG", "dU"), X, T, F)
+    dxp = dwg = dwu = wsp = None
+    lddx = lddw = n
+    wsn = 0
+    if want_dx:
+        dX, dxp, lddx = _out_rows(dX, "dX", X, stream, beta_dx)
+    if want_dw:
+        dWg, dwg, lddw = _out_rows(dWg, "dWg", Wg, stream, beta_dw)
+        dWu, dwu, other = _out_rows(dWu, "dWu", Wg, stream, beta_dw)
+        _pair(lddw, other, "dWg and dWu")
+    want = int(want_dx) + 2 * int(want_dw)
+    if want:
+        workspace = _workspace(workspace, _glu_bytes(T, n, F, act, want) if workspace is None else 0, X.device, stream)
+        wsp, wsn = workspace.data_ptr(), workspace.nbytes
+    _check((_lib or _load()).ff_glu_bwd(T, n, F, act, f, dhp, lddh, xp, ldx, wg, wu, ldw, ap, bp, lda, gp, up, ldg, dgp, dup, lddg,
+                                        beta_dx, dxp, lddx, beta_dw, dwg, dwu, lddw, wsp, wsn, _stream(stream)))
+    return dG, dU, (dX if want_dx else None), (dWg if want_dw else None), (dWu if want_dw else None)
 
 
 def _xent_bytes(T, n, V, act, want):

@@ -15,14 +15,17 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libframeft.so")
-# (source, object name, extra flags): the generic, slab, loss and join kernels are instantiated by one
+# (source, object name, extra flags): the generic, slab, loss, feed-forward and join kernels are instantiated by one
 # source each, compiled once per variant, so that their long compiles run in parallel
 SOURCES = [("capi.cpp", "capi.cpp.o", []), ("framegen.cpp", "framegen.cpp.o", []), ("plan.cpp", "plan.cpp.o", []),
            ("kernels.hip", "kernels.hip.o", []), ("kernels_w128.hip", "kernels_w128.hip.o", []),
            ("optim.hip", "optim.hip.o", []), ("optim_set.hip", "optim_set.hip.o", []), ("group.cpp", "group.cpp.o", []),
            ("lift.hip", "lift.hip.o", []), ("slab.hip", "slab.hip.o", []),
            ("slab_ms.hip", "slab_ms.hip.o", []), ("norm.hip", "norm.hip.o", []), ("dropout.hip", "dropout.hip.o", []),
-           ("xent.hip", "xent.hip.o", []), ("resnorm.hip", "resnorm.hip.o", [])] + [
+           ("xent.hip", "xent.hip.o", []), ("resnorm.hip", "resnorm.hip.o", []),
+           ("glu.hip", "glu.hip.o", [])] + [
+    ("glu_inst.hip", f"glu_{p}_{t}.o", [f"-DGLU_PART={p}", f"-DGLU_BF16={int(t == 'bf16')}"])
+    for p in range(5) for t in ("bf16", "f32")] + [
     ("resnorm_inst.hip", f"resnorm_{c}_{t}.o", [f"-DRESNORM_COMBO={c}", f"-DRESNORM_BF16={int(t == 'bf16')}"])
     for c in range(6) for t in ("bf16", "f32")] + [
     ("xent_inst.hip", f"xent_{l}_{t}.o", [f"-DXENT_LAYOUT={l}", f"-DXENT_BF16={int(t == 'bf16')}"])

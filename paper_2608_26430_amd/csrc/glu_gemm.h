@@ -1,0 +1,636 @@
+// Matrix products of the gated feed-forward (glu.hip has the calls), on the operand tiles of xent_gemm.h.
+//
+//   G = X Wg^T [+ Ag],  U = X Wu^T [+ Au],  H = f(G) U                 projection_kernel, kForward (G and U kept or not)
+//   dU = dH f(G),  dG = dH U f'(G), G and U made again                 projection_kernel, kBackward
+//   dX = dG Wg + dU Wu                                                 gradient_kernel, one sum over both halves of k
+//   dWg = dG^T X,  dWu = dU^T X                                        gradient_kernel, two results
+// Here i runs along the rows of memory of a result, j over its rows, and every product is out[j][i] = sum_k A(i, k) B(j, k).
+//
+// projection_kernel: a workgroup's tile of BM has BM / 2 columns of both products: the same columns of G and U end in the same lane's
+// registers, and f needs nothing from elsewhere.  Its end reads and writes rows of memory, 16 bytes a lane in bf16 where a wave has
+// 32 columns or more.
+#pragma once
+
+#include "xent_gemm.h"
+
+namespace ff {
+namespace glu {
+
+using xent::f32x4;
+using xent::load4;
+using xent::Mma;
+using xent::Operand;
+using xent::ring_wait;
+using xent::store4;
+using xent::store8;
+using xent::u32x4;
+using xent::up;
+
+enum Mode { kForward = 0, kBackward = 1 };
+
+struct ProjArgs {
+  const void* Wg;
+  const void* Wu;
+  const void* X;
+  int64_t ldw, ldx;
+  int F, T, n;            // columns and rows of the results, length of the sums
+  int tm, tn;             // tiles along the columns and the rows
+  int kt;                 // k tiles
+  const void* Ag;         // NULL: none
+  const void* Au;
+  int64_t lda;
+  const void* dH;         // kBackward
+  int64_t lddh;
+  void* H;                // kForward
+  int64_t ldh;
+  void* G;                // kForward: NULL if not kept; kBackward: dG
+  void* U;                //           dU
+  int64_t ldg;
+};
+
+// f(g) and f'(g).  Fast: 1 ulp exponentials and reciprocals, for results that are rounded to bf16.
+__device__ __forceinline__ float exp_of(float x, bool fast) { return fast ? __builtin_amdgcn_exp2f(x * 1.4426950408889634f) : expf(x); }
+__device__ __forceinline__ float inverse(float x, bool fast) { return fast ? __builtin_amdgcn_rcpf(x) : 1.f / x; }
+
+template <int FN, bool FAST>
+__device__ __forceinline__ float2 gated(float g) {
+  if constexpr (FN == FF_GLU_SILU) {
+    const float s = inverse(1.f + exp_of(-g, FAST), FAST);
+    return make_float2(g * s, s * fmaf(g, 1.f - s, 1.f));
+  } else if constexpr (FN == FF_GLU_GELU) {
+    // erfc keeps the digits of f where g is far below zero
+    const float cdf = 0.5f * erfcf(g * -0.70710678118654752f);
+    return make_float2(g * cdf, fmaf(g, 0.39894228040143268f * exp_of(-0.5f * g * g, FAST), cdf));
+  } else {
+    // sqrt(2 / pi) (g + 0.044715 g^3), whose tanh is 2 s - 1
+    constexpr float c = 0.79788456080286536f;
+    const float s = inverse(1.f + exp_of(-2.f * c * g * fmaf(0.044715f * g, g, 1.f), FAST), FAST);
+    return make_float2(g * s, fmaf(g * s * (1.f - s), 2.f * c * fmaf(3.f * 0.044715f * g, g, 1.f), s));
+  }
+}
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+
+// W (4 or 8) consecutive elements.
+template <int W>
+__device__ __forceinline__ void load_run(const __bf16* p, float (&v)[W]) {
+  if constexpr (W == 8) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+      v[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+    }
+  } else {
+    const f32x4 w = load4(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = w[i];
+  }
+}
+template <int W>
+__device__ __forceinline__ void load_run(const float* p, float (&v)[W]) {
+#pragma unroll
+  for (int q = 0; q < W; q += 4) {
+    const f32x4 w = load4(p + q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[q + i] = w[i];
+  }
+}
+template <int W>
+__device__ __forceinline__ void store_run(__bf16* p, const float (&v)[W]) {
+  if constexpr (W == 8) store8(p, f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]});
+  else store4(p, f32x4{v[0], v[1], v[2], v[3]});
+}
+template <int W>
+__device__ __forceinline__ void store_run(float* p, const float (&v)[W]) {
+#pragma unroll
+  for (int q = 0; q < W; q += 4) store4(p + q, f32x4{v[q], v[q + 1], v[q + 2], v[q + 3]});
+}
+
+// The end of W columns from c of row t: what is added, f, and what is written.
+template <class E, int FN, int MODE, int W>
+__device__ __forceinline__ void finish_run(const ProjArgs& a, int64_t t, int c, float (&g)[W], float (&u)[W]) {
+  constexpr bool kFast = sizeof(E) == 2;
+  if (a.Ag) {
+    float x[W];
+    load_run<W>(static_cast<const E*>(a.Ag) + t * a.lda + c, x);
+#pragma unroll
+    for (int i = 0; i < W; ++i) g[i] += x[i];
+  }
+  if (a.Au) {
+    float x[W];
+    load_run<W>(static_cast<const E*>(a.Au) + t * a.lda + c, x);
+#pragma unroll
+    for (int i = 0; i < W; ++i) u[i] += x[i];
+  }
+  E* G = static_cast<E*>(a.G) + t * a.ldg + c;
+  E* U = static_cast<E*>(a.U) + t * a.ldg + c;
+  if constexpr (MODE == kForward) {
+    if (a.G) {
+      store_run<W>(G, g);
+      store_run<W>(U, u);
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) g[i] = gated<FN, kFast>(g[i]).x * u[i];
+    store_run<W>(static_cast<E*>(a.H) + t * a.ldh + c, g);
+  } else {
+    float x[W];
+    load_run<W>(static_cast<const E*>(a.dH) + t * a.lddh + c, x);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float2 f = gated<FN, kFast>(g[i]);
+      g[i] = x[i] * u[i] * f.y;
+      u[i] = x[i] * f.x;
+    }
+    store_run<W>(G, g);
+    store_run<W>(U, u);
+  }
+}
+
+template <class E, int BM, int BN, int WVM, int WVN, int NB, int WPE, int FN, int MODE>
+__global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArgs a) {
+  constexpr int NW = WVM * WVN;
+  constexpr int TH = BM / 2 / WVM, TN = BN / WVN;        // columns of each product, rows of a wave
+  constexpr int FH = TH / 16, FM = 2 * FH, FNT = TN / 16;
+  constexpr int PF = sizeof(E) == 2 && FH >= 2 ? 2 : 0;
+  typedef Operand<E, BM / 2, NW, false, PF> OpA;
+  typedef Operand<E, BN, NW, false, 0> OpB;
+  constexpr int kBuf = 2 * OpA::kBytes + OpB::kBytes;
+  constexpr int kLoads = 2 * OpA::kLoads + OpB::kLoads;
+  constexpr int kK = OpA::kK;
+  constexpr int kReads = FM * OpA::kReads + FNT * OpB::kReads;
+  constexpr int kMmas = FM * FNT * (sizeof(E) == 2 ? 1 : 4);
+  __shared__ __align__(1024) char lds[NB * kBuf];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WVM, wn = wave / WVM;
+  const int total = a.tm * a.tn;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+
+  OpA og, ou;
+  OpB ob;
+  og.init(a.ldw, wave, lane);
+  ou.init(a.ldw, wave, lane);
+  ob.init(a.ldx, wave, lane);
+  int i0, j0, i_next, j_next;
+  auto place = [&](int wg) {
+    int im, in;
+    xent::tile_of(xent::share_of(wg, total), a.tm, a.tn, &im, &in);
+    i_next = im * (BM / 2), j_next = in * BN;
+  };
+  auto issue_last = [&]() {
+    const int left = a.n - (a.kt - 1) * kK;
+    og.issue_last(a.kt - 1, left, a.ldw, i0, a.F, lds0, wave, lane);
+    ou.issue_last(a.kt - 1, left, a.ldw, i0, a.F, lds0 + OpA::kBytes, wave, lane);
+    ob.issue_last(a.kt - 1, left, a.ldx, j0, a.T, lds0 + 2 * OpA::kBytes, wave, lane);
+  };
+  auto issue = [&](int t, int buf) {
+    const unsigned to = lds0 + buf * kBuf;
+    og.issue(t < a.kt, to, wave);
+    ou.issue(t < a.kt, to + OpA::kBytes, wave);
+    ob.issue(t < a.kt, to + 2 * OpA::kBytes, wave);
+  };
+  // k is walked with its last tile first, so that only the first loads look at its end
+  auto start = [&]() {
+    i0 = i_next, j0 = j_next;
+    og.seek(a.Wg, a.ldw, i0, a.F, 0);
+    ou.seek(a.Wu, a.ldw, i0, a.F, 0);
+    ob.seek(a.X, a.ldx, j0, a.T, 0);
+    issue_last();
+#pragma unroll
+    for (int t = 1; t < (NB == 2 ? 2 : NB - 1); ++t) issue(t, t);
+  };
+
+  place(blockIdx.x);
+  start();
+  for (int wg = blockIdx.x;;) {
+    place(wg + gridDim.x);
+    f32x4 acc[FM][FNT];
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+      for (int j = 0; j < FNT; ++j) acc[f][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // fp32: sums of 128 k, then their sum, so that rounding grows with the length of both
+    constexpr bool kBlocked = sizeof(E) == 4;
+    f32x4 sum[kBlocked ? FM : 1][kBlocked ? FNT : 1] = {};
+    auto close_block = [&](bool end) {
+      if constexpr (kBlocked) {
+        if (!end) return;
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int j = 0; j < FNT; ++j) {
+            sum[f][j] += acc[f][j];
+            acc[f][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+      }
+    };
+    auto read = [&](int buf, int kk, f32x4 (&fa)[FM], f32x4 (&fb)[FNT]) {
+      const char* la = lds + buf * kBuf;
+#pragma unroll
+      for (int j = 0; j < FNT; ++j) fb[j] = OpB::read(la + 2 * OpA::kBytes, wn * TN, j, kk, lane);
+#pragma unroll
+      for (int f = 0; f < FH; ++f) {
+        fa[f] = OpA::read(la, wm * TH, f, kk, lane);
+        fa[FH + f] = OpA::read(la + OpA::kBytes, wm * TH, f, kk, lane);
+      }
+    };
+    auto multiply = [&](const f32x4 (&fa)[FM], const f32x4 (&fb)[FNT]) {
+#pragma unroll
+      for (int k = 0; k < Mma<E>::kSteps; ++k)
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int j = 0; j < FNT; ++j) acc[f][j] = Mma<E>::step(k, fa[f], fb[j], acc[f][j]);
+    };
+    if constexpr (NB == 2) {
+      f32x4 fa[2][FM], fb[2][FNT];
+      ring_wait<kLoads>();
+      read(0, 0, fa[0], fb[0]);
+      for (int t0 = 0; t0 < a.kt; t0 += 2) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          if (t0 + b >= a.kt) break;
+          read(b, 1, fa[1], fb[1]);
+          multiply(fa[0], fb[0]);
+          xent::interleave<kReads, kMmas>();
+          ring_wait<0>();
+          if (t0 + b + 2 < a.kt) issue(t0 + b + 2, b);
+          read(1 - b, 0, fa[0], fb[0]);
+          multiply(fa[1], fb[1]);
+          xent::interleave<kReads, kMmas>();
+          close_block((t0 + b) % 4 == 3);
+        }
+      }
+    } else {
+      for (int t0 = 0; t0 < a.kt; t0 += NB) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          if (t0 + b >= a.kt) break;
+          ring_wait<(NB - 2) * kLoads>();
+          issue(t0 + b + NB - 1, (b + NB - 1) % NB);
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            f32x4 fa[FM], fb[FNT];
+            read(b, kk, fa, fb);
+            multiply(fa, fb);
+          }
+          close_block((t0 + b) % 4 == 3);
+        }
+      }
+    }
+    if constexpr (kBlocked) {
+#pragma unroll
+      for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int j = 0; j < FNT; ++j) acc[f][j] += sum[f][j];
+    }
+    const int ci = i0 + wm * TH, cj = j0 + wn * TN;
+    wg += gridDim.x;
+    const bool more = wg < total;
+    if (more) {
+      ring_wait<0>();      // every wave's reads of the buffers are done
+      start();
+    }
+    const int g = lane >> 4, r = lane & 15;
+    constexpr int P = PF ? PF : 1;
+#pragma unroll
+    for (int j = 0; j < FNT; ++j) {
+      const int row = cj + j * 16 + r;
+      if (row >= a.T) continue;
+#pragma unroll
+      for (int f = 0; f < FH; f += P) {
+        const int c = ci + f * 16 + g * (P * 4);
+        if (c >= a.F) continue;
+        float x[4 * P], y[4 * P];
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[4 * q + i] = acc[f + q][j][i], y[4 * q + i] = acc[FH + f + q][j][i];
+        finish_run<E, FN, MODE, 4 * P>(a, row, c, x, y);
+      }
+    }
+    if (!more) break;
+  }
+  // no direct load may be in flight when the workgroup's LDS is given to another one
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// Few tokens: up to 16 FNT rows, 16 columns of each product a workgroup.  Its KS waves share k in chunks of 256 bytes and read the
+// weights straight into the registers of the MFMA (64 bytes of a row in four lanes), the next chunk under the products of one; nothing
+// is read twice but X, which is small.  The waves' sums are added up in a fixed order.
+template <class E, int FNT, int KS, int FN, int MODE>
+__global__ void __launch_bounds__(KS * 64) narrow_kernel(ProjArgs a) {
+  constexpr int kPer = 16 / (int)sizeof(E), kStep = 4 * kPer, kSteps = 4, kChunk = kSteps * kStep;
+  __shared__ f32x4 part[KS][2 * FNT][64];
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c0 = blockIdx.x * 16;
+  // columns past the last read its weights, and their results are not written
+  const int64_t row = c0 + r < a.F ? c0 + r : a.F - 1;
+  const E* wg = static_cast<const E*>(a.Wg) + row * a.ldw + g * kPer;
+  const E* wu = static_cast<const E*>(a.Wu) + row * a.ldw + g * kPer;
+  const E* x[FNT];
+#pragma unroll
+  for (int j = 0; j < FNT; ++j) x[j] = static_cast<const E*>(a.X) + (int64_t)(j * 16 + r < a.T ? j * 16 + r : 0) * a.ldx + g * kPer;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  f32x4 ag[FNT], au[FNT];
+#pragma unroll
+  for (int j = 0; j < FNT; ++j) ag[j] = au[j] = zero;
+  f32x4 fg[kSteps], fu[kSteps], fx[kSteps][FNT];
+  auto load = [&](int k0) {
+    const bool whole = k0 + kChunk <= a.n;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int k = k0 + s * kStep;
+      const bool in = whole || k + g * kPer < a.n;
+      fg[s] = fu[s] = zero;
+      if (in) {
+        fg[s] = *reinterpret_cast<const f32x4*>(wg + k);
+        fu[s] = *reinterpret_cast<const f32x4*>(wu + k);
+      }
+#pragma unroll
+      for (int j = 0; j < FNT; ++j) {
+        fx[s][j] = zero;
+        if (in && j * 16 + r < a.T) fx[s][j] = *reinterpret_cast<const f32x4*>(x[j] + k);
+      }
+    }
+  };
+  int k0 = wave * kChunk;
+  if (k0 < a.n) load(k0);
+  while (k0 < a.n) {
+    f32x4 cg[kSteps], cu[kSteps], cx[kSteps][FNT];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      cg[s] = fg[s], cu[s] = fu[s];
+#pragma unroll
+      for (int j = 0; j < FNT; ++j) cx[s][j] = fx[s][j];
+    }
+    k0 += KS * kChunk;
+    if (k0 < a.n) load(k0);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int q = 0; q < Mma<E>::kSteps; ++q)
+#pragma unroll
+        for (int j = 0; j < FNT; ++j) {
+          ag[j] = Mma<E>::step(q, cg[s], cx[s][j], ag[j]);
+          au[j] = Mma<E>::step(q, cu[s], cx[s][j], au[j]);
+        }
+  }
+#pragma unroll
+  for (int j = 0; j < FNT; ++j) part[wave][2 * j][lane] = ag[j], part[wave][2 * j + 1][lane] = au[j];
+  __syncthreads();
+  if (wave >= FNT) return;
+  f32x4 sg = part[0][2 * wave][lane], su = part[0][2 * wave + 1][lane];
+#pragma unroll
+  for (int w = 1; w < KS; ++w) sg += part[w][2 * wave][lane], su += part[w][2 * wave + 1][lane];
+  const int t = wave * 16 + r, c = c0 + g * 4;
+  if (t >= a.T || c >= a.F) return;
+  float vg[4], vu[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) vg[i] = sg[i], vu[i] = su[i];
+  finish_run<E, FN, MODE, 4>(a, t, c, vg, vu);
+}
+
+struct GradArgs {
+  const void* A[2];       // dX: Wg, Wu; dW: X
+  const void* B[2];       // dG, dU
+  int64_t lda, ldb;
+  int M, N, K;            // dX: n, T, F (of each half of the sum); dW: n, F (of each result), T
+  int tm, tn;             // tiles along i, and j (dW: of one result)
+  int kt, kt_split;       // k tiles (dX: of each half), and those of one split
+  int splits;
+  void* out[2];           // dX: the first; dW: dWg, dWu
+  int64_t ldo;
+  float beta;
+  float* part;            // with splits > 1: [splits][N, dW: 2 N][M] fp32
+};
+
+// TRB: dB stored along j (dW); otherwise along k (dX).
+template <class E, int BM, int BN, int WVM, int WVN, int NB, bool TRB, int WPE>
+__global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs a) {
+  constexpr int NW = WVM * WVN;
+  constexpr int TM = BM / WVM, TN = BN / WVN;
+  constexpr int FM = TM / 16, FNT = TN / 16;
+  typedef Operand<E, BM, NW, true, 0> OpA;
+  typedef Operand<E, BN, NW, TRB, 0> OpB;
+  constexpr int kBuf = OpA::kBytes + OpB::kBytes;
+  constexpr int kLoads = OpA::kLoads + OpB::kLoads;
+  constexpr int kK = OpA::kK;
+  constexpr int kReads = FM * OpA::kReads + FNT * OpB::kReads;
+  constexpr int kMmas = FM * FNT * (sizeof(E) == 2 ? 1 : 4);
+  constexpr int kHalves = TRB ? 1 : 2, kOuts = TRB ? 2 : 1;
+  __shared__ __align__(1024) char lds[NB * kBuf];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WVM, wn = wave / WVM;
+  const int tiles = a.tm * a.tn * kOuts, total = tiles * a.splits;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+
+  OpA oa;
+  OpB ob;
+  oa.init(a.lda, wave, lane);
+  ob.init(a.ldb, wave, lane);
+  int i0, j0, which, split, nk;          // the tile whose operands are being read; nk: its k tiles of a half
+  int i_next, j_next, which_next, split_next;
+  uint64_t second_a = 0, second_b = 0;   // where the second half starts
+  auto place = [&](int wg) {
+    const int id = xent::share_of(wg, total);
+    split_next = id / tiles;
+    int im, in;
+    xent::tile_of(id - split_next * tiles, a.tm, a.tn * kOuts, &im, &in);
+    which_next = kOuts == 2 && in >= a.tn;
+    i_next = im * BM, j_next = (in - which_next * a.tn) * BN;
+  };
+  // A half's last k tile comes first, so that only the first loads look at its end: the sequence is the last tiles of the
+  // halves, then the others of the first, then those of the second.
+  auto issue_last = [&](int h) {
+    const int last = a.K - (split * a.kt_split + nk - 1) * kK;
+    const unsigned to = lds0 + h * kBuf;
+    oa.issue_last(nk - 1, last < kK ? last : kK, a.lda, i0, a.M, to, wave, lane);
+    ob.issue_last(nk - 1, last < kK ? last : kK, a.ldb, j0, a.N, to + OpA::kBytes, wave, lane);
+  };
+  auto issue = [&](int t, int buf) {
+    if (kHalves == 2 && t == nk + 1) oa.base = second_a, ob.base = second_b;
+    const unsigned to = lds0 + buf * kBuf;
+    oa.issue(t < kHalves * nk, to, wave);
+    ob.issue(t < kHalves * nk, to + OpA::kBytes, wave);
+  };
+  auto start = [&]() {
+    i0 = i_next, j0 = j_next, which = which_next, split = split_next;
+    const int kt0 = split * a.kt_split;
+    nk = a.kt - kt0 < a.kt_split ? a.kt - kt0 : a.kt_split;
+    if constexpr (kHalves == 2) {
+      oa.seek(a.A[1], a.lda, i0, a.M, kt0);
+      ob.seek(a.B[1], a.ldb, j0, a.N, kt0);
+      second_a = oa.base, second_b = ob.base;
+    }
+    oa.seek(a.A[0], a.lda, i0, a.M, kt0);
+    ob.seek(a.B[TRB ? which : 0], a.ldb, j0, a.N, kt0);
+    issue_last(0);
+    if constexpr (kHalves == 2) {
+      const uint64_t first_a = oa.base, first_b = ob.base;
+      oa.base = second_a, ob.base = second_b;
+      issue_last(1);
+      oa.base = first_a, ob.base = first_b;
+    }
+#pragma unroll
+    for (int t = kHalves; t < (NB == 2 ? 2 : NB - 1); ++t) issue(t, t);
+  };
+
+  place(blockIdx.x);
+  start();
+  for (int wg = blockIdx.x;;) {
+    place(wg + gridDim.x);
+    const int nkt = kHalves * nk;
+    f32x4 acc[FM][FNT];
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+      for (int j = 0; j < FNT; ++j) acc[f][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr bool kBlocked = sizeof(E) == 4;
+    f32x4 sum[kBlocked ? FM : 1][kBlocked ? FNT : 1] = {};
+    auto close_block = [&](bool end) {
+      if constexpr (kBlocked) {
+        if (!end) return;
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int j = 0; j < FNT; ++j) {
+            sum[f][j] += acc[f][j];
+            acc[f][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+      }
+    };
+    auto read = [&](int buf, int kk, f32x4 (&fa)[FM], f32x4 (&fb)[FNT]) {
+      const char* la = lds + buf * kBuf;
+#pragma unroll
+      for (int j = 0; j < FNT; ++j) fb[j] = OpB::read(la + OpA::kBytes, wn * TN, j, kk, lane);
+#pragma unroll
+      for (int f = 0; f < FM; ++f) fa[f] = OpA::read(la, wm * TM, f, kk, lane);
+    };
+    auto multiply = [&](const f32x4 (&fa)[FM], const f32x4 (&fb)[FNT]) {
+#pragma unroll
+      for (int k = 0; k < Mma<E>::kSteps; ++k)
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int j = 0; j < FNT; ++j) acc[f][j] = Mma<E>::step(k, fa[f], fb[j], acc[f][j]);
+    };
+    if constexpr (NB == 2) {
+      f32x4 fa[2][FM], fb[2][FNT];
+      ring_wait<kLoads>();
+      read(0, 0, fa[0], fb[0]);
+      for (int t0 = 0; t0 < nkt; t0 += 2) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          if (t0 + b >= nkt) break;
+          read(b, 1, fa[1], fb[1]);
+          multiply(fa[0], fb[0]);
+          xent::interleave<kReads, kMmas>();
+          ring_wait<0>();
+          if (t0 + b + 2 < nkt) issue(t0 + b + 2, b);
+          read(1 - b, 0, fa[0], fb[0]);
+          multiply(fa[1], fb[1]);
+          xent::interleave<kReads, kMmas>();
+          close_block((t0 + b) % 4 == 3);
+        }
+      }
+    } else {
+      for (int t0 = 0; t0 < nkt; t0 += NB) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          if (t0 + b >= nkt) break;
+          ring_wait<(NB - 2) * kLoads>();
+          issue(t0 + b + NB - 1, (b + NB - 1) % NB);
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            f32x4 fa[FM], fb[FNT];
+            read(b, kk, fa, fb);
+            multiply(fa, fb);
+          }
+          close_block((t0 + b) % 4 == 3);
+        }
+      }
+    }
+    if constexpr (kBlocked) {
+#pragma unroll
+      for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int j = 0; j < FNT; ++j) acc[f][j] += sum[f][j];
+    }
+    const int ci = i0 + wm * TM, cj = j0 + wn * TN, out = which, part = split;
+    wg += gridDim.x;
+    const bool more = wg < total;
+    if (more) {
+      ring_wait<0>();      // every wave's reads of the buffers are done
+      start();
+    }
+    const int g = lane >> 4, r = lane & 15;
+#pragma unroll
+    for (int j = 0; j < FNT; ++j) {
+      const int row = cj + j * 16 + r;
+      if (row >= a.N) continue;
+#pragma unroll
+      for (int f = 0; f < FM; ++f) {
+        const int c = ci + f * 16 + g * 4;
+        if (c >= a.M) continue;
+        f32x4 v = acc[f][j];
+        if (a.splits > 1) {
+          store4(a.part + (((int64_t)part * kOuts + out) * a.N + row) * a.M + c, v);
+        } else {
+          E* p = static_cast<E*>(a.out[out]) + (int64_t)row * a.ldo + c;
+          if (a.beta != 0.f) v += a.beta * load4(p);
+          store4(p, v);
+        }
+      }
+    }
+    if (!more) break;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// G and U kept: dG and dU element by element, 16 bytes a thread.
+struct PointArgs {
+  const void* dH;
+  const void* G;
+  const void* U;
+  void* dG;
+  void* dU;
+  int64_t lddh, ldg, lddg;
+  int64_t first, items;   // pieces of 16 bytes
+  int pieces;             // of a row
+};
+
+template <class E, int FN>
+__global__ void __launch_bounds__(256) point_kernel(PointArgs a) {
+  constexpr int W = 16 / (int)sizeof(E);
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= a.items) return;
+  const int64_t item = a.first + at;
+  const int64_t t = item <= 0xffffffffll ? (int64_t)((unsigned)item / (unsigned)a.pieces) : item / a.pieces;
+  const int c = (int)(item - t * a.pieces) * W;
+  float g[W], u[W], x[W];
+  load_run<W>(static_cast<const E*>(a.G) + t * a.ldg + c, g);
+  load_run<W>(static_cast<const E*>(a.U) + t * a.ldg + c, u);
+  load_run<W>(static_cast<const E*>(a.dH) + t * a.lddh + c, x);
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    const float2 f = gated<FN, sizeof(E) == 2>(g[i]);
+    g[i] = x[i] * u[i] * f.y;
+    u[i] = x[i] * f.x;
+  }
+  store_run<W>(static_cast<E*>(a.dG) + t * a.lddg + c, g);
+  store_run<W>(static_cast<E*>(a.dU) + t * a.lddg + c, u);
+}
+
+// tile: xent::Tile, or the few-token kernel (ks waves) where ks > 0
+hipError_t launch_projection(int bf16, int fn, int mode, int tile, int ks, const ProjArgs& a, hipStream_t s);
+hipError_t launch_point(int bf16, int fn, const PointArgs& a, hipStream_t s);
+hipError_t launch_gradient(int bf16, int trb, int tile, const GradArgs& a, hipStream_t s);
+
+}  // namespace glu
+}  // namespace ff

@@ -1,0 +1,79 @@
+"""Which kernels, tiles and splits the sizes of test_gpu_glu.py run (csrc/glu_plan.h, compiled and asked on the CPU), so that a change
+of a cost table cannot take a kernel out of the tests unnoticed; and the calls that are refused on the host."""
+import ctypes
+import os
+import shutil
+import subprocess
+
+import pytest
+
+pytest.importorskip("torch")
+from paper_2608_26430_amd import binding  # noqa: E402
+from tests.test_gpu_glu import BIG, SIZES  # noqa: E402
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+LARGE, MEDIUM, SMALL = 0, 1, 2
+
+
+@pytest.fixture(scope="module")
+def plans(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    exe = str(tmp_path_factory.mktemp("plans") / "glu_plans")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I" + os.path.join(ROOT, "include"),
+                    "-I" + os.path.join(ROOT, "paper_2608_26430_amd", "csrc"), os.path.join(HERE, "plans", "glu_plans.cpp"),
+                    "-o", exe], check=True, timeout=300)
+
+    def ask(T, n, F, bf16):
+        w = subprocess.run([exe], input=f"{T} {n} {F} {int(bf16)}\n", capture_output=True, text=True, check=True, timeout=60).stdout
+        w = [int(x) for x in w.split()]
+        return dict(proj=w[0], ks=w[1], proj_tiles=w[2], dx=w[3], dx_splits=w[4], dx_tiles=w[6], dw=w[7], dw_splits=w[8], dw_tiles=w[10])
+
+    return ask
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_sizes_run_every_kernel(plans, bf16):
+    p = [plans(*s, bf16) for s in SIZES + (BIG if bf16 else [])]
+    assert {q["ks"] for q in p} >= {0, 4, 8, 16}
+    # few tokens: one and two groups of 16, with each number of waves that both run
+    few = {(plans(*s, bf16)["ks"], s[0] > 16) for s in SIZES if s[0] <= 32}
+    assert few == {(4, False), (8, False), (16, False), (4, True), (8, True)}, few
+    tiles = {MEDIUM, SMALL} | ({LARGE} if bf16 else set())
+    assert {q["proj"] for q in p if q["ks"] == 0} == tiles
+    assert {q["dx"] for q in p} == tiles and {q["dw"] for q in p} == tiles
+    for k in ("dx", "dw"):
+        assert {q[k + "_splits"] > 1 for q in p} == {True, False}
+    if bf16:       # large tiles, more of them than workgroups
+        for k in ("proj", "dx", "dw"):
+            assert any(q[k] == LARGE and q[k + "_tiles"] > 256 and (k != "proj" or q["ks"] == 0) for q in p), k
+
+
+def test_calls_refused_on_the_host():
+    lib, q = binding._load(), 1 << 20
+    p = ctypes.c_void_p(q)
+
+    def fwd(T=4, n=64, F=32, act=1, fn=0, X=p, ldx=64, Wg=p, Wu=p, ldw=64, Ag=None, Au=None, lda=32, H=p, ldh=32, G=None, U=None, ldg=32):
+        return binding._STATUS[lib.ff_glu_fwd(T, n, F, act, fn, X, ldx, Wg, Wu, ldw, Ag, Au, lda, H, ldh, G, U, ldg, None)]
+
+    odd = ctypes.c_void_p(q + 8)
+    for kw in (dict(T=-1), dict(T=(1 << 28) + 1), dict(n=60), dict(n=0), dict(F=36), dict(F=(1 << 18) + 8), dict(act=2), dict(fn=3),
+               dict(fn=-1), dict(X=None), dict(ldx=56), dict(ldx=68), dict(ldx=(1 << 20) + 8), dict(Wg=None), dict(Wu=odd), dict(ldw=60),
+               dict(Ag=odd), dict(Au=p, lda=24), dict(H=None), dict(ldh=36), dict(G=p), dict(U=p), dict(G=p, U=p, ldg=24)):
+        assert fwd(**kw) == "FF_EINVAL", kw
+    assert fwd(T=0, X=None, H=None) == "FF_OK"
+
+    def bwd(T=4, dH=p, X=p, Wg=p, Wu=p, G=p, U=p, dG=p, dU=p, dX=p, dWg=None, dWu=None, lddw=64, ws=p, wsn=1 << 30):
+        return binding._STATUS[lib.ff_glu_bwd(T, 64, 32, 1, 0, dH, 32, X, 64, Wg, Wu, 64, None, None, 32, G, U, 32, dG, dU, 32, 0.0, dX,
+                                              64, 0.0, dWg, dWu, lddw, ws, wsn, None)]
+
+    for kw in (dict(dH=None), dict(G=None), dict(U=None), dict(G=None, U=None, X=None), dict(dG=None), dict(dU=odd), dict(dX=odd),
+               dict(dWg=p), dict(dWg=p, dWu=p, X=None), dict(Wg=None), dict(dWg=p, dWu=p, lddw=60), dict(ws=None),
+               dict(ws=ctypes.c_void_p(q + 16)), dict(wsn=0)):
+        assert bwd(**kw) == "FF_EINVAL", kw
+    assert bwd(T=0, dH=None, dG=None, dX=None) == "FF_OK"
+    v = ctypes.c_int64()
+    for a in ((4, 64, 32, 1, 4), (4, 64, 32, 1, -1), (4, 63, 32, 1, 1), (4, 64, 32, 3, 1)):
+        assert binding._STATUS[lib.ff_glu_workspace(*a, ctypes.byref(v))] == "FF_EINVAL"
+    assert binding._STATUS[lib.ff_glu_workspace(4, 64, 32, 1, 3, None)] == "FF_EINVAL"

@@ -1,0 +1,313 @@
+"""The gated feed-forward (ff_glu_fwd, ff_glu_bwd) against the definitions in 64 bits, stage by stage: each stage's reference takes
+what the stage before has stored.
+
+Bounds per element, u the type's unit roundoff, v = 2^-24.  A product summed over n in fp32, in any order, is off by at most (n + 4) v
+times the sum of its absolute terms (and of what is added).  f and its factors: a few ulp (2^-23) relative, times the argument's size
+where it enters an exponential: f by rf = (2 |z| + 8) 2^-23 relative, z the exponent's argument, f' by rf of the sum of its absolute
+terms.  |f'| <= 1.13 and |f''| <= 1.2 for the three functions carry the argument's error on.  Results add u of themselves."""
+import math
+
+import pytest
+
+from paper_2608_26430_amd import inputs
+from tests.parity_util import torch_act
+
+torch = pytest.importorskip("torch")
+import paper_2608_26430_amd as ff  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+V = 2.0 ** -24
+U = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+FNS = ("silu", "gelu", "gelu_tanh")
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+    return torch.device("cuda:0")
+
+
+def f_of(fn, g):
+    """f, f', and the error bounds of both as the kernels compute them."""
+    if fn == "silu":
+        s = torch.sigmoid(g)
+        t = (g * s * (1 - s)).abs()
+        f, df, z = g * s, s + g * s * (1 - s), g.abs()
+    elif fn == "gelu":
+        s = 0.5 * torch.erfc(-g / math.sqrt(2))
+        t = (g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)).abs()
+        f, df, z = g * s, s + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi), g * g
+    else:
+        c = math.sqrt(2 / math.pi)
+        s = torch.sigmoid(2 * c * (g + 0.044715 * g ** 3))
+        d = g * s * (1 - s) * 2 * c * (1 + 3 * 0.044715 * g * g)
+        f, df, t, z = g * s, s + d, d.abs(), 2 * c * (g + 0.044715 * g ** 3).abs()
+    rf = (2 * z + 8) * 2 * V
+    # a factor s (and 1 - s, an exponential) below the least normal number, 2^-126, may be taken as 0: f = g s is then off by 2^-126 |g|,
+    # f' = s + g s' by 2^-126 (1 + |g| max(1, dz/dg)), where s' = s (1 - s) dz/dg or the exponential itself
+    dz = 2 * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * g * g) if fn == "gelu_tanh" else 1.0
+    tiny = 2.0 ** -126
+    return f, df, rf * f.abs() + tiny * g.abs() + 1e-37, rf * (s + t) + tiny * (1 + g.abs() * dz) + 1e-37
+
+
+def mm(a, b):
+    return a.double() @ b.double()
+
+
+def close(got, want, bound, what):
+    err = (got.double() - want).abs()
+    bad = ~(err <= bound * 1.02 + 1e-37)
+    assert not bool(bad.any()), (what, int(bad.sum()), float((err / (bound + 1e-37)).max()))
+
+
+def data(T, n, F, dtype, dev, seed, adapters=False):
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(seed)
+    dt = DT[dtype]
+
+    def randn(*s):
+        return torch.randn(s, generator=gen, device=dev)
+    d = dict(X=randn(T, n).to(dt), Wg=(randn(F, n) * 2 / math.sqrt(n)).to(dt), Wu=(randn(F, n) / math.sqrt(n)).to(dt),
+             dH=randn(T, F).to(dt), Ag=None, Au=None)
+    if adapters:
+        d["Ag"], d["Au"] = randn(T, F).to(dt), randn(T, F).to(dt)
+    return d
+
+
+def forward_reference(d, fn):
+    X, n = d["X"], d["X"].shape[1]
+    out = []
+    for w, a in (("Wg", "Ag"), ("Wu", "Au")):
+        p = mm(X, d[w].t())
+        s = mm(X.abs(), d[w].abs().t())
+        if d[a] is not None:
+            p, s = p + d[a].double(), s + d[a].double().abs()
+        out += [p, (n + 4) * V * s]
+    return out
+
+
+def check_forward(d, fn, H, G=None, U_=None):
+    u = U[d["X"].dtype]
+    g, eg, p, ep = forward_reference(d, fn)
+    f, df, ef, _ = f_of(fn, g)
+    ef = ef + 1.13 * eg
+    close(H, f * p, u * (f * p).abs() + ef * p.abs() + (f.abs() + ef) * ep + 2 * V * (f * p).abs(), "H")
+    if G is not None:
+        close(G, g, u * g.abs() + eg, "G")
+        close(U_, p, u * p.abs() + ep, "U")
+
+
+def check_point(d, fn, dG, dU, g, eg, p, ep):
+    """dG and dU from g and p, known to eg and ep."""
+    u, x = U[d["X"].dtype], d["dH"].double()
+    f, df, ef, edf = f_of(fn, g)
+    ef, edf = ef + 1.13 * eg, edf + 1.2 * eg
+    close(dU, x * f, u * (x * f).abs() + x.abs() * ef + 2 * V * (x * f).abs(), "dU")
+    close(dG, x * p * df, u * (x * p * df).abs() + x.abs() * (p.abs() * edf + (df.abs() + edf) * ep) + 3 * V * (x * p * df).abs(), "dG")
+
+
+def check_products(d, dG, dU, dX, dWg=None, dWu=None, beta=0.0, oX=None, oWg=None, oWu=None):
+    """dX and the weights' gradients from the stored dG and dU, with beta times what was there."""
+    u, (T, n), F = U[d["X"].dtype], d["X"].shape, d["Wg"].shape[0]
+    if dX is not None:
+        want, s = mm(dG, d["Wg"]) + mm(dU, d["Wu"]), mm(dG.abs(), d["Wg"].abs()) + mm(dU.abs(), d["Wu"].abs())
+        old = beta * oX.double() if beta else torch.zeros_like(want)
+        close(dX, want + old, u * (want + old).abs() + (2 * F + 4) * V * s + 2 * V * old.abs(), "dX")
+    for g, w, o, name in ((dG, dWg, oWg, "dWg"), (dU, dWu, oWu, "dWu")):
+        if w is not None:
+            want, s = mm(g.t().contiguous(), d["X"]), mm(g.abs().t().contiguous(), d["X"].abs())
+            old = beta * o.double() if beta else torch.zeros_like(want)
+            close(w, want + old, u * (want + old).abs() + (T + 4) * V * s + 2 * V * old.abs(), name)
+
+
+def whole(d, fn, want_dw=True):
+    """A kept step and one that makes G and U again, both checked."""
+    H, G, P = ff.glu_fwd(d["X"], d["Wg"], d["Wu"], fn, d["Ag"], d["Au"], save=True)
+    alone = ff.glu_fwd(d["X"], d["Wg"], d["Wu"], fn, d["Ag"], d["Au"])
+    kept = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], fn, G=G, U=P, want_dw=want_dw)
+    made = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], fn, Ag=d["Ag"], Au=d["Au"], want_dw=want_dw)
+    torch.cuda.synchronize()
+    assert torch.equal(H, alone)
+    check_forward(d, fn, H, G, P)
+    zero = torch.zeros((), device=G.device, dtype=torch.float64)
+    check_point(d, fn, kept[0], kept[1], G.double(), zero, P.double(), zero)
+    check_point(d, fn, made[0], made[1], *forward_reference(d, fn))
+    check_products(d, *kept)
+    check_products(d, *made)
+    return kept, made
+
+
+# few tokens (one to 32, with 4, 8 and 16 waves sharing k, k shorter than a chunk and ragged, columns that end inside a tile), small,
+# medium and large tiles, splits of k for dX and dW; test_glu_plans.py says which size runs what
+SIZES = [(1, 8, 8), (1, 4096, 1032), (5, 136, 24), (16, 1000, 104), (17, 1000, 4104), (32, 520, 2056), (31, 2048, 72), (3, 8, 8200),
+         (2, 264, 8200), (33, 64, 64), (100, 520, 1000), (300, 128, 1400), (1500, 136, 136), (129, 1032, 2056), (700, 1032, 1544),
+         (1003, 768, 2304), (257, 2048, 136), (7, 520, 4104), (20, 64, 520),
+         (900, 1024, 4096)]
+BIG = [(2003, 1024, 4096), (4200, 2056, 11016), (2104, 4104, 11016)]
+
+
+@pytest.mark.parametrize("T,n,F", SIZES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sizes(dev, T, n, F, dtype):
+    for i, fn in enumerate(FNS):
+        d = data(T, n, F, dtype, dev, T + n + F + i, adapters=(i + T) % 2 == 0)
+        whole(d, fn)
+
+
+@pytest.mark.parametrize("T,n,F", BIG)
+def test_large_tiles_and_walks(dev, T, n, F):
+    """256 x 256 tiles, more of them than workgroups, in every product; two runs give the same bits."""
+    d = data(T, n, F, "bf16", dev, T, adapters=True)
+    kept, _ = whole(d, "silu")
+    H, G, P = ff.glu_fwd(d["X"], d["Wg"], d["Wu"], "silu", d["Ag"], d["Au"], save=True)
+    again = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], "silu", G=G, U=P, want_dw=True)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(kept, again))
+
+
+@pytest.mark.parametrize("T,n,F", [(9, 264, 136), (70, 264, 136), (300, 520, 776)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_halves_of_one_weight_and_accumulation(dev, T, n, F, dtype):
+    """Weights as halves of one, rows inside wider ones, one adapter alone, results added to; nothing outside the rows is written
+    or used (NaN there)."""
+    d = data(T, n, F, dtype, dev, T, adapters=True)
+    dt = DT[dtype]
+
+    def inside(t, more):
+        buf = torch.full((t.shape[0] + 1, t.shape[1] + more), float("nan"), device=dev, dtype=dt)
+        buf[:t.shape[0], :t.shape[1]] = t
+        return buf[:t.shape[0], :t.shape[1]], buf
+    both = torch.full((2 * F + 1, n + 16), float("nan"), device=dev, dtype=dt)
+    both[:F, :n], both[F:2 * F, :n] = d["Wg"], d["Wu"]
+    Wg, Wu = both[:F, :n], both[F:2 * F, :n]
+    X, dH, Au = (inside(d[k], m)[0] for k, m in (("X", 8), ("dH", 24), ("Au", 16)))
+    d["Ag"] = None
+    outs = {k: inside(torch.zeros(s, device=dev, dtype=dt), 8) for k, s in (("H", (T, F)), ("G", (T, F)), ("U", (T, F)), ("dG", (T, F)),
+                                                                            ("dU", (T, F)))}
+    o = {k: v[0] for k, v in outs.items()}
+    ff.glu_fwd(X, Wg, Wu, "gelu_tanh", Au=Au, H=o["H"], G=o["G"], U=o["U"], save=True)
+    old = {k: torch.randn(s, device=dev).to(dt) for k, s in (("dX", (T, n)), ("dWg", (F, n)), ("dWu", (F, n)))}
+    grads = {k: inside(t, 32) for k, t in old.items()}
+    ff.glu_bwd(dH, X, Wg, Wu, "gelu_tanh", G=o["G"], U=o["U"], dG=o["dG"], dU=o["dU"], dX=grads["dX"][0], dWg=grads["dWg"][0],
+               dWu=grads["dWu"][0], beta_dx=0.5, beta_dw=0.5, want_dw=True)
+    torch.cuda.synchronize()
+    check_forward(d, "gelu_tanh", o["H"], o["G"], o["U"])
+    zero = torch.zeros((), device=dev, dtype=torch.float64)
+    check_point(d, "gelu_tanh", o["dG"], o["dU"], o["G"].double(), zero, o["U"].double(), zero)
+    check_products(d, o["dG"], o["dU"], *(grads[k][0] for k in ("dX", "dWg", "dWu")), 0.5, *(old[k] for k in ("dX", "dWg", "dWu")))
+    for k, (t, buf) in {**outs, **grads}.items():
+        assert bool(buf[t.shape[0]:].isnan().all()) and bool(buf[:, t.shape[1]:].isnan().all()), k
+    # dG over dH, and made again
+    dU = inside(torch.zeros((T, F), device=dev, dtype=dt), 24)[0]
+    dG, dU, _, _, _ = ff.glu_bwd(dH, X, Wg, Wu, "gelu_tanh", Au=Au, dG=dH, dU=dU, want_dx=False)
+    torch.cuda.synchronize()
+    check_point(d, "gelu_tanh", dG, dU, *forward_reference(d, "gelu_tanh"))
+
+
+def test_dg_and_du_over_what_was_kept(dev):
+    d = data(130, 256, 512, "bf16", dev, 1)
+    H, G, P = ff.glu_fwd(d["X"], d["Wg"], d["Wu"], save=True)
+    want = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], G=G, U=P)
+    got = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], G=G, U=P, dG=G, dU=P)
+    torch.cuda.synchronize()
+    assert got[0] is G and all(torch.equal(a, b) for a, b in zip(want[:3], got[:3]))
+
+
+def test_large_arguments(dev):
+    """|G| up to some hundred: f ends in 0 or the argument, no NaN; bf16 and fp32, tiles and few tokens."""
+    for dtype in ("bf16", "f32"):
+        for T in (4, 200):
+            d = data(T, 64, 128, dtype, dev, T)
+            d["X"] = d["X"] * 60
+            for fn in FNS:
+                whole(d, fn)
+
+
+def test_end_to_end_gradient_against_differences(dev):
+    """The loss sum(H R) in fp32: its difference along a direction is the gradients' product with it."""
+    T, n, F = 40, 64, 96
+    for fn in FNS:
+        d = data(T, n, F, "f32", dev, 3, adapters=True)
+        _, _, dX, dWg, dWu = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], fn, Ag=d["Ag"], Au=d["Au"], want_dw=True)
+        torch.cuda.synchronize()
+        for name, grad in (("X", dX), ("Wg", dWg), ("Wu", dWu)):
+            step = torch.randn_like(d[name]).double()
+            step /= step.norm()
+
+            def loss(h):
+                e = {k: None if v is None else v.double() for k, v in d.items()}
+                e[name] = e[name] + h * step
+                g, p = e["X"] @ e["Wg"].t() + e["Ag"], e["X"] @ e["Wu"].t() + e["Au"]
+                return float((f_of(fn, g)[0] * p * e["dH"]).sum())
+            want = (loss(1e-5) - loss(-1e-5)) / 2e-5
+            got = float((grad.double() * step).sum())
+            # the gradients' own errors: (n + F) v of their absolute sums, 1e-5 relative at these sizes
+            assert abs(got - want) <= 1e-5 * float((grad.double() * step).abs().sum()) + 1e-6, (fn, name)
+
+
+def test_no_tokens(dev):
+    X = torch.empty((0, 64), device=dev)
+    W = torch.ones((32, 64), device=dev)
+    e = torch.empty((0, 32), device=dev)
+    H = ff.glu_fwd(X, W, W)
+    dG, dU, dX, dWg, dWu = ff.glu_bwd(e, X, W, W, want_dw=True)
+    torch.cuda.synchronize()
+    assert H.shape == (0, 32) and dX.shape == (0, 64) and not bool(dWg.any()) and not bool(dWu.any())
+    a, b = torch.full((32, 64), 2.0, device=dev), torch.full((32, 64), 4.0, device=dev)
+    ff.glu_bwd(e, X, W, W, dWg=a, dWu=b, beta_dw=0.5, want_dw=True)
+    torch.cuda.synchronize()
+    assert bool((a == 1).all()) and bool((b == 2).all())
+
+
+def test_refusals(dev):
+    d = data(8, 64, 32, "bf16", dev, 1)
+    X, Wg, Wu = d["X"], d["Wg"], d["Wu"]
+    bad = [lambda: ff.glu_fwd(X, Wg, Wu, "relu"), lambda: ff.glu_fwd(X, Wg, Wu[:16]), lambda: ff.glu_fwd(X, Wg.float(), Wu.float()),
+           lambda: ff.glu_fwd(X, Wg, Wu, Ag=torch.zeros((8, 33), device=dev, dtype=X.dtype)),
+           lambda: ff.glu_fwd(X, Wg, torch.zeros((32, 72), device=dev, dtype=X.dtype)[:, :64]),
+           lambda: ff.glu_fwd(X[0], Wg, Wu), lambda: ff.glu_bwd(d["dH"], X, Wg, Wu, G=d["dH"]),
+           lambda: ff.glu_bwd(d["dH"].float(), X, Wg, Wu), lambda: ff.glu_bwd(d["dH"], X, Wg, Wu, beta_dx=1.0)]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    for T, n, F in ((8, 60, 32), (8, 64, 36)):
+        e = data(T, n, F, "bf16", dev, 1)
+        with pytest.raises(ff.FrameFTError) as ei:
+            ff.glu_fwd(e["X"], e["Wg"], e["Wu"])
+        assert ei.value.name == "FF_EINVAL"
+    with pytest.raises(ff.FrameFTError):
+        ff.glu_fwd(torch.zeros((8, 72), device=dev, dtype=X.dtype)[:, 1:65], Wg, Wu)      # off 16-byte alignment
+    with pytest.raises(ff.FrameFTError):
+        ff.glu_bwd(d["dH"], X, Wg, Wu, workspace=torch.empty(16, dtype=torch.uint8, device=dev))
+
+
+def test_captured_and_replayed(dev):
+    """Forward and backward captured once and replayed with new values, eager calls with another workspace between, on the default and
+    on another stream."""
+    d = data(600, 1024, 2048, "bf16", dev, 1, adapters=True)
+    ws, ws2 = (ff.glu_workspace(600, 1024, 2048, torch.bfloat16, True, True) for _ in range(2))
+
+    def step(ws, stream=None):
+        H, G, P = ff.glu_fwd(d["X"], d["Wg"], d["Wu"], "silu", d["Ag"], d["Au"], save=True, stream=stream)
+        return (H, G, P) + ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], "silu", G=G, U=P, want_dw=True, workspace=ws, stream=stream)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(ws)
+    for seed in range(3):
+        new = data(600, 1024, 2048, "bf16", dev, seed + 5, adapters=True)
+        for k in d:
+            d[k].copy_(new[k])
+        graph.replay()
+        eager = step(ws2)
+        torch.cuda.synchronize()
+        other = step(ws2, side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) and torch.equal(b, c) for a, b, c in zip(out, eager, other))
