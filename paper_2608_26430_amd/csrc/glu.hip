@@ -95,6 +95,7 @@ hipError_t run_projection(const Call& c, int mode, ProjArgs a, hipStream_t s) {
   const int kk = kk_of(c.bf16 ? 2 : 4), bm = xent::tile_m(p.tile) / 2, bn = xent::tile_n(p.tile);
   a.F = (int)c.F, a.T = (int)c.T, a.n = (int)c.n;
   a.tm = (int)(up(c.F, bm) / bm), a.tn = (int)(up(c.T, bn) / bn), a.kt = (int)(up(c.n, kk) / kk);
+  a.rest = p.ks ? 0 : rest_of(p.tile, a.tm * a.tn);
   return launch_projection(c.bf16, c.fn, mode, p.tile, p.ks, a, s);
 }
 

@@ -35,6 +35,7 @@ struct ProjArgs {
   int64_t ldw, ldx;
   int F, T, n;            // columns and rows of the results, length of the sums
   int tm, tn;             // tiles along the columns and the rows
+  int rest;               // of them, those that are halved (at most as many as half of the workgroups)
   int kt;                 // k tiles
   const void* Ag;         // NULL: none
   const void* Au;
@@ -58,9 +59,25 @@ __device__ __forceinline__ float2 gated(float g) {
     const float s = inverse(1.f + exp_of(-g, FAST), FAST);
     return make_float2(g * s, s * fmaf(g, 1.f - s, 1.f));
   } else if constexpr (FN == FF_GLU_GELU) {
-    // erfc keeps the digits of f where g is far below zero
-    const float cdf = 0.5f * erfcf(g * -0.70710678118654752f);
-    return make_float2(g * cdf, fmaf(g, 0.39894228040143268f * exp_of(-0.5f * g * g, FAST), cdf));
+    const float e = exp_of(-0.5f * g * g, FAST);
+    float cdf;
+    if constexpr (FAST) {
+      // erfc(x) = exp(-x^2) Q(1 / (1 + 0.33 x)) for x = |g| / sqrt 2: Q is a polynomial fitted here to the least relative error over
+      // x from 0 to 10, 1e-7 (4e-7 in fp32 arithmetic).  The library's erfc took 7 of 41 us (2003 tokens, 1024 -> 4096).
+      const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.33f * 0.70710678118654752f, 1.f));
+      float q = fmaf(t, -0.135348532f, 0.460249317f);
+      q = fmaf(t, q, -0.351171446f);
+      q = fmaf(t, q, 0.408520793f);
+      q = fmaf(t, q, 0.0472091254f);
+      q = fmaf(t, q, 0.201227576f);
+      q = fmaf(t, q, 0.182955311f);
+      q = fmaf(t, q, 0.186357848f);
+      const float half = 0.5f * t * q * e;
+      cdf = g < 0.f ? half : 1.f - half;
+    } else {
+      cdf = 0.5f * erfcf(g * -0.70710678118654752f);   // keeps the digits of f where g is far below zero
+    }
+    return make_float2(g * cdf, fmaf(g, 0.39894228040143268f * e, cdf));
   } else {
     // sqrt(2 / pi) (g + 0.044715 g^3), whose tanh is 2 s - 1
     constexpr float c = 0.79788456080286536f;
@@ -107,21 +124,39 @@ __device__ __forceinline__ void store_run(float* p, const float (&v)[W]) {
   for (int q = 0; q < W; q += 4) store4(p + q, f32x4{v[q], v[q + 1], v[q + 2], v[q + 3]});
 }
 
+// What the end of a tile reads, W columns from c of row t, as it lies in memory: all of a wave's are on their way at once.
+template <class E, int W, int MODE>
+struct RawExtra {
+  typedef unsigned Raw __attribute__((ext_vector_type(W * (int)sizeof(E) / 4)));
+  Raw g, u, x;
+  __device__ __forceinline__ void load(const ProjArgs& a, int64_t t, int c) {
+    if (a.Ag) g = *reinterpret_cast<const Raw*>(static_cast<const E*>(a.Ag) + t * a.lda + c);
+    if (a.Au) u = *reinterpret_cast<const Raw*>(static_cast<const E*>(a.Au) + t * a.lda + c);
+    if constexpr (MODE == kBackward) x = *reinterpret_cast<const Raw*>(static_cast<const E*>(a.dH) + t * a.lddh + c);
+  }
+  static __device__ __forceinline__ float at(const Raw& r, int i) {
+    if constexpr (sizeof(E) == 4) {
+      const unsigned v = r[i];
+      return __builtin_bit_cast(float, v);
+    } else {
+      const unsigned v = r[i / 2];
+      return __builtin_bit_cast(float, i % 2 ? v & 0xffff0000u : v << 16);
+    }
+  }
+};
+
 // The end of W columns from c of row t: what is added, f, and what is written.
 template <class E, int FN, int MODE, int W>
-__device__ __forceinline__ void finish_run(const ProjArgs& a, int64_t t, int c, float (&g)[W], float (&u)[W]) {
+__device__ __forceinline__ void finish_run(const ProjArgs& a, int64_t t, int c, float (&g)[W], float (&u)[W],
+                                           const RawExtra<E, W, MODE>& r) {
   constexpr bool kFast = sizeof(E) == 2;
   if (a.Ag) {
-    float x[W];
-    load_run<W>(static_cast<const E*>(a.Ag) + t * a.lda + c, x);
 #pragma unroll
-    for (int i = 0; i < W; ++i) g[i] += x[i];
+    for (int i = 0; i < W; ++i) g[i] += r.at(r.g, i);
   }
   if (a.Au) {
-    float x[W];
-    load_run<W>(static_cast<const E*>(a.Au) + t * a.lda + c, x);
 #pragma unroll
-    for (int i = 0; i < W; ++i) u[i] += x[i];
+    for (int i = 0; i < W; ++i) u[i] += r.at(r.u, i);
   }
   E* G = static_cast<E*>(a.G) + t * a.ldg + c;
   E* U = static_cast<E*>(a.U) + t * a.ldg + c;
@@ -134,21 +169,21 @@ __device__ __forceinline__ void finish_run(const ProjArgs& a, int64_t t, int c, 
     for (int i = 0; i < W; ++i) g[i] = gated<FN, kFast>(g[i]).x * u[i];
     store_run<W>(static_cast<E*>(a.H) + t * a.ldh + c, g);
   } else {
-    float x[W];
-    load_run<W>(static_cast<const E*>(a.dH) + t * a.lddh + c, x);
 #pragma unroll
     for (int i = 0; i < W; ++i) {
       const float2 f = gated<FN, kFast>(g[i]);
-      g[i] = x[i] * u[i] * f.y;
-      u[i] = x[i] * f.x;
+      const float x = r.at(r.x, i);
+      g[i] = x * u[i] * f.y;
+      u[i] = x * f.x;
     }
     store_run<W>(G, g);
     store_run<W>(U, u);
   }
 }
 
-template <class E, int BM, int BN, int WVM, int WVN, int NB, int WPE, int FN, int MODE>
-__global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArgs a) {
+// A workgroup's share of `total` tiles: numbers wg, wg + step, ..; place(number, &i0, &j0) is where a tile is.
+template <class E, int BM, int BN, int WVM, int WVN, int NB, int FN, int MODE, class Place>
+__device__ __forceinline__ void project(const ProjArgs& a, char* lds, int wg, int step, int total, const Place& place_of) {
   constexpr int NW = WVM * WVN;
   constexpr int TH = BM / 2 / WVM, TN = BN / WVN;        // columns of each product, rows of a wave
   constexpr int FH = TH / 16, FM = 2 * FH, FNT = TN / 16;
@@ -160,12 +195,10 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArg
   constexpr int kK = OpA::kK;
   constexpr int kReads = FM * OpA::kReads + FNT * OpB::kReads;
   constexpr int kMmas = FM * FNT * (sizeof(E) == 2 ? 1 : 4);
-  __shared__ __align__(1024) char lds[NB * kBuf];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WVM, wn = wave / WVM;
-  const int total = a.tm * a.tn;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
   OpA og, ou;
@@ -174,11 +207,7 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArg
   ou.init(a.ldw, wave, lane);
   ob.init(a.ldx, wave, lane);
   int i0, j0, i_next, j_next;
-  auto place = [&](int wg) {
-    int im, in;
-    xent::tile_of(xent::share_of(wg, total), a.tm, a.tn, &im, &in);
-    i_next = im * (BM / 2), j_next = in * BN;
-  };
+  auto place = [&](int at) { place_of(at, &i_next, &j_next); };
   auto issue_last = [&]() {
     const int left = a.n - (a.kt - 1) * kK;
     og.issue_last(a.kt - 1, left, a.ldw, i0, a.F, lds0, wave, lane);
@@ -202,10 +231,10 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArg
     for (int t = 1; t < (NB == 2 ? 2 : NB - 1); ++t) issue(t, t);
   };
 
-  place(blockIdx.x);
+  place(wg);
   start();
-  for (int wg = blockIdx.x;;) {
-    place(wg + gridDim.x);
+  for (;;) {
+    place(wg + step);
     f32x4 acc[FM][FNT];
 #pragma unroll
     for (int f = 0; f < FM; ++f)
@@ -287,34 +316,77 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArg
         for (int j = 0; j < FNT; ++j) acc[f][j] += sum[f][j];
     }
     const int ci = i0 + wm * TH, cj = j0 + wn * TN;
-    wg += gridDim.x;
+    wg += step;
     const bool more = wg < total;
     if (more) {
       ring_wait<0>();      // every wave's reads of the buffers are done
       start();
     }
-    const int g = lane >> 4, r = lane & 15;
-    constexpr int P = PF ? PF : 1;
+    int own = lane;
+    asm volatile("" : "+v"(own));      // places made here, not kept (and spilled) from one tile to the next
+    const int g = own >> 4, r = own & 15;
+    constexpr int P = PF ? PF : 1, W = 4 * P;
+    constexpr int JB = FNT > 2 && sizeof(E) == 2 ? 2 : 1;    // more rows' at once would spill
 #pragma unroll
-    for (int j = 0; j < FNT; ++j) {
-      const int row = cj + j * 16 + r;
-      if (row >= a.T) continue;
+    for (int j0 = 0; j0 < FNT; j0 += JB) {
+      RawExtra<E, W, MODE> extra[JB][FH / P];
+      if (MODE == kBackward || a.Ag || a.Au) {
+        // (rows and columns past the last read those of the last, and are not written)
 #pragma unroll
-      for (int f = 0; f < FH; f += P) {
-        const int c = ci + f * 16 + g * (P * 4);
-        if (c >= a.F) continue;
-        float x[4 * P], y[4 * P];
+        for (int j = 0; j < JB; ++j)
 #pragma unroll
-        for (int q = 0; q < P; ++q)
+          for (int f = 0; f < FH; f += P) {
+            const int row = cj + (j0 + j) * 16 + r, c = ci + f * 16 + g * W;
+            extra[j][f / P].load(a, row < a.T ? row : a.T - 1, c < a.F ? c : a.F - W);
+          }
+      }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[4 * q + i] = acc[f + q][j][i], y[4 * q + i] = acc[FH + f + q][j][i];
-        finish_run<E, FN, MODE, 4 * P>(a, row, c, x, y);
+      for (int j = 0; j < JB; ++j) {
+        const int row = cj + (j0 + j) * 16 + r;
+#pragma unroll
+        for (int f = 0; f < FH; f += P) {
+          const int c = ci + f * 16 + g * W;
+          float x[W], y[W];
+#pragma unroll
+          for (int q = 0; q < P; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * q + i] = acc[f + q][j0 + j][i], y[4 * q + i] = acc[FH + f + q][j0 + j][i];
+          if (row < a.T && c < a.F) finish_run<E, FN, MODE, W>(a, row, c, x, y, extra[j][f / P]);
+        }
       }
     }
     if (!more) break;
   }
   // no direct load may be in flight when the workgroup's LDS is given to another one
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+template <class E, int BM, int BN, int WVM, int WVN, int NB, int WPE, int FN, int MODE>
+__global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArgs a) {
+  __shared__ __align__(1024) char lds[NB * (BM + BN) * xent::kTileBytes];
+  const int full = a.tm * a.tn - a.rest;
+  if ((int)blockIdx.x < full)
+    project<E, BM, BN, WVM, WVN, NB, FN, MODE>(a, lds, blockIdx.x, gridDim.x, full, [&](int at, int* i, int* j) {
+      int im, in;
+      xent::tile_of(xent::share_of(at, full), a.tm, a.tn, &im, &in);
+      *i = im * (BM / 2), *j = in * BN;
+    });
+  // Large tiles: those of a last round that would leave half of the CUs idle go out as halves of fewer rows.
+  if constexpr (BN == 256) {
+    const int halves = 2 * a.rest;
+    if ((int)blockIdx.x >= halves) return;
+    auto half = [&](int at, int* i, int* j) {
+      const int id = xent::share_of(at, halves);
+      int im, in;
+      xent::tile_of(full + id / 2, a.tm, a.tn, &im, &in);
+      *i = im * (BM / 2), *j = in * BN + id % 2 * (BN / 2);
+    };
+    int i, j;
+    half(blockIdx.x, &i, &j);
+    if (j >= a.T) return;          // the second half of a last tile of few rows
+    __syncthreads();
+    project<E, BM, BN / 2, 2 * WVM, WVN / 2, NB, FN, MODE>(a, lds, blockIdx.x, halves, halves, half);
+  }
 }
 
 // Few tokens: up to 16 FNT rows, 16 columns of each product a workgroup.  Its KS waves share k in chunks of 256 bytes and read the
@@ -391,7 +463,9 @@ __global__ void __launch_bounds__(KS * 64) narrow_kernel(ProjArgs a) {
   float vg[4], vu[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) vg[i] = sg[i], vu[i] = su[i];
-  finish_run<E, FN, MODE, 4>(a, t, c, vg, vu);
+  RawExtra<E, 4, MODE> extra;
+  extra.load(a, t, c);
+  finish_run<E, FN, MODE, 4>(a, t, c, vg, vu, extra);
 }
 
 struct GradArgs {

@@ -34,6 +34,12 @@ inline Projection projection(int64_t T, int64_t n, int64_t F, bool bf16) {
   return {xent::choose(2 * F, T, up(n, kk) / kk, false, bf16).tile, 0};
 }
 
+// Of `tiles` tiles those of a last round of large ones that are halved, where their halves fit one round.
+inline int rest_of(int tile, int64_t tiles) {
+  const int rest = (int)(tiles % xent::kCUs);
+  return tile == xent::kLarge && tiles > xent::kCUs && rest <= xent::kCUs / 2 ? rest : 0;
+}
+
 // Both halves of the sum over F are split alike: kt_split counts k tiles of one half.
 inline Product dx_product(int64_t T, int64_t n, int64_t F, bool bf16) {
   const int kk = kk_of(bf16 ? 2 : 4);
