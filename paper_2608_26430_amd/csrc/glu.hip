@@ -90,13 +90,24 @@ struct Call {
   int fn;
 };
 
-hipError_t run_projection(const Call& c, int mode, ProjArgs a, hipStream_t s) {
-  const Projection p = projection(c.T, c.n, c.F, c.bf16);
-  const int kk = kk_of(c.bf16 ? 2 : 4), bm = xent::tile_m(p.tile) / 2, bn = xent::tile_n(p.tile);
-  a.F = (int)c.F, a.T = (int)c.T, a.n = (int)c.n;
-  a.tm = (int)(up(c.F, bm) / bm), a.tn = (int)(up(c.T, bn) / bn), a.kt = (int)(up(c.n, kk) / kk);
-  a.rest = p.ks ? 0 : rest_of(p.tile, a.tm * a.tn);
-  return launch_projection(c.bf16, c.fn, mode, p.tile, p.ks, a, s);
+hipError_t run_projection(const Call& c, int mode, const ProjArgs& call, hipStream_t s) {
+  const Parts p = projection(c.T, c.n, c.F, c.bf16);
+  const int esz = c.bf16 ? 2 : 4, kk = kk_of(esz);
+  for (int i = 0; i < p.count; ++i) {
+    const Part& q = p.part[i];
+    const int bm = tile_m(q.tile) / 2, bn = tile_n(q.tile);
+    auto in = [&](const void* x, int64_t ld) { return x ? static_cast<const char*>(x) + q.t0 * ld * esz : nullptr; };
+    auto out = [&](void* x, int64_t ld) { return x ? static_cast<char*>(x) + q.t0 * ld * esz : nullptr; };
+    ProjArgs a = call;
+    a.X = in(a.X, a.ldx), a.Ag = in(a.Ag, a.lda), a.Au = in(a.Au, a.lda), a.dH = in(a.dH, a.lddh);
+    a.H = out(a.H, a.ldh), a.G = out(a.G, a.ldg), a.U = out(a.U, a.ldg);
+    a.F = (int)c.F, a.T = (int)q.T, a.n = (int)c.n;
+    a.tm = (int)(up(c.F, bm) / bm), a.tn = (int)(up(q.T, bn) / bn), a.kt = (int)(up(c.n, kk) / kk);
+    a.rest = q.ks ? 0 : rest_of(q.tile, (int64_t)a.tm * a.tn);
+    const hipError_t e = launch_projection(c.bf16, c.fn, mode, q.tile, q.ks, a, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t run_point(const Call& c, PointArgs a, hipStream_t s) {
@@ -111,17 +122,30 @@ hipError_t run_point(const Call& c, PointArgs a, hipStream_t s) {
 }
 
 // trb: dW; otherwise dX
-hipError_t run_gradient(const Call& c, bool trb, GradArgs a, float* ws, hipStream_t s) {
-  const Product p = trb ? dw_product(c.T, c.n, c.F, c.bf16) : dx_product(c.T, c.n, c.F, c.bf16);
-  const int kk = kk_of(c.bf16 ? 2 : 4), bm = xent::tile_m(p.tile), bn = xent::tile_n(p.tile);
-  const int64_t N = trb ? c.F : c.T, K = trb ? c.T : c.F;
-  a.M = (int)c.n, a.N = (int)N, a.K = (int)K;
-  a.tm = (int)(up(c.n, bm) / bm), a.tn = (int)(up(N, bn) / bn);
-  a.kt = (int)(up(K, kk) / kk), a.kt_split = p.kt_split, a.splits = p.splits;
-  a.part = ws;
-  const hipError_t e = launch_gradient(c.bf16, trb, p.tile, a, s);
-  if (e != hipSuccess || p.splits == 1) return e;
-  return run_sum(c.bf16, ws, p.splits, trb ? 2 * N : N, N, c.n, a.beta, a.out[0], a.out[1], a.ldo, s);
+hipError_t run_gradient(const Call& c, bool trb, const GradArgs& call, float* ws, hipStream_t s) {
+  const Parts p = trb ? dw_product(c.T, c.n, c.F, c.bf16) : dx_product(c.T, c.n, c.F, c.bf16);
+  const int esz = c.bf16 ? 2 : 4, kk = kk_of(esz);
+  for (int i = 0; i < p.count; ++i) {
+    const Part& q = p.part[i];
+    const int bm = tile_m(q.tile), bn = tile_n(q.tile);
+    const int64_t K = trb ? c.T : c.F;
+    GradArgs a = call;
+    for (int h = 0; h < 2; ++h) {
+      // a part's rows: tokens of dG and dU, or their columns
+      a.B[h] = static_cast<const char*>(a.B[h]) + q.t0 * (trb ? 1 : a.ldb) * esz;
+      a.out[h] = static_cast<char*>(a.out[h]) + q.t0 * a.ldo * esz;
+    }
+    a.M = (int)c.n, a.N = (int)q.T, a.K = (int)K;
+    a.tm = (int)(up(c.n, bm) / bm), a.tn = (int)(up(q.T, bn) / bn);
+    a.kt = (int)(up(K, kk) / kk), a.kt_split = q.kt_split, a.splits = q.splits;
+    a.rest = rest_of(q.tile, (int64_t)a.tm * a.tn * (trb ? 2 : 1) * a.splits);
+    a.part = ws;
+    hipError_t e = launch_gradient(c.bf16, trb, q.tile, a, s);
+    if (e == hipSuccess && q.splits > 1)
+      e = run_sum(c.bf16, ws, q.splits, trb ? 2 * q.T : q.T, q.T, c.n, a.beta, a.out[0], a.out[1], a.ldo, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // ------------------------------------------------------------------------------------------- argument checks

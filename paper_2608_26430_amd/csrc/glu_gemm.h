@@ -28,6 +28,14 @@ using xent::up;
 
 enum Mode { kForward = 0, kBackward = 1 };
 
+// The lane's number, made anew: where a tile starts and ends it would otherwise take a register (and with it a spill) over the
+// whole main loop.
+__device__ __forceinline__ int fresh_lane() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
 struct ProjArgs {
   const void* Wg;
   const void* Wu;
@@ -207,12 +215,18 @@ __device__ __forceinline__ void project(const ProjArgs& a, char* lds, int wg, in
   ou.init(a.ldw, wave, lane);
   ob.init(a.ldx, wave, lane);
   int i0, j0, i_next, j_next;
-  auto place = [&](int at) { place_of(at, &i_next, &j_next); };
+  // (the same for all lanes: kept in scalar registers)
+  auto place = [&](int at) {
+    int i, j;
+    place_of(at, &i, &j);
+    i_next = __builtin_amdgcn_readfirstlane(i), j_next = __builtin_amdgcn_readfirstlane(j);
+  };
   auto issue_last = [&]() {
     const int left = a.n - (a.kt - 1) * kK;
-    og.issue_last(a.kt - 1, left, a.ldw, i0, a.F, lds0, wave, lane);
-    ou.issue_last(a.kt - 1, left, a.ldw, i0, a.F, lds0 + OpA::kBytes, wave, lane);
-    ob.issue_last(a.kt - 1, left, a.ldx, j0, a.T, lds0 + 2 * OpA::kBytes, wave, lane);
+    const int own = fresh_lane();
+    og.issue_last(a.kt - 1, left, a.ldw, i0, a.F, lds0, wave, own);
+    ou.issue_last(a.kt - 1, left, a.ldw, i0, a.F, lds0 + OpA::kBytes, wave, own);
+    ob.issue_last(a.kt - 1, left, a.ldx, j0, a.T, lds0 + 2 * OpA::kBytes, wave, own);
   };
   auto issue = [&](int t, int buf) {
     const unsigned to = lds0 + buf * kBuf;
@@ -322,8 +336,7 @@ __device__ __forceinline__ void project(const ProjArgs& a, char* lds, int wg, in
       ring_wait<0>();      // every wave's reads of the buffers are done
       start();
     }
-    int own = lane;
-    asm volatile("" : "+v"(own));      // places made here, not kept (and spilled) from one tile to the next
+    const int own = fresh_lane();
     const int g = own >> 4, r = own & 15;
     constexpr int P = PF ? PF : 1, W = 4 * P;
     constexpr int JB = FNT > 2 && sizeof(E) == 2 ? 2 : 1;    // more rows' at once would spill
@@ -389,7 +402,7 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArg
   }
 }
 
-// Few tokens: up to 16 FNT rows, 16 columns of each product a workgroup.  Its KS waves share k in chunks of 256 bytes and read the
+// Few tokens, or few columns: 16 FNT rows, 16 columns of each product a workgroup.  Its KS waves share k in chunks of 256 bytes and read the
 // weights straight into the registers of the MFMA (64 bytes of a row in four lanes), the next chunk under the products of one; nothing
 // is read twice but X, which is small.  The waves' sums are added up in a fixed order.
 template <class E, int FNT, int KS, int FN, int MODE>
@@ -398,14 +411,16 @@ __global__ void __launch_bounds__(KS * 64) narrow_kernel(ProjArgs a) {
   __shared__ f32x4 part[KS][2 * FNT][64];
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c0 = blockIdx.x * 16;
+  // an XCD's workgroups take all rows of a run of columns, whose weights are then read into one L2
+  const int rows = (a.T + 16 * FNT - 1) / (16 * FNT), id = xent::share_of(blockIdx.x, gridDim.x);
+  const int c0 = id / rows * 16, t0 = id % rows * (16 * FNT);
   // columns past the last read its weights, and their results are not written
   const int64_t row = c0 + r < a.F ? c0 + r : a.F - 1;
   const E* wg = static_cast<const E*>(a.Wg) + row * a.ldw + g * kPer;
   const E* wu = static_cast<const E*>(a.Wu) + row * a.ldw + g * kPer;
   const E* x[FNT];
 #pragma unroll
-  for (int j = 0; j < FNT; ++j) x[j] = static_cast<const E*>(a.X) + (int64_t)(j * 16 + r < a.T ? j * 16 + r : 0) * a.ldx + g * kPer;
+  for (int j = 0; j < FNT; ++j) x[j] = static_cast<const E*>(a.X) + (int64_t)(t0 + j * 16 + r < a.T ? t0 + j * 16 + r : 0) * a.ldx + g * kPer;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 ag[FNT], au[FNT];
 #pragma unroll
@@ -425,7 +440,7 @@ __global__ void __launch_bounds__(KS * 64) narrow_kernel(ProjArgs a) {
 #pragma unroll
       for (int j = 0; j < FNT; ++j) {
         fx[s][j] = zero;
-        if (in && j * 16 + r < a.T) fx[s][j] = *reinterpret_cast<const f32x4*>(x[j] + k);
+        if (in && t0 + j * 16 + r < a.T) fx[s][j] = *reinterpret_cast<const f32x4*>(x[j] + k);
       }
     }
   };
@@ -458,7 +473,7 @@ __global__ void __launch_bounds__(KS * 64) narrow_kernel(ProjArgs a) {
   f32x4 sg = part[0][2 * wave][lane], su = part[0][2 * wave + 1][lane];
 #pragma unroll
   for (int w = 1; w < KS; ++w) sg += part[w][2 * wave][lane], su += part[w][2 * wave + 1][lane];
-  const int t = wave * 16 + r, c = c0 + g * 4;
+  const int t = t0 + wave * 16 + r, c = c0 + g * 4;
   if (t >= a.T || c >= a.F) return;
   float vg[4], vu[4];
 #pragma unroll
@@ -476,15 +491,21 @@ struct GradArgs {
   int tm, tn;             // tiles along i, and j (dW: of one result)
   int kt, kt_split;       // k tiles (dX: of each half), and those of one split
   int splits;
+  int rest;               // of all tiles, those that are halved
   void* out[2];           // dX: the first; dW: dWg, dWu
   int64_t ldo;
   float beta;
   float* part;            // with splits > 1: [splits][N, dW: 2 N][M] fp32
 };
 
-// TRB: dB stored along j (dW); otherwise along k (dX).
-template <class E, int BM, int BN, int WVM, int WVN, int NB, bool TRB, int WPE>
-__global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs a) {
+// Where a tile is: which result, split of k, first column and row.
+struct GradPlace {
+  int which, split, i, j;
+};
+
+// A workgroup's share of `total` tiles: numbers wg, wg + step, ..  TRB: dG and dU stored along j (dW); otherwise along k (dX).
+template <class E, int BM, int BN, int WVM, int WVN, int NB, bool TRB, class Place>
+__device__ __forceinline__ void gradient(const GradArgs& a, char* lds, int wg, int step, int total, const Place& place_of) {
   constexpr int NW = WVM * WVN;
   constexpr int TM = BM / WVM, TN = BN / WVN;
   constexpr int FM = TM / 16, FNT = TN / 16;
@@ -496,12 +517,10 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
   constexpr int kReads = FM * OpA::kReads + FNT * OpB::kReads;
   constexpr int kMmas = FM * FNT * (sizeof(E) == 2 ? 1 : 4);
   constexpr int kHalves = TRB ? 1 : 2, kOuts = TRB ? 2 : 1;
-  __shared__ __align__(1024) char lds[NB * kBuf];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WVM, wn = wave / WVM;
-  const int tiles = a.tm * a.tn * kOuts, total = tiles * a.splits;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
   OpA oa;
@@ -509,23 +528,30 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
   oa.init(a.lda, wave, lane);
   ob.init(a.ldb, wave, lane);
   int i0, j0, which, split, nk;          // the tile whose operands are being read; nk: its k tiles of a half
-  int i_next, j_next, which_next, split_next;
+  GradPlace next;
   uint64_t second_a = 0, second_b = 0;   // where the second half starts
-  auto place = [&](int wg) {
-    const int id = xent::share_of(wg, total);
-    split_next = id / tiles;
-    int im, in;
-    xent::tile_of(id - split_next * tiles, a.tm, a.tn * kOuts, &im, &in);
-    which_next = kOuts == 2 && in >= a.tn;
-    i_next = im * BM, j_next = (in - which_next * a.tn) * BN;
+  // Large tiles of dX: the places that A's fragments are read from (as Operand::read has them) differ in three bits, and are made
+  // from the first one's for each half tile.  Kept over the loop they leave no room for the places of the loads, whose reloading from
+  // scratch waits for every load on its way (4096 tokens, 4096 <- 2 x 11008: 709 us, 545 without).
+  constexpr bool kLean = sizeof(E) == 2 && BM == 256 && !TRB;
+  unsigned a0 = 0;
+  if constexpr (kLean) {
+    const int k = (lane >> 4) * 8 + ((lane & 15) >> 2), cb = wm * TM * 2 + (lane & 3) * 8;
+    a0 = k * OpA::kRow + (((cb >> 4) ^ OpA::swizzle(k)) << 4 | (cb & 15));
+  }
+  auto place = [&](int at) {
+    const GradPlace p = place_of(at);
+    next.which = __builtin_amdgcn_readfirstlane(p.which), next.split = __builtin_amdgcn_readfirstlane(p.split);
+    next.i = __builtin_amdgcn_readfirstlane(p.i), next.j = __builtin_amdgcn_readfirstlane(p.j);
   };
   // A half's last k tile comes first, so that only the first loads look at its end: the sequence is the last tiles of the
   // halves, then the others of the first, then those of the second.
   auto issue_last = [&](int h) {
     const int last = a.K - (split * a.kt_split + nk - 1) * kK;
     const unsigned to = lds0 + h * kBuf;
-    oa.issue_last(nk - 1, last < kK ? last : kK, a.lda, i0, a.M, to, wave, lane);
-    ob.issue_last(nk - 1, last < kK ? last : kK, a.ldb, j0, a.N, to + OpA::kBytes, wave, lane);
+    const int own = fresh_lane();
+    oa.issue_last(nk - 1, last < kK ? last : kK, a.lda, i0, a.M, to, wave, own);
+    ob.issue_last(nk - 1, last < kK ? last : kK, a.ldb, j0, a.N, to + OpA::kBytes, wave, own);
   };
   auto issue = [&](int t, int buf) {
     if (kHalves == 2 && t == nk + 1) oa.base = second_a, ob.base = second_b;
@@ -534,7 +560,7 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
     ob.issue(t < kHalves * nk, to + OpA::kBytes, wave);
   };
   auto start = [&]() {
-    i0 = i_next, j0 = j_next, which = which_next, split = split_next;
+    i0 = next.i, j0 = next.j, which = next.which, split = next.split;
     const int kt0 = split * a.kt_split;
     nk = a.kt - kt0 < a.kt_split ? a.kt - kt0 : a.kt_split;
     if constexpr (kHalves == 2) {
@@ -555,10 +581,10 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
     for (int t = kHalves; t < (NB == 2 ? 2 : NB - 1); ++t) issue(t, t);
   };
 
-  place(blockIdx.x);
+  place(wg);
   start();
-  for (int wg = blockIdx.x;;) {
-    place(wg + gridDim.x);
+  for (;;) {
+    place(wg + step);
     const int nkt = kHalves * nk;
     f32x4 acc[FM][FNT];
 #pragma unroll
@@ -583,8 +609,21 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
       const char* la = lds + buf * kBuf;
 #pragma unroll
       for (int j = 0; j < FNT; ++j) fb[j] = OpB::read(la + OpA::kBytes, wn * TN, j, kk, lane);
+      if constexpr (kLean) {
+        unsigned at = a0;
+        asm volatile("" : "+v"(at));
 #pragma unroll
-      for (int f = 0; f < FM; ++f) fa[f] = OpA::read(la, wm * TM, f, kk, lane);
+        for (int f = 0; f < FM; ++f) {
+          const char* p = la + (at ^ (f * 32)) + kk * 32 * OpA::kRow;
+          const xent::s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) xent::s16x4*)p);
+          const xent::s16x4 hi =
+              __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) xent::s16x4*)(p + 4 * OpA::kRow));
+          fa[f] = __builtin_bit_cast(f32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+      } else {
+#pragma unroll
+        for (int f = 0; f < FM; ++f) fa[f] = OpA::read(la, wm * TM, f, kk, lane);
+      }
     };
     auto multiply = [&](const f32x4 (&fa)[FM], const f32x4 (&fb)[FNT]) {
 #pragma unroll
@@ -637,13 +676,14 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
         for (int j = 0; j < FNT; ++j) acc[f][j] += sum[f][j];
     }
     const int ci = i0 + wm * TM, cj = j0 + wn * TN, out = which, part = split;
-    wg += gridDim.x;
+    wg += step;
     const bool more = wg < total;
     if (more) {
       ring_wait<0>();      // every wave's reads of the buffers are done
       start();
     }
-    const int g = lane >> 4, r = lane & 15;
+    const int own = fresh_lane();
+    const int g = own >> 4, r = own & 15;
 #pragma unroll
     for (int j = 0; j < FNT; ++j) {
       const int row = cj + j * 16 + r;
@@ -664,7 +704,41 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
     }
     if (!more) break;
   }
+  // no direct load may be in flight when the LDS is given to another tile or workgroup
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+template <class E, int BM, int BN, int WVM, int WVN, int NB, bool TRB, int WPE>
+__global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs a) {
+  constexpr int kOuts = TRB ? 2 : 1;
+  __shared__ __align__(1024) char lds[NB * (BM + BN) * xent::kTileBytes];
+  const int tiles = a.tm * a.tn * kOuts, full = tiles * a.splits - a.rest;
+  auto tile = [&](int id) {
+    GradPlace p;
+    p.split = id / tiles;
+    int im, in;
+    xent::tile_of(id - p.split * tiles, a.tm, a.tn * kOuts, &im, &in);
+    p.which = kOuts == 2 && in >= a.tn;
+    p.i = im * BM, p.j = (in - p.which * a.tn) * BN;
+    return p;
+  };
+  if ((int)blockIdx.x < full)
+    gradient<E, BM, BN, WVM, WVN, NB, TRB>(a, lds, blockIdx.x, gridDim.x, full,
+                                           [&](int at) { return tile(xent::share_of(at, full)); });
+  // as in projection_kernel
+  if constexpr (BN == 256) {
+    const int halves = 2 * a.rest;
+    if ((int)blockIdx.x >= halves) return;
+    auto half = [&](int at) {
+      const int id = xent::share_of(at, halves);
+      GradPlace p = tile(full + id / 2);
+      p.j += id % 2 * (BN / 2);
+      return p;
+    };
+    if (half(blockIdx.x).j >= a.N) return;
+    __syncthreads();
+    gradient<E, BM, BN / 2, 2 * WVM, WVN / 2, NB, TRB>(a, lds, blockIdx.x, halves, halves, half);
+  }
 }
 
 // G and U kept: dG and dU element by element, 16 bytes a thread.

@@ -25,7 +25,8 @@ template <int MODE>
 static void project(int tile, int ks, const ProjArgs& a, hipStream_t s) {
   constexpr int FN = GLU_PART;
   if (ks) {
-    const dim3 grid((unsigned)((a.F + 15) / 16));
+    const int rows = a.T > 16 ? 32 : 16;
+    const dim3 grid((unsigned)((a.F + 15) / 16) * (unsigned)((a.T + rows - 1) / rows));
 #define GLU_NARROW(NT, KS) hipLaunchKernelGGL((narrow_kernel<E, NT, KS, FN, MODE>), grid, dim3(KS * 64), 0, s, a)
     if (a.T > 16 && ks == 4) GLU_NARROW(2, 4);
     else if (a.T > 16) GLU_NARROW(2, 8);

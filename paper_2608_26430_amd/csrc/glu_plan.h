@@ -1,5 +1,5 @@
-// Plan of a call of the gated feed-forward (glu.hip): kernels, tiles and splits of its products, size of its workspace.  Plain
-// arithmetic, shared by the host code and by a test that asks which instances a size runs.
+// Plan of a call of the gated feed-forward (glu.hip): kernels, tiles, splits and parts of its products, size of its workspace.
+// Plain arithmetic, shared by the host code and by a test that asks which instances a size runs.
 #pragma once
 
 #include "xent_plan.h"
@@ -7,67 +7,167 @@
 namespace ff {
 namespace glu {
 
-using xent::Product;
+using xent::kCUs;
+using xent::kLarge;
+using xent::kMedium;
+using xent::kSmall;
+using xent::tile_m;
+using xent::tile_n;
 using xent::up;
 
 constexpr int kk_of(int esz) { return 128 / esz; }   // k of a tile
 
-constexpr int64_t kNarrowTokens = 32;   // tokens up to which the few-token kernel makes the projections
-
-struct Projection {
-  int tile;    // xent::Tile
-  int ks;      // waves of a few-token workgroup, 0: tiles
+// Microseconds of a k tile (128 bytes of k) with few workgroups on the card, with one on every CU, and with all `slots` taken; and
+// the k tiles that a tile's start and end cost.  Measured, projections of T tokens, n -> F, bf16:
+//   large   4096 x 4096 -> 8192 (1024 tiles) 386 us, 2981 x 3712 -> 1408 (132) 77, 256 x 4096 -> 11008 (86) 81
+//   medium  2048 x 4096 -> 4096 (1024) 120 (large 108), 2981 x 3712 -> 1408 (528) 87, 64 x 4096 -> 11008 (172) 46, 800 x 3968 -> 128
+//           (14) 29
+//   small   64 x 4096 -> 11008 (344) 37, 100 x 1024 -> 4096 (256) 8, 800 x 3968 -> 128 (50) 19
+// fp32:
+//   medium  500 x 768 -> 2048 (128 tiles) 56, 1658 x 1024 -> 4096 (832) 250;  small  31 (512), 231 (3328); 64 x 1024 -> 4096 (128) 23
+struct TileCost {
+  int slots;
+  double few, one, full, ends;
 };
-
-// Waves that share k in the few-token kernel: enough of them on the card to read at its rate, each with a chunk of 256 bytes at
-// least.
-inline int narrow_waves(int64_t T, int64_t n, int64_t F, int esz) {
-  const int64_t groups = up(F, 16) / 16, chunks = up(n * esz, 256) / 256;
-  for (int ks : {4, 8})
-    if (groups * ks >= 2048 || chunks <= ks) return ks;
-  return T > 16 ? 8 : 16;    // sixteen waves of two groups of tokens spill
-}
-
-inline Projection projection(int64_t T, int64_t n, int64_t F, bool bf16) {
-  const int esz = bf16 ? 2 : 4, kk = kk_of(esz);
-  if (T <= kNarrowTokens) return {xent::kSmall, narrow_waves(T, n, F, esz)};
-  return {xent::choose(2 * F, T, up(n, kk) / kk, false, bf16).tile, 0};
-}
+constexpr TileCost kTileCosts[2][3] = {{{0, 0, 0, 0, 0}, {512, 2.0, 2.2, 3.84, 2}, {512, 0.60, 0.72, 1.08, 2}},
+                                       {{256, 1.15, 1.53, 1.53, 5}, {512, 0.45, 0.80, 0.92, 3}, {512, 0.25, 0.40, 0.45, 4}}};
+constexpr double kLaunch = 2.0;
 
 // Of `tiles` tiles those of a last round of large ones that are halved, where their halves fit one round.
 inline int rest_of(int tile, int64_t tiles) {
-  const int rest = (int)(tiles % xent::kCUs);
-  return tile == xent::kLarge && tiles > xent::kCUs && rest <= xent::kCUs / 2 ? rest : 0;
+  const int rest = (int)(tiles % kCUs);
+  return tile == kLarge && tiles > kCUs && rest <= kCUs / 2 ? rest : 0;
 }
 
-// Both halves of the sum over F are split alike: kt_split counts k tiles of one half.
-inline Product dx_product(int64_t T, int64_t n, int64_t F, bool bf16) {
-  const int kk = kk_of(bf16 ? 2 : 4);
-  const int64_t kt = up(F, kk) / kk;
-  Product p = xent::choose(n, T, 2 * kt, true, bf16);
-  const int64_t per = (kt + p.splits - 1) / p.splits;
-  p.splits = (int)((kt + per - 1) / per), p.kt_split = (int)per;
+inline double tiles_time(bool bf16, int tile, int64_t tiles, int64_t kt) {
+  const TileCost& c = kTileCosts[bf16][tile];
+  const int64_t rounds = tiles / c.slots, left = tiles % c.slots;
+  double last = 0;
+  // (two fp32 tiles on a CU take as long as when every CU has two: the matrix units bound them)
+  if (left > kCUs) last = bf16 ? c.one + (c.full - c.one) * (double)(left - kCUs) / kCUs : c.full;
+  else if (left) last = c.few + (c.one - c.few) * (double)left / kCUs;
+  if (rest_of(tile, tiles)) last *= 0.6;
+  return kLaunch + ((double)rounds * c.full + last) * ((double)kt + c.ends);
+}
+
+inline int64_t tiles_of(int64_t M, int64_t N, int tile) { return xent::tiles_of(M, N, tile); }
+
+// ------------------------------------------------------------------------------------------- projections
+
+// The few-token kernel: workgroups of 16 columns and 16 or 32 tokens, bound by what they read through the L2 (bf16, 256 tokens 1024 ->
+// 4096: 31 us where tiles take 10; 100 tokens 1024 -> 1024: 6.7 and 7.5; one token 512 -> 640: 3.6 and 5.1; fp32, 100 tokens 1024 ->
+// 1024: 11.7 and 22.9; at 4096 -> 11008 tiles are faster from the first token on, 27 and 30).
+inline int64_t narrow_groups(int64_t T, int64_t F) { return up(F, 16) / 16 * (up(T, T > 16 ? 32 : 16) / (T > 16 ? 32 : 16)); }
+inline double narrow_time(int64_t T, int64_t n, int64_t F, bool bf16) {
+  const int64_t rows = 32 + (T > 16 ? 32 : T);
+  return kLaunch + 1.0 + (double)(narrow_groups(T, F) * rows * n) * (bf16 ? 2 : 4) / (bf16 ? 8.0e6 : 6.5e6);
+}
+// Waves that share k: enough of them on the card, each with a chunk of 256 bytes at least.
+inline int narrow_waves(int64_t T, int64_t n, int64_t F, int esz) {
+  const int64_t groups = narrow_groups(T, F), chunks = up(n * esz, 256) / 256;
+  for (int ks : {4, 8})
+    if (groups * ks >= 1024 || chunks <= ks) return ks;
+  return T > 16 ? 8 : 16;    // sixteen waves of two groups of tokens spill
+}
+
+// Some of the tokens of a call; a call has one or two of them, one after the other.
+struct Part {
+  int64_t t0, T;
+  int tile;        // xent::Tile
+  int ks;          // waves of a few-token workgroup; 0: tiles
+  int splits;      // gradients: of k
+  int kt_split;    // k tiles of a split
+};
+struct Parts {
+  int count;
+  Part part[2];
+  double time;
+};
+
+// One part for all rows, or two: as many rows as fill whole rounds of workgroups, and the others in what suits them.  one(T) is the best
+// single part of T rows, columns(tile) the tiles along the other side.
+template <class One, class Columns, class Time>
+inline Parts parts_of(int64_t T, bool bf16, const One& one, const Columns& columns, const Time& time) {
+  Parts best = one(T);
+  for (int tile = bf16 ? kLarge : kMedium; tile <= kMedium; ++tile) {
+    const int64_t tm = columns(tile), tn = up(T, tile_n(tile)) / tile_n(tile), slots = kTileCosts[bf16][tile].slots;
+    for (int64_t rounds = tm * tn / slots, tries = 0; rounds > 0 && tries < 3; --rounds, ++tries) {
+      const int64_t rows = rounds * slots / tm;
+      if (rows < 1 || rows >= tn) continue;
+      const int64_t t1 = rows * tile_n(tile);
+      const Parts other = one(T - t1);
+      const double t = time(tile, tm * rows) + other.time;
+      if (t >= 0.97 * best.time) continue;
+      best.count = 2, best.time = t;
+      best.part[0] = {0, t1, tile, 0, 1, 0};
+      best.part[1] = other.part[0];
+      best.part[1].t0 = t1;
+    }
+  }
+  return best;
+}
+
+inline Parts projection(int64_t T, int64_t n, int64_t F, bool bf16) {
+  const int esz = bf16 ? 2 : 4;
+  const int64_t kt = up(n, kk_of(esz)) / kk_of(esz);
+  auto one = [&](int64_t rows) {
+    Parts p{1, {{0, rows, kSmall, narrow_waves(rows, n, F, esz), 1, 0}}, narrow_time(rows, n, F, bf16)};
+    for (int tile = bf16 ? kLarge : kMedium; tile <= kSmall; ++tile) {
+      const double t = tiles_time(bf16, tile, tiles_of(2 * F, rows, tile), kt);
+      if (t < p.time) p = Parts{1, {{0, rows, tile, 0, 1, 0}}, t};
+    }
+    return p;
+  };
+  return parts_of(T, bf16, one, [&](int tile) { return up(2 * F, tile_m(tile)) / tile_m(tile); },
+                  [&](int tile, int64_t tiles) { return tiles_time(bf16, tile, tiles, kt); });
+}
+
+// ------------------------------------------------------------------------------------------- gradients
+
+// M columns and `rows` rows of `outs` results, kt k tiles in each of `halves` parts of the sum, which are split alike.  Partial sums are
+// written and read at about 4.5 TB/s by a launch more; those of large results are not worth the pass through memory.
+inline Parts gradient(int64_t rows, int64_t M, int64_t kt, int halves, int outs, bool bf16) {
+  auto one = [&](int64_t N) {
+    Parts p{1, {{0, N, kSmall, 0, 1, (int)kt}}, 1e30};
+    for (int tile = bf16 ? kLarge : kMedium; tile <= kSmall; ++tile) {
+      const int64_t tiles = outs * tiles_of(M, N, tile);
+      for (int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64}) {
+        if (s > 1 && (halves * kt < 4 * s || (outs == 2 && 2 * rows > 4096))) break;
+        const int64_t per = (kt + s - 1) / s, splits = (kt + per - 1) / per;
+        double t = tiles_time(bf16, tile, tiles * splits, halves * per);
+        if (splits > 1) t += 4.5 + (double)(splits * outs * N * M) * 8.0 / 4.5e6;
+        if (t < p.time) p = Parts{1, {{0, N, tile, 0, (int)splits, (int)per}}, t};
+        if (tiles * splits >= 4 * kCUs) break;
+      }
+    }
+    return p;
+  };
+  Parts p = parts_of(rows, bf16, one, [&](int tile) { return outs * (up(M, tile_m(tile)) / tile_m(tile)); },
+                     [&](int tile, int64_t tiles) { return tiles_time(bf16, tile, tiles, halves * kt); });
+  if (p.count == 2) p.part[0].kt_split = (int)kt;
   return p;
 }
-
-inline Product dw_product(int64_t T, int64_t n, int64_t F, bool bf16) {
+inline Parts dx_product(int64_t T, int64_t n, int64_t F, bool bf16) {
   const int kk = kk_of(bf16 ? 2 : 4);
-  // partial sums of large weights are not worth a pass through memory
-  return xent::choose(n, 2 * F, up(T, kk) / kk, 2 * F <= 4096, bf16);
+  return gradient(T, n, up(F, kk) / kk, 2, 1, bf16);
+}
+inline Parts dw_product(int64_t T, int64_t n, int64_t F, bool bf16) {
+  const int kk = kk_of(bf16 ? 2 : 4);
+  return gradient(F, n, up(T, kk) / kk, 1, 2, bf16);
 }
 
 inline int64_t workspace(int64_t T, int64_t n, int64_t F, bool bf16, bool dx, bool dw) {
   int64_t bytes = 256;
   if (T == 0) return bytes;
-  auto more = [&](int64_t b) { bytes = b > bytes ? up(b, 256) : bytes; };
-  if (dx) {
-    const Product p = dx_product(T, n, F, bf16);
-    if (p.splits > 1) more((int64_t)p.splits * T * n * 4);
-  }
-  if (dw) {
-    const Product p = dw_product(T, n, F, bf16);
-    if (p.splits > 1) more((int64_t)p.splits * 2 * F * n * 4);
-  }
+  auto more = [&](const Parts& p, int outs) {
+    for (int i = 0; i < p.count; ++i)
+      if (p.part[i].splits > 1) {
+        const int64_t b = up((int64_t)p.part[i].splits * outs * p.part[i].T * n * 4, 256);
+        if (b > bytes) bytes = b;
+      }
+  };
+  if (dx) more(dx_product(T, n, F, bf16), 1);
+  if (dw) more(dw_product(T, n, F, bf16), 2);
   return bytes;
 }
 

@@ -1,20 +1,31 @@
-// The plan of a gated feed-forward's call (csrc/glu_plan.h), asked from a test: lines of "T n F bf16" in, tiles and splits out.
+// The plan of a gated feed-forward's call (csrc/glu_plan.h), asked from a test: lines of "T n F bf16" in; for the projections, dX and
+// dW: number of parts, and for each rows, tile, waves (few tokens), splits of k, tiles, halved tiles.
 #include <cstdio>
 
 #include "glu_plan.h"
 
 using namespace ff::glu;
 
+static void print(const Parts& p, int64_t M, int outs) {
+  std::printf("%d ", p.count);
+  int64_t at = 0;
+  for (int i = 0; i < p.count; ++i) {
+    const Part& q = p.part[i];
+    const int64_t tiles = outs * tiles_of(M, q.T, q.tile) * q.splits;
+    std::printf(" %lld %d %d %d %lld %d ", (long long)q.T, q.tile, q.ks, q.splits, (long long)tiles, rest_of(q.tile, tiles));
+    if (q.t0 != at) std::printf(" gap ");
+    at += q.T;
+  }
+}
+
 int main() {
-  long T, n, F;
+  long long T, n, F;
   int bf16;
-  while (std::scanf("%ld %ld %ld %d", &T, &n, &F, &bf16) == 4) {
-    const Projection p = projection(T, n, F, bf16);
-    const Product x = dx_product(T, n, F, bf16), w = dw_product(T, n, F, bf16);
-    const long pt = (long)ff::xent::tiles_of(2 * F, T, p.tile), xt = (long)ff::xent::tiles_of(n, T, x.tile) * x.splits;
-    const long wt = 2 * (long)ff::xent::tiles_of(n, F, w.tile) * w.splits;
-    std::printf("%d %d %ld  %d %d %d %ld  %d %d %d %ld  %ld\n", p.tile, p.ks, pt, x.tile, x.splits, x.kt_split, xt, w.tile, w.splits,
-                w.kt_split, wt, (long)workspace(T, n, F, bf16, true, true));
+  while (std::scanf("%lld %lld %lld %d", &T, &n, &F, &bf16) == 4) {
+    print(projection(T, n, F, bf16), 2 * F, 1);
+    print(dx_product(T, n, F, bf16), n, 1);
+    print(dw_product(T, n, F, bf16), n, 2);
+    std::printf(" %lld\n", (long long)workspace(T, n, F, bf16, true, true));
   }
   return 0;
 }

@@ -26,9 +26,15 @@ def plans(tmp_path_factory):
                     "-o", exe], check=True, timeout=300)
 
     def ask(T, n, F, bf16):
-        w = subprocess.run([exe], input=f"{T} {n} {F} {int(bf16)}\n", capture_output=True, text=True, check=True, timeout=60).stdout
-        w = [int(x) for x in w.split()]
-        return dict(proj=w[0], ks=w[1], proj_tiles=w[2], dx=w[3], dx_splits=w[4], dx_tiles=w[6], dw=w[7], dw_splits=w[8], dw_tiles=w[10])
+        out = subprocess.run([exe], input=f"{T} {n} {F} {int(bf16)}\n", capture_output=True, text=True, check=True, timeout=60).stdout
+        w = [int(x) for x in out.split()]       # ("gap": not a number)
+        plan = {}
+        for name, rows in (("proj", T), ("dx", T), ("dw", F)):
+            parts = [dict(zip(("rows", "tile", "ks", "splits", "tiles", "rest"), [w.pop(0) for _ in range(6)]))
+                     for _ in range(w.pop(0))]
+            assert sum(p["rows"] for p in parts) == rows
+            plan[name] = parts
+        return plan
 
     return ask
 
@@ -36,18 +42,22 @@ def plans(tmp_path_factory):
 @pytest.mark.parametrize("bf16", [True, False])
 def test_sizes_run_every_kernel(plans, bf16):
     p = [plans(*s, bf16) for s in SIZES + (BIG if bf16 else [])]
-    assert {q["ks"] for q in p} >= {0, 4, 8, 16}
-    # few tokens: one and two groups of 16, with each number of waves that both run
-    few = {(plans(*s, bf16)["ks"], s[0] > 16) for s in SIZES if s[0] <= 32}
+    proj = [q for x in p for q in x["proj"]]
+    # few tokens and few columns: 16 and 32 tokens a workgroup, with each number of waves that both run, and several groups of tokens
+    few = {(q["ks"], q["rows"] > 16) for q in proj if q["ks"]}
     assert few == {(4, False), (8, False), (16, False), (4, True), (8, True)}, few
+    assert any(q["ks"] and q["rows"] > 32 for q in proj)
     tiles = {MEDIUM, SMALL} | ({LARGE} if bf16 else set())
-    assert {q["proj"] for q in p if q["ks"] == 0} == tiles
-    assert {q["dx"] for q in p} == tiles and {q["dw"] for q in p} == tiles
+    assert {q["tile"] for q in proj if not q["ks"]} == tiles
     for k in ("dx", "dw"):
-        assert {q[k + "_splits"] > 1 for q in p} == {True, False}
-    if bf16:       # large tiles, more of them than workgroups
-        for k in ("proj", "dx", "dw"):
-            assert any(q[k] == LARGE and q[k + "_tiles"] > 256 and (k != "proj" or q["ks"] == 0) for q in p), k
+        parts = [q for x in p for q in x[k]]
+        assert {q["tile"] for q in parts} == tiles, k
+        assert {q["splits"] > 1 for q in parts} == {True, False}
+    for k in ("proj", "dx", "dw") if bf16 else ():
+        # large tiles, more of them than workgroups, and halved ones; calls in two parts
+        assert any(q["tile"] == LARGE and q["tiles"] > 256 and not q["ks"] for x in p for q in x[k]), k
+        assert any(q["rest"] and not q["ks"] for x in p for q in x[k]), k
+        assert any(len(x[k]) == 2 for x in p), k
 
 
 def test_calls_refused_on_the_host():
