@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -567,8 +568,9 @@ class AdamWSet:
             with torch.cuda.device(self.device):
                 return self.read(stream)
         m, v = (_new(self.m_all.shape, torch.bfloat16, self.device, stream) for _ in range(2))
-        pm, pv = ((ctypes.c_void_p * len(self.offsets))(*[t.data_ptr() + 2 * o for o in self.offsets]) for t in (m, v))
-        _check((_lib or _load()).ff_adamw_set_read(self._h, pm, pv, _stream(stream)))
+        at = 2 * np.asarray(self.offsets, dtype=np.uint64)
+        pm, pv = at + np.uint64(m.data_ptr()), at + np.uint64(v.data_ptr())
+        _check((_lib or _load()).ff_adamw_set_read(self._h, pm.ctypes.data, pv.ctypes.data, _stream(stream)))
         return m, v
 
     def close(self):
@@ -899,47 +901,43 @@ def layernorm_bwd(X, G, weight, mean, rstd, dX=None, dweight=None, dbias=None, b
     return (dX if want_dx else None), (dweight if want_dw else None), (dbias if want_dw else None)
 
 
-class _Resnorm(ctypes.Structure):
-    _fields_ = [("T", ctypes.c_int64), ("n", ctypes.c_int64), ("act", ctypes.c_int), ("w_dtype", ctypes.c_int),
-                ("gate_dtype", ctypes.c_int), ("post", ctypes.c_int), ("norm", ctypes.c_int), ("post_weight", ctypes.c_void_p),
-                ("post_bias", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
-                ("gate", ctypes.c_void_p), ("ldgate", ctypes.c_int64), ("groups", ctypes.c_int64),
-                ("res_scale", ctypes.c_float), ("block_scale", ctypes.c_float), ("post_eps", ctypes.c_float),
-                ("eps", ctypes.c_float)]
-
-
 _NORMS = {"none": 0, None: 0, "rms": 1, "layer": 2}
+_RESNORM = struct.Struct("@2q5i4x5P2q4f")       # the fields of ff_resnorm
 
 
 def _resnorm(T, n, act, dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps, post_eps):
-    """The description of a join, and the number of its gate rows."""
+    """The description of a join, whether it has a norm of its result, and the number of its gate rows."""
     torch = _T or _torch()
     f32, bf16 = torch.float32, torch.bfloat16
-    if post not in _NORMS or norm not in _NORMS:
+    post_code, norm_code = _NORMS.get(post), _NORMS.get(norm)
+    if post_code is None or norm_code is None:
         raise ValueError(f"unknown norms {post!r}, {norm!r}: 'none', 'rms' or 'layer'")
-    wt = None
-    for v, name, there in ((post_weight, "post_weight", _NORMS[post]), (post_bias, "post_bias", _NORMS[post]),
-                           (weight, "weight", _NORMS[norm]), (bias, "bias", _NORMS[norm])):
+    wt, ptrs = None, []
+    for v, name, there in ((post_weight, "post_weight", post_code), (post_bias, "post_bias", post_code),
+                           (weight, "weight", norm_code), (bias, "bias", norm_code)):
         if v is None:
+            ptrs.append(0)
             continue
         if not there:
             raise ValueError(f"{name} of a norm that is not there")
-        if v.dtype not in (f32, bf16) or (wt is not None and v.dtype is not wt):
-            raise ValueError("the norms' vectors must all be fp32 or all bf16")
-        wt = v.dtype
-    groups, gp, ldgate, gdt = 1, None, n, 0
+        if wt is None:
+            wt = v.dtype
+            if wt is not f32 and wt is not bf16:
+                raise ValueError("the norms' vectors must all be fp32 or all bf16")
+        ptrs.append(_array(v, name, n, wt, dev))
+    groups, gp, ldgate, gate_bf16 = 1, 0, n, 0
     if gate is not None:
-        if gate.dtype not in (f32, bf16):
+        gate_bf16 = int(gate.dtype is bf16)
+        if not gate_bf16 and gate.dtype is not f32:
             raise ValueError("gate must be fp32 or bf16")
-        g2 = gate if gate.dim() == 2 else gate.view(1, -1)
-        groups = g2.shape[0]
-        if g2.shape[1] != n or g2.get_device() != dev or (n != 1 and g2.stride(1) != 1) or groups < 1 or T % groups:
+        rows = gate.dim() == 2
+        groups = gate.shape[0] if rows else 1
+        if (gate.shape[-1] != n or gate.dim() > 2 or gate.get_device() != dev or (n != 1 and gate.stride(-1) != 1) or groups < 1
+                or T % groups):
             raise ValueError(f"gate must have {n} elements, or rows of {n} whose number divides {T}, on device {dev}")
-        gp, ldgate, gdt = g2.data_ptr(), (n if groups < 2 else g2.stride(0)), int(gate.dtype is bf16)
-    return _Resnorm(T, n, act, int(wt is bf16), gdt, _NORMS[post], _NORMS[norm], _norm_vector(post_weight, "post_weight", n, dev),
-                    _norm_vector(post_bias, "post_bias", n, dev), _norm_vector(weight, "weight", n, dev),
-                    _norm_vector(bias, "bias", n, dev), gp, ldgate, groups, res_scale, block_scale,
-                    eps if post_eps is None else post_eps, eps), groups
+        gp, ldgate = gate.data_ptr(), (gate.stride(0) if groups > 1 else n)
+    return _RESNORM.pack(T, n, act, int(wt is bf16), gate_bf16, post_code, norm_code, *ptrs, gp, ldgate, groups, res_scale,
+                         block_scale, eps if post_eps is None else post_eps, eps), norm_code, groups
 
 
 def resnorm_fwd(R, B, gate=None, post="none", post_weight=None, post_bias=None, norm="rms", weight=None, bias=None,
@@ -955,19 +953,19 @@ def resnorm_fwd(R, B, gate=None, post="none", post_weight=None, post_bias=None, 
             return resnorm_fwd(R, B, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps,
                                post_eps, X, Y, stats, want_stats, stream)
     bp, ldb = _rows(B, "B", R)
-    d, _ = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps,
+    d, has_norm, _ = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps,
                     post_eps)
     X, xp, ldx = _out_rows(X, "X", R, stream)
     yp, ldy, sp = None, n, None
-    if d.norm:
+    if has_norm:
         Y, yp, ldy = _out_rows(Y, "Y", R, stream)
     if stats is not None:
         sp = _stats(stats, T, dev)
     elif want_stats:
         stats = _new((T, 4), torch.float32, R.device, stream)
         sp = stats.data_ptr()
-    _check((_lib or _load()).ff_resnorm_fwd(ctypes.byref(d), rp, ldr, bp, ldb, xp, ldx, yp, ldy, sp, _stream(stream)))
-    return X, (Y if d.norm else None), stats
+    _check((_lib or _load()).ff_resnorm_fwd(d, rp, ldr, bp, ldb, xp, ldx, yp, ldy, sp, _stream(stream)))
+    return X, (Y if has_norm else None), stats
 
 
 def _stats(t, T, dev):
@@ -1005,42 +1003,49 @@ def resnorm_bwd(R, B, dX, dY, stats, gate=None, post="none", post_weight=None, p
                                block_scale, eps, post_eps, dR, dB, dgate, dpost_weight, dpost_bias, dweight, dbias, accumulate,
                                want_dr, want_db, want_vectors, workspace, stream)
     bp, ldb = _rows(B, "B", R)
-    d, groups = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale,
+    d, has_norm, groups = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale,
                          eps, post_eps)
     dxp, lddx = _rows(dX, "dX", R) if dX is not None else (None, n)
-    if d.norm and dY is None:
+    if has_norm and dY is None:
         raise ValueError("a norm needs dY")
-    dyp, lddy = _rows(dY, "dY", R) if d.norm else (None, n)
+    dyp, lddy = _rows(dY, "dY", R) if has_norm else (None, n)
     drp = dbp = None
     lddr = lddb = n
     if want_dr:
         dR, drp, lddr = _out_rows(dR, "dR", R, stream)
     if want_db:
         dB, dbp, lddb = _out_rows(dB, "dB", R, stream)
-    outs, ptrs = [], []
-    for given, out, name in ((post_weight, dpost_weight, "dpost_weight"), (post_bias, dpost_bias, "dpost_bias"),
-                             (weight, dweight, "dweight"), (bias, dbias, "dbias")):
-        p = None
-        if out is not None or (want_vectors and given is not None):
-            if accumulate and out is None:
+    outs, ptrs, made = [dgate, dpost_weight, dpost_bias, dweight, dbias], [None] * 5, []
+    for i, (given, name) in enumerate(((gate, "dgate"), (post_weight, "dpost_weight"), (post_bias, "dpost_bias"),
+                                       (weight, "dweight"), (bias, "dbias"))):
+        if outs[i] is None:
+            if not want_vectors or given is None:
+                continue
+            if accumulate:
                 raise ValueError(f"accumulate needs an existing {name}")
-            out, p = _out_array(out, name, n, R.device, stream)
-        outs.append(out)
-        ptrs.append(p)
-    gp = None
-    if dgate is not None or (want_vectors and gate is not None):
-        if gate is None or (accumulate and dgate is None):
-            raise ValueError("dgate needs a gate, and accumulate an existing dgate")
-        if dgate is None:
-            dgate = _new(gate.shape, f32, R.device, stream)
-        elif dgate.dtype is not f32 or dgate.shape != gate.shape or dgate.get_device() != dev or not dgate.is_contiguous():
-            raise ValueError("dgate must be a contiguous fp32 tensor of the gate's shape")
-        gp = dgate.data_ptr()
+            if i == 0 and groups > 1:
+                outs[0] = _new(gate.shape, f32, R.device, stream)
+                ptrs[0] = outs[0].data_ptr()
+            else:
+                made.append(i)
+        elif i == 0:
+            if gate is None or dgate.dtype is not f32 or dgate.shape != gate.shape or dgate.get_device() != dev \
+                    or not dgate.is_contiguous():
+                raise ValueError("dgate must be a contiguous fp32 tensor of the gate's shape")
+            ptrs[0] = dgate.data_ptr()
+        else:
+            ptrs[i] = _array(outs[i], name, n, f32, dev)
+    if made:            # the results of n elements in one allocation
+        block = _new((len(made), n), f32, R.device, stream)
+        at = block.data_ptr()
+        for i, t in zip(made, block.unbind(0)):
+            outs[i] = t if i or gate.dim() == 1 else t.view(1, n)
+            ptrs[i] = at
+            at += 4 * n
     workspace = _workspace(workspace, _resnorm_bytes(T, n, groups) if workspace is None else 0, R.device, stream)
     _check((_lib or _load()).ff_resnorm_bwd(
-        ctypes.byref(d), rp, ldr, bp, ldb, dxp, lddx, dyp, lddy, _stats(stats, T, dev), drp, lddr, dbp, lddb, int(accumulate), gp,
-        *ptrs, workspace.data_ptr(), workspace.nbytes, _stream(stream)))
-    return ((dR if want_dr else None), (dB if want_db else None), dgate, *outs)
+        d, rp, ldr, bp, ldb, dxp, lddx, dyp, lddy, _stats(stats, T, dev), drp, lddr, dbp, lddb, int(accumulate), *ptrs, workspace.data_ptr(), workspace.nbytes, _stream(stream)))
+    return ((dR if want_dr else None), (dB if want_db else None), *outs)
 
 
 def dropout(X, p: float, seed: int, offset: int = 0, residual=None, Y=None, offset_dev=None, stream=None):

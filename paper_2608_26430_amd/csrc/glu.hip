@@ -122,8 +122,7 @@ hipError_t run_point(const Call& c, PointArgs a, hipStream_t s) {
 }
 
 // trb: dW; otherwise dX
-hipError_t run_gradient(const Call& c, bool trb, const GradArgs& call, float* ws, hipStream_t s) {
-  const Parts p = trb ? dw_product(c.T, c.n, c.F, c.bf16) : dx_product(c.T, c.n, c.F, c.bf16);
+hipError_t run_gradient(const Call& c, bool trb, const Parts& p, const GradArgs& call, float* ws, hipStream_t s) {
   const int esz = c.bf16 ? 2 : 4, kk = kk_of(esz);
   for (int i = 0; i < p.count; ++i) {
     const Part& q = p.part[i];
@@ -224,7 +223,10 @@ ff_status ff_glu_workspace(int64_t T, int64_t n, int64_t F, int act, int want, i
   GLU_CHECK(check_sizes(T, n, F, act, FF_GLU_SILU));
   if (want < 0 || want > (FF_GLU_DX | FF_GLU_DW)) return ff::fail(FF_EINVAL, "unknown outputs %d", want);
   if (!bytes) return ff::fail(FF_EINVAL, "bytes is NULL");
-  *bytes = workspace(T, n, F, act == FF_BF16, want & FF_GLU_DX, want & FF_GLU_DW);
+  Parts dx{}, dw{};
+  if (T && (want & FF_GLU_DX)) dx = dx_product(T, n, F, act == FF_BF16);
+  if (T && (want & FF_GLU_DW)) dw = dw_product(T, n, F, act == FF_BF16);
+  *bytes = workspace(n, &dx, &dw);
   return FF_OK;
 }
 
@@ -264,7 +266,10 @@ ff_status ff_glu_bwd(int64_t T, int64_t n, int64_t F, int act, int fn, const voi
   GLU_CHECK(check_rows("dG", dG, lddg, F, act));
   GLU_CHECK(check_rows("dU", dU, lddg, F, act));
   if (dX) GLU_CHECK(check_rows("dX", dX, lddx, n, act));
-  const int64_t need = workspace(T, n, F, c.bf16, dX != nullptr, dWg != nullptr);
+  Parts dx{}, dw{};
+  if (dX) dx = dx_product(T, n, F, c.bf16);
+  if (dWg) dw = dw_product(T, n, F, c.bf16);
+  const int64_t need = workspace(n, &dx, &dw);
   if ((dX || dWg) && (!ws || (uintptr_t)ws % 256)) return ff::fail(FF_EINVAL, "the workspace is NULL or not 256-byte aligned");
   if ((dX || dWg) && workspace_bytes < need)
     return ff::fail(FF_EINVAL, "the workspace holds %lld bytes, the call needs %lld", (long long)workspace_bytes, (long long)need);
@@ -284,13 +289,13 @@ ff_status ff_glu_bwd(int64_t T, int64_t n, int64_t F, int act, int fn, const voi
     GradArgs a{};
     a.A[0] = Wg, a.A[1] = Wu, a.lda = ldw, a.B[0] = dG, a.B[1] = dU, a.ldb = lddg;
     a.out[0] = a.out[1] = dX, a.ldo = lddx, a.beta = beta_dx;
-    GLU_CHECK(done(run_gradient(c, false, a, static_cast<float*>(ws), s), "gated feed-forward backward"));
+    GLU_CHECK(done(run_gradient(c, false, dx, a, static_cast<float*>(ws), s), "gated feed-forward backward"));
   }
   if (dWg) {
     GradArgs a{};
     a.A[0] = a.A[1] = X, a.lda = ldx, a.B[0] = dG, a.B[1] = dU, a.ldb = lddg;
     a.out[0] = dWg, a.out[1] = dWu, a.ldo = lddw, a.beta = beta_dw;
-    GLU_CHECK(done(run_gradient(c, true, a, static_cast<float*>(ws), s), "gated feed-forward backward"));
+    GLU_CHECK(done(run_gradient(c, true, dw, a, static_cast<float*>(ws), s), "gated feed-forward backward"));
   }
   return FF_OK;
 }

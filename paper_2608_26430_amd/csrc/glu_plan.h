@@ -156,19 +156,19 @@ inline Parts dw_product(int64_t T, int64_t n, int64_t F, bool bf16) {
   return gradient(F, n, up(T, kk) / kk, 1, 2, bf16);
 }
 
-inline int64_t workspace(int64_t T, int64_t n, int64_t F, bool bf16, bool dx, bool dw) {
-  int64_t bytes = 256;
-  if (T == 0) return bytes;
-  auto more = [&](const Parts& p, int outs) {
-    for (int i = 0; i < p.count; ++i)
-      if (p.part[i].splits > 1) {
-        const int64_t b = up((int64_t)p.part[i].splits * outs * p.part[i].T * n * 4, 256);
-        if (b > bytes) bytes = b;
-      }
-  };
-  if (dx) more(dx_product(T, n, F, bf16), 1);
-  if (dw) more(dw_product(T, n, F, bf16), 2);
+// Bytes of partial sums of `outs` results of n columns.
+inline int64_t part_bytes(const Parts& p, int64_t n, int outs) {
+  int64_t bytes = 0;
+  for (int i = 0; i < p.count; ++i)
+    if (p.part[i].splits > 1) {
+      const int64_t b = (int64_t)p.part[i].splits * outs * p.part[i].T * n * 4;
+      if (b > bytes) bytes = b;
+    }
   return bytes;
+}
+inline int64_t workspace(int64_t n, const Parts* dx, const Parts* dw) {
+  const int64_t x = dx ? part_bytes(*dx, n, 1) : 0, w = dw ? part_bytes(*dw, n, 2) : 0, most = x > w ? x : w;
+  return most ? up(most, 256) : 256;
 }
 
 }  // namespace glu

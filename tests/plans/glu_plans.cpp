@@ -23,9 +23,10 @@ int main() {
   int bf16;
   while (std::scanf("%lld %lld %lld %d", &T, &n, &F, &bf16) == 4) {
     print(projection(T, n, F, bf16), 2 * F, 1);
-    print(dx_product(T, n, F, bf16), n, 1);
-    print(dw_product(T, n, F, bf16), n, 2);
-    std::printf(" %lld\n", (long long)workspace(T, n, F, bf16, true, true));
+    const Parts dx = dx_product(T, n, F, bf16), dw = dw_product(T, n, F, bf16);
+    print(dx, n, 1);
+    print(dw, n, 2);
+    std::printf(" %lld\n", (long long)workspace(n, &dx, &dw));
   }
   return 0;
 }

@@ -55,6 +55,34 @@ def test_gradients_are_those_of_differences(post, norm, gate):
             assert (value(hi) - value(lo)) / 2e-6 == pytest.approx(np.ravel(o[d])[at], rel=1e-6, abs=1e-6), (k, at)
 
 
+FIELDS = ("T", "n", "act", "w_dtype", "gate_dtype", "post", "norm", "post_weight", "post_bias", "weight", "bias", "gate", "ldgate",
+          "groups", "res_scale", "block_scale", "post_eps", "eps")
+
+
+def _packed(**d):
+    return binding._RESNORM.pack(*(d.get(k, 0) for k in FIELDS))
+
+
+def test_description_is_laid_out_as_the_header_has_it(tmp_path):
+    """The binding's packed fields against the struct of include/frameft.h, compiled."""
+    import os
+    import shutil
+    import subprocess
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "layout.cpp"
+    src.write_text('#include <cstdio>\n#include <cstddef>\n#include "frameft.h"\nint main() {' + "".join(
+        f'std::printf("%zu ", offsetof(ff_resnorm, {f}));' for f in FIELDS) + 'std::printf("%zu", sizeof(ff_resnorm)); }')
+    exe = str(tmp_path / "layout")
+    subprocess.run(["g++", "-I" + os.path.join(root, "include"), str(src), "-o", exe], check=True, timeout=120)
+    want = [int(x) for x in subprocess.run([exe], capture_output=True, text=True, check=True, timeout=60).stdout.split()]
+    for f, at in zip(FIELDS, want):
+        one = binding._RESNORM.pack(*(1 if k == f else 0 for k in FIELDS))
+        assert [i for i, b in enumerate(one) if b] and min(i for i, b in enumerate(one) if b) // 4 * 4 == at, f
+    assert binding._RESNORM.size == want[-1]
+
+
 def test_calls_refused_on_the_host():
     lib, p = binding._load(), ctypes.c_void_p(1 << 20)
     q = 1 << 20
@@ -63,7 +91,7 @@ def test_calls_refused_on_the_host():
         d = dict(T=4, n=64, act=0, w_dtype=0, gate_dtype=0, post=1, norm=1, groups=1, ldgate=64, res_scale=1.0, block_scale=1.0,
                  post_eps=1e-5, eps=1e-5)
         d.update(kw)
-        return binding._STATUS[lib.ff_resnorm_fwd(ctypes.byref(binding._Resnorm(**d)), R, ldr, B, ldb, X, ldx, Y, ldy, stats, None)]
+        return binding._STATUS[lib.ff_resnorm_fwd(_packed(**d), R, ldr, B, ldb, X, ldx, Y, ldy, stats, None)]
 
     bad = [dict(T=-1), dict(T=(1 << 30) + 1), dict(n=0), dict(n=(1 << 24) + 1), dict(act=2), dict(w_dtype=3), dict(gate_dtype=-1),
            dict(post=3), dict(norm=-1), dict(gate=q, groups=3), dict(gate=q, groups=0), dict(gate=q, groups=2, ldgate=63),
@@ -79,7 +107,7 @@ def test_calls_refused_on_the_host():
     def bwd(dX=p, dY=p, stats=p, dR=p, dB=p, dgate=None, dpw=None, dpb=None, dw=None, db=None, ws=p, wsn=1 << 30, **kw):
         d = dict(T=4, n=64, act=0, post=1, norm=1, groups=1, ldgate=64, res_scale=1.0, block_scale=1.0, post_eps=1e-5, eps=1e-5)
         d.update(kw)
-        return binding._STATUS[lib.ff_resnorm_bwd(ctypes.byref(binding._Resnorm(**d)), p, 64, p, 64, dX, 64, dY, 64, stats, dR, 64,
+        return binding._STATUS[lib.ff_resnorm_bwd(_packed(**d), p, 64, p, 64, dX, 64, dY, 64, stats, dR, 64,
                                                   dB, 64, 0, dgate, dpw, dpb, dw, db, ws, wsn, None)]
 
     for kw in (dict(dgate=p), dict(post=0, dpw=p), dict(norm=0, db=p), dict(dY=None), dict(stats=None),
