@@ -79,7 +79,8 @@ class Block:
         dh = torch.mm(dy, self.Wd)
         _, grads["C_d"] = ff.adapter_bwd(self.down, h, dy, q["C_d"], s, dX=dh, beta_dx=1.0)
         # dg and du take the place of g and u
-        dg, du, dh1, _, _ = ff.glu_bwd(dh, h1, self.Wg, self.Wu, "silu", G=g, U=u, dG=g, dU=u, workspace=self.ws_glu)
+        dg, du, dh1, _, _ = ff.glu_bwd(dh, h1, self.Wg, self.Wu, "silu", G=g, U=u, dG=g.view(x.dtype), dU=u.view(x.dtype),
+                                      workspace=self.ws_glu)
         _, grads["C_g"] = ff.adapter_bwd(self.up, h1, dg, q["C_g"], s, dX=dh1, beta_dx=1.0)
         _, grads["C_u"] = ff.adapter_bwd(self.up, h1, du, q["C_u"], s, dX=dh1, beta_dx=1.0)
         dx, db, _, grads["norm_a"], _, grads["norm_b"], _ = ff.resnorm_bwd(

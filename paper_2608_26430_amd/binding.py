@@ -1091,26 +1091,33 @@ def _pair(ld, other, names):
     return ld
 
 
-def _hidden(t, name, X, T, F):
-    """Pointer and leading dimension of a T x F tensor of X's type and device."""
+def _hidden(t, name, X, T, F, dtype=None):
+    """Pointer and leading dimension of a T x F tensor of X's device and type, or that given."""
     st = t.stride()
-    if t.dtype is not X.dtype or t.shape != (T, F) or t.get_device() != X.get_device() or (st[1] != 1 and F != 1):
-        raise ValueError(f"{name} must be a {T} x {F} {X.dtype} tensor with unit column stride on {X.device}")
+    if t.dtype is not (dtype or X.dtype) or t.shape != (T, F) or t.get_device() != X.get_device() or (st[1] != 1 and F != 1):
+        raise ValueError(f"{name} must be a {T} x {F} {dtype or X.dtype} tensor with unit column stride on {X.device}")
     return t.data_ptr(), F if T < 2 else st[0]
 
 
-def _hidden_pair(a, b, names, X, T, F):
+def _hidden_pair(a, b, names, X, T, F, dtype=None):
     """The pointers of two T x F tensors, either of which may be None, and their leading dimension."""
-    pa, la = _hidden(a, names[0], X, T, F) if a is not None else (None, None)
-    pb, lb = _hidden(b, names[1], X, T, F) if b is not None else (None, None)
+    pa, la = _hidden(a, names[0], X, T, F, dtype) if a is not None else (None, None)
+    pb, lb = _hidden(b, names[1], X, T, F, dtype) if b is not None else (None, None)
     if la is not None and lb is not None:
         _pair(la, lb, f"{names[0]} and {names[1]}")
     return pa, pb, la if la is not None else (lb if lb is not None else F)
 
 
+def _kept(X):
+    """Type of the tensors that keep G and U."""
+    torch = _T or _torch()
+    return torch.int16 if X.dtype is torch.bfloat16 else X.dtype
+
+
 def glu_fwd(X, Wg, Wu, fn: str = "silu", Ag=None, Au=None, H=None, G=None, U=None, save: bool = False, stream=None):
     """H = f(X Wg^T [+ Ag]) * (X Wu^T [+ Au]), fn "silu", "gelu" or "gelu_tanh": returns H, with `save` (H, G, U), the last two what f
-    and the product were taken of, for glu_bwd (ff_glu_fwd).  Wg and Wu: F x n with one row stride, e.g. halves of one weight."""
+    and the product were taken of, for glu_bwd (ff_glu_fwd): fp32, or for bf16 activations int16 tensors of words with ten significant
+    bits.  Wg and Wu: F x n with one row stride, e.g. halves of one weight."""
     torch = _T or _torch()
     T, n, F, act, xp, ldx, wg, wu, ldw, dev = _glu_weights(X, Wg, Wu)
     if _elsewhere(dev):
@@ -1126,9 +1133,9 @@ def glu_fwd(X, Wg, Wu, fn: str = "silu", Ag=None, Au=None, H=None, G=None, U=Non
     gp = up = None
     ldg = F
     if save:
-        G = _new((T, F), X.dtype, X.device, stream) if G is None else G
-        U = _new((T, F), X.dtype, X.device, stream) if U is None else U
-        gp, up, ldg = _hidden_pair(G, U, ("G", "U"), X, T, F)
+        G = _new((T, F), _kept(X), X.device, stream) if G is None else G
+        U = _new((T, F), _kept(X), X.device, stream) if U is None else U
+        gp, up, ldg = _hidden_pair(G, U, ("G", "U"), X, T, F, _kept(X))
     _check((_lib or _load()).ff_glu_fwd(T, n, F, act, f, xp, ldx, wg, wu, ldw, ap, bp, lda, hp, ldh, gp, up, ldg, _stream(stream)))
     return (H, G, U) if save else H
 
@@ -1152,7 +1159,7 @@ def glu_bwd(dH, X, Wg, Wu, fn: str = "silu", G=None, U=None, Ag=None, Au=None, d
             beta_dx: float = 0.0, beta_dw: float = 0.0, want_dx: bool = True, want_dw: bool = False, workspace=None, stream=None):
     """Backward of glu_fwd from the gradient dH of H: returns (dG, dU, dX, dWg, dWu), the last three None where not wanted
     (ff_glu_bwd).  G, U: kept by the forward; without them they are made again, and Ag and Au are what the forward added.  dG and dU
-    are also the gradients of what adapters added; dG or dU may be dH, dG may be G, dU may be U."""
+    are also the gradients of what adapters added; dG or dU may be dH, and they may take the memory of G and U (G.view(X.dtype))."""
     torch = _T or _torch()
     T, n, F, act, xp, ldx, wg, wu, ldw, dev = _glu_weights(X, Wg, Wu)
     if _elsewhere(dev):
@@ -1163,7 +1170,7 @@ def glu_bwd(dH, X, Wg, Wu, fn: str = "silu", G=None, U=None, Ag=None, Au=None, d
     if (G is None) != (U is None):
         raise ValueError("G and U are kept together")
     dhp, lddh = _hidden(dH, "dH", X, T, F)
-    gp, up, ldg = _hidden_pair(G, U, ("G", "U"), X, T, F)
+    gp, up, ldg = _hidden_pair(G, U, ("G", "U"), X, T, F, _kept(X))
     ap, bp, lda = _hidden_pair(Ag, Au, ("Ag", "Au"), X, T, F)
     dG = _new((T, F), X.dtype, X.device, stream) if dG is None else dG
     dU = _new((T, F), X.dtype, X.device, stream) if dU is None else dU

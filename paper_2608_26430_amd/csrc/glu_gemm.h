@@ -52,7 +52,7 @@ struct ProjArgs {
   int64_t lddh;
   void* H;                // kForward
   int64_t ldh;
-  void* G;                // kForward: NULL if not kept; kBackward: dG
+  void* G;                // kForward: NULL if not kept (Kept words); kBackward: dG
   void* U;                //           dU
   int64_t ldg;
 };
@@ -132,6 +132,55 @@ __device__ __forceinline__ void store_run(float* p, const float (&v)[W]) {
   for (int q = 0; q < W; q += 4) store4(p + q, f32x4{v[q], v[q + 1], v[q + 2], v[q + 3]});
 }
 
+// G and U as they are kept: fp32 as they are, for bf16 activations words of 16 bits with ten significant ones: a sign, 6 bits of
+// exponent (bias 37: 1.5e-11 to 6.7e7 in full, smaller ones as subnormals, larger ones as infinity), 9 of mantissa.  In bf16, with
+// eight, their roundings would be as large as those of dG and dU themselves and add to them: 4096 tokens 4096 -> 11008, dU 0.0030
+// off and dX 0.0031 (relative norm), 0.0018 and 0.0024 so.
+constexpr float kKeepDown = 0x1p-90f, kKeepUp = 0x1p90f;     // fp32's exponent to the words' and back
+constexpr float kKeepMost = 0x1p-64f;                        // of a value times kKeepDown: the word of infinity
+template <class E>
+struct Kept;
+template <>
+struct Kept<float> {
+  typedef float Word;
+  template <int W>
+  static __device__ __forceinline__ void put(float* p, const float (&v)[W]) {
+    store_run<W>(p, v);
+  }
+  template <int W>
+  static __device__ __forceinline__ void get(const float* p, float (&v)[W]) {
+    load_run<W>(p, v);
+  }
+};
+template <>
+struct Kept<__bf16> {
+  typedef uint16_t Word;
+  static __device__ __forceinline__ unsigned word(float x) {
+    // rounded to nearest, halves away from zero; the sign moves down beside the six bits of exponent
+    const unsigned b = (__builtin_bit_cast(unsigned, __builtin_amdgcn_fmed3f(x * kKeepDown, -kKeepMost, kKeepMost)) + 0x2000u) >> 14;
+    return (b & 0x7fffu) | (b >> 2 & 0x8000u);
+  }
+  static __device__ __forceinline__ float value(unsigned w) {
+    const float x = __builtin_bit_cast(float, (w & 0x7fffu) << 14 | (w & 0x8000u) << 16);
+    return fabsf(x) < kKeepMost ? x * kKeepUp : x * INFINITY;
+  }
+  template <int W>
+  static __device__ __forceinline__ void put(uint16_t* p, const float (&v)[W]) {
+    unsigned x[W / 2];
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) x[i] = word(v[2 * i]) | word(v[2 * i + 1]) << 16;
+    if constexpr (W == 8) *reinterpret_cast<u32x4*>(p) = u32x4{x[0], x[1], x[2], x[3]};
+    else *reinterpret_cast<u32x2*>(p) = u32x2{x[0], x[1]};
+  }
+  template <int W>
+  static __device__ __forceinline__ void get(const uint16_t* p, float (&v)[W]) {
+    static_assert(W == 8, "a whole piece");
+    const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) v[2 * i] = value(x[i] & 0xffffu), v[2 * i + 1] = value(x[i] >> 16);
+  }
+};
+
 // What the end of a tile reads, W columns from c of row t, as it lies in memory: all of a wave's are on their way at once.
 template <class E, int W, int MODE>
 struct RawExtra {
@@ -166,12 +215,11 @@ __device__ __forceinline__ void finish_run(const ProjArgs& a, int64_t t, int c, 
 #pragma unroll
     for (int i = 0; i < W; ++i) u[i] += r.at(r.u, i);
   }
-  E* G = static_cast<E*>(a.G) + t * a.ldg + c;
-  E* U = static_cast<E*>(a.U) + t * a.ldg + c;
   if constexpr (MODE == kForward) {
+    typedef typename Kept<E>::Word Word;
     if (a.G) {
-      store_run<W>(G, g);
-      store_run<W>(U, u);
+      Kept<E>::put(static_cast<Word*>(a.G) + t * a.ldg + c, g);
+      Kept<E>::put(static_cast<Word*>(a.U) + t * a.ldg + c, u);
     }
 #pragma unroll
     for (int i = 0; i < W; ++i) g[i] = gated<FN, kFast>(g[i]).x * u[i];
@@ -184,8 +232,8 @@ __device__ __forceinline__ void finish_run(const ProjArgs& a, int64_t t, int c, 
       g[i] = x * u[i] * f.y;
       u[i] = x * f.x;
     }
-    store_run<W>(G, g);
-    store_run<W>(U, u);
+    store_run<W>(static_cast<E*>(a.G) + t * a.ldg + c, g);
+    store_run<W>(static_cast<E*>(a.U) + t * a.ldg + c, u);
   }
 }
 
@@ -378,28 +426,30 @@ template <class E, int BM, int BN, int WVM, int WVN, int NB, int WPE, int FN, in
 __global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArgs a) {
   __shared__ __align__(1024) char lds[NB * (BM + BN) * xent::kTileBytes];
   const int full = a.tm * a.tn - a.rest;
-  if ((int)blockIdx.x < full)
-    project<E, BM, BN, WVM, WVN, NB, FN, MODE>(a, lds, blockIdx.x, gridDim.x, full, [&](int at, int* i, int* j) {
-      int im, in;
-      xent::tile_of(xent::share_of(at, full), a.tm, a.tn, &im, &in);
-      *i = im * (BM / 2), *j = in * BN;
-    });
-  // Large tiles: those of a last round that would leave half of the CUs idle go out as halves of fewer rows.
+  // Large tiles: those of a last round that would leave half of the CUs idle go out as halves of fewer rows.  They come first: their
+  // workgroups' tiles then end at other times than the others', and the ends share the memory.
   if constexpr (BN == 256) {
     const int halves = 2 * a.rest;
-    if ((int)blockIdx.x >= halves) return;
     auto half = [&](int at, int* i, int* j) {
       const int id = xent::share_of(at, halves);
       int im, in;
       xent::tile_of(full + id / 2, a.tm, a.tn, &im, &in);
       *i = im * (BM / 2), *j = in * BN + id % 2 * (BN / 2);
     };
-    int i, j;
-    half(blockIdx.x, &i, &j);
-    if (j >= a.T) return;          // the second half of a last tile of few rows
-    __syncthreads();
-    project<E, BM, BN / 2, 2 * WVM, WVN / 2, NB, FN, MODE>(a, lds, blockIdx.x, halves, halves, half);
+    if ((int)blockIdx.x < halves) {
+      int i, j;
+      half(blockIdx.x, &i, &j);
+      // (not the second half of a last tile of few rows)
+      if (j < a.T) project<E, BM, BN / 2, WVM, WVN, NB, FN, MODE>(a, lds, blockIdx.x, halves, halves, half);
+      __syncthreads();
+    }
   }
+  if ((int)blockIdx.x < full)
+    project<E, BM, BN, WVM, WVN, NB, FN, MODE>(a, lds, blockIdx.x, gridDim.x, full, [&](int at, int* i, int* j) {
+      int im, in;
+      xent::tile_of(xent::share_of(at, full), a.tm, a.tn, &im, &in);
+      *i = im * (BM / 2), *j = in * BN;
+    });
 }
 
 // Few tokens, or few columns: 16 FNT rows, 16 columns of each product a workgroup.  Its KS waves share k in chunks of 256 bytes and read the
@@ -762,8 +812,9 @@ __global__ void __launch_bounds__(256) point_kernel(PointArgs a) {
   const int64_t t = item <= 0xffffffffll ? (int64_t)((unsigned)item / (unsigned)a.pieces) : item / a.pieces;
   const int c = (int)(item - t * a.pieces) * W;
   float g[W], u[W], x[W];
-  load_run<W>(static_cast<const E*>(a.G) + t * a.ldg + c, g);
-  load_run<W>(static_cast<const E*>(a.U) + t * a.ldg + c, u);
+  typedef typename Kept<E>::Word Word;
+  Kept<E>::get(static_cast<const Word*>(a.G) + t * a.ldg + c, g);
+  Kept<E>::get(static_cast<const Word*>(a.U) + t * a.ldg + c, u);
   load_run<W>(static_cast<const E*>(a.dH) + t * a.lddh + c, x);
 #pragma unroll
   for (int i = 0; i < W; ++i) {

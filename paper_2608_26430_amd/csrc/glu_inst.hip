@@ -31,8 +31,7 @@ static void project(int tile, int ks, const ProjArgs& a, hipStream_t s) {
     if (a.T > 16 && ks == 4) GLU_NARROW(2, 4);
     else if (a.T > 16) GLU_NARROW(2, 8);
     else if (ks == 4) GLU_NARROW(1, 4);
-    else if (ks == 8) GLU_NARROW(1, 8);
-    else GLU_NARROW(1, 16);
+    else GLU_NARROW(1, 8);
     return;
   }
   const int total = a.tm * a.tn;

@@ -62,12 +62,10 @@ inline double narrow_time(int64_t T, int64_t n, int64_t F, bool bf16) {
   const int64_t rows = 32 + (T > 16 ? 32 : T);
   return kLaunch + 1.0 + (double)(narrow_groups(T, F) * rows * n) * (bf16 ? 2 : 4) / (bf16 ? 8.0e6 : 6.5e6);
 }
-// Waves that share k: enough of them on the card, each with a chunk of 256 bytes at least.
+// Waves that share k: eight where four would leave the card empty and each has a chunk of 256 bytes (sixteen spill, and are slower).
 inline int narrow_waves(int64_t T, int64_t n, int64_t F, int esz) {
   const int64_t groups = narrow_groups(T, F), chunks = up(n * esz, 256) / 256;
-  for (int ks : {4, 8})
-    if (groups * ks >= 1024 || chunks <= ks) return ks;
-  return T > 16 ? 8 : 16;    // sixteen waves of two groups of tokens spill
+  return groups >= 256 || chunks <= 4 ? 4 : 8;
 }
 
 // Some of the tokens of a call; a call has one or two of them, one after the other.

@@ -57,6 +57,21 @@ def mm(a, b):
     return a.double() @ b.double()
 
 
+def kept_values(t):
+    """Values of a tensor that keeps G or U: as it is, or from int16 words (sign, 6 bits of exponent with bias 37, 9 of mantissa)."""
+    if t.dtype is not torch.int16:
+        return t.double()
+    w = t.int() & 0xFFFF
+    e, m = (w >> 9) & 63, (w & 511).double() / 512
+    v = torch.where(e > 0, (1 + m) * torch.exp2(e.double() - 37), m * 2.0 ** -36)
+    v = torch.where(e == 63, torch.full_like(v, float("inf")), v)
+    return torch.where(w >= 0x8000, -v, v)
+
+
+# unit roundoff of what is kept
+KEPT = {torch.bfloat16: 2.0 ** -10, torch.float32: 2.0 ** -24}
+
+
 def close(got, want, bound, what):
     err = (got.double() - want).abs()
     bad = ~(err <= bound * 1.02 + 1e-37)
@@ -96,8 +111,9 @@ def check_forward(d, fn, H, G=None, U_=None):
     ef = ef + 1.13 * eg
     close(H, f * p, u * (f * p).abs() + ef * p.abs() + (f.abs() + ef) * ep + 2 * V * (f * p).abs(), "H")
     if G is not None:
-        close(G, g, u * g.abs() + eg, "G")
-        close(U_, p, u * p.abs() + ep, "U")
+        k = KEPT[d["X"].dtype]
+        close(kept_values(G), g, k * g.abs() + eg + 2.0 ** -45, "G")
+        close(kept_values(U_), p, k * p.abs() + ep + 2.0 ** -45, "U")
 
 
 def check_point(d, fn, dG, dU, g, eg, p, ep):
@@ -133,14 +149,14 @@ def whole(d, fn, want_dw=True):
     assert torch.equal(H, alone)
     check_forward(d, fn, H, G, P)
     zero = torch.zeros((), device=G.device, dtype=torch.float64)
-    check_point(d, fn, kept[0], kept[1], G.double(), zero, P.double(), zero)
+    check_point(d, fn, kept[0], kept[1], kept_values(G), zero, kept_values(P), zero)
     check_point(d, fn, made[0], made[1], *forward_reference(d, fn))
     check_products(d, *kept)
     check_products(d, *made)
     return kept, made
 
 
-# few tokens (one to 32, with 4, 8 and 16 waves sharing k, k shorter than a chunk and ragged, columns that end inside a tile), small,
+# few tokens (one to 32, with 4 and 8 waves sharing k, k shorter than a chunk and ragged, columns that end inside a tile), small,
 # medium and large tiles, splits of k for dX and dW; test_glu_plans.py says which size runs what
 SIZES = [(1, 8, 8), (1, 4096, 1032), (5, 136, 24), (16, 1000, 104), (17, 1000, 4104), (32, 520, 2056), (31, 2048, 72), (3, 8, 8200),
          (2, 264, 8200), (33, 64, 64), (100, 520, 1000), (300, 128, 1400), (1500, 136, 136), (4000, 136, 136), (129, 1032, 2056), (700, 1032, 1544),
@@ -176,8 +192,10 @@ def test_strides_halves_of_one_weight_and_accumulation(dev, T, n, F, dtype):
     d = data(T, n, F, dtype, dev, T, adapters=True)
     dt = DT[dtype]
 
+    kept = torch.int16 if dtype == "bf16" else dt
+
     def inside(t, more):
-        buf = torch.full((t.shape[0] + 1, t.shape[1] + more), float("nan"), device=dev, dtype=dt)
+        buf = torch.full((t.shape[0] + 1, t.shape[1] + more), 12345 if t.dtype is torch.int16 else float("nan"), device=dev, dtype=t.dtype)
         buf[:t.shape[0], :t.shape[1]] = t
         return buf[:t.shape[0], :t.shape[1]], buf
     both = torch.full((2 * F + 1, n + 16), float("nan"), device=dev, dtype=dt)
@@ -185,8 +203,7 @@ def test_strides_halves_of_one_weight_and_accumulation(dev, T, n, F, dtype):
     Wg, Wu = both[:F, :n], both[F:2 * F, :n]
     X, dH, Au = (inside(d[k], m)[0] for k, m in (("X", 8), ("dH", 24), ("Au", 16)))
     d["Ag"] = None
-    outs = {k: inside(torch.zeros(s, device=dev, dtype=dt), 8) for k, s in (("H", (T, F)), ("G", (T, F)), ("U", (T, F)), ("dG", (T, F)),
-                                                                            ("dU", (T, F)))}
+    outs = {k: inside(torch.zeros((T, F), device=dev, dtype=kept if k in ("G", "U") else dt), 8) for k in ("H", "G", "U", "dG", "dU")}
     o = {k: v[0] for k, v in outs.items()}
     ff.glu_fwd(X, Wg, Wu, "gelu_tanh", Au=Au, H=o["H"], G=o["G"], U=o["U"], save=True)
     old = {k: torch.randn(s, device=dev).to(dt) for k, s in (("dX", (T, n)), ("dWg", (F, n)), ("dWu", (F, n)))}
@@ -196,10 +213,11 @@ def test_strides_halves_of_one_weight_and_accumulation(dev, T, n, F, dtype):
     torch.cuda.synchronize()
     check_forward(d, "gelu_tanh", o["H"], o["G"], o["U"])
     zero = torch.zeros((), device=dev, dtype=torch.float64)
-    check_point(d, "gelu_tanh", o["dG"], o["dU"], o["G"].double(), zero, o["U"].double(), zero)
+    check_point(d, "gelu_tanh", o["dG"], o["dU"], kept_values(o["G"]), zero, kept_values(o["U"]), zero)
     check_products(d, o["dG"], o["dU"], *(grads[k][0] for k in ("dX", "dWg", "dWu")), 0.5, *(old[k] for k in ("dX", "dWg", "dWu")))
     for k, (t, buf) in {**outs, **grads}.items():
-        assert bool(buf[t.shape[0]:].isnan().all()) and bool(buf[:, t.shape[1]:].isnan().all()), k
+        for around in (buf[t.shape[0]:], buf[:, t.shape[1]:]):
+            assert bool((around == 12345).all() if t.dtype is torch.int16 else around.isnan().all()), k
     # dG over dH, and made again
     dU = inside(torch.zeros((T, F), device=dev, dtype=dt), 24)[0]
     dG, dU, _, _, _ = ff.glu_bwd(dH, X, Wg, Wu, "gelu_tanh", Au=Au, dG=dH, dU=dU, want_dx=False)
@@ -211,9 +229,31 @@ def test_dg_and_du_over_what_was_kept(dev):
     d = data(130, 256, 512, "bf16", dev, 1)
     H, G, P = ff.glu_fwd(d["X"], d["Wg"], d["Wu"], save=True)
     want = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], G=G, U=P)
-    got = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], G=G, U=P, dG=G, dU=P)
+    got = ff.glu_bwd(d["dH"], d["X"], d["Wg"], d["Wu"], G=G, U=P, dG=G.view(torch.bfloat16), dU=P.view(torch.bfloat16))
     torch.cuda.synchronize()
-    assert got[0] is G and all(torch.equal(a, b) for a, b in zip(want[:3], got[:3]))
+    assert got[0].data_ptr() == G.data_ptr() and all(torch.equal(a, b) for a, b in zip(want[:3], got[:3]))
+
+
+def test_kept_words(dev):
+    """G and U of any size as they are kept: W is the identity, so that G is X and U is X as well.  From subnormals over the whole range to
+    infinity; rounded by at most half a step."""
+    n = 64
+    x = torch.zeros((40, n), device=dev)
+    e = torch.arange(40 * 32, device=dev).view(40, 32) % 100 - 55
+    x[:, :32] = torch.exp2(e.float()) * (1 + torch.rand((40, 32), device=dev))
+    x[:, 32:] = -x[:, :32]
+    x = x.to(torch.bfloat16)
+    eye = torch.eye(n, device=dev, dtype=torch.bfloat16)
+    add = (x.float() * 2.0 ** -8 * torch.rand((40, n), device=dev)).to(torch.bfloat16)      # digits below those of bf16
+    for T in (40, 9):
+        _, G, P = ff.glu_fwd(x[:T], eye, eye, "silu", add[:T], None, save=True)
+        torch.cuda.synchronize()
+        for t, want in ((G, x[:T].float() + add[:T].float()), (P, x[:T].float())):      # sums of two bf16 numbers are exact, nearly
+            got, want = kept_values(t), want.double()
+            inside = want.abs() < 2.0 ** 26 * (1 - 2.0 ** -10)
+            assert bool(got[~inside].isinf().all()) and torch.equal(got.sign(), torch.where(got == 0, torch.zeros_like(want), want.sign()))
+            bound = 2.0 ** -10 * want.abs() + 2.0 ** -46 + V * want.abs()
+            assert bool(((got - want).abs() <= bound)[inside].all()), float(((got - want).abs() / bound)[inside].max())
 
 
 def test_large_arguments(dev):
