@@ -380,12 +380,13 @@ ff_status ff_adamw_step_batched(int64_t count, int64_t n, float* const* c, const
  *                    entries of it may be NULL.
  *     m, v         : device, moments: n[i] fp32, 4-byte aligned (FF_STATES_F32), or n[i] bytes (FF_STATES_8BIT).
  *     m_exp, v_exp : device, ceil(n[i] / 256) bytes each (FF_STATES_8BIT; else NULL).
- *     All zeros are the states of a first step, of either kind.  The memory stays the caller's and must outlive the set.
+ *     All zeros are the states of a first step, of either kind.  The memory stays the caller's and must outlive the set; no two of
+ *     these arrays may overlap.
  *     weight_decay : host, per tensor, or NULL for zeros.
- *     Allocates a table on the current device (88 bytes a tensor, 8 for 4096 elements); on error *out is NULL.
+ *     Allocates a table on the current device (64 bytes a tensor, 8 for 4096 elements) and copies it there; on error *out is NULL.
  *   ff_adamw_set_step : one step of every tensor whose gradient is not NULL.
- *     g : HOST array of `count` device pointers, gradients of type g_dtype, element aligned; read in the call, so that a captured
- *         step keeps the addresses of its capture.
+ *     g : HOST array of `count` device pointers, gradients of type g_dtype, element aligned, outside of what the set writes; read in
+ *         the call, so that a captured step keeps the addresses of its capture.
  *     The hyperparameters are those of ff_adamw_step; gradients are multiplied by grad_scale.  lr_dev, grad_scale_dev (fp32)
  *     and step_dev (int64) are NULL or one device value each, read when the call runs: factors of lr and grad_scale, and an
  *     addend of step (the sum must be at least 1), for captured steps that are replayed.

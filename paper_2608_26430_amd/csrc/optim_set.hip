@@ -14,6 +14,7 @@
 // 65536, the bits from Philox 4x32-10 of (element / 4, step, tensor): a function of the element alone, whatever the
 // launch.  The moments and their place between codes are computed in fp64: in fp32 one element in a million would fall on the other
 // side.
+#include <algorithm>
 #include <cmath>
 #include <memory>
 #include <new>
@@ -381,6 +382,12 @@ hipError_t run_step(const ff_adamw_set* s, const void* const* g, const Hyper& h,
   });
 }
 
+// Memory that a step writes.
+struct Written {
+  uintptr_t first, end;
+  int64_t tensor;
+};
+
 ff_status check_set(const ff_adamw_set* s) {
   if (!s) return fail(FF_EINVAL, "the set is NULL");
   int dev = -1;
@@ -423,6 +430,22 @@ ff_status ff_adamw_set_create(int64_t count, const int64_t* n, int states, int g
   std::unique_ptr<ff_adamw_set> s;
   std::vector<char> host;
   try {
+    // a step's workgroups write all arrays at once: one element in two of them would have two writers
+    std::vector<Written> written;
+    written.reserve((size_t)count * 6);
+    for (int64_t i = 0; i < count; ++i) {
+      if (n[i] == 0) continue;
+      const uintptr_t len = (uintptr_t)n[i], state = eight ? len : 4 * len, blocks = (len + kBlock - 1) / kBlock;
+      auto add = [&](const void* p, uintptr_t bytes) { written.push_back(Written{(uintptr_t)p, (uintptr_t)p + bytes, i}); };
+      add(c[i], 4 * len), add(m[i], state), add(v[i], state);
+      if (copy && copy[i]) add(copy[i], 2 * len);
+      if (eight) add(m_exp[i], blocks), add(v_exp[i], blocks);
+    }
+    std::sort(written.begin(), written.end(), [](const Written& a, const Written& b) { return a.first < b.first; });
+    for (size_t i = 1; i < written.size(); ++i)
+      if (written[i].first < written[i - 1].end)
+        return ff::fail(FF_EINVAL, "arrays of tensors %lld and %lld overlap", (long long)written[i - 1].tensor,
+                        (long long)written[i].tensor);
     s.reset(new ff_adamw_set);
     s->first.resize((size_t)count + 1);
     host.resize((size_t)count * sizeof(Tensor) + (size_t)chunks * sizeof(Place));

@@ -68,8 +68,9 @@ def test_calls_refused_on_the_host():
     lib = binding._load()
     out, p = ctypes.c_void_p(), ctypes.c_void_p(1 << 20)
     n1, arr, wd = (ctypes.c_int64 * 1)(5), (ctypes.c_void_p * 1)(1 << 20), (ctypes.c_double * 1)(0.0)
+    arr_m, arr_v = (ctypes.c_void_p * 1)(2 << 20), (ctypes.c_void_p * 1)(3 << 20)
 
-    def create(count=1, n=n1, states=0, g=0, c=arr, m=arr, v=arr, mx=None, vx=None, copy=None, wd=wd, out=ctypes.byref(out)):
+    def create(count=1, n=n1, states=0, g=0, c=arr, m=arr_m, v=arr_v, mx=None, vx=None, copy=None, wd=wd, out=ctypes.byref(out)):
         return binding._STATUS[lib.ff_adamw_set_create(count, n, states, g, c, copy, m, v, mx, vx, wd, out)]
 
     odd = (ctypes.c_void_p * 1)((1 << 20) + 1)
@@ -79,6 +80,18 @@ def test_calls_refused_on_the_host():
                dict(wd=(ctypes.c_double * 1)(-0.5)), dict(wd=(ctypes.c_double * 1)(float("inf")))):
         assert create(**kw) == "FF_EINVAL", kw
         assert not out
+    # arrays that overlap: a tensor twice, moments that share memory, a copy inside another tensor's parameters, exponents
+    two = (ctypes.c_int64 * 2)(300, 300)
+
+    def ptrs(*a):
+        return (ctypes.c_void_p * len(a))(*a)
+
+    ok = dict(count=2, n=two, c=ptrs(0x100000, 0x101000), m=ptrs(0x102000, 0x103000), v=ptrs(0x104000, 0x105000), wd=None)
+    for kw in (dict(c=ptrs(0x100000, 0x100000)), dict(c=ptrs(0x100000, 0x100000 + 1196)), dict(v=ptrs(0x102000, 0x105000)),
+               dict(m=ptrs(0x102000, 0x1020a0)), dict(copy=ptrs(0x106000, 0x101004)), dict(copy=ptrs(0x106000, 0x106002))):
+        assert create(**{**ok, **kw}) == "FF_EINVAL" and "overlap" in lib.ff_last_error().decode(), kw
+    kw = dict(ok, states=1, mx=ptrs(0x106000, 0x106001), vx=ptrs(0x107000, 0x107002))
+    assert create(**kw) == "FF_EINVAL" and "overlap" in lib.ff_last_error().decode()
     assert binding._STATUS[lib.ff_adamw_set_step(None, arr, p, None)] == "FF_EINVAL"
     assert binding._STATUS[lib.ff_adamw_set_read(None, arr, arr, None)] == "FF_EINVAL"
     lib.ff_adamw_set_destroy(None)
