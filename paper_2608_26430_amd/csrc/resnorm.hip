@@ -397,6 +397,7 @@ ff_status ff_resnorm_fwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
   RESNORM_CHECK(check_rows("B", B, ldb, d->n, esz));
   RESNORM_CHECK(check_rows("X", X, ldx, d->n, esz));
   if (d->norm) RESNORM_CHECK(check_rows("Y", Y, ldy, d->n, esz));
+  if (d->norm && X == Y) return ff::fail(FF_EINVAL, "X and Y are the same memory");
   if ((uintptr_t)stats % 16) return ff::fail(FF_EINVAL, "stats is not 16-byte aligned");
   a.R = R, a.ldr = ldr, a.B = B, a.ldb = ldb, a.X = X, a.ldx = ldx, a.Y = Y, a.ldy = ldy;
   a.stats = reinterpret_cast<float4*>(stats);
@@ -440,6 +441,7 @@ ff_status ff_resnorm_bwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
     if (d->norm) RESNORM_CHECK(check_rows("dY", dY, lddy, d->n, esz));
     if (dR) RESNORM_CHECK(check_rows("dR", dR, lddr, d->n, esz));
     if (dB) RESNORM_CHECK(check_rows("dB", dB, lddb, d->n, esz));
+    if (dR && dR == dB) return ff::fail(FF_EINVAL, "dR and dB are the same memory");
     if (!stats || (uintptr_t)stats % 16) return ff::fail(FF_EINVAL, "stats is NULL or not 16-byte aligned");
     const Space at = space_of(a.T, d->n, a.groups, sh.wv == 0);
     if (vectors || dgate || sh.wv == 0) {
@@ -467,14 +469,18 @@ ff_status ff_resnorm_bwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
   const int nv = !!dpost_weight + !!dpost_bias + !!dweight + !!dbias;
   // (with T = 0 there are no partial rows: the sums are zero)
   const bool gate_sum = dgate && per_group != 1;
-  for (int64_t g0 = 0; g0 == 0 || (gate_sum && g0 < a.groups); g0 += 32768) {
-    const int64_t ng = !gate_sum ? 0 : (a.groups - g0 < 32768 ? a.groups - g0 : 32768);
+  const int64_t blocks = (d->n + 31) / 32;
+  // gate rows of a launch: it has fewer than 2^32 threads, and the four vectors' take at most half of them
+  int64_t most = ((int64_t)1 << 31) / (blocks * 1024);
+  most = most < 1 ? 1 : (most > 32768 ? 32768 : most);
+  for (int64_t g0 = 0; g0 == 0 || (gate_sum && g0 < a.groups); g0 += most) {
+    const int64_t ng = !gate_sum ? 0 : (a.groups - g0 < most ? a.groups - g0 : most);
     const int v = g0 == 0 ? nv : 0;
     if (v + ng == 0) break;
     SumArgs q{a.part, (int)groups, {dpost_weight, dpost_bias, dweight, dbias},
               a.gate_part ? a.gate_part + g0 * per_group * d->n : nullptr, (int)per_group, dgate ? dgate + g0 * d->n : nullptr,
               a.n, accumulate};
-    hipLaunchKernelGGL(sum_kernel, dim3((unsigned)((d->n + 31) / 32), (unsigned)(v + ng)), dim3(1024), 0, s, q, v);
+    hipLaunchKernelGGL(sum_kernel, dim3((unsigned)blocks, (unsigned)(v + ng)), dim3(1024), 0, s, q, v);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return ff::fail(FF_EDEVICE, "join backward: %s", hipGetErrorString(e));
   }
