@@ -210,6 +210,7 @@ ff_status ff_glu_fwd(int64_t T, int64_t n, int64_t F, int act, int fn, const voi
   if (G) {
     GLU_CHECK(check_rows("G", G, ldg, F, act));
     GLU_CHECK(check_rows("U", U, ldg, F, act));
+    if (G == U || G == H || U == H) return ff::fail(FF_EINVAL, "two of H, G and U are the same memory");
   }
   ProjArgs a{};
   a.Wg = Wg, a.Wu = Wu, a.X = X, a.ldw = ldw, a.ldx = ldx, a.Ag = Ag, a.Au = Au, a.lda = lda;
@@ -239,6 +240,7 @@ ff_status ff_glu_bwd(int64_t T, int64_t n, int64_t F, int act, int fn, const voi
   GLU_CHECK(check_sizes(T, n, F, act, fn));
   if (!G != !U) return ff::fail(FF_EINVAL, "G and U are kept together");
   if (!dWg != !dWu) return ff::fail(FF_EINVAL, "dWg and dWu are made together");
+  if (dWg && dWg == dWu) return ff::fail(FF_EINVAL, "dWg and dWu are the same memory");
   const Call c{T, n, F, act == FF_BF16, fn};
   const hipStream_t s = (hipStream_t)stream;
   if (dWg) {
@@ -265,6 +267,10 @@ ff_status ff_glu_bwd(int64_t T, int64_t n, int64_t F, int act, int fn, const voi
   }
   GLU_CHECK(check_rows("dG", dG, lddg, F, act));
   GLU_CHECK(check_rows("dU", dU, lddg, F, act));
+  if (dG == dU) return ff::fail(FF_EINVAL, "dG and dU are the same memory");
+  for (const void* p : {(const void*)dG, (const void*)dU})
+    if ((p == dH && lddg != lddh) || (G && (p == G || p == U) && lddg != ldg))
+      return ff::fail(FF_EINVAL, "dG or dU over dH, G or U needs the same leading dimension");
   if (dX) GLU_CHECK(check_rows("dX", dX, lddx, n, act));
   Parts dx{}, dw{};
   if (dX) dx = dx_product(T, n, F, c.bf16);

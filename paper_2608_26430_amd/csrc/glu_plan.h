@@ -51,6 +51,9 @@ inline double tiles_time(bool bf16, int tile, int64_t tiles, int64_t kt) {
 }
 
 inline int64_t tiles_of(int64_t M, int64_t N, int tile) { return xent::tiles_of(M, N, tile); }
+// A launch has fewer than 2^32 threads; large tiles are walked by one workgroup a CU.
+inline bool fits(int64_t groups, int threads) { return groups * threads < (int64_t)1 << 32; }
+inline bool tiles_fit(int tile, int64_t tiles) { return tile == kLarge || fits(tiles, 256); }
 
 // ------------------------------------------------------------------------------------------- projections
 
@@ -95,7 +98,7 @@ inline Parts parts_of(int64_t T, bool bf16, const One& one, const Columns& colum
       const int64_t t1 = rows * tile_n(tile);
       const Parts other = one(T - t1);
       const double t = time(tile, tm * rows) + other.time;
-      if (t >= 0.97 * best.time) continue;
+      if (t >= 0.97 * best.time || !tiles_fit(tile, tm * rows)) continue;
       best.count = 2, best.time = t;
       best.part[0] = {0, t1, tile, 0, 1, 0};
       best.part[1] = other.part[0];
@@ -109,10 +112,12 @@ inline Parts projection(int64_t T, int64_t n, int64_t F, bool bf16) {
   const int esz = bf16 ? 2 : 4;
   const int64_t kt = up(n, kk_of(esz)) / kk_of(esz);
   auto one = [&](int64_t rows) {
-    Parts p{1, {{0, rows, kSmall, narrow_waves(rows, n, F, esz), 1, 0}}, narrow_time(rows, n, F, bf16)};
+    const int ks = narrow_waves(rows, n, F, esz);
+    Parts p{1, {{0, rows, kSmall, ks, 1, 0}}, fits(narrow_groups(rows, F), ks * 64) ? narrow_time(rows, n, F, bf16) : 1e30};
     for (int tile = bf16 ? kLarge : kMedium; tile <= kSmall; ++tile) {
-      const double t = tiles_time(bf16, tile, tiles_of(2 * F, rows, tile), kt);
-      if (t < p.time) p = Parts{1, {{0, rows, tile, 0, 1, 0}}, t};
+      const int64_t tiles = tiles_of(2 * F, rows, tile);
+      const double t = tiles_time(bf16, tile, tiles, kt);
+      if (t < p.time && tiles_fit(tile, tiles)) p = Parts{1, {{0, rows, tile, 0, 1, 0}}, t};
     }
     return p;
   };
@@ -134,7 +139,7 @@ inline Parts gradient(int64_t rows, int64_t M, int64_t kt, int halves, int outs,
         const int64_t per = (kt + s - 1) / s, splits = (kt + per - 1) / per;
         double t = tiles_time(bf16, tile, tiles * splits, halves * per);
         if (splits > 1) t += 4.5 + (double)(splits * outs * N * M) * 8.0 / 4.5e6;
-        if (t < p.time) p = Parts{1, {{0, N, tile, 0, (int)splits, (int)per}}, t};
+        if (t < p.time && tiles_fit(tile, tiles * splits)) p = Parts{1, {{0, N, tile, 0, (int)splits, (int)per}}, t};
         if (tiles * splits >= 4 * kCUs) break;
       }
     }

@@ -60,6 +60,21 @@ def test_sizes_run_every_kernel(plans, bf16):
         assert any(len(x[k]) == 2 for x in p), k
 
 
+@pytest.mark.parametrize("T,n,F", [(1 << 28, 8, 8), (1 << 28, 8, 64), (1 << 28, 64, 8), (1 << 26, 8, 512), (1 << 20, 8, 1 << 16),
+                                   (4, 1 << 18, 1 << 18), (1 << 18, 1 << 18, 64)])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_largest_calls_fit_their_launches(plans, T, n, F, bf16):
+    """Workgroups times threads stay below 2^32, and tile numbers in 31 bits, at the longest calls that a card's memory holds."""
+    p = plans(T, n, F, bf16)
+    for name in p:
+        for q in p[name]:
+            if q["ks"]:
+                groups = -(-F // 16) * -(-q["rows"] // 32)
+                assert groups * q["ks"] * 64 < 2 ** 32
+            else:
+                assert q["tiles"] < 2 ** 31 and (q["tile"] == LARGE or q["tiles"] * 256 < 2 ** 32), (name, q)
+
+
 def test_calls_refused_on_the_host():
     lib, q = binding._load(), 1 << 20
     p = ctypes.c_void_p(q)
@@ -67,18 +82,24 @@ def test_calls_refused_on_the_host():
     def fwd(T=4, n=64, F=32, act=1, fn=0, X=p, ldx=64, Wg=p, Wu=p, ldw=64, Ag=None, Au=None, lda=32, H=p, ldh=32, G=None, U=None, ldg=32):
         return binding._STATUS[lib.ff_glu_fwd(T, n, F, act, fn, X, ldx, Wg, Wu, ldw, Ag, Au, lda, H, ldh, G, U, ldg, None)]
 
+    def at(i):
+        return ctypes.c_void_p(q + (i << 12))
+
     odd = ctypes.c_void_p(q + 8)
     for kw in (dict(T=-1), dict(T=(1 << 28) + 1), dict(n=60), dict(n=0), dict(F=36), dict(F=(1 << 18) + 8), dict(act=2), dict(fn=3),
                dict(fn=-1), dict(X=None), dict(ldx=56), dict(ldx=68), dict(ldx=(1 << 20) + 8), dict(Wg=None), dict(Wu=odd), dict(ldw=60),
-               dict(Ag=odd), dict(Au=p, lda=24), dict(H=None), dict(ldh=36), dict(G=p), dict(U=p), dict(G=p, U=p, ldg=24)):
+               dict(Ag=odd), dict(Au=p, lda=24), dict(H=None), dict(ldh=36), dict(G=p), dict(U=p), dict(G=p, U=p, ldg=24),
+               dict(G=p, U=at(9)), dict(G=at(9), U=at(9))):
         assert fwd(**kw) == "FF_EINVAL", kw
     assert fwd(T=0, X=None, H=None) == "FF_OK"
 
-    def bwd(T=4, dH=p, X=p, Wg=p, Wu=p, G=p, U=p, dG=p, dU=p, dX=p, dWg=None, dWu=None, lddw=64, ws=p, wsn=1 << 30):
-        return binding._STATUS[lib.ff_glu_bwd(T, 64, 32, 1, 0, dH, 32, X, 64, Wg, Wu, 64, None, None, 32, G, U, 32, dG, dU, 32, 0.0, dX,
-                                              64, 0.0, dWg, dWu, lddw, ws, wsn, None)]
+    def bwd(T=4, dH=at(1), X=p, Wg=p, Wu=p, G=at(2), U=at(3), dG=at(4), dU=at(5), dX=at(6), dWg=None, dWu=None, lddw=64, lddg=32,
+            ws=p, wsn=1 << 30):
+        return binding._STATUS[lib.ff_glu_bwd(T, 64, 32, 1, 0, dH, 32, X, 64, Wg, Wu, 64, None, None, 32, G, U, 32, dG, dU, lddg, 0.0,
+                                              dX, 64, 0.0, dWg, dWu, lddw, ws, wsn, None)]
 
-    for kw in (dict(dH=None), dict(G=None), dict(U=None), dict(G=None, U=None, X=None), dict(dG=None), dict(dU=odd), dict(dX=odd),
+    for kw in (dict(dU=at(4)), dict(dG=at(1), lddg=40), dict(dU=at(2), lddg=40), dict(dG=at(2), lddg=40), dict(dWg=at(7), dWu=at(7)),
+               dict(dH=None), dict(G=None), dict(U=None), dict(G=None, U=None, X=None), dict(dG=None), dict(dU=odd), dict(dX=odd),
                dict(dWg=p), dict(dWg=p, dWu=p, X=None), dict(Wg=None), dict(dWg=p, dWu=p, lddw=60), dict(ws=None),
                dict(ws=ctypes.c_void_p(q + 16)), dict(wsn=0)):
         assert bwd(**kw) == "FF_EINVAL", kw
