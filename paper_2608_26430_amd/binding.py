@@ -453,10 +453,10 @@ class _AdamWHyper(ctypes.Structure):
 
 
 class _Grads:
-    """Gradients of an AdamWSet: the tensors, kept alive, and their addresses."""
+    """Gradients of an AdamWSet: the set that checked them, the tensors, kept alive, and their addresses."""
 
-    def __init__(self, tensors, ptrs):
-        self.tensors, self.ptrs = tensors, ptrs
+    def __init__(self, owner, tensors, ptrs):
+        self.owner, self.tensors, self.ptrs = owner, tensors, ptrs
 
 
 class AdamWSet:
@@ -464,7 +464,7 @@ class AdamWSet:
 
     params: contiguous fp32 device tensors, stepped in place.  weight_decay: one number or one for each tensor.  states: "f32"
     or "8bit".  copies: None, or bf16 tensors (None for some) that every step writes the parameters to.  seed: of the random
-    rounding of 8-bit states.  The states are made here, zero: flat arrays (m_all, v_all) that hold tensor i from element
+    rounding of 8-bit states.  The states are made here, zero, on the current stream: flat arrays (m_all, v_all) that hold tensor i from element
     offsets[i], a multiple of 256, on; m, v (and m_exp, v_exp, exponents of the blocks of 8-bit states) are the tensors'
     views of them, 1-D, to be saved and restored as they are."""
 
@@ -535,7 +535,7 @@ class AdamWSet:
             if g.dtype is not self.grad_dtype or g.numel() != n or g.device != self.device or not g.is_contiguous():
                 raise ValueError(f"gradient {i} must be a contiguous {self.grad_dtype} tensor of {n} elements on {self.device}")
             out.append(g.data_ptr())
-        return _Grads(list(tensors), (ctypes.c_void_p * len(out))(*out))
+        return _Grads(self, list(tensors), (ctypes.c_void_p * len(out))(*out))
 
     def step(self, grads, lr: float, step: int, grad_scale: float = 1.0, lr_dev=None, grad_scale_dev=None, step_dev=None,
              stream=None):
@@ -549,6 +549,8 @@ class AdamWSet:
                 return self.step(grads, lr, step, grad_scale, lr_dev, grad_scale_dev, step_dev, stream)
         if not isinstance(grads, _Grads):
             grads = self.grads(grads)
+        elif grads.owner is not self:
+            raise ValueError("these gradients were checked for another set")
 
         def one(t, name, dtype):
             return None if t is None else _array(t.view(1), name, 1, dtype, dev)
@@ -953,8 +955,8 @@ def resnorm_fwd(R, B, gate=None, post="none", post_weight=None, post_bias=None, 
             return resnorm_fwd(R, B, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps,
                                post_eps, X, Y, stats, want_stats, stream)
     bp, ldb = _rows(B, "B", R)
-    d, has_norm, _ = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps,
-                    post_eps)
+    d, has_norm, _ = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale,
+                              block_scale, eps, post_eps)
     X, xp, ldx = _out_rows(X, "X", R, stream)
     yp, ldy, sp = None, n, None
     if has_norm:
@@ -992,8 +994,8 @@ def resnorm_bwd(R, B, dX, dY, stats, gate=None, post="none", post_weight=None, p
                 stream=None):
     """Backward of resnorm_fwd from the gradients dX (None: zero) and dY (None without a norm): returns (dR, dB, dgate,
     dpost_weight, dpost_bias, dweight, dbias), the last five fp32 and, with want_vectors, those of the gate and of the vectors that
-    were given (and of given outputs); None for the others (ff_resnorm_bwd).  accumulate: the five are added to the given ones.  dR and dB may
-    be any of the inputs."""
+    were given (and of given outputs); None for the others (ff_resnorm_bwd).  accumulate: the five are added to the given ones.
+    dR and dB may each be any of R, B, dX and dY."""
     torch = _T or _torch()
     f32 = torch.float32
     rp, ldr, T, n, dev = _input(R, "R")
@@ -1003,8 +1005,8 @@ def resnorm_bwd(R, B, dX, dY, stats, gate=None, post="none", post_weight=None, p
                                block_scale, eps, post_eps, dR, dB, dgate, dpost_weight, dpost_bias, dweight, dbias, accumulate,
                                want_dr, want_db, want_vectors, workspace, stream)
     bp, ldb = _rows(B, "B", R)
-    d, has_norm, groups = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale,
-                         eps, post_eps)
+    d, has_norm, groups = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale,
+                                   block_scale, eps, post_eps)
     dxp, lddx = _rows(dX, "dX", R) if dX is not None else (None, n)
     if has_norm and dY is None:
         raise ValueError("a norm needs dY")
@@ -1044,7 +1046,8 @@ def resnorm_bwd(R, B, dX, dY, stats, gate=None, post="none", post_weight=None, p
             at += 4 * n
     workspace = _workspace(workspace, _resnorm_bytes(T, n, groups) if workspace is None else 0, R.device, stream)
     _check((_lib or _load()).ff_resnorm_bwd(
-        d, rp, ldr, bp, ldb, dxp, lddx, dyp, lddy, _stats(stats, T, dev), drp, lddr, dbp, lddb, int(accumulate), *ptrs, workspace.data_ptr(), workspace.nbytes, _stream(stream)))
+        d, rp, ldr, bp, ldb, dxp, lddx, dyp, lddy, _stats(stats, T, dev), drp, lddr, dbp, lddb, int(accumulate), *ptrs,
+        workspace.data_ptr(), workspace.nbytes, _stream(stream)))
     return ((dR if want_dr else None), (dB if want_db else None), *outs)
 
 

@@ -269,7 +269,7 @@ ff_status ff_glu_bwd(int64_t T, int64_t n, int64_t F, int act, int fn, const voi
   GLU_CHECK(check_rows("dU", dU, lddg, F, act));
   if (dG == dU) return ff::fail(FF_EINVAL, "dG and dU are the same memory");
   for (const void* p : {(const void*)dG, (const void*)dU})
-    if ((p == dH && lddg != lddh) || (G && (p == G || p == U) && lddg != ldg))
+    if (T > 1 && ((p == dH && lddg != lddh) || (G && (p == G || p == U) && lddg != ldg)))
       return ff::fail(FF_EINVAL, "dG or dU over dH, G or U needs the same leading dimension");
   if (dX) GLU_CHECK(check_rows("dX", dX, lddx, n, act));
   Parts dx{}, dw{};

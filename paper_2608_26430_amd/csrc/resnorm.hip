@@ -1,6 +1,7 @@
 // Join of two blocks: the calls, the forward's instances, rows of any width, and the sums of the vectors' gradients
 // (resnorm.h has the kernels and their formulas).
 #include <cmath>
+#include <utility>
 
 #include "resnorm.h"
 
@@ -397,6 +398,7 @@ ff_status ff_resnorm_fwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
   RESNORM_CHECK(check_rows("B", B, ldb, d->n, esz));
   RESNORM_CHECK(check_rows("X", X, ldx, d->n, esz));
   if (d->norm) RESNORM_CHECK(check_rows("Y", Y, ldy, d->n, esz));
+  if (X == R && a.T > 1 && ldx != ldr) return ff::fail(FF_EINVAL, "X over R needs the same leading dimension");
   if (d->norm && X == Y) return ff::fail(FF_EINVAL, "X and Y are the same memory");
   if ((uintptr_t)stats % 16) return ff::fail(FF_EINVAL, "stats is not 16-byte aligned");
   a.R = R, a.ldr = ldr, a.B = B, a.ldb = ldb, a.X = X, a.ldx = ldx, a.Y = Y, a.ldy = ldy;
@@ -441,6 +443,9 @@ ff_status ff_resnorm_bwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
     if (d->norm) RESNORM_CHECK(check_rows("dY", dY, lddy, d->n, esz));
     if (dR) RESNORM_CHECK(check_rows("dR", dR, lddr, d->n, esz));
     if (dB) RESNORM_CHECK(check_rows("dB", dB, lddb, d->n, esz));
+    for (const auto& [p, ld] : {std::make_pair(dR, lddr), std::make_pair(dB, lddb)})
+      if (p && a.T > 1 && ((p == R && ld != ldr) || (p == B && ld != ldb) || (p == dX && ld != lddx) || (d->norm && p == dY && ld != lddy)))
+        return ff::fail(FF_EINVAL, "dR or dB over R, B, dX or dY needs the same leading dimension");
     if (dR && dR == dB) return ff::fail(FF_EINVAL, "dR and dB are the same memory");
     if (!stats || (uintptr_t)stats % 16) return ff::fail(FF_EINVAL, "stats is NULL or not 16-byte aligned");
     const Space at = space_of(a.T, d->n, a.groups, sh.wv == 0);

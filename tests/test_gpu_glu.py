@@ -225,6 +225,44 @@ def test_strides_halves_of_one_weight_and_accumulation(dev, T, n, F, dtype):
     check_point(d, "gelu_tanh", dG, dU, *forward_reference(d, "gelu_tanh"))
 
 
+@pytest.mark.parametrize("T,n,F,ld,ldw", [(65600, 64, 40, 65600, 64), (70, 40, 4200, 4200, 1 << 20), (3, 40, 4200, 4200, 1 << 20)])
+def test_offsets_past_32_bits(dev, T, n, F, ld, ldw):
+    """Rows of activations, then of weights and their gradients, that end past 2^32 elements: bits equal to those of packed rows."""
+    if torch.cuda.mem_get_info()[0] < 24 * 2 ** 30:
+        pytest.skip("needs 24 GiB")
+    gen = torch.Generator(device=dev).manual_seed(5)
+    bf = torch.bfloat16
+    X, dH, Wg, Wu = (torch.randn(s, device=dev, generator=gen).to(bf) for s in ((T, n), (T, F), (F, n), (F, n)))
+    near, far = {}, {}
+    if T > F:
+        buf = torch.empty(T * ld, device=dev, dtype=bf).view(T, ld)
+        at = 0
+        for k, src in (("X", X), ("dH", dH), ("H", None), ("dG", None), ("dU", None), ("G", None), ("U", None), ("dX", None)):
+            c = n if k in ("X", "dX") else F
+            v = buf[:, at:at + c]
+            far[k] = v.view(torch.int16) if k in ("G", "U") else v
+            if src is not None:
+                v.copy_(src)
+            at += c
+    else:
+        buf = torch.empty(F * ldw, device=dev, dtype=bf).view(F, ldw)
+        for i, (k, src) in enumerate((("Wg", Wg), ("Wu", Wu), ("dWg", None), ("dWu", None))):
+            far[k] = buf[:, i * n:(i + 1) * n]
+            if src is not None:
+                far[k].copy_(src)
+    got = []
+    for d in (near, far):
+        x, dh, wg, wu = d.get("X", X), d.get("dH", dH), d.get("Wg", Wg), d.get("Wu", Wu)
+        H, G, P = ff.glu_fwd(x, wg, wu, "gelu", H=d.get("H"), G=d.get("G"), U=d.get("U"), save=True)
+        out = ff.glu_bwd(dh, x, wg, wu, "gelu", G=G, U=P, dG=d.get("dG"), dU=d.get("dU"), dX=d.get("dX"), dWg=d.get("dWg"),
+                         dWu=d.get("dWu"), want_dw=True)
+        again = ff.glu_bwd(dh, x, wg, wu, "gelu", want_dx=False)[:2]
+        got.append((H, G, P, *out, *again))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert all(bool(t.isfinite().all()) and bool((t != 0).any(dim=1).all()) for t in (got[0][0], *got[0][3:]))
+
+
 def test_dg_and_du_over_what_was_kept(dev):
     d = data(130, 256, 512, "bf16", dev, 1)
     H, G, P = ff.glu_fwd(d["X"], d["Wg"], d["Wu"], save=True)

@@ -290,6 +290,10 @@ def test_refusals_write_nothing(dev):
     with pytest.raises(ValueError):
         s.step([g.bfloat16()], 0.1, 1)
     with pytest.raises(ValueError):
+        s.step(ff.AdamWSet([torch.ones(7, device=dev)]).grads([torch.ones(7, device=dev)]), 0.1, 1)
+    with pytest.raises(ff.FrameFTError):
+        ff.AdamWSet([c, c])
+    with pytest.raises(ValueError):
         s.step([torch.ones(200, device=dev)[::2]], 0.1, 1)
     for kw in (dict(lr=0.1, step=0), dict(lr=-0.1, step=1), dict(lr=float("nan"), step=1), dict(lr=0.1, step=1, grad_scale=float("inf"))):
         with pytest.raises(ff.FrameFTError) as ei:

@@ -218,6 +218,28 @@ def test_strides_places_and_outputs_over_inputs(dev, n, ld, at, dtype, post, nor
         assert np.isnan(to_np(buf)[out]).all(), name
 
 
+def test_offsets_past_32_bits(dev):
+    """Rows 65,600 elements apart, 65,600 of them: bits equal to those of packed rows."""
+    T, ld, n = 65600, 65600, 40
+    if torch.cuda.mem_get_info()[0] < 12 * 2 ** 30:
+        pytest.skip("needs 12 GiB")
+    buf = torch.empty(T * ld, device=dev, dtype=torch.bfloat16).view(T, ld)
+    gen = torch.Generator(device=dev).manual_seed(3)
+    far = [buf[:, 48 * i:48 * i + n] for i in range(8)]
+    near = [torch.randn((T, n), device=dev, generator=gen).bfloat16() for _ in range(4)] + [None] * 4
+    for a, b in zip(far[:4], near[:4]):
+        a.copy_(b)
+    w = torch.randn((2, n), device=dev, generator=gen)
+    how = dict(gate=torch.randn((41, n), device=dev, generator=gen), post="layer", post_weight=w[0], norm="rms", weight=w[1])
+    got = []
+    for R, B, dX, dY, X, Y, dR, dB in (near, far):
+        X, Y, stats = ff.resnorm_fwd(R, B, X=X, Y=Y, **how)
+        got.append((X, Y, stats, *ff.resnorm_bwd(R, B, dX, dY, stats, dR=dR, dB=dB, **how)))
+    torch.cuda.synchronize()
+    assert all((a is None and b is None) or torch.equal(a, b) for a, b in zip(*got))
+    assert bool(got[0][1].isfinite().all()) and bool((got[0][4] != 0).any(dim=1).all())
+
+
 def test_some_gradients_only(dev):
     """No dx, no dr, no db, no vectors, one vector: what is asked for is as in the whole call."""
     c = case(90, 1024, "bf16", "rms", "layer", 3, 5)

@@ -99,20 +99,22 @@ def test_calls_refused_on_the_host():
            dict(post=3), dict(norm=-1), dict(gate=q, groups=3), dict(gate=q, groups=0), dict(gate=q, groups=2, ldgate=63),
            dict(gate=q + 2), dict(weight=q + 1), dict(post_bias=q + 2), dict(eps=-1.0), dict(eps=float("nan")),
            dict(post_eps=float("inf")), dict(res_scale=float("nan")), dict(block_scale=float("inf")),
-           dict(Y=p), dict(R=None), dict(ldr=63), dict(B=None), dict(X=None), dict(Y=None), dict(ldy=10), dict(stats=ctypes.c_void_p(q + 4)),
+           dict(Y=p), dict(ldx=72), dict(R=None), dict(ldr=63), dict(B=None), dict(X=None), dict(Y=None), dict(ldy=10), dict(stats=ctypes.c_void_p(q + 4)),
            dict(R=ctypes.c_void_p(q + 2))]
     for kw in bad:
         assert fwd(**kw) == "FF_EINVAL", kw
     assert fwd(T=0, R=None) == "FF_OK"
     assert binding._STATUS[lib.ff_resnorm_fwd(None, p, 64, p, 64, p, 64, p, 64, p, None)] == "FF_EINVAL"
 
-    def bwd(dX=p, dY=p, stats=p, dR=p, dB=other, dgate=None, dpw=None, dpb=None, dw=None, db=None, ws=p, wsn=1 << 30, **kw):
+    def bwd(dX=p, dY=p, stats=p, dR=p, dB=other, dgate=None, dpw=None, dpb=None, dw=None, db=None, ws=p, wsn=1 << 30, lddr=64, lddb=64,
+            **kw):
         d = dict(T=4, n=64, act=0, post=1, norm=1, groups=1, ldgate=64, res_scale=1.0, block_scale=1.0, post_eps=1e-5, eps=1e-5)
         d.update(kw)
-        return binding._STATUS[lib.ff_resnorm_bwd(_packed(**d), p, 64, p, 64, dX, 64, dY, 64, stats, dR, 64,
-                                                  dB, 64, 0, dgate, dpw, dpb, dw, db, ws, wsn, None)]
+        return binding._STATUS[lib.ff_resnorm_bwd(_packed(**d), p, 64, p, 64, dX, 64, dY, 64, stats, dR, lddr,
+                                                  dB, lddb, 0, dgate, dpw, dpb, dw, db, ws, wsn, None)]
 
-    for kw in (dict(dB=p), dict(dgate=p), dict(post=0, dpw=p), dict(norm=0, db=p), dict(dY=None), dict(stats=None),
+    for kw in (dict(dB=p), dict(lddr=72), dict(dR=None, dB=p, lddb=72), dict(dgate=p), dict(post=0, dpw=p), dict(norm=0, db=p),
+               dict(dY=None), dict(stats=None),
                dict(stats=ctypes.c_void_p(q + 8)), dict(dw=p, ws=None), dict(dw=p, wsn=100), dict(dw=p, ws=ctypes.c_void_p(q + 16)),
                dict(dw=ctypes.c_void_p(q + 2)), dict(n=9001, ws=None)):
         assert bwd(**kw) == "FF_EINVAL", kw
