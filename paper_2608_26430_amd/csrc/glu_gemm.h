@@ -237,6 +237,12 @@ __device__ __forceinline__ void finish_run(const ProjArgs& a, int64_t t, int c, 
   }
 }
 
+constexpr int kHalfNB = 3;      // buffers of a halved large tile, which take its 128 KB and 16 more
+constexpr int lds_bytes(int BM, int BN, int NB) {
+  const int whole = NB * (BM + BN), half = BN == 256 ? kHalfNB * (BM + BN / 2) : 0;
+  return (whole > half ? whole : half) * xent::kTileBytes;
+}
+
 // A workgroup's share of `total` tiles: numbers wg, wg + step, ..; place(number, &i0, &j0) is where a tile is.
 template <class E, int BM, int BN, int WVM, int WVN, int NB, int FN, int MODE, class Place>
 __device__ __forceinline__ void project(const ProjArgs& a, char* lds, int wg, int step, int total, const Place& place_of) {
@@ -249,6 +255,7 @@ __device__ __forceinline__ void project(const ProjArgs& a, char* lds, int wg, in
   constexpr int kBuf = 2 * OpA::kBytes + OpB::kBytes;
   constexpr int kLoads = 2 * OpA::kLoads + OpB::kLoads;
   constexpr int kK = OpA::kK;
+  constexpr bool kAhead = BN > 32;     // a half tile's fragments are read under the other half's products
   constexpr int kReads = FM * OpA::kReads + FNT * OpB::kReads;
   constexpr int kMmas = FM * FNT * (sizeof(E) == 2 ? 1 : 4);
 
@@ -290,7 +297,7 @@ __device__ __forceinline__ void project(const ProjArgs& a, char* lds, int wg, in
     ob.seek(a.X, a.ldx, j0, a.T, 0);
     issue_last();
 #pragma unroll
-    for (int t = 1; t < (NB == 2 ? 2 : NB - 1); ++t) issue(t, t);
+    for (int t = 1; t < (kAhead ? NB : NB - 1); ++t) issue(t, t);
   };
 
   place(wg);
@@ -335,20 +342,20 @@ __device__ __forceinline__ void project(const ProjArgs& a, char* lds, int wg, in
 #pragma unroll
           for (int j = 0; j < FNT; ++j) acc[f][j] = Mma<E>::step(k, fa[f], fb[j], acc[f][j]);
     };
-    if constexpr (NB == 2) {
+    if constexpr (kAhead) {
       f32x4 fa[2][FM], fb[2][FNT];
-      ring_wait<kLoads>();
+      ring_wait<(NB - 1) * kLoads>();
       read(0, 0, fa[0], fb[0]);
-      for (int t0 = 0; t0 < a.kt; t0 += 2) {
+      for (int t0 = 0; t0 < a.kt; t0 += NB) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < NB; ++b) {
           if (t0 + b >= a.kt) break;
           read(b, 1, fa[1], fb[1]);
           multiply(fa[0], fb[0]);
           xent::interleave<kReads, kMmas>();
-          ring_wait<0>();
-          if (t0 + b + 2 < a.kt) issue(t0 + b + 2, b);
-          read(1 - b, 0, fa[0], fb[0]);
+          ring_wait<(NB - 2) * kLoads>();
+          if (NB > 2 || t0 + b + 2 < a.kt) issue(t0 + b + NB, b);
+          read((b + 1) % NB, 0, fa[0], fb[0]);
           multiply(fa[1], fb[1]);
           xent::interleave<kReads, kMmas>();
           close_block((t0 + b) % 4 == 3);
@@ -424,7 +431,7 @@ __device__ __forceinline__ void project(const ProjArgs& a, char* lds, int wg, in
 
 template <class E, int BM, int BN, int WVM, int WVN, int NB, int WPE, int FN, int MODE>
 __global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArgs a) {
-  __shared__ __align__(1024) char lds[NB * (BM + BN) * xent::kTileBytes];
+  __shared__ __align__(1024) char lds[lds_bytes(BM, BN, NB)];
   const int full = a.tm * a.tn - a.rest;
   // Large tiles: those of a last round that would leave half of the CUs idle go out as halves of fewer rows.  They come first: their
   // workgroups' tiles then end at other times than the others', and the ends share the memory.
@@ -440,7 +447,7 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) projection_kernel(ProjArg
       int i, j;
       half(blockIdx.x, &i, &j);
       // (not the second half of a last tile of few rows)
-      if (j < a.T) project<E, BM, BN / 2, WVM, WVN, NB, FN, MODE>(a, lds, blockIdx.x, halves, halves, half);
+      if (j < a.T) project<E, BM, BN / 2, 2 * WVM, WVN / 2, kHalfNB, FN, MODE>(a, lds, blockIdx.x, halves, halves, half);
       __syncthreads();
     }
   }
@@ -564,6 +571,7 @@ __device__ __forceinline__ void gradient(const GradArgs& a, char* lds, int wg, i
   constexpr int kBuf = OpA::kBytes + OpB::kBytes;
   constexpr int kLoads = OpA::kLoads + OpB::kLoads;
   constexpr int kK = OpA::kK;
+  constexpr bool kAhead = BN > 32;     // a half tile's fragments are read under the other half's products
   constexpr int kReads = FM * OpA::kReads + FNT * OpB::kReads;
   constexpr int kMmas = FM * FNT * (sizeof(E) == 2 ? 1 : 4);
   constexpr int kHalves = TRB ? 1 : 2, kOuts = TRB ? 2 : 1;
@@ -628,7 +636,7 @@ __device__ __forceinline__ void gradient(const GradArgs& a, char* lds, int wg, i
       oa.base = first_a, ob.base = first_b;
     }
 #pragma unroll
-    for (int t = kHalves; t < (NB == 2 ? 2 : NB - 1); ++t) issue(t, t);
+    for (int t = kHalves; t < (kAhead ? NB : NB - 1); ++t) issue(t, t);
   };
 
   place(wg);
@@ -683,20 +691,20 @@ __device__ __forceinline__ void gradient(const GradArgs& a, char* lds, int wg, i
 #pragma unroll
           for (int j = 0; j < FNT; ++j) acc[f][j] = Mma<E>::step(k, fa[f], fb[j], acc[f][j]);
     };
-    if constexpr (NB == 2) {
+    if constexpr (kAhead) {
       f32x4 fa[2][FM], fb[2][FNT];
-      ring_wait<kLoads>();
+      ring_wait<(NB - 1) * kLoads>();
       read(0, 0, fa[0], fb[0]);
-      for (int t0 = 0; t0 < nkt; t0 += 2) {
+      for (int t0 = 0; t0 < nkt; t0 += NB) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < NB; ++b) {
           if (t0 + b >= nkt) break;
           read(b, 1, fa[1], fb[1]);
           multiply(fa[0], fb[0]);
           xent::interleave<kReads, kMmas>();
-          ring_wait<0>();
-          if (t0 + b + 2 < nkt) issue(t0 + b + 2, b);
-          read(1 - b, 0, fa[0], fb[0]);
+          ring_wait<(NB - 2) * kLoads>();
+          if (NB > 2 || t0 + b + 2 < nkt) issue(t0 + b + NB, b);
+          read((b + 1) % NB, 0, fa[0], fb[0]);
           multiply(fa[1], fb[1]);
           xent::interleave<kReads, kMmas>();
           close_block((t0 + b) % 4 == 3);
@@ -761,7 +769,7 @@ __device__ __forceinline__ void gradient(const GradArgs& a, char* lds, int wg, i
 template <class E, int BM, int BN, int WVM, int WVN, int NB, bool TRB, int WPE>
 __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs a) {
   constexpr int kOuts = TRB ? 2 : 1;
-  __shared__ __align__(1024) char lds[NB * (BM + BN) * xent::kTileBytes];
+  __shared__ __align__(1024) char lds[lds_bytes(BM, BN, NB)];
   const int tiles = a.tm * a.tn * kOuts, full = tiles * a.splits - a.rest;
   auto tile = [&](int id) {
     GradPlace p;
@@ -787,7 +795,7 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
     };
     if (half(blockIdx.x).j >= a.N) return;
     __syncthreads();
-    gradient<E, BM, BN / 2, 2 * WVM, WVN / 2, NB, TRB>(a, lds, blockIdx.x, halves, halves, half);
+    gradient<E, BM, BN / 2, 2 * WVM, WVN / 2, kHalfNB, TRB>(a, lds, blockIdx.x, halves, halves, half);
   }
 }
 

@@ -1,6 +1,7 @@
 // Instances of the gated feed-forward's kernels (glu_gemm.h), compiled in parts: -DGLU_BF16=0/1 and -DGLU_PART=0..2 (the
 // projections with that function) or 3, 4 (dX, dW).
 #include "glu_gemm.h"
+#include "glu_plan.h"
 
 #if !defined(GLU_BF16) || !defined(GLU_PART)
 #error "GLU_BF16 and GLU_PART select the instances"
@@ -36,7 +37,7 @@ static void project(int tile, int ks, const ProjArgs& a, hipStream_t s) {
   }
   const int total = a.tm * a.tn;
   // large tiles: one workgroup per CU walks all of its tiles, each tile's first loads under the last one's results
-  const dim3 grid((unsigned)(total > xent::kCUs && tile == xent::kLarge ? xent::kCUs : total));
+  const dim3 grid((unsigned)tile_groups(tile, total, a.rest));
 #if GLU_BF16
   if (tile == xent::kLarge) {
     hipLaunchKernelGGL((projection_kernel<E, 256, 256, 2, 4, 2, 2, FN, MODE>), grid, dim3(512), 0, s, a);
@@ -63,10 +64,16 @@ hipError_t GLU_NAME(launch_point)(const PointArgs& a, hipStream_t s) {
 hipError_t GLU_NAME(launch_gradient)(int tile, const GradArgs& a, hipStream_t s) {
   constexpr bool TRB = GLU_PART == 4;
   const int total = a.tm * a.tn * (TRB ? 2 : 1) * a.splits;
-  const dim3 grid((unsigned)(total > xent::kCUs && tile == xent::kLarge ? xent::kCUs : total));
+  const dim3 grid((unsigned)tile_groups(tile, total, a.rest));
 #if GLU_BF16
   if (tile == xent::kLarge) {
     hipLaunchKernelGGL((gradient_kernel<E, 256, 256, 2, 4, 2, TRB, 2>), grid, dim3(512), 0, s, a);
+    return hipGetLastError();
+  }
+#endif
+#if GLU_BF16 && GLU_PART == 3
+  if (tile == xent::kMedium && dx_deep(true, total, 2 * a.kt_split)) {
+    hipLaunchKernelGGL((gradient_kernel<E, 128, 128, 2, 2, 4, TRB, 1>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
   }
 #endif

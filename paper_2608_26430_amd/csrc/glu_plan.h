@@ -22,7 +22,7 @@ constexpr int kk_of(int esz) { return 128 / esz; }   // k of a tile
 //   large   4096 x 4096 -> 8192 (1024 tiles) 386 us, 2981 x 3712 -> 1408 (132) 77, 256 x 4096 -> 11008 (86) 81
 //   medium  2048 x 4096 -> 4096 (1024) 120 (large 108), 2981 x 3712 -> 1408 (528) 87, 64 x 4096 -> 11008 (172) 46, 800 x 3968 -> 128
 //           (14) 29
-//   small   64 x 4096 -> 11008 (344) 37, 100 x 1024 -> 4096 (256) 8, 800 x 3968 -> 128 (50) 19
+//   small   64 x 4096 -> 11008 (344) 37, 100 x 1024 -> 4096 (256) 8, 800 x 3968 -> 128 (50) 19, 700 x 4096 -> 1024 (352) 30
 // fp32:
 //   medium  500 x 768 -> 2048 (128 tiles) 56, 1658 x 1024 -> 4096 (832) 250;  small  31 (512), 231 (3328); 64 x 1024 -> 4096 (128) 23
 struct TileCost {
@@ -30,13 +30,24 @@ struct TileCost {
   double few, one, full, ends;
 };
 constexpr TileCost kTileCosts[2][3] = {{{0, 0, 0, 0, 0}, {512, 2.0, 2.2, 3.84, 2}, {512, 0.60, 0.72, 1.08, 2}},
-                                       {{256, 1.15, 1.53, 1.53, 5}, {512, 0.45, 0.80, 0.92, 3}, {512, 0.25, 0.40, 0.45, 4}}};
+                                       {{256, 1.15, 1.53, 1.53, 5}, {512, 0.45, 0.80, 0.92, 3}, {512, 0.26, 0.28, 0.45, 4}}};
 constexpr double kLaunch = 2.0;
 
-// Of `tiles` tiles those of a last round of large ones that are halved, where their halves fit one round.
+// Of `tiles` tiles those of a last (or only) round of large ones that are halved, where their halves fit one round.  256 tokens, 4096 ->
+// 11008 (86 tiles) 80 us whole, 54 as halves; dX of 1700 tokens, 2304 <- 2 x 6000 (63 tiles x 2 splits) 134 and 94.
 inline int rest_of(int tile, int64_t tiles) {
   const int rest = (int)(tiles % kCUs);
-  return tile == kLarge && tiles > kCUs && rest <= kCUs / 2 ? rest : 0;
+  return tile == kLarge && rest <= kCUs / 2 ? rest : 0;
+}
+// Medium tiles of dX that have a CU each, and k tiles enough, take four buffers instead of two (of its steps, `kt`): 1003 tokens, 768 <-
+// 2 x 2304 51 us -> 38 (48 tiles), 32 -> 28 (96), 22 -> 22 (192); 256 tokens, 4096 <- 2 x 11008 71 -> 55 (256); 4 k tiles 7.8 -> 8.8.
+// The projections and dW gained nothing (500 x 768 -> 2304 10.2 -> 11.7, 512 x 2048 -> 4096 23.6 -> 21.7; dW 19 -> 17 to 12 -> 12).
+inline bool dx_deep(bool bf16, int64_t tiles, int64_t kt) { return bf16 && tiles <= kCUs && kt >= 12; }
+constexpr double kDeepFew = 0.40, kDeepOne = 0.55, kDeepEnds = 6;
+// Workgroups of a launch of `tiles` tiles: large ones are walked by one workgroup a CU.
+inline int tile_groups(int tile, int tiles, int rest) {
+  if (tile != kLarge) return tiles;
+  return tiles > kCUs ? kCUs : (rest ? 2 * rest : tiles);
 }
 
 inline double tiles_time(bool bf16, int tile, int64_t tiles, int64_t kt) {
@@ -46,7 +57,7 @@ inline double tiles_time(bool bf16, int tile, int64_t tiles, int64_t kt) {
   // (two fp32 tiles on a CU take as long as when every CU has two: the matrix units bound them)
   if (left > kCUs) last = bf16 ? c.one + (c.full - c.one) * (double)(left - kCUs) / kCUs : c.full;
   else if (left) last = c.few + (c.one - c.few) * (double)left / kCUs;
-  if (rest_of(tile, tiles)) last *= 0.6;
+  if (rest_of(tile, tiles)) last *= 0.56;
   return kLaunch + ((double)rounds * c.full + last) * ((double)kt + c.ends);
 }
 
@@ -128,7 +139,7 @@ inline Parts projection(int64_t T, int64_t n, int64_t F, bool bf16) {
 // ------------------------------------------------------------------------------------------- gradients
 
 // M columns and `rows` rows of `outs` results, kt k tiles in each of `halves` parts of the sum, which are split alike.  Partial sums are
-// written and read at about 4.5 TB/s by a launch more; those of large results are not worth the pass through memory.
+// written and read at about 7 TB/s (small ones through the caches) by a launch more; those of large results are not worth the pass through memory.
 inline Parts gradient(int64_t rows, int64_t M, int64_t kt, int halves, int outs, bool bf16) {
   auto one = [&](int64_t N) {
     Parts p{1, {{0, N, kSmall, 0, 1, (int)kt}}, 1e30};
@@ -138,7 +149,9 @@ inline Parts gradient(int64_t rows, int64_t M, int64_t kt, int halves, int outs,
         if (s > 1 && (halves * kt < 4 * s || (outs == 2 && 2 * rows > 4096))) break;
         const int64_t per = (kt + s - 1) / s, splits = (kt + per - 1) / per;
         double t = tiles_time(bf16, tile, tiles * splits, halves * per);
-        if (splits > 1) t += 4.5 + (double)(splits * outs * N * M) * 8.0 / 4.5e6;
+        if (tile == kMedium && halves == 2 && dx_deep(bf16, tiles * splits, halves * per))
+          t = kLaunch + (kDeepFew + (kDeepOne - kDeepFew) * (double)(tiles * splits) / kCUs) * ((double)(halves * per) + kDeepEnds);
+        if (splits > 1) t += 4.5 + (double)(splits * outs * N * M) * 8.0 / 7e6;
         if (t < p.time && tiles_fit(tile, tiles * splits)) p = Parts{1, {{0, N, tile, 0, (int)splits, (int)per}}, t};
         if (tiles * splits >= 4 * kCUs) break;
       }

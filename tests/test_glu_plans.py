@@ -57,6 +57,7 @@ def test_sizes_run_every_kernel(plans, bf16):
         # large tiles, more of them than workgroups, and halved ones; calls in two parts
         assert any(q["tile"] == LARGE and q["tiles"] > 256 and not q["ks"] for x in p for q in x[k]), k
         assert any(q["rest"] and not q["ks"] for x in p for q in x[k]), k
+        assert any(q["rest"] == q["tiles"] and not q["ks"] for x in p for q in x[k]), k
         assert any(len(x[k]) == 2 for x in p), k
 
 
@@ -73,6 +74,17 @@ def test_largest_calls_fit_their_launches(plans, T, n, F, bf16):
                 assert groups * q["ks"] * 64 < 2 ** 32
             else:
                 assert q["tiles"] < 2 ** 31 and (q["tile"] == LARGE or q["tiles"] * 256 < 2 ** 32), (name, q)
+
+
+def test_deep_tiles_of_dx_are_run(plans):
+    """Medium tiles with four buffers, of split sums and of whole ones, with a last k tile that is not full."""
+    deep = set()
+    for T, n, F in SIZES:
+        for q in plans(T, n, F, True)["dx"]:
+            per = -(-(-(-F // 64)) // q["splits"])
+            if q["tile"] == MEDIUM and q["tiles"] <= 256 and 2 * per >= 12 and F % 64:
+                deep.add(q["splits"] > 1)
+    assert deep == {True, False}
 
 
 def test_calls_refused_on_the_host():

@@ -161,7 +161,7 @@ def whole(d, fn, want_dw=True):
 SIZES = [(1, 8, 8), (1, 4096, 1032), (5, 136, 24), (16, 1000, 104), (17, 1000, 4104), (32, 520, 2056), (31, 2048, 72), (3, 8, 8200),
          (2, 264, 8200), (33, 64, 64), (100, 520, 1000), (300, 128, 1400), (1500, 136, 136), (4000, 136, 136), (129, 1032, 2056), (700, 1032, 1544),
          (1003, 768, 2304), (257, 2048, 136), (7, 520, 4104), (7, 520, 2056), (20, 64, 520),
-         (900, 1024, 4096)]
+         (900, 1024, 4096), (700, 4104, 1032), (300, 2056, 4104), (900, 1032, 3000)]
 BIG = [(2003, 1024, 4096), (4200, 4104, 8456), (2104, 4104, 11016), (2981, 3712, 1408), (4500, 4616, 4104)]
 
 
