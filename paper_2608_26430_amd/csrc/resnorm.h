@@ -10,7 +10,7 @@
 // forward had it before its rounding, so that y's gradient is that of the y that was returned.  Sums and statistics are
 // fp32.  Bound by memory: forward 4 T n, backward 6 T n elements moved.
 //
-// A row belongs to WV waves (1, 4 or 8) whose threads hold 8 or 16 elements.  Workgroups walk the rows with a stride, the
+// A row belongs to WV waves (1, 4 or 8) whose threads hold a piece of 16 bytes to 16 elements.  Workgroups walk the rows with a stride, the
 // vectors of their columns in registers, the next row read under the arithmetic of one.  The backward's walk a slice of the
 // rows of one gate row at a time and leave one partial row of each vector's gradient, added up in a fixed order by a second
 // launch: the same inputs give the same bits.

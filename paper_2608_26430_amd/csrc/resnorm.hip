@@ -237,11 +237,18 @@ RESNORM_INST(0) RESNORM_INST(1) RESNORM_INST(2) RESNORM_INST(3) RESNORM_INST(4) 
 
 namespace {
 
-Shape shape_of(int64_t n, int esz) {
+// Rows of up to 4 KB: four waves of a piece a thread where one wave would hold a whole row in few workgroups (16 x 1000 fp32, both
+// norms layer norms: backward 14.5 us, 7.6 with four waves; 300 x 768 bf16 forward 4.7 and 4.4, 1001 5.1 and 5.6, 12,608 19 and 32),
+// and in the backward wherever the wave's threads would hold 16 elements in fp32, whose sums spill (12,608 x 1000 100 and 62 us).  Wider
+// rows in fp32 take 8 elements a thread for the same reason (4000 x 2048 70 us with 16, 43 with 8; 4000 x 4096 123 and 96), but for the
+// widest: sixteen waves have no more registers in all (4000 x 5000 247 and 237).  bf16 spills little (4000 x 4096 63 either way).
+Shape shape_of(int64_t n, int esz, int64_t T, bool backward) {
   const int per = 16 / esz, whole = 16 / per;      // pieces of 16 elements a thread
   const int64_t p = (n + per - 1) / per;
   const bool part = n % per != 0;
   if (n < per) return {0, 0, part};
+  if (p > 64 && p <= 256 && (T <= 512 || p > whole * 64 || (backward && p > 128))) return {1, 4, part};
+  if (backward && esz == 4 && p > 256 && p <= 1024) return {2, p <= 512 ? 4 : 8, part};
   if (p <= whole / 2 * 64) return {whole / 2, 1, part};
   for (int wv : {1, 4, 8})
     if (p <= (int64_t)whole * wv * 64) return {whole, wv, part};
@@ -273,7 +280,7 @@ void launch_fwd(const Args& a, const Shape& sh, unsigned groups, hipStream_t s) 
 
 template <class E>
 hipError_t run_fwd(const Args& a, hipStream_t s) {
-  const Shape sh = shape_of(a.n, (int)sizeof(E));
+  const Shape sh = shape_of(a.n, (int)sizeof(E), a.T, false);
   constexpr int k = 16 / Pack<E>::kN;
   const unsigned groups = (unsigned)fwd_groups(a.T, sh);
   if (sh.wv == 0) {
@@ -282,6 +289,8 @@ hipError_t run_fwd(const Args& a, hipStream_t s) {
     launch_fwd<E, k / 2, 1>(a, sh, groups, s);
   } else if (sh.wv == 1) {
     launch_fwd<E, k, 1>(a, sh, groups, s);
+  } else if (sh.wv == 4 && sh.nv < k) {
+    launch_fwd<E, 1, 4>(a, sh, groups, s);
   } else if (sh.wv == 4) {
     launch_fwd<E, k, 4>(a, sh, groups, s);
   } else {
@@ -412,7 +421,7 @@ ff_status ff_resnorm_workspace(int64_t T, int64_t n, int64_t groups, int64_t* by
   ff::clear_error();
   RESNORM_CHECK(check_sizes(T, n, groups));
   if (!bytes) return ff::fail(FF_EINVAL, "bytes is NULL");
-  *bytes = space_of(T, n, groups, shape_of(n, 2).wv == 0 || shape_of(n, 4).wv == 0).bytes;
+  *bytes = space_of(T, n, groups, shape_of(n, 2, T, true).wv == 0 || shape_of(n, 4, T, true).wv == 0).bytes;
   return FF_OK;
 }
 
@@ -432,7 +441,7 @@ ff_status ff_resnorm_bwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
     return ff::fail(FF_EINVAL, "a vector's gradient is misaligned");
   const bool vectors = dpost_weight || dpost_bias || dweight || dbias;
   const bool bf16 = d->act == FF_BF16;
-  const Shape sh = shape_of(d->n, bf16 ? 2 : 4);
+  const Shape sh = shape_of(d->n, bf16 ? 2 : 4, d->T, true);
   unsigned groups = 0, per_group = 0;
   const hipStream_t s = (hipStream_t)stream;
   if (a.T > 0) {

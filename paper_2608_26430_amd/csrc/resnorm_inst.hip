@@ -33,9 +33,13 @@ static void go(const Args& a, const Shape& sh, unsigned groups, hipStream_t s) {
 
 hipError_t RESNORM_NAME(RESNORM_COMBO, RESNORM_BF16)(const Args& a, const Shape& sh, unsigned groups, hipStream_t s) {
   constexpr int k = 16 / Pack<E>::kN;      // pieces of 16 elements
-  if (sh.wv == 1 && sh.nv < k) go<k / 2, 1>(a, sh, groups, s);
-  else if (sh.wv == 1) go<k, 1>(a, sh, groups, s);
-  else if (sh.wv == 4) go<k, 4>(a, sh, groups, s);
+  // (shape_of: in fp32 16 elements a thread are left to the widest rows)
+  constexpr bool kF32 = sizeof(E) == 4;
+  if (sh.wv == 1 && sh.nv == k / 2) go<k / 2, 1>(a, sh, groups, s);
+  else if (sh.wv == 1) go<2, 1>(a, sh, groups, s);
+  else if (sh.wv == 4 && sh.nv == 1) go<1, 4>(a, sh, groups, s);
+  else if (sh.wv == 4) go<2, 4>(a, sh, groups, s);
+  else if (kF32 && sh.nv == 2) go<2, 8>(a, sh, groups, s);
   else go<k, 8>(a, sh, groups, s);
   return hipGetLastError();
 }

@@ -140,10 +140,10 @@ def check(c, dtype, post, norm, X, Y, stats, grads):
             close(g, o[name], B[name], name)
 
 
-# one row to many; widths of every instance (one wave with 8 and with 16 elements a lane, four and eight waves), odd ones, and
+# one row to many; widths of every instance (one, four and eight waves, 4 to 16 elements a lane), odd ones, and
 # ones that are read several times
 SIZES = [(1, 1), (3, 2), (7, 64), (66, 509), (513, 768), (130, 1000), (40, 1021), (5, 2048), (9, 2056), (700, 1024), (17, 4096),
-         (33, 8192), (3, 5001), (20, 8191), (2, 28672), (3, 9001), (600, 15)]
+         (33, 8192), (3, 5001), (20, 8191), (2, 28672), (3, 9001), (600, 15), (600, 509)]
 KINDS = [("rms", "rms"), ("layer", "layer"), ("none", "rms"), ("none", "layer"), ("layer", "none"), ("none", "none"), ("layer", "rms")]
 
 
