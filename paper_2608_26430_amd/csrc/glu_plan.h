@@ -57,7 +57,7 @@ inline double tiles_time(bool bf16, int tile, int64_t tiles, int64_t kt) {
   // (two fp32 tiles on a CU take as long as when every CU has two: the matrix units bound them)
   if (left > kCUs) last = bf16 ? c.one + (c.full - c.one) * (double)(left - kCUs) / kCUs : c.full;
   else if (left) last = c.few + (c.one - c.few) * (double)left / kCUs;
-  if (rest_of(tile, tiles)) last *= 0.56;
+  if (rest_of(tile, tiles)) last *= 0.58;
   return kLaunch + ((double)rounds * c.full + last) * ((double)kt + c.ends);
 }
 
