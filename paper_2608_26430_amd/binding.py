@@ -800,6 +800,14 @@ def _rows(t, name, like):
     return t.data_ptr(), t.shape[1] if t.shape[0] < 2 else st[0]
 
 
+def _matrix(t, name, shape, dtype, dev, T, n):
+    """_rows for a matrix whose shape T x n, type and device are known."""
+    st = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or (st[1] != 1 and n != 1):
+        raise ValueError(f"{name} must be a {T} x {n} {dtype} tensor with unit column stride on device {dev}")
+    return t.data_ptr(), (st[0] if T > 1 else n)
+
+
 def _input(t, name):
     """Pointer, leading dimension, sizes and device index of an activation that the call takes type and device from."""
     st = t.stride()
@@ -914,30 +922,34 @@ def _resnorm(T, n, act, dev, gate, post, post_weight, post_bias, norm, weight, b
     post_code, norm_code = _NORMS.get(post), _NORMS.get(norm)
     if post_code is None or norm_code is None:
         raise ValueError(f"unknown norms {post!r}, {norm!r}: 'none', 'rms' or 'layer'")
-    wt, ptrs = None, []
-    for v, name, there in ((post_weight, "post_weight", post_code), (post_bias, "post_bias", post_code),
-                           (weight, "weight", norm_code), (bias, "bias", norm_code)):
+    wt, ptrs, at = None, [0, 0, 0, 0], -1
+    for v in (post_weight, post_bias, weight, bias):
+        at += 1
         if v is None:
-            ptrs.append(0)
             continue
-        if not there:
-            raise ValueError(f"{name} of a norm that is not there")
         if wt is None:
             wt = v.dtype
-            if wt is not f32 and wt is not bf16:
-                raise ValueError("the norms' vectors must all be fp32 or all bf16")
-        ptrs.append(_array(v, name, n, wt, dev))
+        if (v.dtype is not wt or (wt is not f32 and wt is not bf16) or v.shape != (n,) or v.get_device() != dev
+                or not v.is_contiguous() or not (post_code if at < 2 else norm_code)):
+            name = ("post_weight", "post_bias", "weight", "bias")[at]
+            if not (post_code if at < 2 else norm_code):
+                raise ValueError(f"{name} of a norm that is not there")
+            raise ValueError(f"{name} must be a contiguous tensor of {n} elements on device {dev}; the norms' vectors must all be "
+                             "fp32 or all bf16")
+        ptrs[at] = v.data_ptr()
     groups, gp, ldgate, gate_bf16 = 1, 0, n, 0
     if gate is not None:
         gate_bf16 = int(gate.dtype is bf16)
         if not gate_bf16 and gate.dtype is not f32:
             raise ValueError("gate must be fp32 or bf16")
-        rows = gate.dim() == 2
-        groups = gate.shape[0] if rows else 1
-        if (gate.shape[-1] != n or gate.dim() > 2 or gate.get_device() != dev or (n != 1 and gate.stride(-1) != 1) or groups < 1
+        shape, st = gate.shape, gate.stride()
+        dims = len(st)
+        if dims == 2:
+            groups = shape[0]
+        if (dims < 1 or dims > 2 or shape[-1] != n or gate.get_device() != dev or (n != 1 and st[-1] != 1) or groups < 1
                 or T % groups):
             raise ValueError(f"gate must have {n} elements, or rows of {n} whose number divides {T}, on device {dev}")
-        gp, ldgate = gate.data_ptr(), (gate.stride(0) if groups > 1 else n)
+        gp, ldgate = gate.data_ptr(), (st[0] if groups > 1 else n)
     return _RESNORM.pack(T, n, act, int(wt is bf16), gate_bf16, post_code, norm_code, *ptrs, gp, ldgate, groups, res_scale,
                          block_scale, eps if post_eps is None else post_eps, eps), norm_code, groups
 
@@ -954,13 +966,24 @@ def resnorm_fwd(R, B, gate=None, post="none", post_weight=None, post_bias=None, 
         with torch.cuda.device(dev):
             return resnorm_fwd(R, B, gate, post, post_weight, post_bias, norm, weight, bias, res_scale, block_scale, eps,
                                post_eps, X, Y, stats, want_stats, stream)
-    bp, ldb = _rows(B, "B", R)
+    shape, dtype = R.shape, R.dtype
+    bp, ldb = _matrix(B, "B", shape, dtype, dev, T, n)
     d, has_norm, _ = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale,
                               block_scale, eps, post_eps)
-    X, xp, ldx = _out_rows(X, "X", R, stream)
-    yp, ldy, sp = None, n, None
+    plain = stream is None and R.is_contiguous()
+    ldx = ldy = n
+    yp = sp = None
+    if X is None:
+        X = torch.empty_like(R) if plain else _new(shape, dtype, R.device, stream)
+        xp = X.data_ptr()
+    else:
+        xp, ldx = _matrix(X, "X", shape, dtype, dev, T, n)
     if has_norm:
-        Y, yp, ldy = _out_rows(Y, "Y", R, stream)
+        if Y is None:
+            Y = torch.empty_like(R) if plain else _new(shape, dtype, R.device, stream)
+            yp = Y.data_ptr()
+        else:
+            yp, ldy = _matrix(Y, "Y", shape, dtype, dev, T, n)
     if stats is not None:
         sp = _stats(stats, T, dev)
     elif want_stats:
@@ -1004,19 +1027,29 @@ def resnorm_bwd(R, B, dX, dY, stats, gate=None, post="none", post_weight=None, p
             return resnorm_bwd(R, B, dX, dY, stats, gate, post, post_weight, post_bias, norm, weight, bias, res_scale,
                                block_scale, eps, post_eps, dR, dB, dgate, dpost_weight, dpost_bias, dweight, dbias, accumulate,
                                want_dr, want_db, want_vectors, workspace, stream)
-    bp, ldb = _rows(B, "B", R)
+    shape, dtype = R.shape, R.dtype
+    bp, ldb = _matrix(B, "B", shape, dtype, dev, T, n)
     d, has_norm, groups = _resnorm(T, n, _act_code(R), dev, gate, post, post_weight, post_bias, norm, weight, bias, res_scale,
                                    block_scale, eps, post_eps)
-    dxp, lddx = _rows(dX, "dX", R) if dX is not None else (None, n)
+    dxp, lddx = _matrix(dX, "dX", shape, dtype, dev, T, n) if dX is not None else (None, n)
     if has_norm and dY is None:
         raise ValueError("a norm needs dY")
-    dyp, lddy = _rows(dY, "dY", R) if has_norm else (None, n)
+    dyp, lddy = _matrix(dY, "dY", shape, dtype, dev, T, n) if has_norm else (None, n)
+    plain = stream is None and R.is_contiguous()
     drp = dbp = None
     lddr = lddb = n
     if want_dr:
-        dR, drp, lddr = _out_rows(dR, "dR", R, stream)
+        if dR is None:
+            dR = torch.empty_like(R) if plain else _new(shape, dtype, R.device, stream)
+            drp = dR.data_ptr()
+        else:
+            drp, lddr = _matrix(dR, "dR", shape, dtype, dev, T, n)
     if want_db:
-        dB, dbp, lddb = _out_rows(dB, "dB", R, stream)
+        if dB is None:
+            dB = torch.empty_like(R) if plain else _new(shape, dtype, R.device, stream)
+            dbp = dB.data_ptr()
+        else:
+            dbp, lddb = _matrix(dB, "dB", shape, dtype, dev, T, n)
     outs, ptrs, made = [dgate, dpost_weight, dpost_bias, dweight, dbias], [None] * 5, []
     for i, (given, name) in enumerate(((gate, "dgate"), (post_weight, "dpost_weight"), (post_bias, "dpost_bias"),
                                        (weight, "dweight"), (bias, "dbias"))):
@@ -1037,7 +1070,10 @@ def resnorm_bwd(R, B, dX, dY, stats, gate=None, post="none", post_weight=None, p
             ptrs[0] = dgate.data_ptr()
         else:
             ptrs[i] = _array(outs[i], name, n, f32, dev)
-    if made:            # the results of n elements in one allocation
+    if len(made) == 1:
+        outs[made[0]] = t = _new((1, n) if made[0] == 0 and gate.dim() == 2 else (n,), f32, R.device, stream)
+        ptrs[made[0]] = t.data_ptr()
+    elif made:          # the results of n elements in one allocation
         block = _new((len(made), n), f32, R.device, stream)
         at = block.data_ptr()
         for i, t in zip(made, block.unbind(0)):
@@ -1084,7 +1120,7 @@ def _glu_weights(X, Wg, Wu):
     gp, ldw, F, nw, wdev = _input(Wg, "Wg")
     if nw != n or Wg.dtype is not X.dtype or wdev != dev:
         raise ValueError(f"Wg must be an F x {n} {X.dtype} tensor on {X.device}")
-    up, ldu = _rows(Wu, "Wu", Wg)
+    up, ldu = _matrix(Wu, "Wu", Wg.shape, Wg.dtype, dev, F, n)
     return T, n, F, _act_code(X), xp, ldx, gp, up, _pair(ldw, ldu, "Wg and Wu"), dev
 
 
@@ -1097,7 +1133,7 @@ def _pair(ld, other, names):
 def _hidden(t, name, X, T, F, dtype=None):
     """Pointer and leading dimension of a T x F tensor of X's device and type, or that given."""
     st = t.stride()
-    if t.dtype is not (dtype or X.dtype) or t.shape != (T, F) or t.get_device() != X.get_device() or (st[1] != 1 and F != 1):
+    if t.dtype is not (dtype or X.dtype) or t.shape != (T, F) or t.get_device() != X.get_device() or st[1] != 1:
         raise ValueError(f"{name} must be a {T} x {F} {dtype or X.dtype} tensor with unit column stride on {X.device}")
     return t.data_ptr(), F if T < 2 else st[0]
 
@@ -1139,6 +1175,8 @@ def glu_fwd(X, Wg, Wu, fn: str = "silu", Ag=None, Au=None, H=None, G=None, U=Non
         G = _new((T, F), _kept(X), X.device, stream) if G is None else G
         U = _new((T, F), _kept(X), X.device, stream) if U is None else U
         gp, up, ldg = _hidden_pair(G, U, ("G", "U"), X, T, F, _kept(X))
+    elif G is not None or U is not None:
+        raise ValueError("G and U are written with save")
     _check((_lib or _load()).ff_glu_fwd(T, n, F, act, f, xp, ldx, wg, wu, ldw, ap, bp, lda, hp, ldh, gp, up, ldg, _stream(stream)))
     return (H, G, U) if save else H
 

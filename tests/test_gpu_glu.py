@@ -346,6 +346,7 @@ def test_refusals(dev):
     bad = [lambda: ff.glu_fwd(X, Wg, Wu, "relu"), lambda: ff.glu_fwd(X, Wg, Wu[:16]), lambda: ff.glu_fwd(X, Wg.float(), Wu.float()),
            lambda: ff.glu_fwd(X, Wg, Wu, Ag=torch.zeros((8, 33), device=dev, dtype=X.dtype)),
            lambda: ff.glu_fwd(X, Wg, torch.zeros((32, 72), device=dev, dtype=X.dtype)[:, :64]),
+           lambda: ff.glu_fwd(X, Wg, Wu, G=torch.zeros((8, 32), device=dev, dtype=torch.int16)),
            lambda: ff.glu_fwd(X[0], Wg, Wu), lambda: ff.glu_bwd(d["dH"], X, Wg, Wu, G=d["dH"]),
            lambda: ff.glu_bwd(d["dH"].float(), X, Wg, Wu), lambda: ff.glu_bwd(d["dH"], X, Wg, Wu, beta_dx=1.0)]
     for call in bad:

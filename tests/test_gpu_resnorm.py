@@ -291,6 +291,33 @@ def test_vectors_and_gates_in_bf16(dev):
     check(c, "f32", "layer", "layer", X, Y, stats, grads)
 
 
+def test_refusals(dev):
+    R = torch.ones((6, 64), device=dev)
+    B, w, half = R * 2, torch.ones(64, device=dev), torch.ones(64, device=dev, dtype=torch.bfloat16)
+    X, Y, stats = ff.resnorm_fwd(R, B, weight=w)
+    bad = [lambda: ff.resnorm_fwd(R, B[0]), lambda: ff.resnorm_fwd(R[0], B[0]), lambda: ff.resnorm_fwd(R, B.bfloat16()),
+           lambda: ff.resnorm_fwd(R, B[:5]), lambda: ff.resnorm_fwd(R, B.t()), lambda: ff.resnorm_fwd(R, B.cpu()),
+           lambda: ff.resnorm_fwd(R, B, norm="batch"), lambda: ff.resnorm_fwd(R, B, weight=w[:63]),
+           lambda: ff.resnorm_fwd(R, B, weight=w.double()), lambda: ff.resnorm_fwd(R, B, weight=w, bias=half),
+           lambda: ff.resnorm_fwd(R, B, weight=torch.ones(128, device=dev)[::2]), lambda: ff.resnorm_fwd(R, B, post_weight=w),
+           lambda: ff.resnorm_fwd(R, B, norm="none", bias=w), lambda: ff.resnorm_fwd(R, B, gate=w[:32]),
+           lambda: ff.resnorm_fwd(R, B, gate=torch.ones((4, 64), device=dev)), lambda: ff.resnorm_fwd(R, B, gate=w.double()),
+           lambda: ff.resnorm_fwd(R, B, gate=torch.ones((), device=dev)), lambda: ff.resnorm_fwd(R, B, X=torch.ones((6, 65), device=dev)),
+           lambda: ff.resnorm_fwd(R, B, stats=torch.ones((6, 3), device=dev)), lambda: ff.resnorm_bwd(R, B, X, None, stats, weight=w),
+           lambda: ff.resnorm_bwd(R, B, X, Y, stats[:5], weight=w), lambda: ff.resnorm_bwd(R, B, X, Y, stats, weight=w, dR=Y[0]),
+           lambda: ff.resnorm_bwd(R, B, X, Y, stats, weight=w, accumulate=True), lambda: ff.resnorm_bwd(R, B, X, Y, stats, dgate=w)]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            print("not refused:", i)
+    for call in (lambda: ff.resnorm_fwd(R, B, eps=-1.0), lambda: ff.resnorm_fwd(R, B, X=Y, Y=Y),
+                 lambda: ff.resnorm_bwd(R, B, X, Y, stats, dR=X, dB=X), lambda: ff.resnorm_bwd(R, B, X, Y, stats, dweight=w, weight=w,
+                                                                                              workspace=torch.empty(16, dtype=torch.uint8, device=dev))):
+        with pytest.raises(ff.FrameFTError) as ei:
+            call()
+        assert ei.value.name == "FF_EINVAL"
+
+
 def test_rows_of_nothing_and_of_one_value(dev):
     """Rows of zeros (rstd = 1 / sqrt(eps)) and constant rows of a layer norm give finite results and gradients."""
     n = 1000
