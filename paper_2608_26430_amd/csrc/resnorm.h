@@ -87,6 +87,19 @@ __device__ __forceinline__ void columns(const void* p, int bf16, float none, int
   }
 }
 
+// A piece of a result.  Of a piece that overlaps the one before only its own elements: the result may lie over an input whose shared
+// elements another wave has yet to read, or has written; what is read there in that case enters nothing.
+template <class E, bool PART, int KN>
+__device__ __forceinline__ void put_own(E* p, const float (&v)[KN], int skip) {
+  if (PART && skip) {
+#pragma unroll
+    for (int k = 1; k < KN; ++k)
+      if (k >= skip) p[k] = (E)v[k];
+  } else {
+    Pack<E>::put(p, v);
+  }
+}
+
 __device__ __forceinline__ const void* gate_row(const Args& a, int64_t group) {
   return a.gate ? static_cast<const char*>(a.gate) + group * a.ldgate * (a.gate_bf16 ? 2 : 4) : nullptr;
 }
@@ -167,9 +180,6 @@ __global__ void __launch_bounds__(threads_of(WV), 2) fwd_kernel(Args a) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int k = 0; k < kN; ++k) x[i][k] = fmaf(a.block * gt[i][k], p[i][k], a.res * x[i][k]);
-    // without a sum over the row, nothing else keeps a wave's results from a wave that has yet to read the elements that
-    // both of their pieces hold (x may be r)
-    if (PART && WV > 1 && !a.post && !a.norm) __syncthreads();
     E* xo = static_cast<E*>(a.X) + t * a.ldx;
     float y[NV][kN];
 #pragma unroll
@@ -179,7 +189,7 @@ __global__ void __launch_bounds__(threads_of(WV), 2) fwd_kernel(Args a) {
     if (a.norm) ns = centre<Rw, WV, PART>(y, a.norm, a.eps, l, a.n, sh[turn][2], sh[turn][3]);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      if (Rw::skip(i, l, a.n) < kN) Pack<E>::put(xo + Rw::at(i, l, a.n), x[i]);
+      if (Rw::skip(i, l, a.n) < kN) put_own<E, PART>(xo + Rw::at(i, l, a.n), x[i], Rw::skip(i, l, a.n));
     if (a.norm) {
       E* yo = static_cast<E*>(a.Y) + t * a.ldy;
 #pragma unroll
@@ -187,7 +197,7 @@ __global__ void __launch_bounds__(threads_of(WV), 2) fwd_kernel(Args a) {
         if (Rw::skip(i, l, a.n) < kN) {
 #pragma unroll
           for (int k = 0; k < kN; ++k) y[i][k] = fmaf(y[i][k] * ns.y, w[i][k], bias[i][k]);
-          Pack<E>::put(yo + Rw::at(i, l, a.n), y[i]);
+          put_own<E, PART>(yo + Rw::at(i, l, a.n), y[i], Rw::skip(i, l, a.n));
         }
       }
     }
@@ -404,21 +414,21 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
         mf = BIAS && a.post == kLayer ? s.x * inv_n : 0.f;
         mp = s.y * inv_n;
       }
-      if (PART && WV > 1 && !POST && !NORM) __syncthreads();   // as in the forward
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        if (Rw::skip(i, l, a.n) < kN) {
+        const int skip = Rw::skip(i, l, a.n);
+        if (skip < kN) {
           const int c = Rw::at(i, l, a.n);
           float o[kN];
           if (a.X) {
 #pragma unroll
             for (int k = 0; k < kN; ++k) o[k] = a.res * D[i][k];
-            Pack<E>::put(static_cast<E*>(a.X) + t * a.ldx + c, o);
+            put_own<E, PART>(static_cast<E*>(a.X) + t * a.ldx + c, o, skip);
           }
           if (a.Y) {
 #pragma unroll
             for (int k = 0; k < kN; ++k) o[k] = POST ? st.y * (f[i][k] - mf - hp[i][k] * mp) : f[i][k];
-            Pack<E>::put(static_cast<E*>(a.Y) + t * a.ldy + c, o);
+            put_own<E, PART>(static_cast<E*>(a.Y) + t * a.ldy + c, o, skip);
           }
         }
       }

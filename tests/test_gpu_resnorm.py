@@ -183,7 +183,7 @@ def _strided(a, dtype, dev, ld, at):
 
 
 @pytest.mark.parametrize("post,norm", [("rms", "rms"), ("none", "layer"), ("layer", "none"), ("none", "none")])
-@pytest.mark.parametrize("n,ld,at", [(1000, 1003, 1), (768, 776, 0), (768, 768, 3), (4097, 4097, 0), (8189, 8192, 2), (9000, 9002, 2)])
+@pytest.mark.parametrize("n,ld,at", [(1000, 1003, 1), (768, 776, 0), (768, 768, 3), (1021, 1027, 1), (4097, 4097, 0), (8189, 8192, 2), (9000, 9002, 2)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strides_places_and_outputs_over_inputs(dev, n, ld, at, dtype, post, norm):
     """Rows inside wider ones, off 16-byte alignment; x over r, dr over dx, db over dy or b; gradients added to what is there;
