@@ -446,10 +446,7 @@ def adamw_step_batched(cs: Sequence, gs: Sequence, ms: Sequence, vs: Sequence, l
     return cs
 
 
-class _AdamWHyper(ctypes.Structure):
-    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
-                ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
-                ("lr_dev", ctypes.c_void_p), ("grad_scale_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p)]
+_HYPER = struct.Struct("@5dqQ3P")       # the fields of ff_adamw_hyper
 
 
 class _Grads:
@@ -551,14 +548,15 @@ class AdamWSet:
             grads = self.grads(grads)
         elif grads.owner is not self:
             raise ValueError("these gradients were checked for another set")
-
-        def one(t, name, dtype):
-            return None if t is None else _array(t.view(1), name, 1, dtype, dev)
-
-        h = _AdamWHyper(lr, self.betas[0], self.betas[1], self.eps, grad_scale, step, self.seed & (1 << 64) - 1,
-                        one(lr_dev, "lr_dev", torch.float32), one(grad_scale_dev, "grad_scale_dev", torch.float32),
-                        one(step_dev, "step_dev", torch.int64))
-        _check((_lib or _load()).ff_adamw_set_step(self._h, grads.ptrs, ctypes.byref(h), _stream(stream)))
+        lrp = scale = at = 0
+        if lr_dev is not None:
+            lrp = _array(lr_dev.view(1), "lr_dev", 1, torch.float32, dev)
+        if grad_scale_dev is not None:
+            scale = _array(grad_scale_dev.view(1), "grad_scale_dev", 1, torch.float32, dev)
+        if step_dev is not None:
+            at = _array(step_dev.view(1), "step_dev", 1, torch.int64, dev)
+        h = _HYPER.pack(lr, *self.betas, self.eps, grad_scale, step, self.seed & 0xffffffffffffffff, lrp, scale, at)
+        _check((_lib or _load()).ff_adamw_set_step(self._h, grads.ptrs, h, _stream(stream)))
 
     def read(self, stream=None):
         """(m, v), laid out as m_all and v_all: the values of the moments, in bf16 for 8-bit states (ff_adamw_set_read), the states

@@ -95,3 +95,24 @@ def test_calls_refused_on_the_host():
     assert binding._STATUS[lib.ff_adamw_set_step(None, arr, p, None)] == "FF_EINVAL"
     assert binding._STATUS[lib.ff_adamw_set_read(None, arr, arr, None)] == "FF_EINVAL"
     lib.ff_adamw_set_destroy(None)
+
+
+def test_hyperparameters_are_laid_out_as_the_header_has_them(tmp_path):
+    """The binding's packed fields against the struct of include/frameft.h, compiled."""
+    import os
+    import shutil
+    import subprocess
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    fields = ("lr", "beta1", "beta2", "eps", "grad_scale", "step", "seed", "lr_dev", "grad_scale_dev", "step_dev")
+    src = tmp_path / "layout.cpp"
+    src.write_text('#include <cstdio>\n#include <cstddef>\n#include "frameft.h"\nint main() {' + "".join(
+        f'std::printf("%zu ", offsetof(ff_adamw_hyper, {f}));' for f in fields) + 'std::printf("%zu", sizeof(ff_adamw_hyper)); }')
+    exe, root = str(tmp_path / "layout"), os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run(["g++", "-I" + os.path.join(root, "include"), str(src), "-o", exe], check=True, timeout=120)
+    want = [int(x) for x in subprocess.run([exe], capture_output=True, text=True, check=True, timeout=60).stdout.split()]
+    for f, at in zip(fields, want):
+        one = binding._HYPER.pack(*(1 if k == f else 0 for k in fields))
+        on = [i for i, b in enumerate(one) if b]
+        assert on and at <= min(on) and max(on) < at + 8, f
+    assert binding._HYPER.size == want[-1]
