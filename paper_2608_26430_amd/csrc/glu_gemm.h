@@ -14,7 +14,7 @@
 // cycles of either), middle ones by LDS and a tile's start and end, those of few tokens by reading the weights.  Measured, bf16:
 // 4096 tokens of 4096 -> 11008 with addends and G, U kept 660 to 700 us (1.06 to 1.12 PFLOP/s), dX 531 to 575 (1.28 to 1.39);
 // 2003 tokens of 1024 -> 4096 with addends and GELU 40 us; one token of 4096 -> 11008 33 to 36 us (5.1 TB/s).  fp32, 500 tokens of
-// 768 -> 2048: 35 us each product (90 TFLOP/s).
+// 768 -> 2048: 33 to 35 us each product (90 to 94 TFLOP/s).
 #pragma once
 
 #include "xent_gemm.h"
@@ -581,6 +581,7 @@ __device__ __forceinline__ void gradient(const GradArgs& a, char* lds, int wg, i
   constexpr int kReads = FM * OpA::kReads + FNT * OpB::kReads;
   constexpr int kMmas = FM * FNT * (sizeof(E) == 2 ? 1 : 4);
   constexpr int kHalves = TRB ? 1 : 2, kOuts = TRB ? 2 : 1;
+  static_assert((kAhead ? NB : NB - 1) >= kHalves, "the halves' last tiles are read before the loop");
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

@@ -20,6 +20,11 @@ typedef float E;
 #define GLU_NAME2(n, p, b) GLU_NAME3(n, p, b)
 #define GLU_NAME(n) GLU_NAME2(n, GLU_PART, GLU_BF16)
 
+// Buffers of small tiles: in fp32, bound by the matrix units, two, so that four workgroups share a CU (500 tokens, 768 -> 2048 dW 35.5 ->
+// 33.4 us, 2048 tokens, 1024 -> 552 projections 58 -> 55, 1658 tokens, 1024 -> 4096 231 -> 225, dW 221 -> 208); dX starts with two tiles
+// and needs three at least.
+constexpr int kSmallNB = sizeof(E) == 4 && GLU_PART != 3 ? 2 : 4;
+
 #if GLU_PART < 3
 
 template <int MODE>
@@ -45,7 +50,7 @@ static void project(int tile, int ks, const ProjArgs& a, hipStream_t s) {
   }
 #endif
   if (tile == xent::kMedium) hipLaunchKernelGGL((projection_kernel<E, 128, 128, 2, 2, 2, 2, FN, MODE>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((projection_kernel<E, 128, 32, 4, 1, 4, 2, FN, MODE>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((projection_kernel<E, 128, 32, 4, 1, kSmallNB, 2, FN, MODE>), grid, dim3(256), 0, s, a);
 }
 
 hipError_t GLU_NAME(launch_projection)(int mode, int tile, int ks, const ProjArgs& a, hipStream_t s) {
@@ -78,7 +83,7 @@ hipError_t GLU_NAME(launch_gradient)(int tile, const GradArgs& a, hipStream_t s)
   }
 #endif
   if (tile == xent::kMedium) hipLaunchKernelGGL((gradient_kernel<E, 128, 128, 2, 2, 2, TRB, 2>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((gradient_kernel<E, 128, 32, 4, 1, 4, TRB, 2>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((gradient_kernel<E, 128, 32, 4, 1, kSmallNB, TRB, 2>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
