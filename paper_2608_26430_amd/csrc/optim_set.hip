@@ -395,9 +395,15 @@ struct Written {
 ff_status check_set(const ff_adamw_set* s) {
   if (!s) return fail(FF_EINVAL, "the set is NULL");
   int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev != s->device)
-    return fail(FF_EINVAL, "current device %d is not the set's device %d", dev, s->device);
+  if (hipGetDevice(&dev) != hipSuccess) (void)hipGetLastError(), dev = -1;
+  if (dev != s->device) return fail(FF_EINVAL, "current device %d is not the set's device %d", dev, s->device);
   return FF_OK;
+}
+
+// A call of the runtime failed; the error is not left for the next launch, which asks for the last one as its own.
+ff_status lost(ff_status st, const char* what) {
+  (void)hipGetLastError();
+  return fail(st, "%s", what);
 }
 
 }  // namespace
@@ -467,13 +473,13 @@ ff_status ff_adamw_set_create(int64_t count, const int64_t* n, int states, int g
     for (int64_t k = 0; k < (n[i] + kChunk - 1) / kChunk; ++k) hp[at++] = Place{(int)i, (int)k};
   }
   s->first[(size_t)count] = at;
-  if (hipGetDevice(&s->device) != hipSuccess) return ff::fail(FF_EDEVICE, "no HIP device");
+  if (hipGetDevice(&s->device) != hipSuccess) return lost(FF_EDEVICE, "no HIP device");
   void* dev = nullptr;
-  if (hipMalloc(&dev, host.size()) != hipSuccess) return ff::fail(FF_ENOMEM, "device allocation of %zu bytes failed", host.size());
+  if (hipMalloc(&dev, host.size()) != hipSuccess) return lost(FF_ENOMEM, "device allocation of the set's table failed");
   s->tensors = static_cast<Tensor*>(dev);
   s->places = reinterpret_cast<Place*>(s->tensors + count);
   if (hipMemcpy(dev, host.data(), host.size(), hipMemcpyHostToDevice) != hipSuccess)
-    return ff::fail(FF_EDEVICE, "copy of the set's table failed");
+    return lost(FF_EDEVICE, "copy of the set's table failed");
   *out = s.release();
   return FF_OK;
 }
