@@ -76,8 +76,9 @@ __device__ __forceinline__ float2 gated(float g) {
     const float e = exp_of(-0.5f * g * g, FAST);
     float cdf;
     if constexpr (FAST) {
-      // erfc(x) = exp(-x^2) Q(1 / (1 + 0.33 x)) for x = |g| / sqrt 2: Q is a polynomial fitted here to the least relative error over
-      // x from 0 to 10, 1e-7 (4e-7 in fp32 arithmetic).  The library's erfc took 7 of 41 us (2003 tokens, 1024 -> 4096).
+      // erfc(x) = exp(-x^2) Q(1 / (1 + 0.33 x)) for x = |g| / sqrt 2: Q is the polynomial of the least relative error over x from 0 to
+      // 10, 1e-7 (at most 1.1e-6 in fp32 arithmetic; tests/test_glu_function.py has the fit and the bound).  The library's erfc took 7
+      // of 41 us (2003 tokens, 1024 -> 4096).
       const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.33f * 0.70710678118654752f, 1.f));
       float q = fmaf(t, -0.135348532f, 0.460249317f);
       q = fmaf(t, q, -0.351171446f);
