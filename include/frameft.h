@@ -399,6 +399,8 @@ ff_status ff_adamw_step_batched(int64_t count, int64_t n, float* const* c, const
  * (v) half of word i mod 4 of Philox 4x32-10 with counter (i / 4 (64 bits), low 32 bits of step, number of the tensor) and key seed.
  * A v > 0 has a code of at least 1; where a moment is not finite in fp32, both of the element become 0.  The parameters are stepped with the
  * moments before their rounding; moments and their place between codes are computed in fp64.
+ * fp32 moments are made in fp64 and rounded to nearest once a step: a change below half a unit in a moment's last place, as the decay of v
+ * alone is for beta2 above 1 - 2^-25, leaves it as it is.
  * Calls on one set must be ordered.  Steps and reads are asynchronous on `stream` and allocate nothing; equal inputs give equal bits.
  * Errors: FF_EINVAL, FF_ENOMEM, FF_EDEVICE; after FF_EDEVICE some tensors may have been stepped.
  */

@@ -174,7 +174,9 @@ __global__ void __launch_bounds__(256) step_kernel(const Tensor* tensors, const 
   if (!g) return;
   const Tensor t = tensors[at.tensor];
   const Step s = step_of(h, t.decay);
-  const float b1 = (float)h.b1, a1 = (float)(1.0 - h.b1), b2 = (float)h.b2, a2 = (float)(1.0 - h.b2), scale = (float)s.scale;
+  // The moments are made in fp64 and rounded once: b and 1 - b rounded to fp32 each do not sum to one, and a long run's v would be
+  // off by the rest over 1 - b2 (1.7e-4 for b2 = 0.9999, 1.3% for 0.999999).
+  const double b1 = h.b1, a1 = 1.0 - h.b1, b2 = h.b2, a2 = 1.0 - h.b2;
   float* pm = static_cast<float*>(t.m);
   float* pv = static_cast<float*>(t.v);
   const int64_t i0 = (int64_t)at.chunk * kChunk + threadIdx.x * 4;
@@ -185,9 +187,9 @@ __global__ void __launch_bounds__(256) step_kernel(const Tensor* tensors, const 
     f32x4 c = get(t.c, i, t.n), gg = get(g, i, t.n), m = get(pm, i, t.n), v = get(pv, i, t.n);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float x = gg[j] * scale;
-      m[j] = fmaf(b1, m[j], a1 * x);
-      v[j] = fmaf(b2, v[j], a2 * (x * x));
+      const double x = (double)gg[j] * s.scale;
+      m[j] = (float)(b1 * (double)m[j] + a1 * x);
+      v[j] = (float)(b2 * (double)v[j] + a2 * (x * x));
       c[j] = stepped(c[j], m[j], v[j], s);
     }
     put(t.c, i, t.n, c);
