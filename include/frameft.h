@@ -534,19 +534,21 @@ ff_status ff_dropout(int64_t T, int64_t n, int act, const void* X, int64_t ldx, 
  *   H      : device, T x F.   G, U : device, T x F, one leading dimension ldg, kept for the backward; NULL to keep nothing.  fp32 for
  *            FF_F32; for FF_BF16 words of 16 bits that hold ten significant ones: from the highest bit on a sign, 6 bits of exponent
  *            (bias 37, 0 for subnormals) and 9 of mantissa, so that values from 1.5e-11 to 6.7e7 keep their digits; larger ones
- *            become infinite.
+ *            become infinite (a NaN the positive infinity).
  * ff_glu_bwd, from the gradient dH (T x F) of H:
  *   dU = dH f(G),   dG = dH U f'(G)                (T x F, one leading dimension lddg; also what the adapters' backwards take)
  *   dX = beta_dx dX + dG Wg + dU Wu                (skipped if NULL)
  *   dWg = beta_dw dWg + dG^T X,   dWu likewise     (F x n, one leading dimension lddw; skipped if both are NULL)
  *   G, U : as the forward kept them; X is then read for dWg and dWu alone, the weights for dX.  Without them (NULL) G and U
  *          are made again from X, the weights, Ag and Au, as the forward had them before their rounding.
+ *          Where a word is infinite, what does not depend on the value it stands for is as it should be (f' is 1 or 0, f of a large
+ *          negative G is 0, dH = 0 gives 0), and dH U and dH f(G) of the others are infinite.
  *   dG or dU may be dH, and dG may be G, dU may be U, with the same leading dimension.  beta = 0 does not read the output.
  *   workspace : device, 256-byte aligned, at least ff_glu_workspace bytes for the same T, n, F, act and the outputs wanted
  *          (FF_GLU_DX, FF_GLU_DW or both); not looked at without them.  It holds fp32 partial sums of products with few results.
  * All matrices but G and U of type act; n and F multiples of 8 (bf16) or 4 (fp32), at most 262144, T at most 2^28; 16-byte aligned, leading
  * dimensions multiples of 8 (4), at most 1048576.  Products accumulate in fp32; H, G, U, dG, dU, dX and the weights' gradients are
- * rounded once each (G and U as they are kept), and the products of the backward read dG and dU so.  Weights, X, dH and what is kept must be finite.
+ * rounded once each (G and U as they are kept), and the products of the backward read dG and dU so.  Weights, X, dH, Ag and Au must be finite.
  * T = 0 writes nothing but dWg = beta_dw dWg and dWu.
  */
 enum { FF_GLU_SILU = 0, FF_GLU_GELU = 1, FF_GLU_GELU_TANH = 2 };

@@ -1154,7 +1154,8 @@ def _kept(X):
 def glu_fwd(X, Wg, Wu, fn: str = "silu", Ag=None, Au=None, H=None, G=None, U=None, save: bool = False, stream=None):
     """H = f(X Wg^T [+ Ag]) * (X Wu^T [+ Au]), fn "silu", "gelu" or "gelu_tanh": returns H, with `save` (H, G, U), the last two what f
     and the product were taken of, for glu_bwd (ff_glu_fwd): fp32, or for bf16 activations int16 tensors of words with ten significant
-    bits.  Wg and Wu: F x n with one row stride, e.g. halves of one weight."""
+    bits: a sign, 6 bits of exponent with bias 37, 9 of mantissa.  Values beyond 6.7e7 are infinite words, G & 0x7e00 == 0x7e00; a
+    backward without G and U has no such limit.  Wg and Wu: F x n with one row stride, e.g. halves of one weight."""
     torch = _T or _torch()
     T, n, F, act, xp, ldx, wg, wu, ldw, dev = _glu_weights(X, Wg, Wu)
     if _elsewhere(dev):

@@ -67,6 +67,8 @@ struct ProjArgs {
 __device__ __forceinline__ float exp_of(float x, bool fast) { return fast ? __builtin_amdgcn_exp2f(x * 1.4426950408889634f) : expf(x); }
 __device__ __forceinline__ float inverse(float x, bool fast) { return fast ? __builtin_amdgcn_rcpf(x) : 1.f / x; }
 
+constexpr float kSaturated = 0x1p60f;      // f' is 1 or 0 there, and from 1e3 on
+
 template <int FN, bool FAST>
 __device__ __forceinline__ float2 gated(float g) {
   if constexpr (FN == FF_GLU_SILU) {
@@ -97,7 +99,8 @@ __device__ __forceinline__ float2 gated(float g) {
     // sqrt(2 / pi) (g + 0.044715 g^3), whose tanh is 2 s - 1
     constexpr float c = 0.79788456080286536f;
     const float s = inverse(1.f + exp_of(-2.f * c * g * fmaf(0.044715f * g, g, 1.f), FAST), FAST);
-    return make_float2(g * s, fmaf(g * s * (1.f - s), 2.f * c * fmaf(3.f * 0.044715f * g, g, 1.f), s));
+    const float b = __builtin_amdgcn_fmed3f(g, -kSaturated, kSaturated);    // whose square is a number; g s (1 - s) is zero long before
+    return make_float2(g * s, fmaf(g * s * (1.f - s), 2.f * c * fmaf(3.f * 0.044715f * b, b, 1.f), s));
   }
 }
 
@@ -142,7 +145,7 @@ __device__ __forceinline__ void store_run(float* p, const float (&v)[W]) {
 // G and U as they are kept: fp32 as they are, for bf16 activations words of 16 bits with ten significant ones: a sign, 6 bits of
 // exponent (bias 37: 1.5e-11 to 6.7e7 in full, smaller ones as subnormals, larger ones as infinity), 9 of mantissa.  In bf16, with
 // eight, their roundings would be as large as those of dG and dU themselves and add to them: 4096 tokens 4096 -> 11008, dU 0.0030
-// off and dX 0.0031 (relative norm), 0.0018 and 0.0024 so.
+// off and dX 0.0031 (relative norm), 0.0018 and 0.0024 so.  A NaN is kept as the positive infinity, whose f is infinite too.
 constexpr float kKeepDown = 0x1p-90f, kKeepUp = 0x1p90f;     // fp32's exponent to the words' and back
 constexpr float kKeepMost = 0x1p-64f;                        // of a value times kKeepDown: the word of infinity
 template <class E>
@@ -154,22 +157,30 @@ struct Kept<float> {
   static __device__ __forceinline__ void put(float* p, const float (&v)[W]) {
     store_run<W>(p, v);
   }
-  template <int W>
-  static __device__ __forceinline__ void get(const float* p, float (&v)[W]) {
-    load_run<W>(p, v);
+  typedef f32x4 Raw;
+  static __device__ __forceinline__ bool infinite(Raw, Raw) { return false; }
+  static __device__ __forceinline__ float any_value(float x) { return x; }
+  static __device__ __forceinline__ void get(Raw r, float (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = r[i];
   }
 };
 template <>
 struct Kept<__bf16> {
   typedef uint16_t Word;
   static __device__ __forceinline__ unsigned word(float x) {
-    // rounded to nearest, halves away from zero; the sign moves down beside the six bits of exponent
-    const unsigned b = (__builtin_bit_cast(unsigned, __builtin_amdgcn_fmed3f(x * kKeepDown, -kKeepMost, kKeepMost)) + 0x2000u) >> 14;
+    // rounded to nearest, halves away from zero; the sign moves down beside the six bits of exponent.  (Of -x, as a NaN comes out as the
+    // lower limit; the sum turns the sign back.)
+    const unsigned b = (__builtin_bit_cast(unsigned, __builtin_amdgcn_fmed3f(x * -kKeepDown, -kKeepMost, kKeepMost)) + 0x80002000u) >> 14;
     return (b & 0x7fffu) | (b >> 2 & 0x8000u);
   }
+  // of a word that is not infinite, and of any
   static __device__ __forceinline__ float value(unsigned w) {
-    const float x = __builtin_bit_cast(float, (w & 0x7fffu) << 14 | (w & 0x8000u) << 16);
-    return fabsf(x) < kKeepMost ? x * kKeepUp : x * INFINITY;
+    return __builtin_bit_cast(float, (w & 0x7fffu) << 14 | (w & 0x8000u) << 16) * kKeepUp;
+  }
+  static __device__ __forceinline__ float any_value(unsigned w) {
+    const float x = value(w);
+    return fabsf(x) < kKeepMost * kKeepUp ? x : x * INFINITY;
   }
   template <int W>
   static __device__ __forceinline__ void put(uint16_t* p, const float (&v)[W]) {
@@ -179,12 +190,17 @@ struct Kept<__bf16> {
     if constexpr (W == 8) *reinterpret_cast<u32x4*>(p) = u32x4{x[0], x[1], x[2], x[3]};
     else *reinterpret_cast<u32x2*>(p) = u32x2{x[0], x[1]};
   }
-  template <int W>
-  static __device__ __forceinline__ void get(const uint16_t* p, float (&v)[W]) {
-    static_assert(W == 8, "a whole piece");
-    const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+  typedef u32x4 Raw;
+  // Whether one of two pieces' words has an exponent of ones: it then carries into the sign's place.
+  static __device__ __forceinline__ bool infinite(Raw a, Raw b) {
+    unsigned any = 0;
 #pragma unroll
-    for (int i = 0; i < W / 2; ++i) v[2 * i] = value(x[i] & 0xffffu), v[2 * i + 1] = value(x[i] >> 16);
+    for (int i = 0; i < 4; ++i) any |= ((a[i] & 0x7e007e00u) + 0x02000200u) | ((b[i] & 0x7e007e00u) + 0x02000200u);
+    return any & 0x80008000u;
+  }
+  static __device__ __forceinline__ void get(Raw r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = value(r[i] & 0xffffu), v[2 * i + 1] = value(r[i] >> 16);
   }
 };
 
@@ -807,8 +823,8 @@ __global__ void __launch_bounds__(WVM * WVN * 64, WPE) gradient_kernel(GradArgs 
   }
 }
 
-// G and U kept: dG and dU element by element, 16 bytes a thread (4096 x 11008 bf16 70 us: 451 MB at 6.4 TB/s, part of it from the
-// last-level cache).
+// G and U kept: dG and dU element by element, 16 bytes a thread (4096 x 11008 bf16 82 us, 70 behind the forward that kept them: 451 MB
+// at 5.5 and 6.4 TB/s, part of it from the last-level cache).
 struct PointArgs {
   const void* dH;
   const void* G;
@@ -830,17 +846,40 @@ __global__ void __launch_bounds__(256) point_kernel(PointArgs a) {
   const int c = (int)(item - t * a.pieces) * W;
   float g[W], u[W], x[W];
   typedef typename Kept<E>::Word Word;
-  Kept<E>::get(static_cast<const Word*>(a.G) + t * a.ldg + c, g);
-  Kept<E>::get(static_cast<const Word*>(a.U) + t * a.ldg + c, u);
-  load_run<W>(static_cast<const E*>(a.dH) + t * a.lddh + c, x);
+  typedef typename Kept<E>::Raw Raw;
+  const Word* pg = static_cast<const Word*>(a.G) + t * a.ldg + c;
+  const Word* pu = static_cast<const Word*>(a.U) + t * a.ldg + c;
+  const E* px = static_cast<const E*>(a.dH) + t * a.lddh + c;
+  E* og = static_cast<E*>(a.dG) + t * a.lddg + c;
+  E* ou = static_cast<E*>(a.dU) + t * a.lddg + c;
+  const Raw rg = *reinterpret_cast<const Raw*>(pg), ru = *reinterpret_cast<const Raw*>(pu);
+  load_run<W>(px, x);
+#pragma unroll
+  for (int i = 0; i < W; ++i) asm volatile("" : "+v"(x[i]));     // read with the words, not behind the question
+  if (Kept<E>::infinite(rg, ru)) {
+    // An infinite word stands for a value that is not known but large: f' is that of any such value, f zero below and infinite above,
+    // and a factor of zero gives zero (rows that are masked by dH = 0 would otherwise reach dX and every weight's gradient as NaN).
+    // Few pieces have one: element by element, from memory again.
+#pragma unroll 1
+    for (int i = 0; i < W; ++i) {
+      const float gi = Kept<E>::any_value(pg[i]), ui = Kept<E>::any_value(pu[i]), xi = (float)px[i];
+      const float2 f = gated<FN, sizeof(E) == 2>(__builtin_amdgcn_fmed3f(gi, -kSaturated, kSaturated));
+      const bool none = xi == 0.f;
+      og[i] = (E)(none || f.y == 0.f ? 0.f : xi * ui * f.y);
+      ou[i] = (E)(none ? 0.f : xi * (gi > kSaturated ? gi : f.x));
+    }
+    return;
+  }
+  Kept<E>::get(rg, g);
+  Kept<E>::get(ru, u);
 #pragma unroll
   for (int i = 0; i < W; ++i) {
     const float2 f = gated<FN, sizeof(E) == 2>(g[i]);
     g[i] = x[i] * u[i] * f.y;
     u[i] = x[i] * f.x;
   }
-  store_run<W>(static_cast<E*>(a.dG) + t * a.lddg + c, g);
-  store_run<W>(static_cast<E*>(a.dU) + t * a.lddg + c, u);
+  store_run<W>(og, g);
+  store_run<W>(ou, u);
 }
 
 // tile: xent::Tile, or the few-token kernel (ks waves) where ks > 0
