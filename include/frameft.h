@@ -481,6 +481,7 @@ ff_status ff_layernorm_bwd(int64_t T, int64_t n, int act, const void* X, int64_t
  *     dgate        = [dgate +] block_scale sum over a gate row's rows of D p     (fp32, groups x n, contiguous)
  *     dpost_weight, dpost_bias, dweight, dbias = [... +] the norms' vectors' gradients   (fp32, n each)
  *   Any of the five may be NULL; they are added to what is there when accumulate != 0.  With T = 0 they become zero (or stay).
+ *   No two may share memory (a vector that two norms share takes the sum of two results).
  *   workspace : device, 256-byte aligned, at least ff_resnorm_workspace bytes for the same T, n and groups (1 without a gate).
  * X, Y, R, B, dX, dY, dR, dB: element alignment, any leading dimension >= n.  Sums and statistics are fp32.
  */

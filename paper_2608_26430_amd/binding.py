@@ -1015,8 +1015,8 @@ def resnorm_bwd(R, B, dX, dY, stats, gate=None, post="none", post_weight=None, p
                 stream=None):
     """Backward of resnorm_fwd from the gradients dX (None: zero) and dY (None without a norm): returns (dR, dB, dgate,
     dpost_weight, dpost_bias, dweight, dbias), the last five fp32 and, with want_vectors, those of the gate and of the vectors that
-    were given (and of given outputs); None for the others (ff_resnorm_bwd).  accumulate: the five are added to the given ones.
-    dR and dB may each be any of R, B, dX and dY."""
+    were given (and of given outputs); None for the others (ff_resnorm_bwd).  accumulate: the five are added to the given ones;
+    no two of them may share memory.  dR and dB may each be any of R, B, dX and dY."""
     torch = _T or _torch()
     f32 = torch.float32
     rp, ldr, T, n, dev = _input(R, "R")

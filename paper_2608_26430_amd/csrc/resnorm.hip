@@ -1,6 +1,7 @@
 // Join of two blocks: the calls, the forward's instances, rows of any width, and the sums of the vectors' gradients
 // (resnorm.h has the kernels and their formulas).
 #include <cmath>
+#include <initializer_list>
 #include <utility>
 
 #include "resnorm.h"
@@ -338,6 +339,20 @@ ff_status check_sizes(int64_t T, int64_t n, int64_t groups) {
   return FF_OK;
 }
 
+// Outputs of rows of n fp32 each, NULL for none: two that share memory would have two writers.
+struct Out {
+  const float* p;
+  int64_t rows;
+};
+ff_status check_apart(int64_t n, std::initializer_list<Out> outs) {
+  for (const Out* a = outs.begin(); a != outs.end(); ++a)
+    for (const Out* b = outs.begin(); b != a; ++b)
+      if (a->p && b->p && (uintptr_t)a->p < (uintptr_t)b->p + (uintptr_t)(4 * n * b->rows) &&
+          (uintptr_t)b->p < (uintptr_t)a->p + (uintptr_t)(4 * n * a->rows))
+        return fail(FF_EINVAL, "two vectors' gradients share memory");
+  return FF_OK;
+}
+
 int64_t up(int64_t x) { return (x + 255) / 256 * 256; }
 
 // Places in the workspace: partial rows of the four vectors, of the gate, the row sums of wide rows.
@@ -439,6 +454,7 @@ ff_status ff_resnorm_bwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
   if ((uintptr_t)dgate % 4 || (uintptr_t)dpost_weight % 4 || (uintptr_t)dpost_bias % 4 || (uintptr_t)dweight % 4 ||
       (uintptr_t)dbias % 4)
     return ff::fail(FF_EINVAL, "a vector's gradient is misaligned");
+  RESNORM_CHECK(check_apart(d->n, {{dgate, a.groups}, {dpost_weight, 1}, {dpost_bias, 1}, {dweight, 1}, {dbias, 1}}));
   const bool vectors = dpost_weight || dpost_bias || dweight || dbias;
   const bool bf16 = d->act == FF_BF16;
   const Shape sh = shape_of(d->n, bf16 ? 2 : 4, d->T, true);
