@@ -11,7 +11,7 @@
 // fp32.  Bound by memory: forward 4 T n, backward 6 T n elements moved.
 //
 // A row belongs to WV waves (1, 4 or 8) whose threads hold a piece of 16 bytes to 16 elements.  Workgroups walk the rows with a stride, the
-// vectors of their columns in registers, the next row read under the arithmetic of one.  The backward's walk a slice of the
+// vectors of their columns in registers (forward) or LDS (backward), the next row read under the arithmetic of one.  The backward's walk a slice of the
 // rows of one gate row at a time and leave one partial row of each vector's gradient, added up in a fixed order by a second
 // launch: the same inputs give the same bits.
 //
@@ -20,6 +20,7 @@
 // 16 x 4096 forward 5.2.
 #pragma once
 
+#include "resnorm_plan.h"
 #include "rows.h"
 
 namespace ff {
@@ -478,14 +479,6 @@ __global__ void __launch_bounds__(threads_of(WV), 2) bwd_kernel(Args a) {
   if constexpr (NORM) flush(dw, part + 2 * (int64_t)a.n, 0);
   if constexpr (NORM && BIAS) flush(db, part + 3 * (int64_t)a.n, 0);
 }
-
-// The instance of a row of n: 16-byte pieces of a thread, waves of a row (0: rows are read several times), overlapping last
-// piece.
-struct Shape {
-  int nv, wv;
-  bool part;
-};
-
 
 }  // namespace resnorm
 }  // namespace ff

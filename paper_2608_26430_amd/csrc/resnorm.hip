@@ -192,7 +192,7 @@ struct SumArgs {
 
 // out = [out +] sum over the partial rows, in a fixed order: 32 columns x 32 shares of the rows per workgroup.  blockIdx.y: the
 // vectors that are wanted, then the gate's rows.
-__global__ void __launch_bounds__(1024) sum_kernel(SumArgs a, int vectors) {
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(SumArgs a, int vectors) {
   __shared__ float sh[32][33];
   const int k = threadIdx.x & 31, q = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + k;
@@ -237,40 +237,6 @@ __global__ void __launch_bounds__(1024) sum_kernel(SumArgs a, int vectors) {
 RESNORM_INST(0) RESNORM_INST(1) RESNORM_INST(2) RESNORM_INST(3) RESNORM_INST(4) RESNORM_INST(5)
 
 namespace {
-
-// Rows of up to 4 KB: four waves of a piece a thread where one wave would hold a whole row in few workgroups (16 x 1000 fp32, both
-// norms layer norms: backward 14.5 us, 7.6 with four waves; 300 x 768 bf16 forward 4.7 and 4.4, 1001 5.1 and 5.6, 12,608 19 and 32),
-// and in the backward wherever the wave's threads would hold 16 elements in fp32, whose sums spill (12,608 x 1000 100 and 62 us).  Wider
-// rows in fp32 take 8 elements a thread for the same reason (4000 x 2048 70 us with 16, 43 with 8; 4000 x 4096 123 and 96), but for the
-// widest: sixteen waves have no more registers in all (4000 x 5000 247 and 237).  bf16 spills little (4000 x 4096 63 either way).
-Shape shape_of(int64_t n, int esz, int64_t T, bool backward) {
-  const int per = 16 / esz, whole = 16 / per;      // pieces of 16 elements a thread
-  const int64_t p = (n + per - 1) / per;
-  const bool part = n % per != 0;
-  if (n < per) return {0, 0, part};
-  if (p > 64 && p <= 256 && (T <= 512 || p > whole * 64 || (backward && p > 128))) return {1, 4, part};
-  if (backward && esz == 4 && p > 256 && p <= 1024) return {2, p <= 512 ? 4 : 8, part};
-  if (p <= whole / 2 * 64) return {whole / 2, 1, part};
-  for (int wv : {1, 4, 8})
-    if (p <= (int64_t)whole * wv * 64) return {whole, wv, part};
-  return {0, 0, part};
-}
-
-int64_t fwd_groups(int64_t T, const Shape& s) {
-  const int rows = s.wv == 1 ? 4 : 1;
-  const int64_t g = (T + rows - 1) / rows;
-  return g < 1024 ? g : 1024;
-}
-
-// Workgroups of a backward, at most: each leaves partial rows to be added up.
-constexpr int kGroups = 512;
-int64_t most_groups(int64_t n) { return n <= 4096 ? kGroups : kGroups / 2; }
-
-// Slices of a group of `rows` rows: all groups' together fill the workgroups.
-int64_t slices_of(int64_t rows, int64_t groups, int64_t n, int at_once) {
-  const int64_t most = (rows + at_once - 1) / at_once, want = most_groups(n) / groups;
-  return want < 1 ? 1 : (want < most ? want : most);
-}
 
 template <class E, int NV, int WV>
 void launch_fwd(const Args& a, const Shape& sh, unsigned groups, hipStream_t s) {
@@ -351,23 +317,6 @@ ff_status check_apart(int64_t n, std::initializer_list<Out> outs) {
           (uintptr_t)b->p < (uintptr_t)a->p + (uintptr_t)(4 * n * a->rows))
         return fail(FF_EINVAL, "two vectors' gradients share memory");
   return FF_OK;
-}
-
-int64_t up(int64_t x) { return (x + 255) / 256 * 256; }
-
-// Places in the workspace: partial rows of the four vectors, of the gate, the row sums of wide rows.
-struct Space {
-  int64_t gate, sums, bytes;
-};
-Space space_of(int64_t T, int64_t n, int64_t groups, bool wide) {
-  const int64_t G = most_groups(n), rows = T < G ? (T ? T : 1) : G;
-  Space s;
-  s.gate = up(rows * 4 * n * 4);
-  // a group of one slice needs none
-  s.sums = s.gate + (groups < G ? up(rows * n * 4) : 0);
-  s.bytes = s.sums + (wide ? up(T * 16) : 0);
-  if (s.bytes < 256) s.bytes = 256;
-  return s;
 }
 
 ff_status fill_args(const ff_resnorm* d, Args* a) {
@@ -499,20 +448,17 @@ ff_status ff_resnorm_bwd(const ff_resnorm* d, const void* R, int64_t ldr, const 
   const int nv = !!dpost_weight + !!dpost_bias + !!dweight + !!dbias;
   // (with T = 0 there are no partial rows: the sums are zero)
   const bool gate_sum = dgate && per_group != 1;
-  const int64_t blocks = (d->n + 31) / 32;
-  // gate rows of a launch: it has fewer than 2^32 threads, and the four vectors' take at most half of them
-  int64_t most = ((int64_t)1 << 31) / (blocks * 1024);
-  most = most < 1 ? 1 : (most > 32768 ? 32768 : most);
-  for (int64_t g0 = 0; g0 == 0 || (gate_sum && g0 < a.groups); g0 += most) {
-    const int64_t ng = !gate_sum ? 0 : (a.groups - g0 < most ? a.groups - g0 : most);
+  for (int64_t g0 = 0, ng = 0;; g0 += ng) {
     const int v = g0 == 0 ? nv : 0;
+    ng = gate_sum ? sum_rows(d->n, v, a.groups - g0) : 0;
     if (v + ng == 0) break;
     SumArgs q{a.part, (int)groups, {dpost_weight, dpost_bias, dweight, dbias},
               a.gate_part ? a.gate_part + g0 * per_group * d->n : nullptr, (int)per_group, dgate ? dgate + g0 * d->n : nullptr,
               a.n, accumulate};
-    hipLaunchKernelGGL(sum_kernel, dim3((unsigned)blocks, (unsigned)(v + ng)), dim3(1024), 0, s, q, v);
+    hipLaunchKernelGGL(sum_kernel, dim3((unsigned)sum_blocks(d->n), (unsigned)(v + ng)), dim3(kSumThreads), 0, s, q, v);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return ff::fail(FF_EDEVICE, "join backward: %s", hipGetErrorString(e));
+    if (!gate_sum) break;
   }
   return FF_OK;
 }
