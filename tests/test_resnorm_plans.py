@@ -1,4 +1,5 @@
-"""The launches of the join's sums (csrc/resnorm_plan.h, compiled and asked on the CPU)."""
+"""Which instances of the join's kernels the sizes of the GPU tests run, and the launches of its sums (csrc/resnorm_plan.h, compiled and
+asked on the CPU)."""
 import os
 import shutil
 import subprocess
@@ -31,3 +32,20 @@ def test_launches_of_the_sums_have_fewer_than_two_to_the_32_threads(ask, n, vect
         row, = ask([f"sums {n} {vectors} {groups}"])
         threads, rows = row[::2], row[1::2]
         assert all(0 < t < 2 ** 32 for t in threads) and all(r > 0 for r in rows) and sum(rows) == groups, (groups, row)
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+@pytest.mark.parametrize("esz", [2, 4])
+def test_sizes_run_every_instance(ask, esz, backward):
+    pytest.importorskip("torch")
+    from tests.test_gpu_resnorm_instances import KINDS, SIZES
+    widths = sorted({n + d for n in [1, 4, 8, 9000, 20000] + [1 << k for k in range(4, 15)] for d in range(-9, 10) if n + d > 0} | set(range(3, 9000, 97)))
+    every = [(T, n) for T in (1, 512, 513, 100_000) for n in widths]
+    shapes = {tuple(s) for s in ask([f"shape {T} {n} {esz} {backward}" for T, n in every]) if s[1]}
+    run = {tuple(s) for s in ask([f"shape {T} {n} {esz} {backward}" for T, n in SIZES]) if s[1]}
+    assert run == shapes, (shapes - run, run - shapes)
+    # rows that are read several times, too
+    assert any(not s[1] for s in ask([f"shape {T} {n} {esz} {backward}" for T, n in SIZES]))
+    # the backward's groups of instances: norms on both sides, after, before, none, each as RMS without biases and otherwise
+    assert {(post != "none", norm != "none", bias or "layer" in (post, norm)) for post, norm, bias in KINDS} == {
+        (True, True, False), (True, True, True), (False, True, False), (False, True, True), (True, False, True), (False, False, False)}
