@@ -39,6 +39,10 @@ inline int rest_of(int tile, int64_t tiles) {
   const int rest = (int)(tiles % kCUs);
   return tile == kLarge && rest <= kCUs / 2 ? rest : 0;
 }
+// What a round of halves takes of one of whole tiles.  Over 210 products (70 each of the projections, dX and dW, 64 to 4096 tokens) whose
+// plan the number decides, the chosen plans take over the fastest of those timed 3.8% more with 0.50, 2.5 with 0.54, 2.0 with 0.56, 1.8 with
+// 0.58, 1.6 with 0.60, 1.8 with 0.62, 2.0 with 0.68 and above (never halved there).
+constexpr double kHalved = 0.60;
 // Medium tiles of dX that have a CU each, and k tiles enough, take four buffers instead of two (of its steps, `kt`): 1003 tokens, 768 <-
 // 2 x 2304 51 us -> 38 (48 tiles), 32 -> 28 (96), 22 -> 22 (192); 256 tokens, 4096 <- 2 x 11008 71 -> 55 (256); 4 k tiles 7.8 -> 8.8.
 // The projections and dW gained nothing (500 x 768 -> 2304 10.2 -> 11.7, 512 x 2048 -> 4096 23.6 -> 21.7; dW 19 -> 17 to 12 -> 12).
@@ -57,7 +61,7 @@ inline double tiles_time(bool bf16, int tile, int64_t tiles, int64_t kt) {
   // (two fp32 tiles on a CU take as long as when every CU has two: the matrix units bound them)
   if (left > kCUs) last = bf16 ? c.one + (c.full - c.one) * (double)(left - kCUs) / kCUs : c.full;
   else if (left) last = c.few + (c.one - c.few) * (double)left / kCUs;
-  if (rest_of(tile, tiles)) last *= 0.58;
+  if (rest_of(tile, tiles)) last *= kHalved;
   return kLaunch + ((double)rounds * c.full + last) * ((double)kt + c.ends);
 }
 
