@@ -390,7 +390,8 @@ ff_status ff_adamw_step_batched(int64_t count, int64_t n, float* const* c, const
  *     The hyperparameters are those of ff_adamw_step; gradients are multiplied by grad_scale.  lr_dev, grad_scale_dev (fp32)
  *     and step_dev (int64) are NULL or one device value each, read when the call runs: factors of lr and grad_scale, and an
  *     addend of step (the sum must be at least 1), for captured steps that are replayed.
- *   ff_adamw_set_read : the values of 8-bit moments in bf16, which holds them exactly: m[i], v[i] (HOST arrays of device
+ *   ff_adamw_set_read : the values of 8-bit moments in bf16, which holds them exactly (but for 2^128, to which a moment just
+ *     below it may be rounded, and which reads as infinity): m[i], v[i] (HOST arrays of device
  *     pointers, NULL to skip one) receive n[i] values and zeros up to the next multiple of 256.
  * 8-bit moments: each block of 256 elements of a tensor has a unit 2^(m_exp - 120); the code a (of v: the byte; of m: its low 7
  * bits, bit 7 the sign) stands for a units below 16 and (8 + a mod 8) 2^(a div 8 - 1) from there on.  A step takes the block's

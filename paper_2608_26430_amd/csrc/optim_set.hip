@@ -15,9 +15,12 @@
 // launch.  The moments and their place between codes are computed in fp64: in fp32 one element in a million would fall on the other
 // side.
 //
-// Bound by memory: 28 bytes an element with fp32 moments and gradients, 16 with 8-bit ones, bf16 gradients and copies.  Measured:
-// three tensors of 1000 and 256 elements 2.4 us; 289 of 20,000 and 4096, 92 MB, 16.7 us (5.5 TB/s, part of it from the last-level
-// cache); three of 45 million in 8 bits 420 to 475 us (2.17 GB, 4.6 to 5.2 TB/s), their moments read in 157 (0.81 GB, 5.2 TB/s).
+// With fp32 moments bound by memory: 28 bytes an element with fp32 gradients.  Measured: three tensors of 1000 and 256 elements 2.4 us; 289
+// of 7000 to 20,000 and 4096, 92 MB, 16.7 us (5.5 TB/s, part of it from the last-level cache); three of 45, 27 and 38 million elements
+// with bf16 gradients and copies, 28 bytes an element, 587 us (3.09 GB, 5.25 TB/s).
+// In 8 bits, with bf16 gradients and copies, 16 bytes and 146 vector instructions an element: the same three tensors 412 to 475 us (1.76 GB,
+// 3.7 to 4.3 TB/s; 246,000 vector instructions on each SIMD in 0.9 million cycles), their moments read in 155 to 162 (0.66 GB, 4.1 to
+// 4.3 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <memory>

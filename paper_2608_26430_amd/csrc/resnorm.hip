@@ -11,6 +11,10 @@ namespace resnorm {
 
 // ------------------------------------------------------------------------------------------- rows of any width
 
+// Rows over 8192 elements, and those narrower than a piece: an element a thread and access, a row read up to five times forward (two layer
+// norms) and four times backward.  4096 x 12,288 bf16, RMS norms on both sides: forward 305 us, backward 882 (1.3 and 0.7 TB/s of what a
+// single reading moves; 4096 x 8192, held in registers, 4.4).
+
 // What a column of a row comes to; the same steps as in the kernels that hold their rows.
 template <class E>
 struct Column {
