@@ -402,7 +402,8 @@ ff_status ff_adamw_step_batched(int64_t count, int64_t n, float* const* c, const
  * moments before their rounding; moments and their place between codes are computed in fp64.
  * fp32 moments are made in fp64 and rounded to nearest once a step: a change below half a unit in a moment's last place, as the decay of v
  * alone is for beta2 above 1 - 2^-25, leaves it as it is.
- * Calls on one set must be ordered.  Steps and reads are asynchronous on `stream` and allocate nothing; equal inputs give equal bits.
+ * Calls on one set must be ordered, and a graph that holds one must not be replayed after the set's destruction (its table is freed).
+ * Steps and reads are asynchronous on `stream` and allocate nothing; equal inputs give equal bits.
  * Errors: FF_EINVAL, FF_ENOMEM, FF_EDEVICE; after FF_EDEVICE some tensors may have been stepped.
  */
 enum { FF_STATES_F32 = 0, FF_STATES_8BIT = 1 };

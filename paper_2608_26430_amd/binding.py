@@ -463,7 +463,7 @@ class AdamWSet:
     or "8bit".  copies: None, or bf16 tensors (None for some) that every step writes the parameters to.  seed: of the random
     rounding of 8-bit states.  The states are made here, zero, on the current stream: flat arrays (m_all, v_all) that hold tensor i from element
     offsets[i], a multiple of 256, on; m, v (and m_exp, v_exp, exponents of the blocks of 8-bit states) are the tensors'
-    views of them, 1-D, to be saved and restored as they are."""
+    views of them, 1-D, to be saved and restored as they are.  The set must live as long as graphs that hold its steps are replayed."""
 
     def __init__(self, params: Sequence, weight_decay=0.0, states: str = "f32", copies: Optional[Sequence] = None,
                  grad_dtype=None, betas=(0.9, 0.999), eps: float = 1e-8, seed: int = 0):

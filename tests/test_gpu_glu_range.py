@@ -128,3 +128,20 @@ def test_where_words_become_infinite(dev):
                         device=dev, dtype=torch.float64).repeat(n // 8)
     kept = torch.stack((kept, -kept))
     assert torch.equal(kept_values(G), kept) and torch.equal(kept_values(P), kept)
+
+
+def test_gradients_over_what_they_are_made_of(dev):
+    """dG and dU over G and U, over U and G, dG or dU over dH, with infinite words among the others: as in memory of their own."""
+    bf = torch.bfloat16
+    d, _ = large(70, 64, 200, "bf16", dev, 6)
+    args = d["X"], d["Wg"], d["Wu"], "gelu_tanh"
+    _, G, P = ff.glu_fwd(*args, d["Ag"], d["Au"], save=True)
+    want = ff.glu_bwd(d["dH"], *args, G=G, U=P, want_dx=False)[:2]
+    got = []
+    for place in ("words", "words crossed", "dG over dH", "dU over dH"):
+        x, g, p = d["dH"].clone(), G.clone(), P.clone()
+        own = {"words": (g.view(bf), p.view(bf)), "words crossed": (p.view(bf), g.view(bf)), "dG over dH": (x, None), "dU over dH": (None, x)}[place]
+        got.append(ff.glu_bwd(x, *args, G=g, U=p, dG=own[0], dU=own[1], want_dx=False)[:2])
+    torch.cuda.synchronize()
+    # (an infinity's sign counts, a zero's does not)
+    assert all(torch.equal(a, b) for pair in got for a, b in zip(pair, want))
